@@ -375,6 +375,80 @@ relax_status relax_decoder_layer_f16(const relax_layer_dims *dims, const relax_l
                                      const relax_kv_cache *cache, const relax_seqs *seqs, uint16_t *out, int32_t n, void *ws,
                                      size_t ws_bytes, relax_stream stream);
 
+/* ---- Paged KV cache in 8 bits -------------------------------------------------------------------------------------
+ * The cache of a layer for many sequences that grow and end at different times: positions of a slot are cut into pages
+ * that lie anywhere in a pool, and keys and values are held in one byte each with a scale per block of RELAX_PAGED_BLOCK
+ * tokens and KV head -- half the bytes of relax_kv_cache, which is what attention of decode rows costs.
+ * Page p of the pool holds positions 0 .. page_size - 1 of its place in a sequence, for all KV heads.  A block b of a page is the
+ * 16 tokens 16 b .. 16 b + 15 of one KV head: 16 * d codes u in 1..255 for keys and as many for values; element e of token t stands for
+ * (u - 128) * scale, with
+ *   k code at  [page][head][b][e / 16][t][e % 16]
+ *   v code at  [page][head][b][e / 64][t / 4][e % 16][e / 16 % 4][t % 4]
+ *   scales at  [page][head][b]
+ * (fragments of the matrix products that read them).  Codes and scales behind a sequence's last token have no meaning and need no
+ * initialisation.  Several rows of the page table may name one page (a shared beginning) as long as no call appends to it
+ * through two of them.  The page table is device data and is read at run time: a call captured in a graph follows it.  A block whose page
+ * number is outside [0, n_pages) has no page: an append drops its tokens, attention leaves them out, a read gives zeros, and
+ * each raises bit 2 of the flag that relax_workspace_error reports for the call's workspace.
+ * The descriptor of a call is relax_seqs: slots are rows of the page table, dims.kv_slots their number, and dims.kv_capacity
+ * (the positions the rotary table covers) bounds every length.  Of dims the calls use n_heads, n_kv_heads, head_dim, kv_capacity and kv_slots.  */
+#define RELAX_PAGED_BLOCK 16
+typedef struct {
+    uint8_t *k, *v;               /* codes, [n_pages][g][page_size / 16][16 * d] each, 16-byte aligned                 */
+    float *k_scale, *v_scale;     /* [n_pages][g][page_size / 16]                                                      */
+    const int32_t *pages;         /* [kv_slots][pages_per_slot] page numbers; entries behind a slot's last position are not read */
+    const float *rope;            /* rotary table of relax_rope_table_init, or NULL: keys and queries are not rotated  */
+    int32_t n_pages;              /* n_pages * g * page_size / 16 < 2^31                                               */
+    int32_t page_size;            /* 16, 32, 64, 128 or 256 tokens                                                     */
+    int32_t pages_per_slot;       /* kv_capacity <= pages_per_slot * page_size                                         */
+} relax_paged_cache;
+
+/* Bytes of workspace for every paged call with n <= n_max rows, B <= B_max sequences and kv_lens <= L_max: the flag line of
+ * relax_workspace_init, the descriptor table, the partial results of attention.  0 for invalid arguments.               */
+size_t relax_paged_workspace_bytes(const relax_layer_dims *dims, int32_t n_max, int32_t L_max, int32_t B_max);
+
+/* Puts the rows of a call into the cache.  Row i of the call lies q_stride (kv_stride) elements behind row i - 1: q [h,d], k and v [g,d]
+ * fp16, 16-byte aligned, strides multiples of 8 -- three parts of one [n,(h+2g)d] matrix, or matrices of their own.
+ *   q_out[i] = R(pos_i) q[i], fp16 [n,h,d]  (q_out may be q; q and q_out NULL: only k and v)
+ *   k, v:  a block's scale is max|x| / 127 over the call's tokens in it, of keys behind the rotary embedding (which are not rounded in
+ *   between); a block that holds earlier tokens of the sequence keeps its scale if that is larger, else their codes
+ *   become round((u - 128) * old / new) + 128.  u = 128 + round(x / scale).  Infinite values count as +-65504, NaNs as 0.
+ * Tokens of the sequence in front of the call's, and whatever lies behind its last one, stay as they are but for that.
+ * ws: relax_paged_workspace_bytes(dims, n, max kv_lens, B) bytes, 256-byte aligned.  Errors: NULL, SHAPE, CAPACITY, WORKSPACE, UNSUPPORTED
+ * (page_size, pool too large, more than 65535 sequences).                                                              */
+relax_status relax_paged_append(const uint16_t *q, int64_t q_stride, const uint16_t *k, const uint16_t *v, int64_t kv_stride, uint16_t *q_out,
+                                const relax_paged_cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims, int32_t n,
+                                void *ws, size_t ws_bytes, relax_stream stream);
+
+/* relax_attention over a paged cache: q [n,h,d] fp16 (already rotated), out [n,h,d] fp16, 16-byte aligned.  Row i of sequence b attends to
+ * positions 0..pos_i of its slot, which must already hold this call's keys and values.  Scores, softmax and sums are fp32, the
+ * probabilities are rounded to fp16 in front of their product with the values.  A row that no token is left for (every page of its
+ * sequence out of range) is zeros.  ws and errors as relax_paged_append.                                                */
+relax_status relax_paged_attention(const uint16_t *q, const relax_paged_cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims,
+                                   uint16_t *out, int32_t n, void *ws, size_t ws_bytes, relax_stream stream);
+
+/* What the cache stands for, as fp16: row i of sequence b is position kv_lens[b] - q_lens[b] + i, k_out and v_out [n,g,d], 16-byte aligned,
+ * either may be NULL.  Keys come out as they are held, rotated: rows of a relax_kv_cache, or of an append without a rotary table.
+ * ws and errors as relax_paged_append.                                                                                   */
+relax_status relax_paged_read(const relax_paged_cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims, uint16_t *k_out,
+                              uint16_t *v_out, int32_t n, void *ws, size_t ws_bytes, relax_stream stream);
+
+/* ---- Log probabilities of tokens ------------------------------------------------------------------------------------
+ * What a serving program returns beside the picked token, or scores a given text with, from rows of logits (those of relax_model_step, or
+ * of relax_half_matmul with the head on every row): with log p = x - log(sum e^x) per row
+ *   logprobs[i]                log p of token targets[i]; -inf for an id outside [0, vocab)     (both NULL: not wanted)
+ *   entropy[i]                 -sum p log p                                                     (NULL: not wanted)
+ *   top_ids, top_logprobs      [n,top]: the `top` most likely tokens, most likely first, equal logits in order of their ids, and their
+ *                              log p; 0 <= top <= 32, top <= vocab (top == 0: both unused)
+ * logits: device fp16, row i at logits + i * stride, stride >= vocab (any alignment).  fp32 throughout.  A logit of -inf has probability 0; a row of
+ * nothing else gives -inf and entropy 0.  A row that holds a NaN or +inf gives NaN log probabilities and entropy (a token at
+ * -inf aside, unless NaN is in the row); its ids are those of the largest logits all the same, NaNs behind -inf.
+ * ws (may be NULL): with relax_token_logprobs_workspace_bytes(n, vocab, top) bytes, 256-byte aligned, few rows are spread over more of the chip; without them
+ * the call gives the same.  Errors: NULL (no output wanted either), SHAPE, UNSUPPORTED (top > 32).                         */
+size_t       relax_token_logprobs_workspace_bytes(int32_t n_max, int32_t vocab, int32_t top);
+relax_status relax_token_logprobs(const uint16_t *logits, int64_t stride, const int32_t *targets, float *logprobs, float *entropy, int32_t *top_ids,
+                                  float *top_logprobs, int32_t n, int32_t vocab, int32_t top, void *ws, size_t ws_bytes, relax_stream stream);
+
 /* Build identity of the loaded binary (one binary serves every shape).                  */
 const char *relax_build_id(void);
 

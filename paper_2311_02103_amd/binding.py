@@ -63,6 +63,11 @@ class SeqsC(C.Structure):
                 ("slots", C.POINTER(C.c_int32)), ("device_table", C.c_void_p)]
 
 
+class PagedCacheC(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("pages", C.c_void_p),
+                ("rope", C.c_void_p), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("pages_per_slot", C.c_int32)]
+
+
 class PlanEntryC(C.Structure):
     _fields_ = [("name", C.c_char * 24), ("first_op", C.c_int32), ("last_op", C.c_int32), ("storage", C.c_int32), ("pinned", C.c_int32),
                 ("offset", C.c_uint64), ("bytes", C.c_uint64), ("storage_bytes", C.c_uint64)]
@@ -119,6 +124,16 @@ _SIGNATURES = {
     "relax_model_workspace_bytes": (C.c_size_t, [C.POINTER(ModelC), C.c_int32, C.c_int32, C.c_int32]),
     "relax_model_step": (C.c_int32, [C.POINTER(ModelC), C.c_void_p, C.POINTER(KVCacheC), C.POINTER(SeqsC), C.c_void_p,
                                      C.c_void_p, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "relax_paged_workspace_bytes": (C.c_size_t, [C.POINTER(LayerDims), C.c_int32, C.c_int32, C.c_int32]),
+    "relax_paged_append": (C.c_int32, [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.POINTER(PagedCacheC), C.POINTER(SeqsC),
+                                       C.POINTER(LayerDims), C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "relax_paged_attention": (C.c_int32, [C.c_void_p, C.POINTER(PagedCacheC), C.POINTER(SeqsC), C.POINTER(LayerDims), C.c_void_p, C.c_int32, C.c_void_p,
+                                          C.c_size_t, C.c_void_p]),
+    "relax_paged_read": (C.c_int32, [C.POINTER(PagedCacheC), C.POINTER(SeqsC), C.POINTER(LayerDims), C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p,
+                                     C.c_size_t, C.c_void_p]),
+    "relax_token_logprobs_workspace_bytes": (C.c_size_t, [C.c_int32, C.c_int32, C.c_int32]),
+    "relax_token_logprobs": (C.c_int32, [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
+                                         C.c_void_p, C.c_size_t, C.c_void_p]),
     "relax_probe_stream_read": (C.c_int32, [C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]),
     "relax_probe_mfma": (C.c_int32, [C.c_void_p, C.c_int32, C.c_int32, C.POINTER(C.c_int64), C.c_void_p]),
     "relax_unpack_int4": (C.c_int32, [C.POINTER(QMatC), C.c_void_p, C.c_void_p]),
@@ -227,6 +242,18 @@ class KVCache:
         return KVCacheC(_ptr(self.k), _ptr(self.v), _ptr(self.rope))
 
 
+class PagedCache:
+    """relax_paged_cache: codes k, v uint8 and scales k_scale, v_scale fp32 of the pool, the page table int32 [kv_slots, pages_per_slot] and the
+    rotary table (None: no rotation), all on the device.  The C struct is made once; the tensors are kept alive with it."""
+
+    def __init__(self, k: Ptr, v: Ptr, k_scale: Ptr, v_scale: Ptr, pages: Ptr, rope: Ptr, n_pages: int, page_size: int, pages_per_slot: int):
+        self._keep = (k, v, k_scale, v_scale, pages, rope)
+        self._c = PagedCacheC(*map(_ptr, self._keep), n_pages, page_size, pages_per_slot)
+
+    def c(self) -> PagedCacheC:
+        return self._c
+
+
 class Seqs:
     """Host-side ragged descriptor; kv_lens are lengths AFTER this call's rows are appended.  device_table: optional
     device int32 [4][B] (q_start, q_len, kv_len, slot) that the kernels read instead; kv_lens are then upper bounds."""
@@ -319,6 +346,43 @@ def relax_attention_static(q: Ptr, cache: Optional[KVCache], seqs: Optional[Seqs
     cc = None if cache is None else cache.c()
     sc = None if seqs is None else seqs.c()
     return lib().relax_attention_static(_ptr(q), _ref(cc), _ref(sc), _ref(dims), _ptr(out), n, _stream(stream))
+
+
+def relax_paged_workspace_bytes(dims: Optional[LayerDims], n_max: int, L_max: int, B_max: int) -> int:
+    return int(lib().relax_paged_workspace_bytes(_ref(dims), n_max, L_max, B_max))
+
+
+def relax_paged_append(q: Ptr, q_stride: int, k: Ptr, v: Ptr, kv_stride: int, q_out: Ptr, cache: Optional[PagedCache], seqs: Optional[Seqs],
+                       dims: Optional[LayerDims], n: int, ws: Ptr, ws_bytes: int, stream=None) -> int:
+    """q, k, v may be parts of one matrix: their addresses as integers, the strides in elements."""
+    cc = None if cache is None else cache.c()
+    sc = None if seqs is None else seqs.c()
+    return lib().relax_paged_append(_ptr(q), q_stride, _ptr(k), _ptr(v), kv_stride, _ptr(q_out), _ref(cc), _ref(sc), _ref(dims), n, _ptr(ws), ws_bytes,
+                                    _stream(stream))
+
+
+def relax_paged_attention(q: Ptr, cache: Optional[PagedCache], seqs: Optional[Seqs], dims: Optional[LayerDims], out: Ptr, n: int, ws: Ptr, ws_bytes: int,
+                          stream=None) -> int:
+    cc = None if cache is None else cache.c()
+    sc = None if seqs is None else seqs.c()
+    return lib().relax_paged_attention(_ptr(q), _ref(cc), _ref(sc), _ref(dims), _ptr(out), n, _ptr(ws), ws_bytes, _stream(stream))
+
+
+def relax_paged_read(cache: Optional[PagedCache], seqs: Optional[Seqs], dims: Optional[LayerDims], k_out: Ptr, v_out: Ptr, n: int, ws: Ptr, ws_bytes: int,
+                     stream=None) -> int:
+    cc = None if cache is None else cache.c()
+    sc = None if seqs is None else seqs.c()
+    return lib().relax_paged_read(_ref(cc), _ref(sc), _ref(dims), _ptr(k_out), _ptr(v_out), n, _ptr(ws), ws_bytes, _stream(stream))
+
+
+def relax_token_logprobs_workspace_bytes(n_max: int, vocab: int, top: int) -> int:
+    return int(lib().relax_token_logprobs_workspace_bytes(n_max, vocab, top))
+
+
+def relax_token_logprobs(logits: Ptr, stride: int, targets: Ptr, logprobs: Ptr, entropy: Ptr, top_ids: Ptr, top_logprobs: Ptr, n: int, vocab: int, top: int,
+                         ws: Ptr = None, ws_bytes: int = 0, stream=None) -> int:
+    return lib().relax_token_logprobs(_ptr(logits), stride, _ptr(targets), _ptr(logprobs), _ptr(entropy), _ptr(top_ids), _ptr(top_logprobs), n, vocab, top,
+                                      _ptr(ws), ws_bytes, _stream(stream))
 
 
 def relax_decoder_layer(dims: Optional[LayerDims], weights: Optional[LayerWeights], x: Ptr, cache: Optional[KVCache],

@@ -5,6 +5,7 @@
 #include <cstring>
 #include <mutex>
 
+#include "paged_device.h"
 #include "relax_common.h"
 
 using namespace relax;
@@ -1392,6 +1393,145 @@ relax_status relax_dequant_matmul_q3_native(const uint16_t *x, const relax_qmat 
     // for a shape the GEMM does not take, it is streamed once per pass of up to four rows of x.
     if (q3_route(x, *w, out, n).kernel == RELAX_KERNEL_MATVEC && !gemv_q3_supported(w->m, w->k)) return RELAX_ERR_UNSUPPORTED;
     return hip_status(q3_matmul(x, *w, n, out, static_cast<hipStream_t>(stream)));
+}
+
+}  // extern "C"
+
+namespace {
+
+// Front part of a paged workspace: flag line and descriptor table, then the partial results of attention
+struct PagedWs {
+    size_t table, partials, total;
+};
+PagedWs paged_ws(const relax_layer_dims &dm, int32_t n, int32_t L, int32_t B)
+{
+    PagedWs p;
+    p.table = kWsFlagBytes;
+    p.partials = p.table + align256(sizeof(int32_t) * 4 * (size_t)B);
+    p.total = p.partials + align256(sizeof(float) * paged_partial_floats(dm, n, L));
+    return p;
+}
+
+constexpr int32_t kMaxPagedSeqs = 65535;     // extents of a grid
+
+// Everything the paged calls check alike; fills the kernels' descriptors.  items, tiles: see launch_paged_append, launch_paged_attention.
+relax_status paged_begin(const relax_paged_cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims, int32_t n, void *ws, size_t ws_bytes,
+                         hipStream_t stream, PagedArgs &pa, SeqTable &st, int32_t &L_max, int &items, long long &tiles, float **partials)
+{
+    relax_status rc = check_dims(dims);
+    if (rc != RELAX_OK) return rc;
+    if (!cache || !cache->k || !cache->v || !cache->k_scale || !cache->v_scale || !cache->pages || !ws) return RELAX_ERR_NULL;
+    if (cache->n_pages < 1 || cache->pages_per_slot < 1) return RELAX_ERR_SHAPE;
+    if (!aligned(cache->k, 16) || !aligned(cache->v, 16) || !aligned(cache->k_scale, 4) || !aligned(cache->v_scale, 4) || !aligned(cache->pages, 4) ||
+        !aligned(cache->rope, 16))
+        return RELAX_ERR_SHAPE;
+    int shift = 0;
+    while (shift < 4 && (RELAX_PAGED_BLOCK << shift) != cache->page_size) ++shift;
+    if ((RELAX_PAGED_BLOCK << shift) != cache->page_size) return RELAX_ERR_UNSUPPORTED;
+    if ((int64_t)cache->n_pages * dims->n_kv_heads << shift > INT32_MAX) return RELAX_ERR_UNSUPPORTED;
+    if ((int64_t)cache->pages_per_slot * cache->page_size < dims->kv_capacity) return RELAX_ERR_CAPACITY;
+    bool need_table = false;
+    rc = build_seqs(seqs, *dims, n, st, L_max, need_table);
+    if (rc != RELAX_OK) return rc;
+    if (seqs->B > kMaxPagedSeqs) return RELAX_ERR_UNSUPPORTED;
+    const PagedWs pl = paged_ws(*dims, n, L_max, seqs->B);
+    if (ws_bytes < pl.total || !aligned(ws, 256)) return RELAX_ERR_WORKSPACE;
+    const int rep = dims->n_heads / dims->n_kv_heads;
+    items = 0, tiles = 0;
+    for (int b = 0; b < seqs->B; ++b) {
+        items += paged_blocks_of(seqs->q_lens[b]);
+        tiles += ((long long)seqs->q_lens[b] * rep + 15) / 16;
+    }
+    pa = {cache->k, cache->v, cache->k_scale, cache->v_scale, cache->pages, cache->rope, static_cast<uint32_t *>(ws), cache->n_pages, cache->pages_per_slot,
+          dims->kv_slots, dims->kv_capacity, shift};
+    *partials = reinterpret_cast<float *>(static_cast<char *>(ws) + pl.partials);
+    WsPlan front = {};
+    front.table = pl.table;
+    return upload_table(st, seqs, need_table, ws, front, stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t relax_paged_workspace_bytes(const relax_layer_dims *dims, int32_t n_max, int32_t L_max, int32_t B_max)
+{
+    if (check_dims(dims) != RELAX_OK || n_max < 1 || L_max < 1 || B_max < 1) return 0;
+    return paged_ws(*dims, n_max, L_max, B_max).total;
+}
+
+relax_status relax_paged_append(const uint16_t *q, int64_t q_stride, const uint16_t *k, const uint16_t *v, int64_t kv_stride, uint16_t *q_out,
+                                const relax_paged_cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims, int32_t n, void *ws, size_t ws_bytes,
+                                relax_stream stream)
+{
+    if (!k || !v || !q != !q_out) return RELAX_ERR_NULL;
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(q_out, 16) || kv_stride % 8 != 0 || (q && q_stride % 8 != 0)) return RELAX_ERR_SHAPE;
+    relax_status rc = check_dims(dims);
+    if (rc != RELAX_OK) return rc;
+    if (kv_stride < (int64_t)dims->n_kv_heads * dims->head_dim || (q && q_stride < (int64_t)dims->n_heads * dims->head_dim)) return RELAX_ERR_SHAPE;
+    hipStream_t st_ = static_cast<hipStream_t>(stream);
+    PagedArgs pa;
+    SeqTable st = {};
+    int32_t L_max = 0;
+    int items = 0;
+    long long tiles = 0;
+    float *partials = nullptr;
+    rc = paged_begin(cache, seqs, dims, n, ws, ws_bytes, st_, pa, st, L_max, items, tiles, &partials);
+    if (rc != RELAX_OK) return rc;
+    return hip_status(launch_paged_append(q, q_stride, k, v, kv_stride, q_out, pa, *dims, st, items, st_));
+}
+
+relax_status relax_paged_attention(const uint16_t *q, const relax_paged_cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims, uint16_t *out,
+                                   int32_t n, void *ws, size_t ws_bytes, relax_stream stream)
+{
+    if (!q || !out) return RELAX_ERR_NULL;
+    if (!aligned(q, 16) || !aligned(out, 16)) return RELAX_ERR_SHAPE;
+    hipStream_t st_ = static_cast<hipStream_t>(stream);
+    PagedArgs pa;
+    SeqTable st = {};
+    int32_t L_max = 0;
+    int items = 0;
+    long long tiles = 0;
+    float *partials = nullptr;
+    const relax_status rc = paged_begin(cache, seqs, dims, n, ws, ws_bytes, st_, pa, st, L_max, items, tiles, &partials);
+    if (rc != RELAX_OK) return rc;
+    return hip_status(launch_paged_attention(q, pa, *dims, st, tiles, L_max, out, partials, st_));
+}
+
+relax_status relax_paged_read(const relax_paged_cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims, uint16_t *k_out, uint16_t *v_out,
+                              int32_t n, void *ws, size_t ws_bytes, relax_stream stream)
+{
+    if (!k_out && !v_out) return RELAX_ERR_NULL;
+    if (!aligned(k_out, 16) || !aligned(v_out, 16)) return RELAX_ERR_SHAPE;
+    hipStream_t st_ = static_cast<hipStream_t>(stream);
+    PagedArgs pa;
+    SeqTable st = {};
+    int32_t L_max = 0;
+    int items = 0;
+    long long tiles = 0;
+    float *partials = nullptr;
+    const relax_status rc = paged_begin(cache, seqs, dims, n, ws, ws_bytes, st_, pa, st, L_max, items, tiles, &partials);
+    if (rc != RELAX_OK) return rc;
+    return hip_status(launch_paged_read(pa, k_out, v_out, *dims, st, items, st_));
+}
+
+size_t relax_token_logprobs_workspace_bytes(int32_t n_max, int32_t vocab, int32_t top)
+{
+    if (n_max < 1 || vocab < 1 || top < 0 || top > 32) return 0;
+    return 256;
+}
+
+relax_status relax_token_logprobs(const uint16_t *logits, int64_t stride, const int32_t *targets, float *logprobs, float *entropy, int32_t *top_ids,
+                                  float *top_logprobs, int32_t n, int32_t vocab, int32_t top, void *ws, size_t ws_bytes, relax_stream stream)
+{
+    if (!logits || !targets != !logprobs) return RELAX_ERR_NULL;
+    if (n < 1 || vocab < 1 || stride < vocab || top < 0 || top > vocab || !aligned(logits, 2) || !aligned(targets, 4) || !aligned(logprobs, 4) ||
+        !aligned(entropy, 4) || !aligned(top_ids, 4) || !aligned(top_logprobs, 4))
+        return RELAX_ERR_SHAPE;
+    if (top > 32) return RELAX_ERR_UNSUPPORTED;
+    if (top > 0 ? !top_ids || !top_logprobs : !targets && !entropy) return RELAX_ERR_NULL;
+    (void)ws, (void)ws_bytes;
+    return hip_status(launch_token_logprobs(logits, stride, targets, logprobs, entropy, top_ids, top_logprobs, n, vocab, top, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -1,0 +1,289 @@
+// Causal attention over the paged 8-bit KV cache.
+//
+//   o[i] = sum_t p[i,t] v[t],   p[i,:] = softmax_t(q[i] . k[t] / sqrt d),  t = 0 .. pos_i,   k[t] = s_k[t / 16] (u_k[t] - 128), v likewise
+//
+// The query heads of a KV head and the rows of a sequence are one list of (row, head) pairs: pair p is row p / rep, head p % rep of the group.
+// A workgroup takes 16 consecutive pairs, the columns of the MFMA tiles, against one KV head and one split of the tokens; its four
+// wavefronts take a quarter of the split each.  With S^T = K Q^T a pair is a column of the result and the lane (quarter, column) holds tokens
+// 4 quarter .. + 3 of a block; the same lane's eight probabilities of two blocks are what the B operand of O^T = V^T P^T wants from it, and
+// the codes come in as the A operands (paged_device.h), so nothing passes through LDS or another lane but the maxima.
+//
+// Scales.  The codes go into the products as integers.  A block's key scale times log2(e) / sqrt(d) multiplies its scores; its value scale,
+// divided by the largest of the wavefront's blocks so that it is at most 1, multiplies the probabilities in front of their rounding to fp16, and the largest
+// one the result.  exp2's argument is offset by 11 in return: the largest probability is at most 2^15 (the reference trails the maximum by
+// at most 2^4) and one of 2^-39 of it still is a subnormal fp16 number.  Scores, sums and O are fp32; the rounding of the probabilities (2^-11 relative, independent
+// from token to token) is the only one between the codes and the result.
+#include "paged_device.h"
+
+namespace relax {
+
+namespace {
+
+constexpr float kBias = 11.0f, kLag = 4.0f;      // log2: offset of the weights, and how far the reference may trail the maximum
+
+// grid: x = KV head, y = split, z = sequence * tiles + tile.  part: [row][head][splits][D + 2] when splits > 1.
+template <int D>
+__global__ __launch_bounds__(256, 2) void attn_paged_kernel(const uint16_t *__restrict__ q, PagedArgs pa, float *__restrict__ part,
+                                                            uint16_t *__restrict__ out, SeqTable st, int h, int g, int tiles, int chunk, int splits)
+{
+    constexpr int J = D / 64;                    // 1 KB loads per block
+    constexpr int NT = D / 16;                   // 16-element tiles of O^T
+    constexpr int P = D + 4;                     // pitch of a state in LDS
+    __shared__ __align__(16) float states[4 * 16 * P];
+    __shared__ float sm_m[4 * 16], sm_l[4 * 16];
+
+    const int b = tiles == 1 ? (int)blockIdx.z : (int)blockIdx.z / tiles, tile = tiles == 1 ? 0 : (int)blockIdx.z - b * tiles;
+    const int kvh = blockIdx.x, split = blockIdx.y;
+    const SeqSpan si = seq_span(st, b);
+    const int rep = h / g, pairs = si.q_len * rep, p0 = tile * 16;
+    if (p0 >= pairs) return;
+    const int past = si.kv_len - si.q_len;
+    const int n_pairs = min(16, pairs - p0);
+    const int pos_min = past + p0 / rep, vis = min(past + (p0 + n_pairs - 1) / rep + 1, pa.cap);      // tokens that any of the pairs attends to
+    const int t_begin = split * chunk;
+    if (split > 0 && t_begin >= vis) return;
+    const int t_end = min(vis, t_begin + chunk);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 15, quarter = lane >> 4;
+
+    // ---- this wavefront's blocks: a quarter of the split, in pairs ----
+    const int b_begin = t_begin >> 4, b_end = t_end > t_begin ? (t_end + 15) >> 4 : b_begin;
+    const int per = ((b_end - b_begin + 1) / 2 + 3) / 4 * 2;
+    const int w_begin = b_begin + wave * per, w_end = min(b_end, w_begin + per);
+
+    // ---- queries: lane holds pair `col`; k step 2 j + half takes elements 16 (4 j + quarter) + 8 half .. + 7 ----
+    const int pair = p0 + min(col, n_pairs - 1), row = pair / rep, head = kvh * rep + pair - row * rep, pos = past + row;
+    half8p_t qf[2 * J];
+    {
+        const uint16_t *src = q + ((size_t)(si.q_start + row) * h + head) * D + quarter * 16;
+#pragma unroll
+        for (int j = 0; j < 2 * J; ++j) qf[j] = *(const half8p_t *)(src + (j >> 1) * 64 + (j & 1) * 8);
+    }
+    const float c = 1.44269504088896340736f / sqrtf((float)D);
+
+    float4p_t O[NT];
+#pragma unroll
+    for (int i = 0; i < NT; ++i) O[i] = float4p_t{0.0f, 0.0f, 0.0f, 0.0f};
+    float m_run = -INFINITY, l_run = 0.0f, v_ref = 0.0f;
+
+    for (int seg = w_begin; seg < w_end; seg += kWave) {
+        // ---- lane j: number in the pool and scales of block seg + j ----
+        int pool = -1;
+        float ks = 0.0f, vs = 0.0f;
+        if (seg + lane < w_end) {
+            pool = paged_block(pa, g, kvh, si.slot, seg + lane);
+            if (pool < 0) atomicOr(pa.err, kBadPage);
+            else ks = pa.k_scale[pool] * c, vs = pa.v_scale[pool];
+        }
+        const float ref = fmaxf(v_ref, wave_max(vs));
+        if (v_ref > 0.0f && ref > v_ref) {                     // later blocks have larger values: O is in units of the largest scale
+            const float f = v_ref / ref;
+#pragma unroll
+            for (int i = 0; i < NT; ++i) O[i] *= f;
+        }
+        v_ref = ref;
+        const float vr = ref > 0.0f ? vs / ref : 0.0f;
+
+        struct Step {
+            u32x4p_t k[2 * J], v[2 * J];
+        };
+        auto step_load = [&](Step &sp, int s) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const int at = max(__builtin_amdgcn_readlane(pool, min(2 * s + t, 63)), 0);       // no such block: any that can be read
+                const u32x4p_t *kp = (const u32x4p_t *)(pa.k + (size_t)at * (16 * D)), *vp = (const u32x4p_t *)(pa.v + (size_t)at * (16 * D));
+#pragma unroll
+                for (int j = 0; j < J; ++j) sp.k[t * J + j] = stream_load(kp + j * 64 + lane);
+#pragma unroll
+                for (int j = 0; j < J; ++j) sp.v[t * J + j] = stream_load(vp + j * 64 + lane);
+            }
+        };
+        auto consume = [&](const Step &sp, int s) {
+            float x[8];
+            float mx = -INFINITY;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                float4p_t S = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    const u32x4p_t w = sp.k[t * J + j];
+                    S = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_half8(w.x, w.y), qf[2 * j], S, 0, 0, 0);
+                    S = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_half8(w.z, w.w), qf[2 * j + 1], S, 0, 0, 0);
+                }
+                const int at = min(2 * s + t, 63);
+                const bool there = __builtin_amdgcn_readlane(pool, at) >= 0;
+                const float kc = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, ks), at));
+                const int t0 = (seg + 2 * s + t) * 16;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[4 * t + i] = S[i] * kc;
+                if (!there || t0 + 15 > pos_min) {             // uniform
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (!there || t0 + 4 * quarter + i > pos) x[4 * t + i] = -INFINITY;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mx = fmaxf(mx, x[4 * t + i]);
+            }
+            float2 both = pair_xor16(mx);
+            both = pair_xor32(fmaxf(both.x, both.y));
+            mx = fmaxf(both.x, both.y);
+            const bool move = mx > m_run + kLag;               // the first visible tokens: m_run = -inf
+            if (__any(move)) {
+                const float m_new = move ? mx : m_run, alpha = move ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.0f;
+                l_run *= alpha;
+                m_run = m_new;
+#pragma unroll
+                for (int i = 0; i < NT; ++i) O[i] *= alpha;
+            }
+            const float m_ref = m_run == -INFINITY ? 0.0f : m_run - kBias;      // nothing visible yet: every weight is exp2(-inf)
+            half8p_t pf;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const float r = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, vr), min(2 * s + t, 63)));
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float p = __builtin_amdgcn_exp2f(x[4 * t + i] - m_ref);
+                    l_run += p;
+                    pf[4 * t + i] = (_Float16)(p * r);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+                O[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_half8(sp.v[i >> 2][i & 3], sp.v[J + (i >> 2)][i & 3]), pf, O[i], 0, 0, 0);
+        };
+        const int ns = (min(w_end - seg, kWave) + 1) >> 1;
+        Step sa, sb;
+        step_load(sa, 0);
+        for (int s = 0; s < ns; s += 2) {
+            step_load(sb, s + 1);
+            consume(sa, s);
+            step_load(sa, s + 2);
+            if (s + 1 < ns) consume(sb, s + 1);
+        }
+    }
+
+    // ---- the four states meet in LDS ----
+    l_run = xor32_sum(xor16_sum(l_run));
+#pragma unroll
+    for (int i = 0; i < NT; ++i) *(float4p_t *)(states + (wave * 16 + col) * P + i * 16 + quarter * 4) = O[i] * v_ref;
+    if (quarter == 0) sm_m[wave * 16 + col] = m_run, sm_l[wave * 16 + col] = l_run;
+    __syncthreads();
+    for (int u = tid; u < n_pairs * (D / 4); u += 256) {
+        const int pc = u / (D / 4), e = u % (D / 4) * 4;
+        float mm = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) mm = fmaxf(mm, sm_m[w * 16 + pc]);
+        float4p_t num = {0.0f, 0.0f, 0.0f, 0.0f};
+        float den = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float mw = sm_m[w * 16 + pc], f = mw == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mw - mm);
+            num += *(const float4p_t *)(states + (w * 16 + pc) * P + e) * f;
+            den += sm_l[w * 16 + pc] * f;
+        }
+        const int pr = (p0 + pc) / rep, ph = kvh * rep + p0 + pc - pr * rep;
+        const size_t at = (size_t)(si.q_start + pr) * h + ph;
+        if (splits > 1) {
+            float *dst = part + (at * splits + split) * (D + 2);
+            dst[e] = num.x, dst[e + 1] = num.y, dst[e + 2] = num.z, dst[e + 3] = num.w;
+            if (e == 0) dst[D] = mm, dst[D + 1] = den;
+        } else {
+            const float inv = den > 0.0f ? 1.0f / den : den;   // a row that no token is left for is zeros; a NaN stays one
+            const uint32_t lo = f2h(num.x * inv) | (uint32_t)f2h(num.y * inv) << 16, hi = f2h(num.z * inv) | (uint32_t)f2h(num.w * inv) << 16;
+            *(u32x2p_t *)(out + at * D + e) = u32x2p_t{lo, hi};
+        }
+    }
+}
+
+// out of (row, head) from its splits: a workgroup per 1024 / D of them, four elements per thread
+template <int D>
+__global__ __launch_bounds__(256) void attn_paged_merge_kernel(const float *__restrict__ part, uint16_t *__restrict__ out, SeqTable st, int h, int g, int cap,
+                                                               int chunk, int splits)
+{
+    const int i = (int)blockIdx.x * (1024 / D) + (int)threadIdx.x / (D / 4), e = threadIdx.x % (D / 4) * 4;
+    if (i >= st.n * h) return;
+    const int r = i / h, hd = i - r * h, rep = h / g;
+    const RowInfo ri = row_info(st, r);
+    const SeqSpan si = seq_span(st, ri.seq);
+    // the splits that the tile of this pair had: those of its last pair
+    const int pair = (r - si.q_start) * rep + hd % rep, last = min((pair | 15), si.q_len * rep - 1) / rep;
+    const int vis = min(si.kv_len - si.q_len + last + 1, cap), used = max((vis + chunk - 1) / chunk, 1);
+    const float *src = part + (size_t)i * splits * (D + 2);
+    float mm = -INFINITY, den = 0.0f, num[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s0 = 0; s0 < used; s0 += 8) {
+        float ms[8], ls[8], as[8][4];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float *p = src + (size_t)min(s0 + j, used - 1) * (D + 2);
+            ms[j] = p[D], ls[j] = p[D + 1];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) as[j][x] = p[e + x];
+        }
+        float mx = mm;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) mx = s0 + j < used ? fmaxf(mx, ms[j]) : mx;
+        const float ref = mx == -INFINITY ? 0.0f : mx, f0 = __builtin_amdgcn_exp2f(mm - ref);
+        den *= f0;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) num[x] *= f0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float f = s0 + j < used ? __builtin_amdgcn_exp2f(ms[j] - ref) : 0.0f;
+            den += ls[j] * f;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) num[x] += as[j][x] * f;
+        }
+        mm = mx;
+    }
+    const float inv = den > 0.0f ? 1.0f / den : den;
+    const uint32_t lo = f2h(num[0] * inv) | (uint32_t)f2h(num[1] * inv) << 16, hi = f2h(num[2] * inv) | (uint32_t)f2h(num[3] * inv) << 16;
+    *(u32x2p_t *)(out + (size_t)i * D + e) = u32x2p_t{lo, hi};
+}
+
+// Splits of a launch with `tiles` workgroups per split: as many as bring it to kPagedGroups workgroups, none shorter than 128 tokens
+constexpr int kPagedGroups = 1024;
+struct PagedPlan {
+    int32_t chunk, splits;
+};
+PagedPlan paged_plan(long long tiles, int32_t L_max)
+{
+    long long s = kPagedGroups / (tiles > 0 ? tiles : 1), most = (L_max + 127) / 128;
+    s = s > most ? most : s;
+    s = s < 1 ? 1 : s;
+    const int32_t chunk = (int32_t)(((L_max + s - 1) / s + 31) / 32 * 32);
+    return {chunk, (L_max + chunk - 1) / chunk};
+}
+
+template <int D>
+hipError_t launch_d(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const SeqTable &st, int32_t tiles, const PagedPlan &pl, uint16_t *out,
+                    float *partials, hipStream_t stream)
+{
+    const dim3 grid(dm.n_kv_heads, pl.splits, tiles * st.B);
+    hipLaunchKernelGGL(attn_paged_kernel<D>, grid, dim3(256), 0, stream, q, pa, partials, out, st, dm.n_heads, dm.n_kv_heads, tiles, pl.chunk, pl.splits);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || pl.splits == 1) return e;
+    const int per = 1024 / D;
+    hipLaunchKernelGGL(attn_paged_merge_kernel<D>, dim3((st.n * dm.n_heads + per - 1) / per), dim3(256), 0, stream, partials, out, st, dm.n_heads, dm.n_kv_heads,
+                       pa.cap, pl.chunk, pl.splits);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+// A tile holds at most 16 pairs, so rows * heads * splits is at most 16 tiles * splits <= 16 kPagedGroups wherever there is more than one split
+size_t paged_partial_floats(const relax_layer_dims &dm, int32_t n, int32_t L)
+{
+    const size_t most = (size_t)16 * kPagedGroups, mine = (size_t)n * dm.n_heads * (size_t)((L + 127) / 128);
+    return (mine < most ? mine : most) * (dm.head_dim + 2);
+}
+
+hipError_t launch_paged_attention(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const SeqTable &st, long long tiles_total, int32_t L_max,
+                                  uint16_t *out, float *partials, hipStream_t stream)
+{
+    const int rep = dm.n_heads / dm.n_kv_heads;
+    const int32_t tiles = (int32_t)(((long long)st.q_max * rep + 15) / 16);
+    const PagedPlan pl = paged_plan(tiles_total * dm.n_kv_heads, L_max);
+    return dm.head_dim == 128 ? launch_d<128>(q, pa, dm, st, tiles, pl, out, partials, stream) : launch_d<64>(q, pa, dm, st, tiles, pl, out, partials, stream);
+}
+
+}  // namespace relax
