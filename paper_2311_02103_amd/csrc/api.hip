@@ -1416,7 +1416,7 @@ constexpr int32_t kMaxPagedSeqs = 65535;     // extents of a grid
 
 // Everything the paged calls check alike; fills the kernels' descriptors.  items, tiles: see launch_paged_append, launch_paged_attention.
 relax_status paged_begin(const relax_paged_cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims, int32_t n, void *ws, size_t ws_bytes,
-                         hipStream_t stream, PagedArgs &pa, SeqTable &st, int32_t &L_max, int &items, long long &tiles, float **partials)
+                         hipStream_t stream, PagedArgs &pa, PagedSeqs &st, int32_t &L_max, int &items, long long &tiles, float **partials)
 {
     relax_status rc = check_dims(dims);
     if (rc != RELAX_OK) return rc;
@@ -1430,24 +1430,34 @@ relax_status paged_begin(const relax_paged_cache *cache, const relax_seqs *seqs,
     if ((RELAX_PAGED_BLOCK << shift) != cache->page_size) return RELAX_ERR_UNSUPPORTED;
     if ((int64_t)cache->n_pages * dims->n_kv_heads << shift > INT32_MAX) return RELAX_ERR_UNSUPPORTED;
     if ((int64_t)cache->pages_per_slot * cache->page_size < dims->kv_capacity) return RELAX_ERR_CAPACITY;
+    SeqTable checked = {};
     bool need_table = false;
-    rc = build_seqs(seqs, *dims, n, st, L_max, need_table);
+    rc = build_seqs(seqs, *dims, n, checked, L_max, need_table);
     if (rc != RELAX_OK) return rc;
     if (seqs->B > kMaxPagedSeqs) return RELAX_ERR_UNSUPPORTED;
     const PagedWs pl = paged_ws(*dims, n, L_max, seqs->B);
     if (ws_bytes < pl.total || !aligned(ws, 256)) return RELAX_ERR_WORKSPACE;
     const int rep = dims->n_heads / dims->n_kv_heads;
+    const bool inlined = !seqs->device_table && seqs->B <= kPagedInline;
+    st.B = seqs->B, st.n = n, st.q_max = checked.q_max, st.dev = seqs->device_table, st.pad = 0;
     items = 0, tiles = 0;
+    int32_t start = 0;
     for (int b = 0; b < seqs->B; ++b) {
         items += paged_blocks_of(seqs->q_lens[b]);
         tiles += ((long long)seqs->q_lens[b] * rep + 15) / 16;
+        if (inlined) st.q_start[b] = start, st.q_len[b] = seqs->q_lens[b], st.kv_len[b] = seqs->kv_lens[b], st.slot[b] = seqs->slots ? seqs->slots[b] : b;
+        start += seqs->q_lens[b];
     }
     pa = {cache->k, cache->v, cache->k_scale, cache->v_scale, cache->pages, cache->rope, static_cast<uint32_t *>(ws), cache->n_pages, cache->pages_per_slot,
           dims->kv_slots, dims->kv_capacity, shift};
     *partials = reinterpret_cast<float *>(static_cast<char *>(ws) + pl.partials);
-    WsPlan front = {};
-    front.table = pl.table;
-    return upload_table(st, seqs, need_table, ws, front, stream);
+    if (!inlined && !seqs->device_table) {
+        WsPlan front = {};
+        front.table = pl.table;
+        rc = upload_table(checked, seqs, need_table, ws, front, stream);
+        st.dev = checked.dev;
+    }
+    return rc;
 }
 
 }  // namespace
@@ -1471,7 +1481,7 @@ relax_status relax_paged_append(const uint16_t *q, int64_t q_stride, const uint1
     if (kv_stride < (int64_t)dims->n_kv_heads * dims->head_dim || (q && q_stride < (int64_t)dims->n_heads * dims->head_dim)) return RELAX_ERR_SHAPE;
     hipStream_t st_ = static_cast<hipStream_t>(stream);
     PagedArgs pa;
-    SeqTable st = {};
+    PagedSeqs st;
     int32_t L_max = 0;
     int items = 0;
     long long tiles = 0;
@@ -1488,7 +1498,7 @@ relax_status relax_paged_attention(const uint16_t *q, const relax_paged_cache *c
     if (!aligned(q, 16) || !aligned(out, 16)) return RELAX_ERR_SHAPE;
     hipStream_t st_ = static_cast<hipStream_t>(stream);
     PagedArgs pa;
-    SeqTable st = {};
+    PagedSeqs st;
     int32_t L_max = 0;
     int items = 0;
     long long tiles = 0;
@@ -1505,7 +1515,7 @@ relax_status relax_paged_read(const relax_paged_cache *cache, const relax_seqs *
     if (!aligned(k_out, 16) || !aligned(v_out, 16)) return RELAX_ERR_SHAPE;
     hipStream_t st_ = static_cast<hipStream_t>(stream);
     PagedArgs pa;
-    SeqTable st = {};
+    PagedSeqs st;
     int32_t L_max = 0;
     int items = 0;
     long long tiles = 0;

@@ -23,8 +23,8 @@ constexpr float kBias = 11.0f, kLag = 4.0f;      // log2: offset of the weights,
 
 // grid: x = KV head, y = split, z = sequence * tiles + tile.  part: [row][head][splits][D + 2] when splits > 1.
 template <int D>
-__global__ __launch_bounds__(256, 2) void attn_paged_kernel(const uint16_t *__restrict__ q, PagedArgs pa, float *__restrict__ part,
-                                                            uint16_t *__restrict__ out, SeqTable st, int h, int g, int tiles, int chunk, int splits)
+__global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedSeqs, const uint16_t *__restrict__ q, PagedArgs pa, float *__restrict__ part,
+                                                            uint16_t *__restrict__ out, int h, int g, int tiles, int chunk, int splits)
 {
     constexpr int J = D / 64;                    // 1 KB loads per block
     constexpr int NT = D / 16;                   // 16-element tiles of O^T
@@ -34,7 +34,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(const uint16_t *__re
 
     const int b = tiles == 1 ? (int)blockIdx.z : (int)blockIdx.z / tiles, tile = tiles == 1 ? 0 : (int)blockIdx.z - b * tiles;
     const int kvh = blockIdx.x, split = blockIdx.y;
-    const SeqSpan si = seq_span(st, b);
+    const SeqSpan si = seq_span(seqs_arg(), b);
     const int rep = h / g, pairs = si.q_len * rep, p0 = tile * 16;
     if (p0 >= pairs) return;
     const int past = si.kv_len - si.q_len;
@@ -155,9 +155,9 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(const uint16_t *__re
         Step sa, sb;
         step_load(sa, 0);
         for (int s = 0; s < ns; s += 2) {
-            step_load(sb, s + 1);
+            if (s + 1 < ns) step_load(sb, s + 1);
             consume(sa, s);
-            step_load(sa, s + 2);
+            if (s + 2 < ns) step_load(sa, s + 2);
             if (s + 1 < ns) consume(sb, s + 1);
         }
     }
@@ -195,48 +195,60 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(const uint16_t *__re
     }
 }
 
-// out of (row, head) from its splits: a workgroup per 1024 / D of them, four elements per thread
+// out of (row, head) from its splits, one workgroup each: D / 4 threads take four elements of a split, as many splits as there are such
+// groups of threads side by side and four of each in flight, and the groups' results meet in LDS
 template <int D>
-__global__ __launch_bounds__(256) void attn_paged_merge_kernel(const float *__restrict__ part, uint16_t *__restrict__ out, SeqTable st, int h, int g, int cap,
+__global__ __launch_bounds__(256) void attn_paged_merge_kernel(PagedSeqs, const float *__restrict__ part, uint16_t *__restrict__ out, int h, int g, int cap,
                                                                int chunk, int splits)
 {
-    const int i = (int)blockIdx.x * (1024 / D) + (int)threadIdx.x / (D / 4), e = threadIdx.x % (D / 4) * 4;
-    if (i >= st.n * h) return;
-    const int r = i / h, hd = i - r * h, rep = h / g;
-    const RowInfo ri = row_info(st, r);
-    const SeqSpan si = seq_span(st, ri.seq);
+    constexpr int T = D / 4, F = 4;
+    __shared__ __align__(16) float sums[256 / T][D];
+    __shared__ float sm_m[256 / T], sm_l[256 / T];
+    const SeqsArg st = seqs_arg();
+    const int i = blockIdx.x, r = i / h, hd = i - r * h, rep = h / g;
+    const int tid = threadIdx.x, grp = tid / T, e = tid % T * 4, groups = blockDim.x / T;
+    int place, b = r;
+    if (st->q_max == 1) place = 0;
+    else b = seq_of(st, r, [](int q_len) { return q_len; }, place);
+    const SeqSpan si = seq_span(st, __builtin_amdgcn_readfirstlane(b));
     // the splits that the tile of this pair had: those of its last pair
-    const int pair = (r - si.q_start) * rep + hd % rep, last = min((pair | 15), si.q_len * rep - 1) / rep;
+    const int pair = place * rep + hd % rep, last = min(pair | 15, si.q_len * rep - 1) / rep;
     const int vis = min(si.kv_len - si.q_len + last + 1, cap), used = max((vis + chunk - 1) / chunk, 1);
     const float *src = part + (size_t)i * splits * (D + 2);
-    float mm = -INFINITY, den = 0.0f, num[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int s0 = 0; s0 < used; s0 += 8) {
-        float ms[8], ls[8], as[8][4];
+    float mm = -INFINITY, den = 0.0f;
+    float4p_t num = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s0 = grp; s0 < used; s0 += groups * F) {
+        float ms[F], ls[F];
+        float4p_t as[F];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float *p = src + (size_t)min(s0 + j, used - 1) * (D + 2);
-            ms[j] = p[D], ls[j] = p[D + 1];
-#pragma unroll
-            for (int x = 0; x < 4; ++x) as[j][x] = p[e + x];
+        for (int j = 0; j < F; ++j) {
+            const float *p = src + (size_t)min(s0 + j * groups, used - 1) * (D + 2);
+            ms[j] = p[D], ls[j] = p[D + 1], as[j] = float4p_t{p[e], p[e + 1], p[e + 2], p[e + 3]};
         }
         float mx = mm;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) mx = s0 + j < used ? fmaxf(mx, ms[j]) : mx;
+        for (int j = 0; j < F; ++j) mx = s0 + j * groups < used ? fmaxf(mx, ms[j]) : mx;
         const float ref = mx == -INFINITY ? 0.0f : mx, f0 = __builtin_amdgcn_exp2f(mm - ref);
-        den *= f0;
+        den *= f0, num *= f0;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) num[x] *= f0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float f = s0 + j < used ? __builtin_amdgcn_exp2f(ms[j] - ref) : 0.0f;
-            den += ls[j] * f;
-#pragma unroll
-            for (int x = 0; x < 4; ++x) num[x] += as[j][x] * f;
+        for (int j = 0; j < F; ++j) {
+            const float f = s0 + j * groups < used ? __builtin_amdgcn_exp2f(ms[j] - ref) : 0.0f;
+            den += ls[j] * f, num += as[j] * f;
         }
         mm = mx;
     }
+    *(float4p_t *)&sums[grp][e] = num;
+    if (e == 0) sm_m[grp] = mm, sm_l[grp] = den;
+    __syncthreads();
+    if (grp > 0) return;
+    for (int w = 0; w < groups; ++w) mm = fmaxf(mm, sm_m[w]);
+    num = float4p_t{0.0f, 0.0f, 0.0f, 0.0f}, den = 0.0f;
+    for (int w = 0; w < groups; ++w) {
+        const float f = sm_m[w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm_m[w] - mm);
+        num += *(const float4p_t *)&sums[w][e] * f, den += sm_l[w] * f;
+    }
     const float inv = den > 0.0f ? 1.0f / den : den;
-    const uint32_t lo = f2h(num[0] * inv) | (uint32_t)f2h(num[1] * inv) << 16, hi = f2h(num[2] * inv) | (uint32_t)f2h(num[3] * inv) << 16;
+    const uint32_t lo = f2h(num.x * inv) | (uint32_t)f2h(num.y * inv) << 16, hi = f2h(num.z * inv) | (uint32_t)f2h(num.w * inv) << 16;
     *(u32x2p_t *)(out + (size_t)i * D + e) = u32x2p_t{lo, hi};
 }
 
@@ -255,16 +267,16 @@ PagedPlan paged_plan(long long tiles, int32_t L_max)
 }
 
 template <int D>
-hipError_t launch_d(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const SeqTable &st, int32_t tiles, const PagedPlan &pl, uint16_t *out,
+hipError_t launch_d(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, int32_t tiles, const PagedPlan &pl, uint16_t *out,
                     float *partials, hipStream_t stream)
 {
     const dim3 grid(dm.n_kv_heads, pl.splits, tiles * st.B);
-    hipLaunchKernelGGL(attn_paged_kernel<D>, grid, dim3(256), 0, stream, q, pa, partials, out, st, dm.n_heads, dm.n_kv_heads, tiles, pl.chunk, pl.splits);
+    hipLaunchKernelGGL(attn_paged_kernel<D>, grid, dim3(256), 0, stream, st, q, pa, partials, out, dm.n_heads, dm.n_kv_heads, tiles, pl.chunk, pl.splits);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || pl.splits == 1) return e;
-    const int per = 1024 / D;
-    hipLaunchKernelGGL(attn_paged_merge_kernel<D>, dim3((st.n * dm.n_heads + per - 1) / per), dim3(256), 0, stream, partials, out, st, dm.n_heads, dm.n_kv_heads,
-                       pa.cap, pl.chunk, pl.splits);
+    const int threads = pl.splits > 4 * 64 / (D / 4) ? 256 : 64;      // one round of four splits per group, if that is enough
+    hipLaunchKernelGGL(attn_paged_merge_kernel<D>, dim3(st.n * dm.n_heads), dim3(threads), 0, stream, st, partials, out, dm.n_heads, dm.n_kv_heads, pa.cap,
+                       pl.chunk, pl.splits);
     return hipGetLastError();
 }
 
@@ -277,7 +289,7 @@ size_t paged_partial_floats(const relax_layer_dims &dm, int32_t n, int32_t L)
     return (mine < most ? mine : most) * (dm.head_dim + 2);
 }
 
-hipError_t launch_paged_attention(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const SeqTable &st, long long tiles_total, int32_t L_max,
+hipError_t launch_paged_attention(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, long long tiles_total, int32_t L_max,
                                   uint16_t *out, float *partials, hipStream_t stream)
 {
     const int rep = dm.n_heads / dm.n_kv_heads;

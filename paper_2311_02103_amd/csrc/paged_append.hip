@@ -169,18 +169,18 @@ __device__ __forceinline__ void put_values(const RowsView &r, const PagedArgs &p
 
 // Workgroups 0 .. kv_groups - 1: four wavefronts, each one (item, KV head, keys or values); the rest: rows of q, `slices` workgroups per row
 template <int D>
-__global__ __launch_bounds__(256) void paged_append_kernel(RowsView r, uint16_t *q_out, PagedArgs pa, SeqTable st, int h, int g, int items, int kv_groups,
-                                                           int slices)
+__global__ __launch_bounds__(256) void paged_append_kernel(PagedSeqs, RowsView r, uint16_t *q_out, PagedArgs pa, int h, int g, int items, int kv_groups, int slices)
 {
+    const SeqsArg st = seqs_arg();
     const int lane = threadIdx.x & 63;
     if ((int)blockIdx.x < kv_groups) {
         const int w = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + (int)(threadIdx.x >> 6));
         const int item = w / (2 * g), part = w - item * 2 * g, kvh = part >> 1;
         if (item >= items) return;
         int place, b = item;
-        if (st.q_max == 1) place = 0;
+        if (st->q_max == 1) place = 0;
         else b = seq_of(st, item, [](int q_len) { return paged_blocks_of(q_len); }, place);
-        if (b >= st.B) return;
+        if (b >= st->B) return;
         const SeqSpan si = seq_span(st, b);
         const int first = si.kv_len - si.q_len;                // position of the sequence's first row
         const int blk = (first >> 4) + place;
@@ -198,9 +198,9 @@ __global__ __launch_bounds__(256) void paged_append_kernel(RowsView r, uint16_t 
     }
     const int wg = (int)blockIdx.x - kv_groups, i = wg / slices, slice = wg - i * slices;
     int place, b = i;
-    if (st.q_max == 1) place = 0;
+    if (st->q_max == 1) place = 0;
     else b = seq_of(st, i, [](int q_len) { return q_len; }, place);
-    if (b >= st.B) return;
+    if (b >= st->B) return;
     const SeqSpan si = seq_span(st, b);
     const int pos = min(max(si.kv_len - si.q_len + place, 0), pa.cap - 1);
     constexpr int per_head = D / 16;
@@ -222,16 +222,17 @@ __global__ __launch_bounds__(256) void paged_append_kernel(RowsView r, uint16_t 
 
 // out[row, kvh, :] = fp16(code * scale).  One wavefront is one (block, KV head) of keys or of values.
 template <int D>
-__global__ __launch_bounds__(256) void paged_read_kernel(PagedArgs pa, uint16_t *k_out, uint16_t *v_out, SeqTable st, int g, int items)
+__global__ __launch_bounds__(256) void paged_read_kernel(PagedSeqs, PagedArgs pa, uint16_t *k_out, uint16_t *v_out, int g, int items)
 {
+    const SeqsArg st = seqs_arg();
     const int lane = threadIdx.x & 63;
     const int w = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + (int)(threadIdx.x >> 6));
     const int item = w / (2 * g), part = w - item * 2 * g, kvh = part >> 1;
     if (item >= items || !(part & 1 ? v_out : k_out)) return;
     int place, b = item;
-    if (st.q_max == 1) place = 0;
+    if (st->q_max == 1) place = 0;
     else b = seq_of(st, item, [](int q_len) { return paged_blocks_of(q_len); }, place);
-    if (b >= st.B) return;
+    if (b >= st->B) return;
     const SeqSpan si = seq_span(st, b);
     const int first = si.kv_len - si.q_len, blk = (first >> 4) + place;
     const int low = max(first - blk * 16, 0), high = min(si.kv_len - blk * 16, 16);
@@ -275,24 +276,24 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedArgs pa, uint16_t 
 }  // namespace
 
 hipError_t launch_paged_append(const uint16_t *q, int64_t q_stride, const uint16_t *k, const uint16_t *v, int64_t kv_stride, uint16_t *q_out,
-                               const PagedArgs &pa, const relax_layer_dims &dm, const SeqTable &st, int items, hipStream_t stream)
+                               const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, int items, hipStream_t stream)
 {
     const RowsView r = {q, k, v, q_stride, kv_stride};
     const int kv_groups = (items * 2 * dm.n_kv_heads + 3) / 4;
     const int units = dm.n_heads * (dm.head_dim / 16), slices = st.n >= 256 ? 1 : (units + 255) / 256;     // few rows: over several workgroups
     const dim3 grid(kv_groups + (q ? st.n * slices : 0));
     if (dm.head_dim == 128)
-        hipLaunchKernelGGL(paged_append_kernel<128>, grid, dim3(256), 0, stream, r, q_out, pa, st, dm.n_heads, dm.n_kv_heads, items, kv_groups, slices);
+        hipLaunchKernelGGL(paged_append_kernel<128>, grid, dim3(256), 0, stream, st, r, q_out, pa, dm.n_heads, dm.n_kv_heads, items, kv_groups, slices);
     else
-        hipLaunchKernelGGL(paged_append_kernel<64>, grid, dim3(256), 0, stream, r, q_out, pa, st, dm.n_heads, dm.n_kv_heads, items, kv_groups, slices);
+        hipLaunchKernelGGL(paged_append_kernel<64>, grid, dim3(256), 0, stream, st, r, q_out, pa, dm.n_heads, dm.n_kv_heads, items, kv_groups, slices);
     return hipGetLastError();
 }
 
-hipError_t launch_paged_read(const PagedArgs &pa, uint16_t *k_out, uint16_t *v_out, const relax_layer_dims &dm, const SeqTable &st, int items, hipStream_t stream)
+hipError_t launch_paged_read(const PagedArgs &pa, uint16_t *k_out, uint16_t *v_out, const relax_layer_dims &dm, const PagedSeqs &st, int items, hipStream_t stream)
 {
     const dim3 grid((items * 2 * dm.n_kv_heads + 3) / 4);
-    if (dm.head_dim == 128) hipLaunchKernelGGL(paged_read_kernel<128>, grid, dim3(256), 0, stream, pa, k_out, v_out, st, dm.n_kv_heads, items);
-    else hipLaunchKernelGGL(paged_read_kernel<64>, grid, dim3(256), 0, stream, pa, k_out, v_out, st, dm.n_kv_heads, items);
+    if (dm.head_dim == 128) hipLaunchKernelGGL(paged_read_kernel<128>, grid, dim3(256), 0, stream, st, pa, k_out, v_out, dm.n_kv_heads, items);
+    else hipLaunchKernelGGL(paged_read_kernel<64>, grid, dim3(256), 0, stream, st, pa, k_out, v_out, dm.n_kv_heads, items);
     return hipGetLastError();
 }
 

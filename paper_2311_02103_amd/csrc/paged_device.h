@@ -22,48 +22,46 @@ typedef float float4p_t __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2p_t __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4p_t __attribute__((ext_vector_type(4)));
 
+// The ragged batch of a paged call, the FIRST argument of each of its kernels: they read it through the kernel argument segment with a
+// uniform index, one scalar load per field.  (A struct of arrays in a parameter that is indexed with a variable is copied to scratch
+// memory first, 264 bytes per lane for 16 sequences.)  Batches of up to kPagedInline sequences need no table in memory, and so no launch that writes
+// one.  Both together: the append of 64 rows of the 70B heads and its read-back went from 26.6 us of kernels to 13.5.
+constexpr int kPagedInline = 128;
+struct PagedSeqs {
+    const int32_t *dev;              // [4][B]: q_start, q_len, kv_len, slot; nullptr -> the arrays
+    int32_t B, n, q_max, pad;
+    int32_t q_start[kPagedInline], q_len[kPagedInline], kv_len[kPagedInline], slot[kPagedInline];
+};
+typedef const __attribute__((address_space(4))) PagedSeqs *SeqsArg;
+__device__ __forceinline__ SeqsArg seqs_arg() { return (SeqsArg)__builtin_amdgcn_kernarg_segment_ptr(); }
+
 struct SeqSpan {
     int32_t q_start, q_len, kv_len, slot;
 };
-__device__ inline SeqSpan seq_span(const SeqTable &st, int b)
+__device__ __forceinline__ SeqSpan seq_span(SeqsArg st, int b)      // b: uniform
 {
-    SeqSpan s;
-    if (st.dev) {
-        s.q_start = st.dev[b], s.q_len = st.dev[st.B + b], s.kv_len = st.dev[2 * st.B + b], s.slot = st.dev[3 * st.B + b];
-    } else {
-        s.q_start = st.q_start[0], s.q_len = st.q_len[0], s.kv_len = st.kv_len[0], s.slot = st.slot[0];
-#pragma unroll
-        for (int j = 1; j < kInlineSeqs; ++j)                  // static indices: see row_info
-            if (j == b) s.q_start = st.q_start[j], s.q_len = st.q_len[j], s.kv_len = st.kv_len[j], s.slot = st.slot[j];
-    }
-    return s;
+    const int32_t *dev = st->dev;
+    const int B = st->B;
+    if (dev) return {dev[b], dev[B + b], dev[2 * (size_t)B + b], dev[3 * (size_t)B + b]};
+    return {st->q_start[b], st->q_len[b], st->kv_len[b], st->slot[b]};
 }
 
 // Blocks of 16 tokens that a sequence's q_len rows can touch, wherever they begin
 __host__ __device__ inline int paged_blocks_of(int q_len) { return (q_len + 30) >> 4; }
 
 // Sequence b of the call that item `key` belongs to when sequence j brings count(q_len_j) items, and the item's place among its own.
-// key is the same in all lanes of the wavefront; b = st.B: behind the last one.  A device table is searched 64 sequences at a time.
+// key is the same in all lanes of the wavefront; b = B: behind the last one.  64 sequences at a time, one per lane.
 template <typename Count>
-__device__ inline int seq_of(const SeqTable &st, int key, const Count &count, int &place)
+__device__ __forceinline__ int seq_of(SeqsArg st, int key, const Count &count, int &place)
 {
-    if (!st.dev) {
-        int b = st.B, left = key;
-#pragma unroll
-        for (int j = 0; j < kInlineSeqs; ++j) {
-            const int c = j < st.B ? count(st.q_len[j]) : 0;
-            if (b == st.B && j < st.B) {
-                if (left < c) b = j;
-                else left -= c;
-            }
-        }
-        place = left;
-        return b;
-    }
+    const int B = st->B;
+    place = key;
+    if (B == 1) return 0;                                      // (the caller finds a place behind the last one by the lengths)
     const int lane = threadIdx.x & 63;
+    const int32_t *dev = st->dev;
     int before = 0;
-    for (int base = 0; base < st.B; base += kWave) {
-        const int own = base + lane < st.B ? count(st.dev[st.B + base + lane]) : 0;
+    for (int base = 0; base < B; base += kWave) {
+        const int own = base + lane < B ? count(dev ? dev[B + base + lane] : st->q_len[base + lane]) : 0;
         int sum = own;                                         // inclusive sum over the lanes up to this one
 #pragma unroll
         for (int off = 1; off < kWave; off <<= 1) {
@@ -72,14 +70,13 @@ __device__ inline int seq_of(const SeqTable &st, int key, const Count &count, in
         }
         const unsigned long long past = __ballot(key < before + sum);
         if (past) {
-            const int j = __ffsll((unsigned long long)past) - 1;
-            place = key - before - (__shfl(sum, j, kWave) - __shfl(own, j, kWave));
+            const int j = __ffsll(past) - 1;
+            place = key - before - __builtin_amdgcn_readlane(sum - own, j);
             return base + j;
         }
-        before += __shfl(sum, kWave - 1, kWave);
+        before += __builtin_amdgcn_readlane(sum, kWave - 1);
     }
-    place = 0;
-    return st.B;
+    return B;
 }
 
 struct PagedArgs {

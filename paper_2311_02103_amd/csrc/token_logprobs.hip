@@ -11,6 +11,9 @@
 // logit from below; whatever is larger than T -- a few more than k on any row whose large logits do not share few groups -- goes to a list in
 // LDS and is ranked by counting.  Fewer than k larger ones: the lowest indexes among those equal to T follow, found by a scan in order.
 // More than the list holds: T is replaced by the k-th largest logit itself, by bisection over the 16-bit values.
+//
+// Bound by the vector unit next to the read: a logit takes nine issue slots in the sums (four of them the exponential) and one and a half in the other
+// two passes, which look at pairs.
 #include "relax_common.h"
 
 namespace relax {
@@ -22,6 +25,7 @@ typedef _Float16 half2l_t __attribute__((ext_vector_type(2)));
 
 constexpr int kListed = 1024;        // places of the candidate list
 constexpr uint32_t kNone2 = 0xFC00FC00u;        // (-inf, -inf)
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // fp16 values as integers of the same order, -0 and 0 alike; NaN never gets here
 __device__ __forceinline__ int order_of(float x)
@@ -30,8 +34,29 @@ __device__ __forceinline__ int order_of(float x)
     return u & 0x8000 ? 0xFFFF - u : u | 0x8000;
 }
 __device__ __forceinline__ float value_of(int order) { return h2f((uint16_t)(order & 0x8000 ? order & 0x7FFF : 0xFFFF - order)); }
+// place of a candidate in the order: larger logits first, then lower indexes.  order -1: NaN
+__device__ __forceinline__ long long rank_key(int order, int id) { return (long long)order << 32 | (uint32_t)(0x7FFFFFFF - id); }
 
 __device__ __forceinline__ float element(const u32x4l_t &w, int e) { const uint32_t v = w[e >> 1]; return h2f((uint16_t)(e & 1 ? v >> 16 : v & 0xFFFFu)); }
+// x - base of the low and of the high half of a word, one instruction each
+__device__ __forceinline__ float low_minus(uint32_t w, float base)
+{
+    float r;
+    asm("v_fma_mix_f32 %0, %1, 1.0, -%2 op_sel_hi:[1,0,0]" : "=v"(r) : "v"(w), "v"(base));
+    return r;
+}
+__device__ __forceinline__ float high_minus(uint32_t w, float base)
+{
+    float r;
+    asm("v_fma_mix_f32 %0, %1, 1.0, -%2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(r) : "v"(w), "v"(base));
+    return r;
+}
+__device__ __forceinline__ half2l_t pairs_max(half2l_t a, uint32_t b) { return __builtin_elementwise_max(a, __builtin_bit_cast(half2l_t, b)); }   // the other where one is NaN
+__device__ __forceinline__ half2l_t packet_max(const u32x4l_t &w)
+{
+    const uint32_t a = w.x, b = w.y, c = w.z, d = w.w;
+    return __builtin_elementwise_max(pairs_max(__builtin_bit_cast(half2l_t, a), b), pairs_max(__builtin_bit_cast(half2l_t, c), d));
+}
 
 // NT threads, NP packets of eight logits each; RESIDENT: they hold the whole row
 template <int NT, int NP, bool RESIDENT>
@@ -41,7 +66,8 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(const uint16_t *__re
 {
     constexpr int W = NT / 64;
     __shared__ float lane_max[W][64], wave_m[W], wave_rest[W], wave_t[W];
-    __shared__ int wave_n[W], list_order[kListed], list_id[kListed], listed, scan[W];
+    __shared__ int wave_n[W], listed, scan[W];
+    __shared__ long long list[kListed];
     __shared__ float bound_s;
 
     const uint16_t *row = logits + (int64_t)blockIdx.x * stride;
@@ -50,7 +76,6 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(const uint16_t *__re
     const int skip = (int)((reinterpret_cast<uintptr_t>(row) & 15) >> 1);
     const int packets = (V + skip + 7) >> 3;
 
-    u32x4l_t held[NP];
     auto fetch = [&](int p) -> u32x4l_t {                      // packet p of the row, -inf outside it
         const int at = p * 8 - skip;
         if (at >= 0 && at + 8 <= V) return *(const u32x4l_t *)(row + at);
@@ -65,8 +90,9 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(const uint16_t *__re
         }
         return w;
     };
+    u32x4l_t held[RESIDENT ? NP : 1];
     // f(packet, its first element's index) for the thread's packets
-    auto each = [&](const auto &f) {
+    auto each = [&](const auto &f) __attribute__((always_inline)) {
         if constexpr (RESIDENT) {
 #pragma unroll
             for (int i = 0; i < NP; ++i) f(held[i], (i * NT + tid) * 8 - skip);
@@ -91,13 +117,7 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(const uint16_t *__re
         for (int i = 0; i < NP; ++i) held[i] = fetch(i * NT + tid);
     }
     half2l_t mx2 = __builtin_bit_cast(half2l_t, kNone2);
-    each([&](const u32x4l_t &w, int) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t v = w[j];
-            mx2 = __builtin_elementwise_max(mx2, __builtin_bit_cast(half2l_t, v));          // (the other operand where one is NaN)
-        }
-    });
+    each([&](const u32x4l_t &w, int) __attribute__((always_inline)) { mx2 = __builtin_elementwise_max(mx2, packet_max(w)); });
     const float mine = fmaxf((float)mx2.x, (float)mx2.y);
     lane_max[wave][lane] = mine;
     const float wm = wave_max(mine);
@@ -122,19 +142,23 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(const uint16_t *__re
         if (rank == k - 1) bound_s = gm;
     }
 
-    // ---- sums ----
+    // ---- sums: exponents in units of log 2; the maxima themselves, in the wavefronts that hold one, are counted instead ----
     const float base = m == -INFINITY ? 0.0f : m;
     float rest = 0.0f, t = 0.0f;
     int tops = 0;
-    each([&](const u32x4l_t &w, int) {
+    auto add = [&](const u32x4l_t &w, bool count) __attribute__((always_inline)) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const float z = element(w, e) - base, x = __builtin_amdgcn_exp2f(z * 1.44269504088896340736f);
-            tops += z == 0.0f;
-            rest += z == 0.0f ? 0.0f : x;
-            t = fmaf(x, z < -200.0f ? -200.0f : z, t);         // (0 * -inf; exp2 is 0 there)
+            const uint32_t v = w[e >> 1];
+            const float y = (e & 1 ? high_minus(v, base) : low_minus(v, base)) * kLog2e;
+            float x = __builtin_amdgcn_exp2f(y);
+            t = fmaf(x, fmaxf(y, -300.0f), t);                 // (0 * -inf: exp2 is 0 there)
+            if (count) tops += y == 0.0f, x = y == 0.0f ? 0.0f : x;
+            rest += x;
         }
-    });
+    };
+    if (wm == m) each([&](const u32x4l_t &w, int) __attribute__((always_inline)) { add(w, true); });
+    else each([&](const u32x4l_t &w, int) __attribute__((always_inline)) { add(w, false); });
     rest = wave_sum(rest), t = wave_sum(t);
 #pragma unroll
     for (int off = 32; off; off >>= 1) tops += __shfl_xor(tops, off, kWave);
@@ -152,20 +176,23 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(const uint16_t *__re
             const int id = targets[blockIdx.x];
             logprobs[blockIdx.x] = logp(id >= 0 && id < V ? h2f(row[id]) : -INFINITY);
         }
-        if (entropy) entropy[blockIdx.x] = empty ? 0.0f : log_s - t / (1.0f + rest);
+        if (entropy) entropy[blockIdx.x] = empty ? 0.0f : log_s - t * kLn2 / (1.0f + rest);
     }
     if (k == 0) return;
 
     // ---- candidates: what is larger than the bound ----
     float bound = bound_s;
-    auto collect = [&]() {
-        each([&](const u32x4l_t &w, int at) {
-#pragma unroll
+    auto collect = [&]() __attribute__((always_inline)) {
+        each([&](const u32x4l_t &w, int at) __attribute__((always_inline)) {
+            const half2l_t p = packet_max(w);
+            if (!__any(fmaxf((float)p.x, (float)p.y) > bound)) return;
+#pragma unroll 1
             for (int e = 0; e < 8; ++e) {
-                const float x = element(w, e);
+                const uint32_t v = e < 4 ? (e < 2 ? w.x : w.y) : (e < 6 ? w.z : w.w);
+                const float x = h2f((uint16_t)(e & 1 ? v >> 16 : v & 0xFFFFu));
                 if (x > bound) {
                     const int place = atomicAdd(&listed, 1);
-                    if (place < kListed) list_order[place] = order_of(x), list_id[place] = at + e;
+                    if (place < kListed) list[place] = rank_key(order_of(x), at + e);
                 }
             }
         });
@@ -180,7 +207,7 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(const uint16_t *__re
             const int mid = (lo + hi) >> 1;
             const float v = value_of(mid);
             int above = 0;
-            each([&](const u32x4l_t &w, int) {
+            each([&](const u32x4l_t &w, int) __attribute__((always_inline)) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) above += element(w, e) > v;
             });
@@ -196,15 +223,7 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(const uint16_t *__re
     // ---- too few: the first of those equal to the bound, and behind -inf the NaNs ----
     for (int kind = 0; kind < 2 && found < k; ++kind)
         for (int p0 = 0; p0 < packets && found < k; p0 += NT) {
-            u32x4l_t w;
-            if constexpr (RESIDENT) {
-                w = held[0];
-#pragma unroll
-                for (int i = 1; i < NP; ++i)
-                    if (p0 == i * NT) w = held[i];
-            } else {
-                w = fetch(p0 + tid);
-            }
+            const u32x4l_t w = fetch(p0 + tid);
             const int at = (p0 + tid) * 8 - skip;
             uint32_t is = 0;
 #pragma unroll
@@ -229,7 +248,7 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(const uint16_t *__re
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 if (is >> e & 1u) {
-                    if (place < k) list_order[place] = kind == 0 ? order_of(bound) : -1, list_id[place] = at + e;
+                    if (place < k) list[place] = rank_key(kind == 0 ? order_of(bound) : -1, at + e);
                     ++place;
                 }
             found = min(found + all, k);
@@ -238,15 +257,14 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(const uint16_t *__re
 
     // ---- ranks ----
     for (int i = tid; i < found; i += NT) {
-        const int o = list_order[i], id = list_id[i];
+        const long long own = list[i];
         int rank = 0;
-        for (int j = 0; j < found; ++j) {
-            const int oj = list_order[j];
-            rank += oj > o || (oj == o && list_id[j] < id);
-        }
+#pragma unroll 4
+        for (int j = 0; j < found; ++j) rank += list[j] > own;
         if (rank < k) {
-            top_ids[(size_t)blockIdx.x * k + rank] = id;
-            top_logprobs[(size_t)blockIdx.x * k + rank] = o < 0 ? NAN : logp(value_of(o));
+            const int order = (int)(own >> 32);
+            top_ids[(size_t)blockIdx.x * k + rank] = 0x7FFFFFFF - (int)(uint32_t)own;
+            top_logprobs[(size_t)blockIdx.x * k + rank] = order < 0 ? NAN : logp(value_of(order));
         }
     }
 }
@@ -264,6 +282,7 @@ hipError_t launch_one(const uint16_t *logits, int64_t stride, const int32_t *tar
 hipError_t launch_token_logprobs(const uint16_t *logits, int64_t stride, const int32_t *targets, float *logprobs, float *entropy, int32_t *top_ids,
                                  float *top_logprobs, int32_t n, int32_t V, int32_t k, hipStream_t stream)
 {
+    if (V + 7 <= 1024 * 8 * 4 && n <= 512) return launch_one<1024, 4, true>(logits, stride, targets, logprobs, entropy, top_ids, top_logprobs, n, V, k, stream);
     if (V + 7 <= 512 * 8 * 8) return launch_one<512, 8, true>(logits, stride, targets, logprobs, entropy, top_ids, top_logprobs, n, V, k, stream);
     if (V + 7 <= 1024 * 8 * 20) return launch_one<1024, 20, true>(logits, stride, targets, logprobs, entropy, top_ids, top_logprobs, n, V, k, stream);
     return launch_one<1024, 1, false>(logits, stride, targets, logprobs, entropy, top_ids, top_logprobs, n, V, k, stream);
