@@ -1414,9 +1414,9 @@ PagedWs paged_ws(const relax_layer_dims &dm, int32_t n, int32_t L, int32_t B)
 
 constexpr int32_t kMaxPagedSeqs = 65535;     // extents of a grid
 
-// Everything the paged calls check alike; fills the kernels' descriptors.  items, tiles: see launch_paged_append, launch_paged_attention.
+// Everything the paged calls check alike; fills the kernels' descriptors.  items: see launch_paged_append.
 relax_status paged_begin(const relax_paged_cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims, int32_t n, void *ws, size_t ws_bytes,
-                         hipStream_t stream, PagedArgs &pa, PagedSeqs &st, int32_t &L_max, int &items, long long &tiles, float **partials)
+                         hipStream_t stream, PagedArgs &pa, PagedSeqs &st, int32_t &L_max, int &items, float **partials)
 {
     relax_status rc = check_dims(dims);
     if (rc != RELAX_OK) return rc;
@@ -1437,14 +1437,12 @@ relax_status paged_begin(const relax_paged_cache *cache, const relax_seqs *seqs,
     if (seqs->B > kMaxPagedSeqs) return RELAX_ERR_UNSUPPORTED;
     const PagedWs pl = paged_ws(*dims, n, L_max, seqs->B);
     if (ws_bytes < pl.total || !aligned(ws, 256)) return RELAX_ERR_WORKSPACE;
-    const int rep = dims->n_heads / dims->n_kv_heads;
     const bool inlined = !seqs->device_table && seqs->B <= kPagedInline;
     st.B = seqs->B, st.n = n, st.q_max = checked.q_max, st.dev = seqs->device_table, st.pad = 0;
-    items = 0, tiles = 0;
+    items = 0;
     int32_t start = 0;
     for (int b = 0; b < seqs->B; ++b) {
         items += paged_blocks_of(seqs->q_lens[b]);
-        tiles += ((long long)seqs->q_lens[b] * rep + 15) / 16;
         if (inlined) st.q_start[b] = start, st.q_len[b] = seqs->q_lens[b], st.kv_len[b] = seqs->kv_lens[b], st.slot[b] = seqs->slots ? seqs->slots[b] : b;
         start += seqs->q_lens[b];
     }
@@ -1484,9 +1482,8 @@ relax_status relax_paged_append(const uint16_t *q, int64_t q_stride, const uint1
     PagedSeqs st;
     int32_t L_max = 0;
     int items = 0;
-    long long tiles = 0;
     float *partials = nullptr;
-    rc = paged_begin(cache, seqs, dims, n, ws, ws_bytes, st_, pa, st, L_max, items, tiles, &partials);
+    rc = paged_begin(cache, seqs, dims, n, ws, ws_bytes, st_, pa, st, L_max, items, &partials);
     if (rc != RELAX_OK) return rc;
     return hip_status(launch_paged_append(q, q_stride, k, v, kv_stride, q_out, pa, *dims, st, items, st_));
 }
@@ -1501,11 +1498,10 @@ relax_status relax_paged_attention(const uint16_t *q, const relax_paged_cache *c
     PagedSeqs st;
     int32_t L_max = 0;
     int items = 0;
-    long long tiles = 0;
     float *partials = nullptr;
-    const relax_status rc = paged_begin(cache, seqs, dims, n, ws, ws_bytes, st_, pa, st, L_max, items, tiles, &partials);
+    const relax_status rc = paged_begin(cache, seqs, dims, n, ws, ws_bytes, st_, pa, st, L_max, items, &partials);
     if (rc != RELAX_OK) return rc;
-    return hip_status(launch_paged_attention(q, pa, *dims, st, tiles, L_max, out, partials, st_));
+    return hip_status(launch_paged_attention(q, pa, *dims, st, *seqs, L_max, out, partials, st_));
 }
 
 relax_status relax_paged_read(const relax_paged_cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims, uint16_t *k_out, uint16_t *v_out,
@@ -1518,9 +1514,8 @@ relax_status relax_paged_read(const relax_paged_cache *cache, const relax_seqs *
     PagedSeqs st;
     int32_t L_max = 0;
     int items = 0;
-    long long tiles = 0;
     float *partials = nullptr;
-    const relax_status rc = paged_begin(cache, seqs, dims, n, ws, ws_bytes, st_, pa, st, L_max, items, tiles, &partials);
+    const relax_status rc = paged_begin(cache, seqs, dims, n, ws, ws_bytes, st_, pa, st, L_max, items, &partials);
     if (rc != RELAX_OK) return rc;
     return hip_status(launch_paged_read(pa, k_out, v_out, *dims, st, items, st_));
 }

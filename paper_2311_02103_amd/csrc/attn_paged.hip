@@ -13,6 +13,8 @@
 // one the result.  exp2's argument is offset by 11 in return: the largest probability is at most 2^15 (the reference trails the maximum by
 // at most 2^4) and one of 2^-39 of it still is a subnormal fp16 number.  Scores, sums and O are fp32; the rounding of the probabilities (2^-11 relative, independent
 // from token to token) is the only one between the codes and the result.
+#include <algorithm>
+
 #include "paged_device.h"
 
 namespace relax {
@@ -24,7 +26,7 @@ constexpr float kBias = 11.0f, kLag = 4.0f;      // log2: offset of the weights,
 // grid: x = KV head, y = split, z = sequence * tiles + tile.  part: [row][head][splits][D + 2] when splits > 1.
 template <int D>
 __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedSeqs, const uint16_t *__restrict__ q, PagedArgs pa, float *__restrict__ part,
-                                                            uint16_t *__restrict__ out, int h, int g, int tiles, int chunk, int splits)
+                                                            uint16_t *__restrict__ out, int h, int g, int tiles, int chunk, int splits, int least)
 {
     constexpr int J = D / 64;                    // 1 KB loads per block
     constexpr int NT = D / 16;                   // 16-element tiles of O^T
@@ -36,7 +38,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedSeqs, const uin
     const int kvh = blockIdx.x, split = blockIdx.y;
     const SeqSpan si = seq_span(seqs_arg(), b);
     const int rep = h / g, pairs = si.q_len * rep, p0 = tile * 16;
-    if (p0 >= pairs) return;
+    if (pairs >= least || p0 >= pairs) return;
     const int past = si.kv_len - si.q_len;
     const int n_pairs = min(16, pairs - p0);
     const int pos_min = past + p0 / rep, vis = min(past + (p0 + n_pairs - 1) / rep + 1, pa.cap);      // tokens that any of the pairs attends to
@@ -199,7 +201,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedSeqs, const uin
 // groups of threads side by side and four of each in flight, and the groups' results meet in LDS
 template <int D>
 __global__ __launch_bounds__(256) void attn_paged_merge_kernel(PagedSeqs, const float *__restrict__ part, uint16_t *__restrict__ out, int h, int g, int cap,
-                                                               int chunk, int splits)
+                                                               int chunk, int splits, int least, int ct)
 {
     constexpr int T = D / 4, F = 4;
     __shared__ __align__(16) float sums[256 / T][D];
@@ -212,7 +214,7 @@ __global__ __launch_bounds__(256) void attn_paged_merge_kernel(PagedSeqs, const 
     else b = seq_of(st, r, [](int q_len) { return q_len; }, place);
     const SeqSpan si = seq_span(st, __builtin_amdgcn_readfirstlane(b));
     // the splits that the tile of this pair had: those of its last pair
-    const int pair = place * rep + hd % rep, last = min(pair | 15, si.q_len * rep - 1) / rep;
+    const int pairs = si.q_len * rep, pair = place * rep + hd % rep, last = min(pair | (pairs < least ? 15 : 64 * ct - 1), pairs - 1) / rep;
     const int vis = min(si.kv_len - si.q_len + last + 1, cap), used = max((vis + chunk - 1) / chunk, 1);
     const float *src = part + (size_t)i * splits * (D + 2);
     float mm = -INFINITY, den = 0.0f;
@@ -252,50 +254,80 @@ __global__ __launch_bounds__(256) void attn_paged_merge_kernel(PagedSeqs, const 
     *(u32x2p_t *)(out + (size_t)i * D + e) = u32x2p_t{lo, hi};
 }
 
-// Splits of a launch with `tiles` workgroups per split: as many as bring it to kPagedGroups workgroups, none shorter than 128 tokens
-constexpr int kPagedGroups = 1024;
-struct PagedPlan {
-    int32_t chunk, splits;
-};
-PagedPlan paged_plan(long long tiles, int32_t L_max)
+constexpr int kPagedGroups = 1024;       // workgroups that a launch of 16-pair tiles is split up to, ...
+constexpr int kRowsGroups = 512;         // ... one of larger tiles, ...
+constexpr int kPartials = 65536;         // ... and partial results (row, head, split) that a call may leave at most
+
+// Sequences with at least 64 pairs take the tiles of 64 pairs and more; short ones, and few of them, are ahead with 16.
+constexpr int kLeastPairs = 33;
+
+PagedRows plan(const relax_layer_dims &dm, const relax_seqs &sq, int32_t n, int32_t L_max)
 {
-    long long s = kPagedGroups / (tiles > 0 ? tiles : 1), most = (L_max + 127) / 128;
-    s = s > most ? most : s;
+    const int rep = dm.n_heads / dm.n_kv_heads;
+    long long large[2] = {0, 0}, small = 0, most = 0;            // tiles of 64 and 128 pairs; of 16
+    for (int b = 0; b < sq.B; ++b) {
+        const long long pairs = (long long)sq.q_lens[b] * rep;
+        if (pairs < kLeastPairs) small += (pairs + 15) / 16;
+        else
+            for (int i = 0; i < 2; ++i) large[i] += (pairs + (64 << i) - 1) / (64 << i);
+        most = pairs > most ? pairs : most;
+    }
+    PagedRows p;
+    p.least = kLeastPairs;
+    const int pick = large[1] * dm.n_kv_heads >= 256 ? 1 : 0;
+    p.ct = 1 << pick;
+    p.tiles = most >= kLeastPairs ? (int32_t)((most + 64 * p.ct - 1) / (64 * p.ct)) : 0;
+    const long long groups = (small + large[pick]) * dm.n_kv_heads, target = large[pick] ? kRowsGroups : kPagedGroups;
+    const int32_t shortest = large[pick] ? 256 : 128;
+    long long s = target / groups;
+    s = std::min(s, (long long)(L_max + shortest - 1) / shortest);
+    s = std::min(s, (long long)kPartials / ((long long)n * dm.n_heads));
     s = s < 1 ? 1 : s;
-    const int32_t chunk = (int32_t)(((L_max + s - 1) / s + 31) / 32 * 32);
-    return {chunk, (L_max + chunk - 1) / chunk};
+    p.chunk = (int32_t)(((L_max + s - 1) / s + 63) / 64 * 64);
+    p.splits = (L_max + p.chunk - 1) / p.chunk;
+    return p;
 }
 
 template <int D>
-hipError_t launch_d(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, int32_t tiles, const PagedPlan &pl, uint16_t *out,
+hipError_t launch_d(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, int32_t small_most, const PagedRows &pl, uint16_t *out,
                     float *partials, hipStream_t stream)
 {
-    const dim3 grid(dm.n_kv_heads, pl.splits, tiles * st.B);
-    hipLaunchKernelGGL(attn_paged_kernel<D>, grid, dim3(256), 0, stream, st, q, pa, partials, out, dm.n_heads, dm.n_kv_heads, tiles, pl.chunk, pl.splits);
-    const hipError_t e = hipGetLastError();
+    hipError_t e = hipSuccess;
+    if (pl.tiles > 0) e = launch_paged_rows(q, pa, dm, st, pl, out, partials, stream);
+    if (e != hipSuccess) return e;
+    if (small_most > 0) {
+        const int32_t tiles = (small_most + 15) / 16;
+        hipLaunchKernelGGL(attn_paged_kernel<D>, dim3(dm.n_kv_heads, pl.splits, tiles * st.B), dim3(256), 0, stream, st, q, pa, partials, out, dm.n_heads, dm.n_kv_heads,
+                           tiles, pl.chunk, pl.splits, pl.least);
+        e = hipGetLastError();
+    }
     if (e != hipSuccess || pl.splits == 1) return e;
-    const int threads = pl.splits > 4 * 64 / (D / 4) ? 256 : 64;      // one round of four splits per group, if that is enough
+    const int threads = pl.splits > 4 * 64 / (D / 4) ? 256 : 64;      // one round of four splits per group of threads, if that is enough
     hipLaunchKernelGGL(attn_paged_merge_kernel<D>, dim3(st.n * dm.n_heads), dim3(threads), 0, stream, st, partials, out, dm.n_heads, dm.n_kv_heads, pa.cap,
-                       pl.chunk, pl.splits);
+                       pl.chunk, pl.splits, pl.least, pl.ct);
     return hipGetLastError();
 }
 
 }  // namespace
 
-// A tile holds at most 16 pairs, so rows * heads * splits is at most 16 tiles * splits <= 16 kPagedGroups wherever there is more than one split
+// more than one split leaves n * heads * splits <= kPartials, no split but the last is shorter than 128 tokens
 size_t paged_partial_floats(const relax_layer_dims &dm, int32_t n, int32_t L)
 {
-    const size_t most = (size_t)16 * kPagedGroups, mine = (size_t)n * dm.n_heads * (size_t)((L + 127) / 128);
+    const size_t most = kPartials, mine = (size_t)n * dm.n_heads * (size_t)((L + 127) / 128);
     return (mine < most ? mine : most) * (dm.head_dim + 2);
 }
 
-hipError_t launch_paged_attention(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, long long tiles_total, int32_t L_max,
+hipError_t launch_paged_attention(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, const relax_seqs &sq, int32_t L_max,
                                   uint16_t *out, float *partials, hipStream_t stream)
 {
+    const PagedRows pl = plan(dm, sq, st.n, L_max);
     const int rep = dm.n_heads / dm.n_kv_heads;
-    const int32_t tiles = (int32_t)(((long long)st.q_max * rep + 15) / 16);
-    const PagedPlan pl = paged_plan(tiles_total * dm.n_kv_heads, L_max);
-    return dm.head_dim == 128 ? launch_d<128>(q, pa, dm, st, tiles, pl, out, partials, stream) : launch_d<64>(q, pa, dm, st, tiles, pl, out, partials, stream);
+    int32_t small_most = 0;
+    for (int b = 0; b < sq.B; ++b) {
+        const long long pairs = (long long)sq.q_lens[b] * rep;
+        if (pairs < pl.least && pairs > small_most) small_most = (int32_t)pairs;
+    }
+    return dm.head_dim == 128 ? launch_d<128>(q, pa, dm, st, small_most, pl, out, partials, stream) : launch_d<64>(q, pa, dm, st, small_most, pl, out, partials, stream);
 }
 
 }  // namespace relax

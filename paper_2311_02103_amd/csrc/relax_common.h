@@ -497,15 +497,15 @@ bool attn_prefill_supported(const relax_layer_dims &dm);
 hipError_t launch_attention_prefill(const uint16_t *q, int32_t q_stride, const relax_kv_cache &cache, const relax_layer_dims &dm,
                                     const SeqTable &st, int32_t L_max, uint16_t *out, hipStream_t stream);
 
-// Paged 8-bit KV cache (paged_append.hip, attn_paged.hip; PagedArgs: paged_device.h).  items: blocks of 16 tokens that the call's sequences can touch, tiles:
-// groups of 16 (row, query head of the group) pairs over all sequences, both from the q_lens.
+// Paged 8-bit KV cache (paged_append.hip, attn_paged.hip; PagedArgs: paged_device.h).  items: blocks of 16 tokens that the call's sequences can
+// touch.
 struct PagedArgs;
 struct PagedSeqs;
 hipError_t launch_paged_append(const uint16_t *q, int64_t q_stride, const uint16_t *k, const uint16_t *v, int64_t kv_stride, uint16_t *q_out,
                                const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, int items, hipStream_t stream);
 hipError_t launch_paged_read(const PagedArgs &pa, uint16_t *k_out, uint16_t *v_out, const relax_layer_dims &dm, const PagedSeqs &st, int items, hipStream_t stream);
 size_t paged_partial_floats(const relax_layer_dims &dm, int32_t n, int32_t L);
-hipError_t launch_paged_attention(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, long long tiles, int32_t L_max,
+hipError_t launch_paged_attention(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, const relax_seqs &sq, int32_t L_max,
                                   uint16_t *out, float *partials, hipStream_t stream);
 
 // Log probabilities of rows of logits (token_logprobs.hip)
