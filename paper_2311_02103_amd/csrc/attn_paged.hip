@@ -71,20 +71,12 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedSeqs, const uin
     for (int seg = w_begin; seg < w_end; seg += kWave) {
         // ---- lane j: number in the pool and scales of block seg + j ----
         int pool = -1;
-        float ks = 0.0f, vs = 0.0f;
         if (seg + lane < w_end) {
             pool = paged_block(pa, g, kvh, si.slot, seg + lane);
             if (pool < 0) atomicOr(pa.err, kBadPage);
-            else ks = pa.k_scale[pool] * c, vs = pa.v_scale[pool];
         }
-        const float ref = fmaxf(v_ref, wave_max(vs));
-        if (v_ref > 0.0f && ref > v_ref) {                     // later blocks have larger values: O is in units of the largest scale
-            const float f = v_ref / ref;
-#pragma unroll
-            for (int i = 0; i < NT; ++i) O[i] *= f;
-        }
-        v_ref = ref;
-        const float vr = ref > 0.0f ? vs / ref : 0.0f;
+        float ks = pa.k_scale[max(pool, 0)], vs = pa.v_scale[max(pool, 0)];
+        const int ns = (min(w_end - seg, kWave) + 1) >> 1;
 
         struct Step {
             u32x4p_t k[2 * J], v[2 * J];
@@ -100,6 +92,21 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedSeqs, const uin
                 for (int j = 0; j < J; ++j) sp.v[t * J + j] = stream_load(vp + j * 64 + lane);
             }
         };
+        // the first steps are on their way before the scales are needed, and the scales ahead of them
+        Step sa, sb;
+        __builtin_amdgcn_sched_barrier(0);
+        step_load(sa, 0);
+        if (ns > 1) step_load(sb, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        ks = pool < 0 ? 0.0f : ks * c, vs = pool < 0 ? 0.0f : vs;
+        const float ref = fmaxf(v_ref, wave_max(vs));
+        if (v_ref > 0.0f && ref > v_ref) {                     // later blocks have larger values: O is in units of the largest scale
+            const float f = v_ref / ref;
+#pragma unroll
+            for (int i = 0; i < NT; ++i) O[i] *= f;
+        }
+        v_ref = ref;
+        const float vr = ref > 0.0f ? vs / ref : 0.0f;
         auto consume = [&](const Step &sp, int s) {
             float x[8];
             float mx = -INFINITY;
@@ -153,15 +160,16 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedSeqs, const uin
             for (int i = 0; i < NT; ++i)
                 O[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_half8(sp.v[i >> 2][i & 3], sp.v[J + (i >> 2)][i & 3]), pf, O[i], 0, 0, 0);
         };
-        const int ns = (min(w_end - seg, kWave) + 1) >> 1;
-        Step sa, sb;
-        step_load(sa, 0);
-        for (int s = 0; s < ns; s += 2) {
-            if (s + 1 < ns) step_load(sb, s + 1);
+        // no request behind a branch in the loop: the wait for one step would be for the other, too
+        int s = 0;
+        for (; s + 2 < ns; s += 2) {
             consume(sa, s);
-            if (s + 2 < ns) step_load(sa, s + 2);
-            if (s + 1 < ns) consume(sb, s + 1);
+            step_load(sa, s + 2);
+            consume(sb, s + 1);
+            step_load(sb, min(s + 3, ns - 1));
         }
+        consume(sa, s);
+        if (s + 1 < ns) consume(sb, s + 1);
     }
 
     // ---- the four states meet in LDS ----
@@ -201,7 +209,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedSeqs, const uin
 // groups of threads side by side and four of each in flight, and the groups' results meet in LDS
 template <int D>
 __global__ __launch_bounds__(256) void attn_paged_merge_kernel(PagedSeqs, const float *__restrict__ part, uint16_t *__restrict__ out, int h, int g, int cap,
-                                                               int chunk, int splits, int least, int ct)
+                                                               int chunk, int splits, int least)
 {
     constexpr int T = D / 4, F = 4;
     __shared__ __align__(16) float sums[256 / T][D];
@@ -214,7 +222,8 @@ __global__ __launch_bounds__(256) void attn_paged_merge_kernel(PagedSeqs, const 
     else b = seq_of(st, r, [](int q_len) { return q_len; }, place);
     const SeqSpan si = seq_span(st, __builtin_amdgcn_readfirstlane(b));
     // the splits that the tile of this pair had: those of its last pair
-    const int pairs = si.q_len * rep, pair = place * rep + hd % rep, last = min(pair | (pairs < least ? 15 : 64 * ct - 1), pairs - 1) / rep;
+    const int pairs = si.q_len * rep, pair = place * rep + hd % rep, last = min(pair | 15, pairs - 1) / rep;
+    if (pairs >= least) return;                                // (not split: the other kernel's)
     const int vis = min(si.kv_len - si.q_len + last + 1, cap), used = max((vis + chunk - 1) / chunk, 1);
     const float *src = part + (size_t)i * splits * (D + 2);
     float mm = -INFINITY, den = 0.0f;
@@ -254,57 +263,60 @@ __global__ __launch_bounds__(256) void attn_paged_merge_kernel(PagedSeqs, const 
     *(u32x2p_t *)(out + (size_t)i * D + e) = u32x2p_t{lo, hi};
 }
 
-constexpr int kPagedGroups = 1024;       // workgroups that a launch of 16-pair tiles is split up to, ...
-constexpr int kRowsGroups = 512;         // ... one of larger tiles, ...
-constexpr int kPartials = 65536;         // ... and partial results (row, head, split) that a call may leave at most
+// Splits of a launch with `small` workgroups per split: as many as bring it to kPagedGroups workgroups, none but the last shorter than 128 tokens, and no more
+// than kPartials partial results (row, head, split).  More splits where sequences are short of the longest one (as many as make kPagedGroups workgroups with
+// tokens) cost more in the merge than they balance: 8 x 5 rows of 32 / 8 heads 20.4 -> 24.8 us, 16 decode rows of 64 / 8 heads the same.
+constexpr int kPagedGroups = 1024, kPartials = 65536;
 
-// Sequences with at least 64 pairs take the tiles of 64 pairs and more; short ones, and few of them, are ahead with 16.
-constexpr int kLeastPairs = 33;
+// The kernel of 256-pair tiles takes the sequences that fill one, in calls that have kRowTiles such tiles over all KV heads: it halves the time of long prompts
+// and loses on the rest, where its workgroups are few and each waits 5 us for its first tile (us, tiles of 16 / of 256; heads of 128): 2048 rows of 32 / 32 heads
+// (256 tiles) 114 / 73, 1000 rows on 300 tokens of 40 / 40 (160) 59 / 51, 511 rows of 64 / 8 (128) 24 / 37, 300 rows on 1201 of 32 / 32 (64) 28 / 34,
+// 600 rows on 500 tokens of 16 / 2 heads of 64 (38) 14.5 / 24.
+constexpr int kRowTiles = 160;
 
-PagedRows plan(const relax_layer_dims &dm, const relax_seqs &sq, int32_t n, int32_t L_max)
+struct Plan {
+    int32_t least;                   // pairs from which a sequence is the other kernel's
+    int32_t row_tiles, tiles;        // at most per sequence, of 256 and of 16 pairs
+    int32_t chunk, splits;
+};
+
+Plan plan(const relax_layer_dims &dm, const relax_seqs &sq, int32_t n, int32_t L_max)
 {
     const int rep = dm.n_heads / dm.n_kv_heads;
-    long long large[2] = {0, 0}, small = 0, most = 0;            // tiles of 64 and 128 pairs; of 16
+    auto pairs_of = [&](int b) { return (long long)sq.q_lens[b] * rep; };
+    long long large = 0;
+    for (int b = 0; b < sq.B; ++b)
+        if (pairs_of(b) >= kPagedRowTile) large += (pairs_of(b) + kPagedRowTile - 1) / kPagedRowTile;
+    Plan p;
+    p.least = large * dm.n_kv_heads >= kRowTiles ? kPagedRowTile : INT32_MAX;
+    long long small = 0, most_small = 0, most_large = 0;
     for (int b = 0; b < sq.B; ++b) {
-        const long long pairs = (long long)sq.q_lens[b] * rep;
-        if (pairs < kLeastPairs) small += (pairs + 15) / 16;
-        else
-            for (int i = 0; i < 2; ++i) large[i] += (pairs + (64 << i) - 1) / (64 << i);
-        most = pairs > most ? pairs : most;
+        const long long pairs = pairs_of(b);
+        if (pairs >= p.least) most_large = std::max(most_large, pairs);
+        else small += (pairs + 15) / 16, most_small = std::max(most_small, pairs);
     }
-    PagedRows p;
-    p.least = kLeastPairs;
-    const int pick = large[1] * dm.n_kv_heads >= 256 ? 1 : 0;
-    p.ct = 1 << pick;
-    p.tiles = most >= kLeastPairs ? (int32_t)((most + 64 * p.ct - 1) / (64 * p.ct)) : 0;
-    const long long groups = (small + large[pick]) * dm.n_kv_heads, target = large[pick] ? kRowsGroups : kPagedGroups;
-    const int32_t shortest = large[pick] ? 256 : 128;
-    long long s = target / groups;
-    s = std::min(s, (long long)(L_max + shortest - 1) / shortest);
+    p.row_tiles = (int32_t)((most_large + kPagedRowTile - 1) / kPagedRowTile);
+    p.tiles = (int32_t)((most_small + 15) / 16);
+    long long s = small ? kPagedGroups / (small * dm.n_kv_heads) : 1;
+    s = std::min(s, (long long)(L_max + 127) / 128);
     s = std::min(s, (long long)kPartials / ((long long)n * dm.n_heads));
-    s = s < 1 ? 1 : s;
-    p.chunk = (int32_t)(((L_max + s - 1) / s + 63) / 64 * 64);
+    s = std::max(s, 1LL);
+    p.chunk = (int32_t)(((L_max + s - 1) / s + 31) / 32 * 32);
     p.splits = (L_max + p.chunk - 1) / p.chunk;
     return p;
 }
 
 template <int D>
-hipError_t launch_d(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, int32_t small_most, const PagedRows &pl, uint16_t *out,
-                    float *partials, hipStream_t stream)
+hipError_t launch_d(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, const Plan &pl, uint16_t *out, float *partials,
+                    hipStream_t stream)
 {
-    hipError_t e = hipSuccess;
-    if (pl.tiles > 0) e = launch_paged_rows(q, pa, dm, st, pl, out, partials, stream);
-    if (e != hipSuccess) return e;
-    if (small_most > 0) {
-        const int32_t tiles = (small_most + 15) / 16;
-        hipLaunchKernelGGL(attn_paged_kernel<D>, dim3(dm.n_kv_heads, pl.splits, tiles * st.B), dim3(256), 0, stream, st, q, pa, partials, out, dm.n_heads, dm.n_kv_heads,
-                           tiles, pl.chunk, pl.splits, pl.least);
-        e = hipGetLastError();
-    }
+    hipLaunchKernelGGL(attn_paged_kernel<D>, dim3(dm.n_kv_heads, pl.splits, pl.tiles * st.B), dim3(256), 0, stream, st, q, pa, partials, out, dm.n_heads, dm.n_kv_heads,
+                       pl.tiles, pl.chunk, pl.splits, pl.least);
+    const hipError_t e = hipGetLastError();
     if (e != hipSuccess || pl.splits == 1) return e;
     const int threads = pl.splits > 4 * 64 / (D / 4) ? 256 : 64;      // one round of four splits per group of threads, if that is enough
     hipLaunchKernelGGL(attn_paged_merge_kernel<D>, dim3(st.n * dm.n_heads), dim3(threads), 0, stream, st, partials, out, dm.n_heads, dm.n_kv_heads, pa.cap,
-                       pl.chunk, pl.splits, pl.least, pl.ct);
+                       pl.chunk, pl.splits, pl.least);
     return hipGetLastError();
 }
 
@@ -320,14 +332,12 @@ size_t paged_partial_floats(const relax_layer_dims &dm, int32_t n, int32_t L)
 hipError_t launch_paged_attention(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, const relax_seqs &sq, int32_t L_max,
                                   uint16_t *out, float *partials, hipStream_t stream)
 {
-    const PagedRows pl = plan(dm, sq, st.n, L_max);
-    const int rep = dm.n_heads / dm.n_kv_heads;
-    int32_t small_most = 0;
-    for (int b = 0; b < sq.B; ++b) {
-        const long long pairs = (long long)sq.q_lens[b] * rep;
-        if (pairs < pl.least && pairs > small_most) small_most = (int32_t)pairs;
+    const Plan pl = plan(dm, sq, st.n, L_max);
+    if (pl.row_tiles > 0) {
+        const hipError_t e = launch_paged_rows(q, pa, dm, st, pl.row_tiles, pl.least, out, stream);
+        if (e != hipSuccess || pl.tiles == 0) return e;
     }
-    return dm.head_dim == 128 ? launch_d<128>(q, pa, dm, st, small_most, pl, out, partials, stream) : launch_d<64>(q, pa, dm, st, small_most, pl, out, partials, stream);
+    return dm.head_dim == 128 ? launch_d<128>(q, pa, dm, st, pl, out, partials, stream) : launch_d<64>(q, pa, dm, st, pl, out, partials, stream);
 }
 
 }  // namespace relax

@@ -1,18 +1,23 @@
 // Causal attention over the paged 8-bit KV cache for sequences that bring many (row, head) pairs: prompts, and drafts of long groups.
 //
 // The mathematics, the transposed products, the fragments and the scales are those of attn_paged.hip; here the pairs are many enough to share
-// what a tile of the cache costs.  A workgroup takes 64 CT pairs against one KV head and one split of the tokens, each of its four wavefronts 16 CT of
-// them, and all four meet every tile of 64 tokens in LDS, as fp16 integers in the order of the fragments: the codes are turned into halves
+// what a tile of the cache costs.  A workgroup takes 256 pairs against one KV head and all tokens they see, each of its eight wavefronts 32 of
+// them, and all eight meet every tile of 64 tokens in LDS, as fp16 integers in the order of the fragments: the codes are turned into halves
 // once per workgroup (in the wavefronts they would cost as many issue slots as the softmax), and every read and write is 16 consecutive bytes per lane (V writes
 // 8).  Keys and values have two buffers each.
 //
-// Per 32 tokens and wavefront the matrix pipe has 16 CT MFMAs of 16 cycles, the vector unit about 7 issue slots of 4 cycles for each of 8 CT scores (four of them the
-// exponential) next to staging, and LDS 16 KB for the four wavefronts: at CT = 2 512, 600 and 512 cycles.  None of the three may wait for another, so the
-// order is written out: the scores of the next 32 tokens are computed between the exponentials of these, the products with V between the staging of the next
-// tile, and the operands of both are read PD steps ahead.
+// Per 32 tokens a wavefront has 34 MFMAs of 16 cycles and about 75 vector instructions and 16 exponentials: some 500 cycles of the matrix pipe and as many of
+// the vector unit.  Two wavefronts share a SIMD, one of each half of the workgroup, and the halves
+// take turns: while wavefronts 0 .. 3 multiply (this step's weights with V, the next step's keys with Q), wavefronts 4 .. 7 compute weights and stage their
+// part of the next tile, then the other way round, with a barrier between the turns.  4096 tokens, 32 / 8 heads of 128: 149 us (0.92 PFLOP/s of the causal half); with
+// four wavefronts per workgroup left to themselves, scores and exponentials in one stream of instructions, 170 (the matrix pipe busy 34 % of the time).
+// A turn takes about 1000 cycles at 2 GHz where 544 of the matrix pipe would do: next to the other half's vector work its 34 MFMAs take 970, alone 660.
 //
-// The value scale of a block goes into the exponent here, log2 of its ratio to the largest scale so far, and the block's sum of weights is
-// multiplied by the inverse ratio: one operation per four scores instead of one per score.
+// The value scale of a block, relative to the largest so far, multiplies its codes on their way into LDS here, one more rounding to fp16 (2^-11 of the value;
+// below 2^-32 of the largest value of the split it is coarser): the weights then need no scale of their own, and their sum is one more MFMA
+// with a tile of ones, of the weights as they are rounded for the products.
+#include <type_traits>
+
 #include "paged_device.h"
 
 namespace relax {
@@ -30,41 +35,41 @@ __device__ __forceinline__ void lds_barrier()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-constexpr int kSegment = 768;                    // blocks whose numbers and scales are in LDS at a time
+constexpr int CT = 2;                            // column tiles of 16 pairs per wavefront
+constexpr int kThreads = 512;
+constexpr int kSegment = kThreads;               // blocks whose numbers and scales are in LDS at a time
 
-// What a block needs: c k_scale, log2 of v_scale relative to the reference and its inverse, number in the pool (as bits)
+// What a block needs: c k_scale, v_scale relative to the reference, number in the pool (as bits)
 typedef float4p_t Block;
 
 // grid: x = KV head, y = split, z = sequence * tiles + tile (the last tile of a sequence, with the longest prefix, first)
-template <int D, int CT>
-__global__ __launch_bounds__(256, 2) void attn_paged_rows_kernel(PagedSeqs, const uint16_t *__restrict__ q, PagedArgs pa, float *__restrict__ part,
-                                                                uint16_t *__restrict__ out, int h, int g, int tiles, int chunk, int splits, int least)
+template <int D>
+__global__ __launch_bounds__(kThreads, 2) void attn_paged_rows_kernel(PagedSeqs, const uint16_t *__restrict__ q, PagedArgs pa, uint16_t *__restrict__ out, int h, int g, int tiles,
+                                                                       int least)
 {
     constexpr int J = D / 64, KS = D / 32, NT = D / 16;
     constexpr int G = NT;                        // steps of either product of 32 tokens
-    constexpr int PD = 4;                        // steps that operands are read ahead
+    constexpr int PD = D == 128 ? 8 : 4;         // steps that operands are read ahead
     static_assert(2 * KS == G && PD <= G, "both products of half a tile have as many operands");
-    constexpr int kPairs = 64 * CT;
+    constexpr int kPairs = kPagedRowTile;
+    static_assert(kPairs == 8 * 16 * CT, "eight wavefronts");
     constexpr int kTileBytes = 64 * D * 2;
     __shared__ __align__(16) unsigned char lds[4 * kTileBytes];        // keys: two buffers, values: two
     __shared__ __align__(16) Block blocks[kSegment];
-    __shared__ float v_tops[4];
+    __shared__ float v_tops[8];
     __shared__ int bad_s;
 
     const int b = tiles == 1 ? (int)blockIdx.z : (int)blockIdx.z / tiles, tile = tiles == 1 ? 0 : tiles - 1 - ((int)blockIdx.z - b * tiles);
-    const int kvh = blockIdx.x, split = blockIdx.y;
+    const int kvh = blockIdx.x;
     const SeqSpan si = seq_span(seqs_arg(), b);
     const int rep = h / g, pairs = si.q_len * rep, p0 = tile * kPairs;
     if (pairs < least || p0 >= pairs) return;                          // (fewer pairs: the other kernel's)
     const int past = si.kv_len - si.q_len;
     const int n_pairs = min(kPairs, pairs - p0);
     const int vis = min(past + (p0 + n_pairs - 1) / rep + 1, pa.cap);
-    const int t_begin = split * chunk;
-    if (split > 0 && t_begin >= vis) return;
-    const int t_end = min(vis, t_begin + chunk);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, quarter = lane >> 4;
-    const int b_begin = t_begin >> 4, b_end = t_end > t_begin ? (t_end + 15) >> 4 : b_begin;
+    const int b_end = (max(vis, 0) + 15) >> 4;
 
     // ---- queries ----
     const int wave_min = past + min(p0 + wave * 16 * CT, p0 + n_pairs - 1) / rep;
@@ -81,40 +86,51 @@ __global__ __launch_bounds__(256, 2) void attn_paged_rows_kernel(PagedSeqs, cons
     const float c = 1.44269504088896340736f / sqrtf((float)D);
 
     float4p_t O[NT][CT];
-    float m[CT], l[CT];
+    float m[CT];
+    float4p_t l[CT];                                                   // sums of the weights, in every row of a tile
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-        m[ct] = kUnset, l[ct] = 0.0f;
+        m[ct] = kUnset, l[ct] = float4p_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int i = 0; i < NT; ++i) O[i][ct] = float4p_t{0.0f, 0.0f, 0.0f, 0.0f};
     }
 
     float v_ref = 0.0f;
-    u32x4p_t rk[J], rv[J];
+    u32x4p_t rk[2], rv[2];                                             // of the next two tiles, by their parity
+    float vr[2];                                                       // value scales of what is in rv
+#pragma unroll
+    for (int i = 0; i < 2; ++i) rk[i] = rv[i] = u32x4p_t{0, 0, 0, 0}, vr[i] = 0.0f;
     half8p_t ring[PD], pf[CT];
-    float sum[2][CT];
+    const _Float16 one = (_Float16)1.0f;
+    const half8p_t ones = {one, one, one, one, one, one, one, one};
 
-    // ---- staging: wavefront w brings block w of a tile ----
-    auto pool_of = [&](int t) { return max(__builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, (float)blocks[t * 4 + wave][3])), 0); };
-    auto load_keys = [&](int t) {
-        const u32x4p_t *p = (const u32x4p_t *)(pa.k + (size_t)pool_of(t) * (16 * D));
-#pragma unroll
-        for (int j = 0; j < J; ++j) rk[j] = p[j * 64 + lane];
+    // ---- staging: a tile is 4 J loads of keys and as many of values; with heads of 128 a wavefront brings one of each, with heads of 64 one ----
+    const bool brings_keys = J == 2 || wave < 4, brings_values = J == 2 || wave >= 4;
+    const int blk_w = J == 2 ? wave >> 1 : wave & 3, load_w = J == 2 ? wave & 1 : 0;
+    auto info_of = [&](int t) { return blocks[min(t * 4, kSegment - 4) + blk_w]; };
+    auto packet = [&](const uint8_t *codes, const Block &info) {
+        const int p = max(__builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, (float)info[2])), 0);
+        return ((const u32x4p_t *)(codes + (size_t)p * (16 * D)))[load_w * 64 + lane];
     };
-    auto load_values = [&](int t) {
-        const u32x4p_t *p = (const u32x4p_t *)(pa.v + (size_t)pool_of(t) * (16 * D));
-#pragma unroll
-        for (int j = 0; j < J; ++j) rv[j] = p[j * 64 + lane];
+    auto load_keys = [&](int parity, const Block &info) {
+        rk[parity] = packet(pa.k, info);
     };
-    auto store_key = [&](int kb, int i) {                              // i of 2 J: half of load i / 2
-        const u32x4p_t w = rk[i >> 1];
-        *(half8p_t *)(lds + kb * kTileBytes + (wave * KS * 64 + lane) * 16 + i * 1024) = i & 1 ? codes_to_half8(w.z, w.w) : codes_to_half8(w.x, w.y);
+    auto load_values = [&](int parity, const Block &info) {
+        rv[parity] = packet(pa.v, info), vr[parity] = info[1];
     };
-    auto store_value = [&](int vb, int i) {                            // i of 4 J: the four tokens of one element of load i / 4
-        half2p_t lo, hi;
-        const uint32_t w = rv[i >> 2][i & 3];
-        codes_to_half(w, lo, hi);
-        *(u32x2p_t *)(lds + (2 + vb) * kTileBytes + ((wave >> 1) * NT * 64 + lane) * 16 + (wave & 1) * 8 + i * 1024) =
+    auto store_key = [&](int kb, int i) {                              // half i of the load; the buffer is the tile's parity
+        if (!brings_keys) return;
+        const u32x4p_t w = rk[kb];
+        *(half8p_t *)(lds + kb * kTileBytes + ((blk_w * KS + 2 * load_w + i) * 64 + lane) * 16) = i ? codes_to_half8(w.z, w.w) : codes_to_half8(w.x, w.y);
+    };
+    auto store_value = [&](int vb, int i) {                            // the four tokens of element i of the load
+        if (!brings_values) return;
+        // (u - 128) r to fp16 in one rounding: 128 r is exact, the multiply-add rounds once in fp32
+        const uint32_t w = rv[vb][i];
+        const float r = vr[vb], off = -128.0f * r;
+        const half2p_t lo = {(_Float16)fmaf((float)(w & 255u), r, off), (_Float16)fmaf((float)(w >> 8 & 255u), r, off)};
+        const half2p_t hi = {(_Float16)fmaf((float)(w >> 16 & 255u), r, off), (_Float16)fmaf((float)(w >> 24), r, off)};
+        *(u32x2p_t *)(lds + (2 + vb) * kTileBytes + (((blk_w >> 1) * NT + 4 * load_w + i) * 64 + lane) * 16 + (blk_w & 1) * 8) =
             u32x2p_t{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
     };
 
@@ -134,20 +150,21 @@ __global__ __launch_bounds__(256, 2) void attn_paged_rows_kernel(PagedSeqs, cons
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) O[i][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ring[i % PD], pf[ct], O[i][ct], 0, 0, 0);
     };
-    // piece i of 4 CT: two weights, in the order block, column tile, pair
-    auto weights = [&](const Scores &S, const Block (&bl)[2], int i) {
-        const int u = i / (2 * CT), ct = i / 2 % CT, e = i % 2 * 2;
-        const float off = bl[u][1] + kBias - m[ct];
-        float x0 = __builtin_amdgcn_exp2f(fmaf(S.s[u][ct][e], bl[u][0], off)), x1 = __builtin_amdgcn_exp2f(fmaf(S.s[u][ct][e + 1], bl[u][0], off));
-        asm volatile("" : "+v"(x0), "+v"(x1));                         // computed here and not where they are first used
-        sum[u][ct] = e ? sum[u][ct] + (x0 + x1) : x0 + x1;
-        pf[ct][4 * u + e] = (_Float16)x0, pf[ct][4 * u + e + 1] = (_Float16)x1;
+    auto weights = [&](const Scores &S, const Block (&bl)[2]) {
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            const float off = kBias - m[ct];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) pf[ct][4 * u + i] = (_Float16)__builtin_amdgcn_exp2f(fmaf(S.s[u][ct][i], bl[u][0], off));
+        }
     };
     auto mask = [&](Scores &S, int at, int t0, bool bad) {             // at: the first of the two blocks in the segment
         if (t0 + 31 > wave_min || bad) {                               // uniform
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const bool there = __builtin_bit_cast(int, (float)blocks[at + u][3]) >= 0;
+                const bool there = __builtin_bit_cast(int, (float)blocks[at + u][2]) >= 0;
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
@@ -166,58 +183,49 @@ __global__ __launch_bounds__(256, 2) void attn_paged_rows_kernel(PagedSeqs, cons
 #pragma unroll
             for (int i = 0; i < 4; ++i) top = __builtin_elementwise_max(top, half2p_t{pf[ct][2 * i], pf[ct][2 * i + 1]});
         if (__any(fmaxf((float)top.x, (float)top.y) > kMost)) {
+            auto over_column = [](float v) {                           // maximum over the four lanes of a column
+                float2 both = pair_xor16(v);
+                both = pair_xor32(fmaxf(both.x, both.y));
+                return fmaxf(both.x, both.y);
+            };
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
-                float mx = -INFINITY;
+                float mx = -INFINITY, most = 0.0f;                     // a column moves by itself: no row depends on the others of its tile
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) mx = fmaxf(mx, S.s[u][ct][i] * bl[u][0]);
-                float2 both = pair_xor16(mx);
-                both = pair_xor32(fmaxf(both.x, both.y));
-                mx = fmaxf(both.x, both.y);
-                const float to = mx > m[ct] ? mx : m[ct], alpha = __builtin_amdgcn_exp2f(m[ct] - to);
+                    for (int i = 0; i < 4; ++i) mx = fmaxf(mx, S.s[u][ct][i] * bl[u][0]), most = fmaxf(most, (float)pf[ct][4 * u + i]);
+                mx = over_column(mx), most = over_column(most);
+                const float to = most > kMost && mx > m[ct] ? mx : m[ct], alpha = __builtin_amdgcn_exp2f(m[ct] - to);
                 m[ct] = to, l[ct] *= alpha;
 #pragma unroll
                 for (int i = 0; i < NT; ++i) O[i][ct] *= alpha;
             }
-#pragma unroll
-            for (int i = 0; i < 4 * CT; ++i) weights(S, bl, i);
+            weights(S, bl);
         }
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) l[ct] = fmaf(sum[1][ct], bl[1][2], fmaf(sum[0][ct], bl[0][2], l[ct]));
     };
 
-    for (int seg = b_begin; seg < b_end; seg += kSegment) {
-        // ---- numbers and scales of the segment's blocks, three per thread ----
-        int pool[kSegment / 256];
-        float ks[kSegment / 256], vs[kSegment / 256], top = 0.0f;
-        int bad_any = 0;
-#pragma unroll
-        for (int j = 0; j < kSegment / 256; ++j) {
-            const int blk = seg + j * 256 + tid;
-            pool[j] = -1, ks[j] = vs[j] = 0.0f;
-            if (blk < b_end) {
-                pool[j] = paged_block(pa, g, kvh, si.slot, blk);
-                if (pool[j] < 0) bad_any = 1, atomicOr(pa.err, kBadPage);
-                else ks[j] = pa.k_scale[pool[j]], vs[j] = pa.v_scale[pool[j]];
-            }
+    const bool second = wave >= 4;                                     // of the two halves that take turns
+    for (int seg = 0; seg < b_end; seg += kSegment) {
+        // ---- numbers and scales of the segment's blocks, one per thread ----
+        int pool = -1;
+        float ks = 0.0f, vs = 0.0f;
+        if (seg + tid < b_end) {
+            pool = paged_block(pa, g, kvh, si.slot, seg + tid);
+            if (pool < 0) atomicOr(pa.err, kBadPage);
+            else ks = pa.k_scale[pool], vs = pa.v_scale[pool];
         }
-#pragma unroll
-        for (int j = 0; j < kSegment / 256; ++j) top = fmaxf(top, vs[j]);
-        top = wave_max(top);
+        const float top = wave_max(vs);
         __syncthreads();                                               // the segment before is consumed
         if (tid == 0) bad_s = 0;
         if (lane == 0) v_tops[wave] = top;
         __syncthreads();
-        const float ref = fmaxf(fmaxf(fmaxf(v_tops[0], v_tops[1]), fmaxf(v_tops[2], v_tops[3])), v_ref);
-        if (bad_any) bad_s = 1;
+        float ref = v_ref;
 #pragma unroll
-        for (int j = 0; j < kSegment / 256; ++j) {
-            const float lr = vs[j] > 0.0f ? fmaxf(__builtin_amdgcn_logf(vs[j] / ref), -60.0f) : 0.0f;
-            // (codes of a zero scale are zero; -inf times its factor has to stay -inf)
-            blocks[j * 256 + tid] = Block{fmaxf(ks[j] * c, 0x1p-100f), lr, __builtin_amdgcn_exp2f(-lr), __builtin_bit_cast(float, pool[j])};
-        }
+        for (int w = 0; w < 8; ++w) ref = fmaxf(ref, v_tops[w]);
+        if (pool < 0 && seg + tid < b_end) bad_s = 1;
+        // (codes of a zero scale are zero; -inf times its factor has to stay -inf)
+        blocks[tid] = Block{fmaxf(ks * c, 0x1p-100f), ref > 0.0f ? vs / ref : 0.0f, __builtin_bit_cast(float, pool), 0.0f};
         if (v_ref > 0.0f && ref > v_ref) {                             // O is in units of the largest value scale so far
             const float f = v_ref / ref;
 #pragma unroll
@@ -227,114 +235,112 @@ __global__ __launch_bounds__(256, 2) void attn_paged_rows_kernel(PagedSeqs, cons
         }
         v_ref = ref;
         __syncthreads();
+        // a tile's last blocks may lie behind the end: masked like those without a page, but by their positions
         const bool bad = __builtin_amdgcn_readfirstlane(bad_s) != 0;
 
         // ---- the segment's tiles ----
         const int first = seg * 16, nt = (min(b_end - seg, kSegment) + 3) >> 2;
-        load_keys(0), load_values(0);
+        // Loads are issued without a condition, behind the last tile of any block: behind a branch their number at a wait is not known, and each wait
+        // would be for all of them (turns of the matrix pipe 1000 cycles instead of 850).
+        load_keys(0, info_of(0)), load_values(0, info_of(0)), load_keys(1, info_of(1)), load_values(1, info_of(1));
 #pragma unroll
-        for (int i = 0; i < 2 * J; ++i) store_key(0, i);
+        for (int i = 0; i < 4; ++i) store_key(i >> 1, i & 1);
 #pragma unroll
-        for (int i = 0; i < 4 * J; ++i) store_value(0, i);
-        if (nt > 1) load_keys(1), load_values(1);
+        for (int i = 0; i < 4; ++i) store_value(0, i);
+        load_keys(0, info_of(2)), load_values(0, info_of(2)), load_keys(1, info_of(3));
         lds_barrier();
-        Scores S[2];
-        Block bl[2];
+        if (second) lds_barrier();
+        Scores S;
 #pragma unroll
         for (int i = 0; i < PD; ++i) ring[i] = read_key(0, 0, i);
 #pragma unroll
         for (int i = 0; i < G; ++i) {
-            key_step(S[0], i);
+            key_step(S, i);
             if (i + PD < G) ring[i % PD] = read_key(0, 0, i + PD);
         }
-        mask(S[0], 0, first, bad);
-        for (int t = 0; t < nt; ++t) {
-            const int kb = t & 1;
+        Block bl[2] = {blocks[0], blocks[1]};
+        __builtin_amdgcn_sched_barrier(0);
+        lds_barrier();
+        // two turns of either kind per tile; PARITY: its buffers and registers
+        auto tile_turns = [&](auto PARITY, int t) __attribute__((always_inline)) {
+            constexpr int kb = PARITY;
 #pragma unroll
             for (int sub = 0; sub < 2; ++sub) {
-                Scores &cur = S[sub], &ahead = S[sub ^ 1];
-                // ---- scores of the next 32 tokens between the exponentials of these (behind the last tile: of an old one, not used) ----
-                const int key_buf = sub ? kb ^ 1 : kb, at = t * 4 + 2 * sub;
+                // ---- turn of the vector unit: weights of these 32 tokens; the first operands of the products are asked for ----
+                mask(S, t * 4 + 2 * sub, first + t * 64 + sub * 32, bad);
+                weights(S, bl);
+                settle(S, bl);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int i = 0; i < PD; ++i) ring[i] = read_key(key_buf, sub ^ 1, i);
-                bl[0] = blocks[at], bl[1] = blocks[at + 1];
-#pragma unroll
-                for (int i = 0; i < G; ++i) {
-                    key_step(ahead, i);
-                    ring[i % PD] = i + PD < G ? read_key(key_buf, sub ^ 1, i + PD) : read_value(kb, sub, i + PD - G);
-#pragma unroll
-                    for (int w = i * 4 * CT / G; w < (i + 1) * 4 * CT / G; ++w) weights(cur, bl, w);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-                settle(cur, bl);
-                // ---- products with V between the staging of the next tile: keys, then values ----
+                for (int i = 0; i < PD; ++i) ring[i] = read_value(kb, sub, i);
+                asm volatile("s_barrier" ::: "memory");                // (nothing written in this turn: no wait for the reads)
+                // ---- turn of the matrix pipe: these weights with V, the keys of the next 32 tokens with Q, and what the wavefront brings: in the first turn of
+                // a tile its values of the next one, in the second its keys of the one behind that.  The other half has read either buffer for
+                // the last time one turn before at the latest, and neither is read before two turns have passed ----
+                const int key_buf = sub ? kb ^ 1 : kb;                 // (behind the last tile: an old one, its scores are not used)
+                __builtin_amdgcn_s_setprio(1);
+                bl[0] = blocks[min(t * 4 + 2 * sub + 2, kSegment - 2)], bl[1] = blocks[min(t * 4 + 2 * sub + 3, kSegment - 1)];
+                const Block info_ahead = info_of(t + 3 + sub);
 #pragma unroll
                 for (int i = 0; i < G; ++i) {
                     value_step(i);
-                    if (i + PD < G) ring[i % PD] = read_value(kb, sub, i + PD);
-                    if (sub == 0) {                                    // (behind the last tile: the same once more, not read)
-#pragma unroll
-                        for (int w = i * 2 * J / G; w < (i + 1) * 2 * J / G; ++w) store_key(kb ^ 1, w);
-                    } else {
-#pragma unroll
-                        for (int w = i * 4 * J / G; w < (i + 1) * 4 * J / G; ++w) store_value(kb ^ 1, w);
-                    }
+                    ring[i % PD] = i + PD < G ? read_value(kb, sub, i + PD) : read_key(key_buf, sub ^ 1, i + PD - G);
+                    if (sub == 0 && i >= G / 4 - 1 && i < G / 4 + 3) store_value(kb ^ 1, i - (G / 4 - 1));   // (behind the last tile: the same once more, not read)
+                    if (sub == 1 && i >= 1 && i < 3) store_key(kb, i - 1);
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                mask(ahead, min(at + 2, kSegment - 2), first + t * 64 + (sub + 1) * 32, bad);
-                if (t + 2 < nt) {
-                    if (sub == 0) load_keys(t + 2);
-                    else load_values(t + 2);
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) l[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pf[ct], l[ct], 0, 0, 0);
+                if (sub == 0) load_values(kb ^ 1, info_ahead);
+                if (sub == 1) load_keys(kb, info_ahead);
+#pragma unroll
+                for (int i = 0; i < G; ++i) {
+                    key_step(S, i);
+                    if (i + PD < G) ring[i % PD] = read_key(key_buf, sub ^ 1, i + PD);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
+                __builtin_amdgcn_s_setprio(0);
                 lds_barrier();
             }
+        };
+        for (int t = 0; t < nt; t += 2) {
+            tile_turns(std::integral_constant<int, 0>{}, t);
+            if (t + 1 < nt) tile_turns(std::integral_constant<int, 1>{}, t + 1);
         }
+        if (!second) lds_barrier();
     }
 
     // ---- results: lane holds elements 16 i + 4 quarter .. + 3 of its columns ----
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-        const float den = xor32_sum(xor16_sum(l[ct]));
+        const float den = l[ct][0];
         const int place = (wave * CT + ct) * 16 + col;
         if (place >= n_pairs) continue;
         const int pair = p0 + place, row = pair / rep;
         const size_t at = (size_t)(si.q_start + row) * h + kvh * rep + pair - row * rep;
-        if (splits > 1) {
-            float *dst = part + (at * splits + split) * (D + 2);
+        const float inv = (den > 0.0f ? 1.0f / den : den) * v_ref;
 #pragma unroll
-            for (int i = 0; i < NT; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) dst[i * 16 + quarter * 4 + j] = O[i][ct][j] * v_ref;
-            if (quarter == 0) dst[D] = m[ct], dst[D + 1] = den;
-        } else {
-            const float inv = (den > 0.0f ? 1.0f / den : den) * v_ref;
-#pragma unroll
-            for (int i = 0; i < NT; ++i) {
-                const float4p_t o = O[i][ct] * inv;
-                const uint32_t lo = f2h(o.x) | (uint32_t)f2h(o.y) << 16, hi = f2h(o.z) | (uint32_t)f2h(o.w) << 16;
-                *(u32x2p_t *)(out + at * D + i * 16 + quarter * 4) = u32x2p_t{lo, hi};
-            }
+        for (int i = 0; i < NT; ++i) {
+            const float4p_t o = O[i][ct] * inv;
+            const uint32_t lo = f2h(o.x) | (uint32_t)f2h(o.y) << 16, hi = f2h(o.z) | (uint32_t)f2h(o.w) << 16;
+            *(u32x2p_t *)(out + at * D + i * 16 + quarter * 4) = u32x2p_t{lo, hi};
         }
     }
 }
 
-template <int D, int CT>
-hipError_t launch_one(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, const PagedRows &pl, uint16_t *out, float *partials,
-                      hipStream_t stream)
+template <int D>
+hipError_t launch_one(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, int32_t tiles, int32_t least, uint16_t *out, hipStream_t stream)
 {
-    const dim3 grid(dm.n_kv_heads, pl.splits, pl.tiles * st.B);
-    hipLaunchKernelGGL((attn_paged_rows_kernel<D, CT>), grid, dim3(256), 0, stream, st, q, pa, partials, out, dm.n_heads, dm.n_kv_heads, pl.tiles, pl.chunk, pl.splits,
-                       pl.least);
+    hipLaunchKernelGGL(attn_paged_rows_kernel<D>, dim3(dm.n_kv_heads, 1, tiles * st.B), dim3(kThreads), 0, stream, st, q, pa, out, dm.n_heads, dm.n_kv_heads, tiles, least);
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_paged_rows(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, const PagedRows &pl, uint16_t *out,
-                             float *partials, hipStream_t stream)
+hipError_t launch_paged_rows(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, int32_t tiles, int32_t least, uint16_t *out,
+                             hipStream_t stream)
 {
-    if (dm.head_dim == 128) return pl.ct == 2 ? launch_one<128, 2>(q, pa, dm, st, pl, out, partials, stream) : launch_one<128, 1>(q, pa, dm, st, pl, out, partials, stream);
-    return pl.ct == 2 ? launch_one<64, 2>(q, pa, dm, st, pl, out, partials, stream) : launch_one<64, 1>(q, pa, dm, st, pl, out, partials, stream);
+    return dm.head_dim == 128 ? launch_one<128>(q, pa, dm, st, tiles, least, out, stream) : launch_one<64>(q, pa, dm, st, tiles, least, out, stream);
 }
 
 }  // namespace relax

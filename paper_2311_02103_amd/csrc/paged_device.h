@@ -101,13 +101,10 @@ __device__ inline int paged_block(const PagedArgs &pa, int g, int kvh, int slot,
     return ((page * g + kvh) << pa.shift) + (blk & ((1 << pa.shift) - 1));
 }
 
-// How launch_paged_attention cuts a call: sequences with at least `least` (row, head) pairs go in tiles of 64 ct pairs (attn_paged_rows.hip), the
-// others in tiles of 16 (attn_paged.hip); `tiles` of the former per sequence at most; both in `splits` splits of `chunk` tokens.
-struct PagedRows {
-    int32_t least, ct, tiles, chunk, splits;
-};
-hipError_t launch_paged_rows(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, const PagedRows &pl, uint16_t *out,
-                             float *partials, hipStream_t stream);
+// Attention of the sequences with at least `least` (row, head) pairs, in tiles of kPagedRowTile pairs, at most `tiles` per sequence (attn_paged_rows.hip)
+constexpr int kPagedRowTile = 256;
+hipError_t launch_paged_rows(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, int32_t tiles, int32_t least, uint16_t *out,
+                             hipStream_t stream);
 
 // four codes -> four fp16 integers
 __device__ __forceinline__ void codes_to_half(uint32_t w, half2p_t &lo, half2p_t &hi)

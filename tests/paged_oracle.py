@@ -81,34 +81,39 @@ def values(pool, name, pages, page_size, slot, positions, d):
     return out
 
 
-def attention(q, pool, pages, page_size, q_lens, kv_lens, slots, g, d):
-    """(out, tolerance), float64 [n, h, d].  The tolerance counts what the kernel rounds: the output to fp16, half a step, 2^-11 of it (2^-25
-    below fp16's normal range); each probability to fp16, 2^-11 of it at most, so 2^-11 sum p |v|; the scores in fp32, whose sum of d products and
-    scaling is off by (d + 8) 2^-24 of the sum of magnitudes at most, which changes a probability by that factor, at once in numerator and denominator
-    (2 x); sums of probabilities and of O in fp32, a further 2^-18 of sum p |v| for up to 2^6 roundings in a row of partial sums; and weights
-    below 2^-24 of the largest weight's 2^11, 2^-36 of the largest |v| each."""
+def attention(q, pool, pages, page_size, q_lens, kv_lens, slots, g, d, heads=None):
+    """(out, tolerance), float64 [n, h, d], of the given query heads (None: all).  The tolerance counts what the kernels round, each to nearest, so by half a step, 2^-11, at most:
+      the output to fp16                                                       2^-11 |o|, 2^-25 below fp16's normal range
+      the probabilities to fp16, p (1 + e), |e| <= 2^-11, with a sum of the rounded ones: o becomes sum p (1 + e) v / sum p (1 + e), which is off by
+      sum p (e - mean of e) v                                                  2^-11 (sum p |v| + |o|)
+      the values, scaled, to fp16                                              2^-11 sum p |v|, and 2^-32 of the largest |v| below fp16's normal range
+      scores in fp32, whose sum of d products and scaling is off by (d + 8) 2^-24 of the sum of magnitudes, which changes a probability by
+      that factor, at once in numerator and denominator                        2 (d + 8) 2^-24 |q| |k| sum p |v|
+      sums of probabilities and of O in fp32, 2^6 roundings in a row           2^-18 sum p |v|
+      weights below 2^-24 of the largest weight's 2^11                         2^-36 of the largest |v| each"""
     h = q.shape[1]
     rep = h // g
     out, tol = np.zeros(q.shape), np.zeros(q.shape)
     for row, ql, L, slot in sequences(q_lens, kv_lens, slots):
         k, v = (values(pool, name, pages, page_size, slot, np.arange(L), d) for name in "kv")
         there = ~np.isnan(k[:, 0, 0])
-        for head in range(h):
+        for head in range(h) if heads is None else heads:
             kh, vh = k[there, head // rep], v[there, head // rep]
+            if not len(kh):
+                continue
             t = np.arange(L)[there]
-            s = q[row:row + ql, head] @ kh.T / np.sqrt(d)
-            mag = np.abs(q[row:row + ql, head]) @ np.abs(kh).T / np.sqrt(d)
+            qh = q[row:row + ql, head]
             seen = t[None, :] <= np.arange(L - ql, L)[:, None]
-            s = np.where(seen, s, -np.inf)
-            for i in range(ql):
-                if not seen[i].any():
-                    continue
-                p = np.exp(s[i] - s[i].max())
-                p /= p.sum()
-                o, mean = p @ vh, p @ np.abs(vh)
-                delta = (d + 8) * 2.0 ** -24 * mag[i][seen[i]].max()
-                out[row + i, head] = o
-                tol[row + i, head] = 2.0 ** -11 * np.abs(o) + (2.0 ** -11 + 2 * delta + 2.0 ** -18) * mean + 2.0 ** -25 + len(t) * 2.0 ** -36 * np.abs(vh).max()
+            s = np.where(seen, qh @ kh.T / np.sqrt(d), -np.inf)
+            mag = np.where(seen, np.abs(qh) @ np.abs(kh).T / np.sqrt(d), 0.0)
+            some = seen.any(axis=1)
+            p = np.exp(s - np.where(some, s.max(axis=1), 0.0)[:, None])
+            p /= np.where(some, p.sum(axis=1), 1.0)[:, None]
+            o, mean = p @ vh, p @ np.abs(vh)
+            delta = ((d + 8) * 2.0 ** -24 * mag.max(axis=1))[:, None]
+            out[row:row + ql, head] = o
+            tol[row:row + ql, head] = np.where(some[:, None], 2.0 ** -10 * np.abs(o) + (2.0 ** -10 + 2 * delta + 2.0 ** -18) * mean + 2.0 ** -25 +
+                                               (len(t) * 2.0 ** -36 + 2.0 ** -32) * np.abs(vh).max(), 0.0)
     return out, tol
 
 

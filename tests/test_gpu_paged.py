@@ -254,14 +254,17 @@ def test_zeros(rx):
     assert (b.read() == 0).all() and (b.attention(q_out) == 0).all()
 
 
-def attention_case(rx, rng, shape, page_size, q_lens, kv_lens, slots=None, std=1.0, device_table=False, scale=(0.02, 0.05), edit=None):
+def attention_case(rx, rng, shape, page_size, q_lens, kv_lens, slots=None, std=1.0, device_table=False, scale=(0.02, 0.05), edit=None, heads=None):
     b = Bench(rx, rng, *shape, page_size, q_lens, kv_lens, slots, device_table=device_table, scale=scale)
     if edit:
         edit(b)
     q = half(rng, (b.n, b.h, b.d), std)
     got = b.attention(q).astype(np.float64)
-    want, tol = po.attention(q.astype(np.float64), b.pool, b.pages, page_size, q_lens, kv_lens, slots, b.g, b.d)
+    want, tol = po.attention(q.astype(np.float64), b.pool, b.pages, page_size, q_lens, kv_lens, slots, b.g, b.d, heads)
     bad = ~(np.abs(got - want) <= tol)
+    if heads is not None:
+        bad = bad[:, heads]
+        got, want, tol = got[:, heads], want[:, heads], tol[:, heads]
     assert not bad.any(), (int(bad.sum()), np.abs(got - want)[bad][:5], tol[bad][:5])
     return b
 
@@ -297,6 +300,48 @@ def test_attention_on_large_scores_and_uneven_scales(rx):
             b.dev[key].copy_(torch.from_numpy(b.pool[key]))
     for q_lens, kv_lens in (([200], [200]), ([1], [900]), ([20], [300])):
         attention_case(rx, np.random.default_rng(3), (4, 2, 64), 16, q_lens, kv_lens, edit=uneven)
+
+
+# Calls whose sequences fill tiles of 256 (row, head) pairs, 160 of them and more over all KV heads: (heads, KV heads, d), q_lens, kv_lens, heads to check
+MANY_ROWS = [
+    ((80, 80, 64), [300], [300], None),
+    ((80, 80, 128), [257], [1000], [0, 1, 40, 79]),
+    ((64, 8, 128), [33, 60, 40, 32, 35, 47, 33, 64, 50, 45], [33, 61, 300, 32, 99, 47, 700, 64, 1050, 45], None),
+    ((40, 8, 128), [300, 1, 450, 3, 260], [310, 800, 450, 77, 900], [0, 5, 13, 39]),
+    ((40, 8, 64), [1001], [1001], [0, 9, 39]),
+    ((160, 160, 64), [256], [8200], [0, 77, 159]),                # more blocks than are in LDS at a time
+    ((24, 8, 128), [2000], [2000], [2, 23]),
+]
+
+
+@pytest.mark.parametrize("device_table", [False, True])
+@pytest.mark.parametrize("case", MANY_ROWS, ids=lambda c: "%s_%d" % (c[0], sum(c[1])))
+def test_attention_of_many_rows(rx, case, device_table):
+    shape, q_lens, kv_lens, heads = case
+    rng = np.random.default_rng(seed_of(shape, q_lens))
+    attention_case(rx, rng, shape, [16, 64, 256][len(q_lens) % 3], q_lens, kv_lens, [len(q_lens) - i for i in range(len(q_lens))], device_table=device_table, heads=heads)
+
+
+def test_many_rows_without_pages_with_bad_rows_and_uneven_scales(rx):
+    q_lens, kv_lens, shape, heads = [300, 290, 256, 3], [400, 300, 280, 50], (40, 40, 128), [0, 17, 39]
+
+    def spoil(b):
+        for key in ("ks", "vs"):
+            b.pool[key] *= (10.0 ** np.random.default_rng(4).uniform(-4, 2, b.pool[key].shape)).astype(np.float32)
+            b.pool[key][:, 17, 0] = np.where(np.isnan(b.pool[key][:, 17, 0]), np.nan, 0.0).astype(np.float32)      # blocks of zeros
+            b.dev[key].copy_(torch.from_numpy(b.pool[key]))
+        b.pages[0, 2], b.pages[2] = -5, b.pool["k"].shape[0]            # sequence 2 has no page at all
+        b.dev_pages.copy_(torch.from_numpy(b.pages))
+    b = attention_case(rx, np.random.default_rng(50), shape, 16, q_lens, kv_lens, edit=spoil, heads=heads)
+    assert b.error() == 4
+    q = half(np.random.default_rng(51), (b.n, 40, 128))
+    clean = b.attention(q)
+    assert (clean[590:846] == 0).all()
+    q[7, 3, 5], q[100, 4, :] = np.nan, np.inf
+    got = b.attention(q)
+    same = np.ones((b.n, 40), bool)
+    same[7, 3] = same[100, 4] = False
+    assert np.isnan(got[7, 3]).all() and np.array_equal(got[same], clean[same])
 
 
 def test_a_bad_query_row_stays_alone(rx):
