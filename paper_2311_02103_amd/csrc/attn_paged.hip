@@ -4,7 +4,7 @@
 //
 // The query heads of a KV head and the rows of a sequence are one list of (row, head) pairs: pair p is row p / rep, head p % rep of the group.
 // A workgroup takes 16 consecutive pairs, the columns of the MFMA tiles, against one KV head and one split of the tokens; its four
-// wavefronts take a quarter of the split each.  With S^T = K Q^T a pair is a column of the result and the lane (quarter, column) holds tokens
+// or eight wavefronts take a share of the split each.  With S^T = K Q^T a pair is a column of the result and the lane (quarter, column) holds tokens
 // 4 quarter .. + 3 of a block; the same lane's eight probabilities of two blocks are what the B operand of O^T = V^T P^T wants from it, and
 // the codes come in as the A operands (paged_device.h), so nothing passes through LDS or another lane but the maxima.
 //
@@ -14,6 +14,7 @@
 // at most 2^4) and one of 2^-39 of it still is a subnormal fp16 number.  Scores, sums and O are fp32; the rounding of the probabilities (2^-11 relative, independent
 // from token to token) is the only one between the codes and the result.
 #include <algorithm>
+#include <type_traits>
 
 #include "paged_device.h"
 
@@ -24,15 +25,15 @@ namespace {
 constexpr float kBias = 11.0f, kLag = 4.0f;      // log2: offset of the weights, and how far the reference may trail the maximum
 
 // grid: x = KV head, y = split, z = sequence * tiles + tile.  part: [row][head][splits][D + 2] when splits > 1.
-template <int D>
-__global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedSeqs, const uint16_t *__restrict__ q, PagedArgs pa, float *__restrict__ part,
+template <int D, int W>
+__global__ __launch_bounds__(64 * W, 4) void attn_paged_kernel(PagedSeqs, const uint16_t *__restrict__ q, PagedArgs pa, float *__restrict__ part,
                                                             uint16_t *__restrict__ out, int h, int g, int tiles, int chunk, int splits, int least)
 {
     constexpr int J = D / 64;                    // 1 KB loads per block
     constexpr int NT = D / 16;                   // 16-element tiles of O^T
     constexpr int P = D + 4;                     // pitch of a state in LDS
-    __shared__ __align__(16) float states[4 * 16 * P];
-    __shared__ float sm_m[4 * 16], sm_l[4 * 16];
+    __shared__ __align__(16) float states[W * 16 * P];
+    __shared__ float sm_m[W * 16], sm_l[W * 16];
 
     const int b = tiles == 1 ? (int)blockIdx.z : (int)blockIdx.z / tiles, tile = tiles == 1 ? 0 : (int)blockIdx.z - b * tiles;
     const int kvh = blockIdx.x, split = blockIdx.y;
@@ -48,9 +49,9 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedSeqs, const uin
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, quarter = lane >> 4;
 
-    // ---- this wavefront's blocks: a quarter of the split, in pairs ----
+    // ---- this wavefront's blocks: its share of the split, in pairs ----
     const int b_begin = t_begin >> 4, b_end = t_end > t_begin ? (t_end + 15) >> 4 : b_begin;
-    const int per = ((b_end - b_begin + 1) / 2 + 3) / 4 * 2;
+    const int per = ((b_end - b_begin + 1) / 2 + W - 1) / W * 2;
     const int w_begin = b_begin + wave * per, w_end = min(b_end, w_begin + per);
 
     // ---- queries: lane holds pair `col`; k step 2 j + half takes elements 16 (4 j + quarter) + 8 half .. + 7 ----
@@ -78,25 +79,19 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedSeqs, const uin
         float ks = pa.k_scale[max(pool, 0)], vs = pa.v_scale[max(pool, 0)];
         const int ns = (min(w_end - seg, kWave) + 1) >> 1;
 
-        struct Step {
-            u32x4p_t k[2 * J], v[2 * J];
-        };
-        auto step_load = [&](Step &sp, int s) {
+        u32x4p_t kreg[2 * J], vreg[2 * J];                     // one step: two blocks
+        auto load = [&](u32x4p_t (&reg)[2 * J], const uint8_t *codes, int s) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 const int at = max(__builtin_amdgcn_readlane(pool, min(2 * s + t, 63)), 0);       // no such block: any that can be read
-                const u32x4p_t *kp = (const u32x4p_t *)(pa.k + (size_t)at * (16 * D)), *vp = (const u32x4p_t *)(pa.v + (size_t)at * (16 * D));
+                const u32x4p_t *p = (const u32x4p_t *)(codes + (size_t)at * (16 * D));
 #pragma unroll
-                for (int j = 0; j < J; ++j) sp.k[t * J + j] = stream_load(kp + j * 64 + lane);
-#pragma unroll
-                for (int j = 0; j < J; ++j) sp.v[t * J + j] = stream_load(vp + j * 64 + lane);
+                for (int j = 0; j < J; ++j) reg[t * J + j] = stream_load(p + j * 64 + lane);
             }
         };
-        // the first steps are on their way before the scales are needed, and the scales ahead of them
-        Step sa, sb;
+        // the first step is on its way before the scales are needed, and the scales ahead of it
         __builtin_amdgcn_sched_barrier(0);
-        step_load(sa, 0);
-        if (ns > 1) step_load(sb, 1);
+        load(kreg, pa.k, 0), load(vreg, pa.v, 0);
         __builtin_amdgcn_sched_barrier(0);
         ks = pool < 0 ? 0.0f : ks * c, vs = pool < 0 ? 0.0f : vs;
         const float ref = fmaxf(v_ref, wave_max(vs));
@@ -107,7 +102,8 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedSeqs, const uin
         }
         v_ref = ref;
         const float vr = ref > 0.0f ? vs / ref : 0.0f;
-        auto consume = [&](const Step &sp, int s) {
+        // a step's keys make room for the next one's as soon as the scores are there, its values when they are summed: one step is in flight all the time
+        auto step = [&](int s, auto MORE) __attribute__((always_inline)) {
             float x[8];
             float mx = -INFINITY;
 #pragma unroll
@@ -115,7 +111,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedSeqs, const uin
                 float4p_t S = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
-                    const u32x4p_t w = sp.k[t * J + j];
+                    const u32x4p_t w = kreg[t * J + j];
                     S = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_half8(w.x, w.y), qf[2 * j], S, 0, 0, 0);
                     S = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_half8(w.z, w.w), qf[2 * j + 1], S, 0, 0, 0);
                 }
@@ -133,6 +129,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedSeqs, const uin
 #pragma unroll
                 for (int i = 0; i < 4; ++i) mx = fmaxf(mx, x[4 * t + i]);
             }
+            if constexpr (MORE) load(kreg, pa.k, s + 1);
             float2 both = pair_xor16(mx);
             both = pair_xor32(fmaxf(both.x, both.y));
             mx = fmaxf(both.x, both.y);
@@ -158,35 +155,29 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedSeqs, const uin
             }
 #pragma unroll
             for (int i = 0; i < NT; ++i)
-                O[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_half8(sp.v[i >> 2][i & 3], sp.v[J + (i >> 2)][i & 3]), pf, O[i], 0, 0, 0);
+                O[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_to_half8(vreg[i >> 2][i & 3], vreg[J + (i >> 2)][i & 3]), pf, O[i], 0, 0, 0);
+            if constexpr (MORE) load(vreg, pa.v, s + 1);
         };
-        // no request behind a branch in the loop: the wait for one step would be for the other, too
-        int s = 0;
-        for (; s + 2 < ns; s += 2) {
-            consume(sa, s);
-            step_load(sa, s + 2);
-            consume(sb, s + 1);
-            step_load(sb, min(s + 3, ns - 1));
-        }
-        consume(sa, s);
-        if (s + 1 < ns) consume(sb, s + 1);
+#pragma unroll 1
+        for (int s = 0; s + 1 < ns; ++s) step(s, std::true_type{});
+        step(ns - 1, std::false_type{});
     }
 
-    // ---- the four states meet in LDS ----
+    // ---- the wavefronts' states meet in LDS ----
     l_run = xor32_sum(xor16_sum(l_run));
 #pragma unroll
     for (int i = 0; i < NT; ++i) *(float4p_t *)(states + (wave * 16 + col) * P + i * 16 + quarter * 4) = O[i] * v_ref;
     if (quarter == 0) sm_m[wave * 16 + col] = m_run, sm_l[wave * 16 + col] = l_run;
     __syncthreads();
-    for (int u = tid; u < n_pairs * (D / 4); u += 256) {
+    for (int u = tid; u < n_pairs * (D / 4); u += 64 * W) {
         const int pc = u / (D / 4), e = u % (D / 4) * 4;
         float mm = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) mm = fmaxf(mm, sm_m[w * 16 + pc]);
+        for (int w = 0; w < W; ++w) mm = fmaxf(mm, sm_m[w * 16 + pc]);
         float4p_t num = {0.0f, 0.0f, 0.0f, 0.0f};
         float den = 0.0f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < W; ++w) {
             const float mw = sm_m[w * 16 + pc], f = mw == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mw - mm);
             num += *(const float4p_t *)(states + (w * 16 + pc) * P + e) * f;
             den += sm_l[w * 16 + pc] * f;
@@ -263,10 +254,12 @@ __global__ __launch_bounds__(256) void attn_paged_merge_kernel(PagedSeqs, const 
     *(u32x2p_t *)(out + (size_t)i * D + e) = u32x2p_t{lo, hi};
 }
 
-// Splits of a launch with `small` workgroups per split: as many as bring it to kPagedGroups workgroups, none but the last shorter than 128 tokens, and no more
-// than kPartials partial results (row, head, split).  More splits where sequences are short of the longest one (as many as make kPagedGroups workgroups with
-// tokens) cost more in the merge than they balance: 8 x 5 rows of 32 / 8 heads 20.4 -> 24.8 us, 16 decode rows of 64 / 8 heads the same.
-constexpr int kPagedGroups = 1024, kPartials = 65536;
+// Splits of a launch with `small` workgroups per split: from kUnsplit workgroups on none, below it as many as bring it to kPagedGroups workgroups, none but the last
+// shorter than 128 tokens, and no more than kPartials partial results (row, head, split).  The workgroups of a split launch have eight
+// wavefronts where a split has 256 tokens and more, as many tokens in flight with half the partial results.
+// us, unsplit / split: 16 x 3 rows of 64 / 8 heads (256 workgroups) 18.5 / 23, 4 x 17 rows of them (288) 20 / 25, 16 x 16 rows of 32 / 32 (512) 28 / 38.  16 decode rows
+// of 64 / 8 heads with 768 workgroups 31.6, with 512 35.8, with 1024 32.7, with four wavefronts 36.
+constexpr int kUnsplit = 256, kPagedGroups = 768, kPartials = 65536;
 
 // The kernel of 256-pair tiles takes the sequences that fill one, in calls that have kRowTiles such tiles over all KV heads: it halves the time of long prompts
 // and loses on the rest, where its workgroups are few and each waits 5 us for its first tile (us, tiles of 16 / of 256; heads of 128): 2048 rows of 32 / 32 heads
@@ -277,7 +270,7 @@ constexpr int kRowTiles = 160;
 struct Plan {
     int32_t least;                   // pairs from which a sequence is the other kernel's
     int32_t row_tiles, tiles;        // at most per sequence, of 256 and of 16 pairs
-    int32_t chunk, splits;
+    int32_t chunk, splits, waves;    // wavefronts per workgroup of 16-pair tiles
 };
 
 Plan plan(const relax_layer_dims &dm, const relax_seqs &sq, int32_t n, int32_t L_max)
@@ -297,12 +290,13 @@ Plan plan(const relax_layer_dims &dm, const relax_seqs &sq, int32_t n, int32_t L
     }
     p.row_tiles = (int32_t)((most_large + kPagedRowTile - 1) / kPagedRowTile);
     p.tiles = (int32_t)((most_small + 15) / 16);
-    long long s = small ? kPagedGroups / (small * dm.n_kv_heads) : 1;
+    long long s = small && small * dm.n_kv_heads < kUnsplit ? kPagedGroups / (small * dm.n_kv_heads) : 1;
     s = std::min(s, (long long)(L_max + 127) / 128);
     s = std::min(s, (long long)kPartials / ((long long)n * dm.n_heads));
     s = std::max(s, 1LL);
     p.chunk = (int32_t)(((L_max + s - 1) / s + 31) / 32 * 32);
     p.splits = (L_max + p.chunk - 1) / p.chunk;
+    p.waves = p.splits > 1 && p.chunk >= 256 ? 8 : 4;
     return p;
 }
 
@@ -310,8 +304,11 @@ template <int D>
 hipError_t launch_d(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, const Plan &pl, uint16_t *out, float *partials,
                     hipStream_t stream)
 {
-    hipLaunchKernelGGL(attn_paged_kernel<D>, dim3(dm.n_kv_heads, pl.splits, pl.tiles * st.B), dim3(256), 0, stream, st, q, pa, partials, out, dm.n_heads, dm.n_kv_heads,
-                       pl.tiles, pl.chunk, pl.splits, pl.least);
+    const dim3 grid(dm.n_kv_heads, pl.splits, pl.tiles * st.B);
+    if (pl.waves == 8)
+        hipLaunchKernelGGL((attn_paged_kernel<D, 8>), grid, dim3(512), 0, stream, st, q, pa, partials, out, dm.n_heads, dm.n_kv_heads, pl.tiles, pl.chunk, pl.splits, pl.least);
+    else
+        hipLaunchKernelGGL((attn_paged_kernel<D, 4>), grid, dim3(256), 0, stream, st, q, pa, partials, out, dm.n_heads, dm.n_kv_heads, pl.tiles, pl.chunk, pl.splits, pl.least);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || pl.splits == 1) return e;
     const int threads = pl.splits > 4 * 64 / (D / 4) ? 256 : 64;      // one round of four splits per group of threads, if that is enough
