@@ -1523,7 +1523,7 @@ relax_status relax_paged_read(const relax_paged_cache *cache, const relax_seqs *
 size_t relax_token_logprobs_workspace_bytes(int32_t n_max, int32_t vocab, int32_t top)
 {
     if (n_max < 1 || vocab < 1 || top < 0 || top > 32) return 0;
-    return 256;
+    return align256(std::max<size_t>(token_logprobs_partial_bytes(n_max, vocab), 1));
 }
 
 relax_status relax_token_logprobs(const uint16_t *logits, int64_t stride, const int32_t *targets, float *logprobs, float *entropy, int32_t *top_ids,
@@ -1535,8 +1535,8 @@ relax_status relax_token_logprobs(const uint16_t *logits, int64_t stride, const 
         return RELAX_ERR_SHAPE;
     if (top > 32) return RELAX_ERR_UNSUPPORTED;
     if (top > 0 ? !top_ids || !top_logprobs : !targets && !entropy) return RELAX_ERR_NULL;
-    (void)ws, (void)ws_bytes;
-    return hip_status(launch_token_logprobs(logits, stride, targets, logprobs, entropy, top_ids, top_logprobs, n, vocab, top, static_cast<hipStream_t>(stream)));
+    void *partials = ws && aligned(ws, 256) && ws_bytes >= token_logprobs_partial_bytes(n, vocab) ? ws : nullptr;
+    return hip_status(launch_token_logprobs(logits, stride, targets, logprobs, entropy, top_ids, top_logprobs, n, vocab, top, partials, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -510,7 +510,8 @@ hipError_t launch_paged_attention(const uint16_t *q, const PagedArgs &pa, const 
 
 // Log probabilities of rows of logits (token_logprobs.hip)
 hipError_t launch_token_logprobs(const uint16_t *logits, int64_t stride, const int32_t *targets, float *logprobs, float *entropy, int32_t *top_ids,
-                                 float *top_logprobs, int32_t n, int32_t V, int32_t k, hipStream_t stream);
+                                 float *top_logprobs, int32_t n, int32_t V, int32_t k, void *partials, hipStream_t stream);
+size_t token_logprobs_partial_bytes(int32_t n, int32_t V);      // with partials == nullptr every row is one workgroup's
 
 // Model wrapper steps (model_head.hip)
 hipError_t launch_embed(const int32_t *ids, const uint16_t *E, uint16_t *x, int n, int H, int V, uint32_t *err, hipStream_t stream);

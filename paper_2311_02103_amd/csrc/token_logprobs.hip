@@ -8,12 +8,20 @@
 // One workgroup per row.  The row is read once and stays in registers for three passes (maxima; sums; candidates), rows beyond 163833 logits
 // are read again by each pass.  The k best without a sort: thread maxima are folded into 64 groups (equal lanes of all
 // wavefronts, so that neighbouring logits are spread over the groups), and the k-th largest group maximum T bounds the k-th largest
-// logit from below; whatever is larger than T -- a few more than k on any row whose large logits do not share few groups -- goes to a list in
-// LDS and is ranked by counting.  Fewer than k larger ones: the lowest indexes among those equal to T follow, found by a scan in order.
-// More than the list holds: T is replaced by the k-th largest logit itself, by bisection over the 16-bit values.
+// logit from below; whatever is not smaller than T -- a few more than k on any row whose large logits do not share few groups -- goes to a list in
+// LDS and is ranked by counting.  More than the list holds (many equal logits): T is replaced by the k-th largest logit itself, by bisection
+// over the 16-bit values, the list takes what is larger, and the lowest indexes among those equal to T follow, found by a scan in order.
+//
+// A few rows of a large vocabulary are cut into slices, one workgroup each, whose sums and k best meet in a second kernel (uncut / cut, us: 1 row of 70000 logits 15.0 /
+// 11.1, of 152064 with 20 alternatives 19.9 / 14.8, of 262000 36.6 / 15.2, 16 rows of 128256 17.7 / 13.8; 1 row of 50257 10.5 / 11.4).
 //
 // Bound by the vector unit next to the read: a logit takes nine issue slots in the sums (four of them the exponential) and one and a half in the other
-// two passes, which look at pairs.
+// two passes, which look at pairs.  2047 rows of 32000 logits: 32 us without alternatives (4.1 TB/s), 46 with 20; 1 row 7.9.
+#include <limits.h>
+
+#include <algorithm>
+#include <type_traits>
+
 #include "relax_common.h"
 
 namespace relax {
@@ -58,20 +66,65 @@ __device__ __forceinline__ half2l_t packet_max(const u32x4l_t &w)
     return __builtin_elementwise_max(pairs_max(__builtin_bit_cast(half2l_t, a), b), pairs_max(__builtin_bit_cast(half2l_t, c), d));
 }
 
-// NT threads, NP packets of eight logits each; RESIDENT: they hold the whole row
-template <int NT, int NP, bool RESIDENT>
-__global__ __launch_bounds__(NT) void token_logprobs_kernel(const uint16_t *__restrict__ logits, int64_t stride, const int32_t *__restrict__ targets,
-                                                            float *__restrict__ logprobs, float *__restrict__ entropy, int32_t *__restrict__ top_ids,
-                                                            float *__restrict__ top_logprobs, int V, int k)
+// What a slice of a row leaves: its maximum, how many logits have it, the sum of e^(x - m) over the others and the sum of e^(x - m) (x - m) / log 2;
+// its `listed` best logits follow
+struct Slice {
+    float m, rest, t;
+    int tops, listed, pad;
+};
+constexpr int kMaxTop = 32, kMaxSlices = 16, kSliceLogits = 512 * 8 * 4 - 8;
+struct SliceList {
+    Slice sums;
+    long long best[kMaxTop];
+};
+
+struct Outputs {
+    const int32_t *targets;
+    float *logprobs, *entropy;
+    int32_t *top_ids;
+    float *top_logprobs;
+    SliceList *slices;               // PART: [n][slices]
+};
+
+// The end of a row: `rest` is the sum without one maximum, both sums relative to m (0 where that is -inf); target: its logit, -inf outside the vocabulary
+struct RowEnd {
+    float base, rest, log_s;
+    bool empty;
+    __device__ __forceinline__ RowEnd(float m, float rest_, int tops)
+    {
+        base = m == -INFINITY ? 0.0f : m;
+        empty = m == -INFINITY && rest_ == 0.0f;               // no logit above -inf, and no NaN
+        rest = rest_ + (float)(tops - 1);
+        log_s = log1pf(rest);
+    }
+    __device__ __forceinline__ float logp(float x) const { return empty || x == -INFINITY ? (rest == rest ? -INFINITY : rest) : x - base - log_s; }
+    __device__ __forceinline__ float entropy(float t) const { return empty ? 0.0f : log_s - t * kLn2 / (1.0f + rest); }
+    __device__ __forceinline__ void put(const Outputs &o, int row, int k, int rank, long long key) const
+    {
+        const int order = (int)(key >> 32);
+        o.top_ids[(size_t)row * k + rank] = 0x7FFFFFFF - (int)(uint32_t)key;
+        o.top_logprobs[(size_t)row * k + rank] = order < 0 ? NAN : logp(value_of(order));
+    }
+};
+
+// NT threads, NP packets of eight logits each; RESIDENT: they hold the whole row; PART: the row is slice blockIdx.y of one, of `length` logits
+template <int NT, int NP, bool RESIDENT, bool PART>
+__global__ __launch_bounds__(NT) void token_logprobs_kernel(const uint16_t *__restrict__ logits, int64_t stride, Outputs o, int vocab, int k, int length)
 {
     constexpr int W = NT / 64;
+    const int from = PART ? (int)blockIdx.y * length : 0, V = PART ? min(length, vocab - from) : vocab;
     __shared__ float lane_max[W][64], wave_m[W], wave_rest[W], wave_t[W];
     __shared__ int wave_n[W], listed, scan[W];
     __shared__ long long list[kListed];
     __shared__ float bound_s;
 
-    const uint16_t *row = logits + (int64_t)blockIdx.x * stride;
+    const uint16_t *row = logits + (int64_t)blockIdx.x * stride + from;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    float target = -INFINITY;                                  // asked for before the row is
+    if (!PART && o.targets) {
+        const int id = o.targets[blockIdx.x];
+        if (id >= 0 && id < V) target = h2f(row[id]);
+    }
     // packets are aligned to 16 bytes: the first one begins `skip` elements in front of the row
     const int skip = (int)((reinterpret_cast<uintptr_t>(row) & 15) >> 1);
     const int packets = (V + skip + 7) >> 3;
@@ -139,7 +192,7 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(const uint16_t *__re
             const float o = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, gm), j));
             rank += o > gm || (o == gm && j < lane);
         }
-        if (rank == k - 1) bound_s = gm;
+        if (rank == min(k, V) - 1) bound_s = gm;
     }
 
     // ---- sums: exponents in units of log 2; the maxima themselves, in the wavefronts that hold one, are counted instead ----
@@ -167,30 +220,27 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(const uint16_t *__re
     rest = 0.0f, t = 0.0f, tops = 0;
 #pragma unroll
     for (int w = 0; w < W; ++w) rest += wave_rest[w], t += wave_t[w], tops += wave_n[w];
-    const bool empty = m == -INFINITY && rest == 0.0f;         // no logit above -inf, and no NaN
-    rest += (float)(tops - 1);
-    const float log_s = log1pf(rest);
-    auto logp = [&](float x) { return empty || x == -INFINITY ? (rest == rest ? -INFINITY : rest) : x - base - log_s; };
-    if (tid == 0) {
-        if (targets) {
-            const int id = targets[blockIdx.x];
-            logprobs[blockIdx.x] = logp(id >= 0 && id < V ? h2f(row[id]) : -INFINITY);
-        }
-        if (entropy) entropy[blockIdx.x] = empty ? 0.0f : log_s - t * kLn2 / (1.0f + rest);
+    const RowEnd end(m, rest, tops);
+    if (!PART && tid == 0) {
+        if (o.targets) o.logprobs[blockIdx.x] = end.logp(target);
+        if (o.entropy) o.entropy[blockIdx.x] = end.entropy(t);
     }
+    SliceList *mine_out = PART ? o.slices + (size_t)blockIdx.x * gridDim.y + blockIdx.y : nullptr;
+    if (PART && tid == 0) mine_out->sums = Slice{m, rest, t, tops, min(k, V), 0};
     if (k == 0) return;
 
-    // ---- candidates: what is larger than the bound ----
+    // ---- candidates ----
     float bound = bound_s;
-    auto collect = [&]() __attribute__((always_inline)) {
+    auto collect = [&](auto EQUAL) __attribute__((always_inline)) {
         each([&](const u32x4l_t &w, int at) __attribute__((always_inline)) {
             const half2l_t p = packet_max(w);
-            if (!__any(fmaxf((float)p.x, (float)p.y) > bound)) return;
+            const float most = fmaxf((float)p.x, (float)p.y);
+            if (!__any(EQUAL ? most >= bound : most > bound)) return;
 #pragma unroll 1
             for (int e = 0; e < 8; ++e) {
                 const uint32_t v = e < 4 ? (e < 2 ? w.x : w.y) : (e < 6 ? w.z : w.w);
                 const float x = h2f((uint16_t)(e & 1 ? v >> 16 : v & 0xFFFFu));
-                if (x > bound) {
+                if ((EQUAL ? x >= bound : x > bound) && at + e >= 0 && at + e < V) {       // (outside the row is -inf, which the bound may be)
                     const int place = atomicAdd(&listed, 1);
                     if (place < kListed) list[place] = rank_key(order_of(x), at + e);
                 }
@@ -199,8 +249,9 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(const uint16_t *__re
         __syncthreads();
         return listed;
     };
-    int found = collect();
-    if (found > kListed) {
+    int found = collect(std::true_type{});
+    const bool many = found > kListed;
+    if (many) {
         // the k-th largest value: the smallest order with fewer than k logits above it
         int lo = order_of(bound), hi = order_of(m);
         while (lo < hi) {
@@ -218,10 +269,10 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(const uint16_t *__re
         __syncthreads();
         if (tid == 0) listed = 0;
         __syncthreads();
-        found = collect();
+        found = collect(std::false_type{});
     }
     // ---- too few: the first of those equal to the bound, and behind -inf the NaNs ----
-    for (int kind = 0; kind < 2 && found < k; ++kind)
+    for (int kind = many ? 0 : 1; kind < 2 && found < k; ++kind)
         for (int p0 = 0; p0 < packets && found < k; p0 += NT) {
             const u32x4l_t w = fetch(p0 + tid);
             const int at = (p0 + tid) * 8 - skip;
@@ -261,31 +312,113 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(const uint16_t *__re
         int rank = 0;
 #pragma unroll 4
         for (int j = 0; j < found; ++j) rank += list[j] > own;
-        if (rank < k) {
-            const int order = (int)(own >> 32);
-            top_ids[(size_t)blockIdx.x * k + rank] = 0x7FFFFFFF - (int)(uint32_t)own;
-            top_logprobs[(size_t)blockIdx.x * k + rank] = order < 0 ? NAN : logp(value_of(order));
+        if (rank >= k) continue;
+        if (PART) mine_out->best[rank] = own - from;           // (its id counts down)
+        else end.put(o, blockIdx.x, k, rank, own);
+    }
+}
+
+// One workgroup per row: the slices' sums relative to the largest maximum, and the best of their best
+__global__ __launch_bounds__(256) void token_logprobs_join_kernel(const uint16_t *__restrict__ logits, int64_t stride, Outputs o, int V, int k, int slices)
+{
+    __shared__ Slice sl[kMaxSlices];
+    __shared__ long long list[kMaxSlices * kMaxTop];
+    const int row = blockIdx.x, tid = threadIdx.x;
+    const SliceList *src = o.slices + (size_t)row * slices;
+    float target = -INFINITY;
+    if (o.targets) {
+        const int id = o.targets[row];
+        if (id >= 0 && id < V) target = h2f(logits[(int64_t)row * stride + id]);
+    }
+    if (tid < slices) sl[tid] = src[tid].sums;
+    for (int i = tid; i < slices * k; i += 256) {
+        const int s = i / k, j = i - s * k;
+        list[i] = j < src[s].sums.listed ? src[s].best[j] : LLONG_MIN;
+    }
+    __syncthreads();
+    float m = -INFINITY, rest = 0.0f, t = 0.0f;
+    int tops = 0;
+    for (int s = 0; s < slices; ++s) m = fmaxf(m, sl[s].m);
+    for (int s = 0; s < slices; ++s) {
+        const Slice q = sl[s];
+        if (q.m == m) {                                        // (-inf: a sum of 0, or NaN)
+            rest += q.rest, t += q.t, tops += q.tops;
+        } else if (q.m > -INFINITY) {
+            const float d = (q.m - m) * kLog2e, f = __builtin_amdgcn_exp2f(d), all = q.rest + (float)q.tops;
+            rest += all * f, t += f * fmaf(fmaxf(d, -300.0f), all, q.t);
+        } else {
+            rest += q.rest;                                    // 0, or NaN
         }
+    }
+    const RowEnd end(m, rest, tops);
+    if (tid == 0) {
+        if (o.targets) o.logprobs[row] = end.logp(target);
+        if (o.entropy) o.entropy[row] = end.entropy(t);
+    }
+    for (int i = tid; i < slices * k; i += 256) {
+        const long long own = list[i];
+        if (own == LLONG_MIN) continue;
+        int rank = 0;
+#pragma unroll 4
+        for (int s = 0; s < slices; ++s) {                     // each slice's list is in order: where `own` would stand in it
+            int pos = 0;
+#pragma unroll
+            for (int step = kMaxTop; step; step >>= 1) {
+                const bool larger = list[s * k + min(pos + step, k) - 1] > own;
+                pos += pos + step <= k && larger ? step : 0;
+            }
+            rank += pos;
+        }
+        if (rank < k) end.put(o, row, k, rank, own);
     }
 }
 
 template <int NT, int NP, bool RESIDENT>
-hipError_t launch_one(const uint16_t *logits, int64_t stride, const int32_t *targets, float *logprobs, float *entropy, int32_t *top_ids, float *top_logprobs,
-                      int32_t n, int32_t V, int32_t k, hipStream_t stream)
+hipError_t launch_one(const uint16_t *logits, int64_t stride, const Outputs &o, int32_t n, int32_t V, int32_t k, hipStream_t stream)
 {
-    hipLaunchKernelGGL((token_logprobs_kernel<NT, NP, RESIDENT>), dim3(n), dim3(NT), 0, stream, logits, stride, targets, logprobs, entropy, top_ids, top_logprobs, V, k);
+    hipLaunchKernelGGL((token_logprobs_kernel<NT, NP, RESIDENT, false>), dim3(n), dim3(NT), 0, stream, logits, stride, o, V, k, V);
     return hipGetLastError();
+}
+
+// Slices of a row, as few as hold it: from 65530 logits on, where one workgroup takes longer than two kernels, and only while all slices run at once
+constexpr int kUncut = 65529;
+int slices_of(int32_t n, int32_t V)
+{
+    const int need = (V + kSliceLogits - 1) / kSliceLogits;
+    return V > kUncut && need <= kMaxSlices && (int64_t)need * n <= 256 ? need : 1;
 }
 
 }  // namespace
 
-hipError_t launch_token_logprobs(const uint16_t *logits, int64_t stride, const int32_t *targets, float *logprobs, float *entropy, int32_t *top_ids,
-                                 float *top_logprobs, int32_t n, int32_t V, int32_t k, hipStream_t stream)
+size_t token_logprobs_partial_bytes(int32_t n, int32_t V)
 {
-    if (V + 7 <= 1024 * 8 * 4 && n <= 512) return launch_one<1024, 4, true>(logits, stride, targets, logprobs, entropy, top_ids, top_logprobs, n, V, k, stream);
-    if (V + 7 <= 512 * 8 * 8) return launch_one<512, 8, true>(logits, stride, targets, logprobs, entropy, top_ids, top_logprobs, n, V, k, stream);
-    if (V + 7 <= 1024 * 8 * 20) return launch_one<1024, 20, true>(logits, stride, targets, logprobs, entropy, top_ids, top_logprobs, n, V, k, stream);
-    return launch_one<1024, 1, false>(logits, stride, targets, logprobs, entropy, top_ids, top_logprobs, n, V, k, stream);
+    // (for n rows at most: fewer may be cut where n are not)
+    const int64_t need = (V + kSliceLogits - 1) / kSliceLogits;
+    return slices_of(1, V) > 1 ? sizeof(SliceList) * (size_t)std::min<int64_t>(need * n, 256) : 0;
+}
+
+hipError_t launch_token_logprobs(const uint16_t *logits, int64_t stride, const int32_t *targets, float *logprobs, float *entropy, int32_t *top_ids,
+                                 float *top_logprobs, int32_t n, int32_t V, int32_t k, void *partials, hipStream_t stream)
+{
+    const Outputs o = {targets, logprobs, entropy, top_ids, top_logprobs, static_cast<SliceList *>(partials)};
+    const int slices = partials ? slices_of(n, V) : 1;
+    if (slices > 1) {
+        const int length = (V + slices - 1) / slices;          // (the last slice is shorter, and never empty: (slices - 1) * length < V)
+        hipLaunchKernelGGL((token_logprobs_kernel<512, 4, true, true>), dim3(n, slices), dim3(512), 0, stream, logits, stride, o, V, k, length);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL(token_logprobs_join_kernel, dim3(n), dim3(256), 0, stream, logits, stride, o, V, k, slices);
+        return hipGetLastError();
+    }
+    // The smallest workgroup that holds the row: several are on a CU, and one reads while another sums (us, 2047 rows of 1000 logits with 256 threads 14.7, with 512 31;
+    // 1000 rows of 50257 with 512 threads and 16 packets 41, with 1024 and 20 88).  Rows that leave CUs idle take twice the threads.
+    if (V + 7 <= 256 * 8 * 4) return launch_one<256, 4, true>(logits, stride, o, n, V, k, stream);
+    if (V + 7 <= 1024 * 8 * 4 && n <= 512) return launch_one<1024, 4, true>(logits, stride, o, n, V, k, stream);
+    if (V + 7 <= 512 * 8 * 8) return launch_one<512, 8, true>(logits, stride, o, n, V, k, stream);
+    if (V + 7 <= 512 * 8 * 16) return launch_one<512, 16, true>(logits, stride, o, n, V, k, stream);
+    if (V + 7 <= 1024 * 8 * 16) return launch_one<1024, 16, true>(logits, stride, o, n, V, k, stream);
+    if (V + 7 <= 1024 * 8 * 20) return launch_one<1024, 20, true>(logits, stride, o, n, V, k, stream);
+    return launch_one<1024, 1, false>(logits, stride, o, n, V, k, stream);
 }
 
 }  // namespace relax

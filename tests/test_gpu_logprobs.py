@@ -51,7 +51,7 @@ def check(x, targets, top, got):
 
 @pytest.mark.parametrize("ws", [True, False])
 @pytest.mark.parametrize("n,V,top", [(1, 1, 1), (1, 7, 7), (3, 33, 32), (2, 100, 0), (5, 688, 5), (1, 32000, 5), (4, 32000, 20), (2, 32761, 32), (2, 32762, 1),
-                                     (1, 50257, 10), (2, 65530, 3), (2, 128256, 32), (1, 152064, 20), (2, 163833, 8), (2, 163834, 8), (1, 262144, 32)])
+                                     (1, 50257, 10), (2, 65530, 3), (2, 128256, 32), (1, 152064, 20), (2, 163833, 8), (2, 163834, 8), (1, 262144, 32), (256, 32762, 3), (3, 262016, 32), (2, 262017, 32)])
 def test_rows(rx, n, V, top, ws):
     rng = np.random.default_rng(V)
     x = (rng.standard_normal((n, V)) * 2.5).astype(np.float16)
@@ -124,8 +124,8 @@ def test_many_rows_do_not_touch_each_other(rx):
     t = rng.integers(0, 4099, 700)
     got = call(rx, x, t, 4, offset=5, pad=2)
     check(x, t, 4, got)
-    one = call(rx, x[350:351], t[350:351], 4, ws=False)
-    assert got[0][350] == one[0][0] and got[1][350] == one[1][0]
+    # the row by itself; it is aligned otherwise there, so its sums are taken in another order
+    check(x[350:351], t[350:351], 4, call(rx, x[350:351], t[350:351], 4, ws=False))
 
 
 def test_behind_a_head_and_in_a_graph(rx):
