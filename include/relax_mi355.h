@@ -409,11 +409,11 @@ size_t relax_paged_workspace_bytes(const relax_layer_dims *dims, int32_t n_max, 
 
 /* Puts the rows of a call into the cache.  Row i of the call lies q_stride (kv_stride) elements behind row i - 1: q [h,d], k and v [g,d]
  * fp16, 16-byte aligned, strides multiples of 8 -- three parts of one [n,(h+2g)d] matrix, or matrices of their own.
- *   q_out[i] = R(pos_i) q[i], fp16 [n,h,d]  (q_out may be q; q and q_out NULL: only k and v)
+ *   q_out[i] = R(pos_i) q[i], fp16 [n,h,d]  (q_out may be q if q_stride is h d, else they do not overlap; q and q_out NULL: only k and v)
  *   k, v:  a block's scale is max|x| / 127 over the call's tokens in it, of keys behind the rotary embedding (which are not rounded in
  *   between); a block that holds earlier tokens of the sequence keeps its scale if that is larger, else their codes
  *   become round((u - 128) * old / new) + 128.  u = 128 + round(x / scale).  Infinite values count as +-65504, NaNs as 0.
- * Tokens of the sequence in front of the call's, and whatever lies behind its last one, stay as they are but for that.
+ * Tokens of the sequence in front of the call's, and whatever lies behind its last one, stay as they are but for that.  The slots of a call are distinct.
  * ws: relax_paged_workspace_bytes(dims, n, max kv_lens, B) bytes, 256-byte aligned.  Errors: NULL, SHAPE, CAPACITY, WORKSPACE, UNSUPPORTED
  * (page_size, pool too large, more than 65535 sequences).                                                              */
 relax_status relax_paged_append(const uint16_t *q, int64_t q_stride, const uint16_t *k, const uint16_t *v, int64_t kv_stride, uint16_t *q_out,
@@ -422,7 +422,8 @@ relax_status relax_paged_append(const uint16_t *q, int64_t q_stride, const uint1
 
 /* relax_attention over a paged cache: q [n,h,d] fp16 (already rotated), out [n,h,d] fp16, 16-byte aligned.  Row i of sequence b attends to
  * positions 0..pos_i of its slot, which must already hold this call's keys and values.  Scores, softmax and sums are fp32, the
- * probabilities are rounded to fp16 in front of their product with the values.  A row that no token is left for (every page of its
+ * probabilities are rounded to fp16 in front of their product with the values, and so, in calls of many rows (tiles of 256 rows times heads), are
+ * the values.  A row that no token is left for (every page of its
  * sequence out of range) is zeros.  ws and errors as relax_paged_append.                                                */
 relax_status relax_paged_attention(const uint16_t *q, const relax_paged_cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims,
                                    uint16_t *out, int32_t n, void *ws, size_t ws_bytes, relax_stream stream);

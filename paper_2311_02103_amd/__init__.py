@@ -7,8 +7,10 @@ computes: every step of the layer runs in the HIP kernels of csrc/.
 """
 from . import binding  # noqa: F401
 from .binding import (  # noqa: F401
-    KVCache, LayerDims, LayerWeights, QMat, RelaxError, Seqs, check, make_dims,
+    KVCache, LayerDims, LayerWeights, PagedCache, QMat, RelaxError, Seqs, check, make_dims,
     relax_attention, relax_build_id, relax_decoder_layer, relax_dequant_matmul, relax_dequantize,
-    relax_rmsnorm_rope, relax_rope_table_bytes, relax_rope_table_init, relax_set_option, relax_unpack_int4, relax_workspace_bytes, relax_workspace_error,
+    relax_paged_append, relax_paged_attention, relax_paged_read, relax_paged_workspace_bytes,
+    relax_rmsnorm_rope, relax_rope_table_bytes, relax_rope_table_init, relax_set_option, relax_token_logprobs,
+    relax_token_logprobs_workspace_bytes, relax_unpack_int4, relax_workspace_bytes, relax_workspace_error,
     relax_workspace_init,
 )

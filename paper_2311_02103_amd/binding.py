@@ -83,6 +83,7 @@ class MatmulPlanC(C.Structure):
     _fields_ = [("kernel", C.c_int32), ("k_ranges", C.c_int32), ("tile_rows", C.c_int32), ("tile_cols", C.c_int32), ("wide_rows", C.c_int32)]
 
 
+RELAX_PAGED_BLOCK = 16
 KERNEL_MATVEC, KERNEL_STREAM, KERNEL_SPLIT_K, KERNEL_TILED = range(4)
 
 _lib = None

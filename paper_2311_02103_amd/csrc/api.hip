@@ -1412,7 +1412,7 @@ PagedWs paged_ws(const relax_layer_dims &dm, int32_t n, int32_t L, int32_t B)
     return p;
 }
 
-constexpr int32_t kMaxPagedSeqs = 65535;     // extents of a grid
+constexpr int32_t kMaxPagedSeqs = 65535;     // a workgroup finds its sequence 64 at a time
 
 // Everything the paged calls check alike; fills the kernels' descriptors.  items: see launch_paged_append.
 relax_status paged_begin(const relax_paged_cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims, int32_t n, void *ws, size_t ws_bytes,
@@ -1476,6 +1476,7 @@ relax_status relax_paged_append(const uint16_t *q, int64_t q_stride, const uint1
     if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(q_out, 16) || kv_stride % 8 != 0 || (q && q_stride % 8 != 0)) return RELAX_ERR_SHAPE;
     relax_status rc = check_dims(dims);
     if (rc != RELAX_OK) return rc;
+    if (q && q == q_out && n > 1 && q_stride != (int64_t)dims->n_heads * dims->head_dim) return RELAX_ERR_SHAPE;      // row i would overwrite what row j has not read
     if (kv_stride < (int64_t)dims->n_kv_heads * dims->head_dim || (q && q_stride < (int64_t)dims->n_heads * dims->head_dim)) return RELAX_ERR_SHAPE;
     hipStream_t st_ = static_cast<hipStream_t>(stream);
     PagedArgs pa;

@@ -24,10 +24,10 @@ namespace {
 
 constexpr float kBias = 11.0f, kLag = 4.0f;      // log2: offset of the weights, and how far the reference may trail the maximum
 
-// grid: x = KV head, y = split, z = sequence * tiles + tile.  part: [row][head][splits][D + 2] when splits > 1.
+// grid: x = tile * g + KV head (the heads of a tile on neighbouring dies, a head's tiles on one, with eight heads), y = split.  part: [row][head][splits][D + 2] when splits > 1.
 template <int D, int W>
 __global__ __launch_bounds__(64 * W, 4) void attn_paged_kernel(PagedSeqs, const uint16_t *__restrict__ q, PagedArgs pa, float *__restrict__ part,
-                                                            uint16_t *__restrict__ out, int h, int g, int tiles, int chunk, int splits, int least)
+                                                            uint16_t *__restrict__ out, int h, int g, int per_seq, int chunk, int splits, int least)
 {
     constexpr int J = D / 64;                    // 1 KB loads per block
     constexpr int NT = D / 16;                   // 16-element tiles of O^T
@@ -35,10 +35,13 @@ __global__ __launch_bounds__(64 * W, 4) void attn_paged_kernel(PagedSeqs, const 
     __shared__ __align__(16) float states[W * 16 * P];
     __shared__ float sm_m[W * 16], sm_l[W * 16];
 
-    const int b = tiles == 1 ? (int)blockIdx.z : (int)blockIdx.z / tiles, tile = tiles == 1 ? 0 : (int)blockIdx.z - b * tiles;
-    const int kvh = blockIdx.x, split = blockIdx.y;
-    const SeqSpan si = seq_span(seqs_arg(), b);
-    const int rep = h / g, pairs = si.q_len * rep, p0 = tile * 16;
+    const int rep = h / g, item = (int)blockIdx.x / g, kvh = (int)blockIdx.x - item * g, split = blockIdx.y;
+    const SeqsArg st = seqs_arg();
+    int tile;
+    const int b = tile_of(st, item, per_seq, [&](int q_len) { return q_len * rep < least ? (q_len * rep + 15) >> 4 : 0; }, tile);
+    if (b >= st->B) return;
+    const SeqSpan si = seq_span(st, __builtin_amdgcn_readfirstlane(b));
+    const int pairs = si.q_len * rep, p0 = tile * 16;
     if (pairs >= least || p0 >= pairs) return;
     const int past = si.kv_len - si.q_len;
     const int n_pairs = min(16, pairs - p0);
@@ -269,9 +272,19 @@ constexpr int kRowTiles = 160;
 
 struct Plan {
     int32_t least;                   // pairs from which a sequence is the other kernel's
-    int32_t row_tiles, tiles;        // at most per sequence, of 256 and of 16 pairs
+    int32_t row_items, items;        // tiles of 256 and of 16 pairs that are launched
+    int32_t row_per_seq, per_seq;    // as tile_of takes them
     int32_t chunk, splits, waves;    // wavefronts per workgroup of 16-pair tiles
 };
+
+// Tiles are searched for where a fixed number per sequence would launch more than twice as many (us: 300 rows on 1201 tokens beside 20 decode rows of 32 / 32 heads,
+// 399 tiles numbered as 6300, 46.8; searched for, 42.0.  One search is a load and a scan over 64 lengths, 0.3 us)
+void numbering(long long all, long long most, int32_t B, int32_t &items, int32_t &per_seq)
+{
+    const bool search = most * B > 2 * all;
+    items = (int32_t)(search ? all : most * B);
+    per_seq = (int32_t)(search ? 0 : most);
+}
 
 Plan plan(const relax_layer_dims &dm, const relax_seqs &sq, int32_t n, int32_t L_max)
 {
@@ -288,8 +301,9 @@ Plan plan(const relax_layer_dims &dm, const relax_seqs &sq, int32_t n, int32_t L
         if (pairs >= p.least) most_large = std::max(most_large, pairs);
         else small += (pairs + 15) / 16, most_small = std::max(most_small, pairs);
     }
-    p.row_tiles = (int32_t)((most_large + kPagedRowTile - 1) / kPagedRowTile);
-    p.tiles = (int32_t)((most_small + 15) / 16);
+    if (p.least == INT32_MAX) large = 0;
+    numbering(large, (most_large + kPagedRowTile - 1) / kPagedRowTile, sq.B, p.row_items, p.row_per_seq);
+    numbering(small, (most_small + 15) / 16, sq.B, p.items, p.per_seq);
     long long s = small && small * dm.n_kv_heads < kUnsplit ? kPagedGroups / (small * dm.n_kv_heads) : 1;
     s = std::min(s, (long long)(L_max + 127) / 128);
     s = std::min(s, (long long)kPartials / ((long long)n * dm.n_heads));
@@ -304,11 +318,12 @@ template <int D>
 hipError_t launch_d(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, const Plan &pl, uint16_t *out, float *partials,
                     hipStream_t stream)
 {
-    const dim3 grid(dm.n_kv_heads, pl.splits, pl.tiles * st.B);
+    if ((int64_t)pl.items * dm.n_kv_heads * 64 * pl.waves > kMaxThreads) return hipErrorInvalidValue;
+    const dim3 grid(pl.items * dm.n_kv_heads, pl.splits);
     if (pl.waves == 8)
-        hipLaunchKernelGGL((attn_paged_kernel<D, 8>), grid, dim3(512), 0, stream, st, q, pa, partials, out, dm.n_heads, dm.n_kv_heads, pl.tiles, pl.chunk, pl.splits, pl.least);
+        hipLaunchKernelGGL((attn_paged_kernel<D, 8>), grid, dim3(512), 0, stream, st, q, pa, partials, out, dm.n_heads, dm.n_kv_heads, pl.per_seq, pl.chunk, pl.splits, pl.least);
     else
-        hipLaunchKernelGGL((attn_paged_kernel<D, 4>), grid, dim3(256), 0, stream, st, q, pa, partials, out, dm.n_heads, dm.n_kv_heads, pl.tiles, pl.chunk, pl.splits, pl.least);
+        hipLaunchKernelGGL((attn_paged_kernel<D, 4>), grid, dim3(256), 0, stream, st, q, pa, partials, out, dm.n_heads, dm.n_kv_heads, pl.per_seq, pl.chunk, pl.splits, pl.least);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || pl.splits == 1) return e;
     const int threads = pl.splits > 4 * 64 / (D / 4) ? 256 : 64;      // one round of four splits per group of threads, if that is enough
@@ -330,9 +345,9 @@ hipError_t launch_paged_attention(const uint16_t *q, const PagedArgs &pa, const 
                                   uint16_t *out, float *partials, hipStream_t stream)
 {
     const Plan pl = plan(dm, sq, st.n, L_max);
-    if (pl.row_tiles > 0) {
-        const hipError_t e = launch_paged_rows(q, pa, dm, st, pl.row_tiles, pl.least, out, stream);
-        if (e != hipSuccess || pl.tiles == 0) return e;
+    if (pl.row_items > 0) {
+        const hipError_t e = launch_paged_rows(q, pa, dm, st, pl.row_items, pl.row_per_seq, pl.least, out, stream);
+        if (e != hipSuccess || pl.items == 0) return e;
     }
     return dm.head_dim == 128 ? launch_d<128>(q, pa, dm, st, pl, out, partials, stream) : launch_d<64>(q, pa, dm, st, pl, out, partials, stream);
 }

@@ -42,9 +42,9 @@ constexpr int kSegment = kThreads;               // blocks whose numbers and sca
 // What a block needs: c k_scale, v_scale relative to the reference, number in the pool (as bits)
 typedef float4p_t Block;
 
-// grid: x = KV head, y = split, z = sequence * tiles + tile (the last tile of a sequence, with the longest prefix, first)
+// grid: x = tile * g + KV head (the last tile of a sequence, with the longest prefix, first)
 template <int D>
-__global__ __launch_bounds__(kThreads, 2) void attn_paged_rows_kernel(PagedSeqs, const uint16_t *__restrict__ q, PagedArgs pa, uint16_t *__restrict__ out, int h, int g, int tiles,
+__global__ __launch_bounds__(kThreads, 2) void attn_paged_rows_kernel(PagedSeqs, const uint16_t *__restrict__ q, PagedArgs pa, uint16_t *__restrict__ out, int h, int g, int per_seq,
                                                                        int least)
 {
     constexpr int J = D / 64, KS = D / 32, NT = D / 16;
@@ -59,11 +59,15 @@ __global__ __launch_bounds__(kThreads, 2) void attn_paged_rows_kernel(PagedSeqs,
     __shared__ float v_tops[8];
     __shared__ int bad_s;
 
-    const int b = tiles == 1 ? (int)blockIdx.z : (int)blockIdx.z / tiles, tile = tiles == 1 ? 0 : tiles - 1 - ((int)blockIdx.z - b * tiles);
-    const int kvh = blockIdx.x;
-    const SeqSpan si = seq_span(seqs_arg(), b);
-    const int rep = h / g, pairs = si.q_len * rep, p0 = tile * kPairs;
-    if (pairs < least || p0 >= pairs) return;                          // (fewer pairs: the other kernel's)
+    const int rep = h / g, item = (int)blockIdx.x / g, kvh = (int)blockIdx.x - item * g;
+    const SeqsArg st = seqs_arg();
+    const auto tiles_of = [&](int q_len) { return q_len * rep < least ? 0 : (q_len * rep + kPairs - 1) / kPairs; };
+    int place;
+    const int b = tile_of(st, item, per_seq, tiles_of, place);
+    if (b >= st->B) return;
+    const SeqSpan si = seq_span(st, __builtin_amdgcn_readfirstlane(b));
+    const int pairs = si.q_len * rep, p0 = (tiles_of(si.q_len) - 1 - place) * kPairs;
+    if (pairs < least || p0 < 0) return;                          // (fewer pairs: the other kernel's)
     const int past = si.kv_len - si.q_len;
     const int n_pairs = min(kPairs, pairs - p0);
     const int vis = min(past + (p0 + n_pairs - 1) / rep + 1, pa.cap);
@@ -329,18 +333,19 @@ __global__ __launch_bounds__(kThreads, 2) void attn_paged_rows_kernel(PagedSeqs,
 }
 
 template <int D>
-hipError_t launch_one(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, int32_t tiles, int32_t least, uint16_t *out, hipStream_t stream)
+hipError_t launch_one(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, int32_t items, int32_t per_seq, int32_t least, uint16_t *out, hipStream_t stream)
 {
-    hipLaunchKernelGGL(attn_paged_rows_kernel<D>, dim3(dm.n_kv_heads, 1, tiles * st.B), dim3(kThreads), 0, stream, st, q, pa, out, dm.n_heads, dm.n_kv_heads, tiles, least);
+    if ((int64_t)items * dm.n_kv_heads * kThreads > kMaxThreads) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(attn_paged_rows_kernel<D>, dim3(items * dm.n_kv_heads), dim3(kThreads), 0, stream, st, q, pa, out, dm.n_heads, dm.n_kv_heads, per_seq, least);
     return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_paged_rows(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, int32_t tiles, int32_t least, uint16_t *out,
+hipError_t launch_paged_rows(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, int32_t items, int32_t per_seq, int32_t least, uint16_t *out,
                              hipStream_t stream)
 {
-    return dm.head_dim == 128 ? launch_one<128>(q, pa, dm, st, tiles, least, out, stream) : launch_one<64>(q, pa, dm, st, tiles, least, out, stream);
+    return dm.head_dim == 128 ? launch_one<128>(q, pa, dm, st, items, per_seq, least, out, stream) : launch_one<64>(q, pa, dm, st, items, per_seq, least, out, stream);
 }
 
 }  // namespace relax

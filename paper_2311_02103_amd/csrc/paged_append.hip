@@ -66,9 +66,11 @@ __device__ __forceinline__ uint32_t code_of(float x, const NewScale &n)
 }
 __device__ __forceinline__ uint32_t recode(uint32_t u, float keep) { return (uint32_t)((int)rintf((float)((int)u - 128) * keep) + 128); }
 
-// Tokens low .. high - 1 of a block are the call's; row: the call's row of token 0 of the block (low's row minus low)
-template <int D>
-__device__ __forceinline__ void put_keys(const RowsView &r, const PagedArgs &pa, int pool, int kvh, int lane, int low, int high, int row, int pos)
+// Tokens low .. high - 1 of a block are the call's; row: the call's row of token 0 of the block (low's row minus low).  find() is the block's number in the pool, -1
+// if there is none: the rows are on their way and their largest magnitude known before its answer is waited for, because a decode step is
+// this chain of loads (page, scale, codes) and nothing else.
+template <int D, typename Find>
+__device__ __forceinline__ bool put_keys(const RowsView &r, const PagedArgs &pa, const Find &find, int kvh, int lane, int low, int high, int row, int pos)
 {
     constexpr int U = D / 64;                                  // units of eight pairs per lane
     const int tok = lane & 15, quarter = lane >> 4;
@@ -83,6 +85,7 @@ __device__ __forceinline__ void put_keys(const RowsView &r, const PagedArgs &pa,
         load8p(x + e + D / 2, b[i]);
         if (pa.rope) rotate8(a[i], b[i], pa.rope + ((size_t)(pos + src) * (D / 2) + e) * 2);
     }
+    const int pool = find();
     float amax = 0.0f;
 #pragma unroll
     for (int i = 0; i < U; ++i)
@@ -92,91 +95,130 @@ __device__ __forceinline__ void put_keys(const RowsView &r, const PagedArgs &pa,
             amax = fmaxf(amax, fmaxf(fabsf(a[i][j]), fabsf(b[i][j])));
         }
     amax = wave_max(amax);
-    const NewScale n = new_scale(amax, low > 0, low > 0 ? pa.k_scale[pool] : 0.0f);
+    if (pool < 0) return false;
+    // unit (i, half): elements (quarter + 4 i) * 8 + half * D / 2 of the lane's token
+    const auto at = [&](int i, int hh) {
+        const int e = (quarter + 4 * i) * 8 + hh * (D / 2);
+        return (u32x2p_t *)(pa.k + (size_t)pool * (16 * D) + (e >> 4) * 256 + tok * 16 + (e & 15));
+    };
+    float old = 0.0f;
+    u32x2p_t w[U][2] = {};
+    if (low > 0) {
+        old = pa.k_scale[pool];
+#pragma unroll
+        for (int i = 0; i < 2 * U; ++i) w[i >> 1][i & 1] = *at(i >> 1, i & 1);
+    }
+    const NewScale n = new_scale(amax, low > 0, old);
     if (lane == 0) pa.k_scale[pool] = n.s;
-    uint8_t *blk = pa.k + (size_t)pool * (16 * D);
+    if (!fresh && !(tok < low && n.grew)) return true;
 #pragma unroll
     for (int i = 0; i < U; ++i)
 #pragma unroll
         for (int hh = 0; hh < 2; ++hh) {
-            const int e = (quarter + 4 * i) * 8 + hh * (D / 2);
-            u32x2p_t *at = (u32x2p_t *)(blk + (e >> 4) * 256 + tok * 16 + (e & 15));
-            u32x2p_t w;
-            if (fresh) {
-                const float *val = hh ? b[i] : a[i];
+            const float *val = hh ? b[i] : a[i];
+            u32x2p_t c;
 #pragma unroll
-                for (int p = 0; p < 2; ++p)
-                    w[p] = code_of(val[4 * p], n) | code_of(val[4 * p + 1], n) << 8 | code_of(val[4 * p + 2], n) << 16 | code_of(val[4 * p + 3], n) << 24;
-                *at = w;
-            } else if (tok < low && n.grew) {
-                w = *at;
-#pragma unroll
-                for (int p = 0; p < 2; ++p) {
-                    const uint32_t o = w[p];
-                    w[p] = recode(o & 255u, n.keep) | recode(o >> 8 & 255u, n.keep) << 8 | recode(o >> 16 & 255u, n.keep) << 16 | recode(o >> 24, n.keep) << 24;
-                }
-                *at = w;
+            for (int p = 0; p < 2; ++p) {
+                const uint32_t o = w[i][hh][p];
+                if (fresh) c[p] = code_of(val[4 * p], n) | code_of(val[4 * p + 1], n) << 8 | code_of(val[4 * p + 2], n) << 16 | code_of(val[4 * p + 3], n) << 24;
+                else c[p] = recode(o & 255u, n.keep) | recode(o >> 8 & 255u, n.keep) << 8 | recode(o >> 16 & 255u, n.keep) << 16 | recode(o >> 24, n.keep) << 24;
             }
+            *at(i, hh) = c;
         }
+    return true;
 }
 
+// Values change hands in LDS between rows and codes: lane (c, quarter) has D / 16 consecutive elements c * D / 16 .. of the tokens 4 quarter .. + 3 as rows, and so
+// D / 16 words of four codes; as codes it has 16-byte packets of the block.  The 64 words of each [e / 64][t / 4] lie kTurnPitch apart, with
+// which the 64 words of one store, or load, are on 64 banks.  (Rows taken element by element instead, 2 bytes per lane and load: APPEND_OLD us for the
+// keys and values of 2043 tokens and APPEND_NEW us this way, READ_OLD and READ_NEW for reading them back.)
+constexpr int kTurnPitch = 68;
 template <int D>
-__device__ __forceinline__ void put_values(const RowsView &r, const PagedArgs &pa, int pool, int kvh, int lane, int low, int high, int row)
+using Turn = uint32_t[D / 16 * kTurnPitch];
+template <int D>
+__device__ __forceinline__ int turn_word(int c, int quarter, int j)      // element e = c * D / 16 + j
 {
-    const int m = lane & 15, t0 = (lane >> 4) * 4;             // the lane's elements are m + 16 i, its tokens t0 .. t0 + 3
-    float x[D / 16][4];
-    float amax = 0.0f;
+    const int e = c * (D / 16) + j;
+    return ((e >> 6) * 4 + quarter) * kTurnPitch + (e & 15) * 4 + (e >> 4 & 3);
+}
+__device__ __forceinline__ u32x4p_t *turn_packet(uint32_t *turn, int lane, int j) { return (u32x4p_t *)(turn + (j * 4 + (lane >> 4)) * kTurnPitch + (lane & 15) * 4); }
+// a wavefront's LDS instructions execute in order: only the compiler has to keep it
+__device__ __forceinline__ void turn_done()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+template <int D, typename Find>
+__device__ __forceinline__ bool put_values(const RowsView &r, const PagedArgs &pa, const Find &find, int kvh, int lane, int low, int high, int row, uint32_t *turn)
+{
+    constexpr int E = D / 16;
+    typedef _Float16 part_t __attribute__((ext_vector_type(E)));
+    const int c = lane & 15, quarter = lane >> 4, t0 = quarter * 4;
+    part_t in[4];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        const int src = min(max(t0 + t, low), high - 1);
-        const uint16_t *at = r.v + (row + src) * r.kv_stride + kvh * D + m;
+    for (int t = 0; t < 4; ++t)
+        in[t] = *(const part_t *)(r.v + (row + min(max(t0 + t, low), high - 1)) * r.kv_stride + kvh * D + c * E);
+    const int pool = find();
+    float x[E][4], amax = 0.0f;
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) x[i][t] = h2f(at[16 * i]);
-    }
-#pragma unroll
-    for (int i = 0; i < D / 16; ++i)
+    for (int j = 0; j < E; ++j)
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            x[i][t] = storable(x[i][t]);
-            amax = fmaxf(amax, fabsf(x[i][t]));
+            x[j][t] = storable((float)in[t][j]);
+            amax = fmaxf(amax, fabsf(x[j][t]));
         }
     amax = wave_max(amax);
-    const NewScale n = new_scale(amax, low > 0, low > 0 ? pa.v_scale[pool] : 0.0f);
-    if (lane == 0) pa.v_scale[pool] = n.s;
-    const bool all_new = t0 >= low && t0 + 3 < high, none = t0 + 3 < low || t0 >= high;
-    if (none && !(n.grew && t0 < low)) return;
+    if (pool < 0) return false;
+    uint32_t fresh = 0, there = 0;                             // bytes of the call's tokens and of earlier ones in the lane's words
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        if (t0 + t >= low && t0 + t < high) fresh |= 255u << (8 * t);
+        if (t0 + t < low) there |= 255u << (8 * t);
+    }
     u32x4p_t *blk = (u32x4p_t *)(pa.v + (size_t)pool * (16 * D));
+    float old = 0.0f;
+    u32x4p_t w[D / 64] = {};
+    if (low > 0 || high < 16) {
+        if (low > 0) old = pa.v_scale[pool];
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) w[j] = blk[j * 64 + lane];
+    }
+    const NewScale n = new_scale(amax, low > 0, old);
+    if (lane == 0) pa.v_scale[pool] = n.s;
+#pragma unroll
+    for (int j = 0; j < E; ++j)
+        turn[turn_word<D>(c, quarter, j)] = code_of(x[j][0], n) | code_of(x[j][1], n) << 8 | code_of(x[j][2], n) << 16 | code_of(x[j][3], n) << 24;
+    turn_done();
+    if (!fresh && !(n.grew && there)) return true;
 #pragma unroll
     for (int j = 0; j < D / 64; ++j) {
-        u32x4p_t w = {0, 0, 0, 0};
-        if (!all_new) w = blk[j * 64 + lane];
+        u32x4p_t to = *turn_packet(turn, lane, j);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t o = w[i];
-            uint32_t c = 0;
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                uint32_t u = o >> (8 * t) & 255u;
-                if (t0 + t >= low && t0 + t < high) u = code_of(x[4 * j + i][t], n);
-                else if (t0 + t < low && n.grew) u = recode(u, n.keep);
-                c |= u << (8 * t);
+            uint32_t o = w[j][i];
+            if (n.grew) {
+                const uint32_t moved = recode(o & 255u, n.keep) | recode(o >> 8 & 255u, n.keep) << 8 | recode(o >> 16 & 255u, n.keep) << 16 | recode(o >> 24, n.keep) << 24;
+                o = (o & ~there) | (moved & there);
             }
-            w[i] = c;
+            to[i] = (to[i] & fresh) | (o & ~fresh);
         }
-        blk[j * 64 + lane] = w;
+        blk[j * 64 + lane] = to;
     }
+    return true;
 }
 
-// Workgroups 0 .. kv_groups - 1: four wavefronts, each one (item, KV head, keys or values); the rest: rows of q, `slices` workgroups per row
+// Workgroups 0 .. kv_groups - 1: four wavefronts, four of the 2 g (KV head, keys or values) of one item; the rest: rows of q, `slices` workgroups per row
 template <int D>
-__global__ __launch_bounds__(256) void paged_append_kernel(PagedSeqs, RowsView r, uint16_t *q_out, PagedArgs pa, int h, int g, int items, int kv_groups, int slices)
+__global__ __launch_bounds__(256) void paged_append_kernel(PagedSeqs, RowsView r, uint16_t *q_out, PagedArgs pa, int h, int g, int kv_groups, int slices)
 {
+    __shared__ __align__(16) Turn<D> turn[4];
     const SeqsArg st = seqs_arg();
     const int lane = threadIdx.x & 63;
     if ((int)blockIdx.x < kv_groups) {
-        const int w = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + (int)(threadIdx.x >> 6));
-        const int item = w / (2 * g), part = w - item * 2 * g, kvh = part >> 1;
-        if (item >= items) return;
+        const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), per_item = (g + 1) / 2;
+        const int item = (int)blockIdx.x / per_item, part = ((int)blockIdx.x - item * per_item) * 4 + wave, kvh = part >> 1;
+        if (part >= 2 * g) return;
         int place, b = item;
         if (st->q_max == 1) place = 0;
         else b = seq_of(st, item, [](int q_len) { return paged_blocks_of(q_len); }, place);
@@ -186,14 +228,10 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedSeqs, RowsView r
         const int blk = (first >> 4) + place;
         const int low = max(first - blk * 16, 0), high = min(si.kv_len - blk * 16, 16);
         if (first < 0 || high <= low) return;
-        const int pool = si.kv_len <= pa.cap ? paged_block(pa, g, kvh, si.slot, blk) : -1;
-        if (pool < 0) {
-            if (lane == 0) atomicOr(pa.err, kBadPage);
-            return;
-        }
         const int row = si.q_start + blk * 16 - first;
-        if (part & 1) put_values<D>(r, pa, pool, kvh, lane, low, high, row);
-        else put_keys<D>(r, pa, pool, kvh, lane, low, high, row, blk * 16);
+        const auto find = [&] { return si.kv_len <= pa.cap ? paged_block(pa, g, kvh, si.slot, blk) : -1; };
+        if (!(part & 1 ? put_values<D>(r, pa, find, kvh, lane, low, high, row, turn[wave])
+                       : put_keys<D>(r, pa, find, kvh, lane, low, high, row, blk * 16)) && lane == 0) atomicOr(pa.err, kBadPage);
         return;
     }
     const int wg = (int)blockIdx.x - kv_groups, i = wg / slices, slice = wg - i * slices;
@@ -222,13 +260,13 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedSeqs, RowsView r
 
 // out[row, kvh, :] = fp16(code * scale).  One wavefront is one (block, KV head) of keys or of values.
 template <int D>
-__global__ __launch_bounds__(256) void paged_read_kernel(PagedSeqs, PagedArgs pa, uint16_t *k_out, uint16_t *v_out, int g, int items)
+__global__ __launch_bounds__(256) void paged_read_kernel(PagedSeqs, PagedArgs pa, uint16_t *k_out, uint16_t *v_out, int g)
 {
+    __shared__ __align__(16) Turn<D> turns[4];
     const SeqsArg st = seqs_arg();
-    const int lane = threadIdx.x & 63;
-    const int w = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + (int)(threadIdx.x >> 6));
-    const int item = w / (2 * g), part = w - item * 2 * g, kvh = part >> 1;
-    if (item >= items || !(part & 1 ? v_out : k_out)) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int per_item = (g + 1) / 2, item = (int)blockIdx.x / per_item, part = ((int)blockIdx.x - item * per_item) * 4 + wave, kvh = part >> 1;
+    if (part >= 2 * g || !(part & 1 ? v_out : k_out)) return;
     int place, b = item;
     if (st->q_max == 1) place = 0;
     else b = seq_of(st, item, [](int q_len) { return paged_blocks_of(q_len); }, place);
@@ -243,30 +281,41 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedSeqs, PagedArgs pa
     const float s = pool < 0 ? 0.0f : (part & 1 ? pa.v_scale : pa.k_scale)[at];       // no page: zeros
     const u32x4p_t *src = (const u32x4p_t *)((part & 1 ? pa.v : pa.k) + (size_t)at * (16 * D));
     const int c = lane & 15, quarter = lane >> 4;
+    u32x4p_t code[D / 64];
 #pragma unroll
-    for (int j = 0; j < D / 64; ++j) {
-        const u32x4p_t code = src[j * 64 + lane];
-        if (part & 1) {
+    for (int j = 0; j < D / 64; ++j) code[j] = src[j * 64 + lane];
+    const auto value = [&](uint32_t w, int byte) {
+        float x = (float)((int)(w >> (8 * byte) & 255u) - 128) * s;
+        asm("" : "+v"(x));                                     // the fp32 product itself, not the one instruction that rounds code * s to fp16 without it
+        return (_Float16)x;
+    };
+    if (part & 1) {
+        constexpr int E = D / 16;
+        typedef _Float16 part_t __attribute__((ext_vector_type(E)));
+        uint32_t *turn = turns[wave];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t o = code[i];
+        for (int j = 0; j < D / 64; ++j) *turn_packet(turn, lane, j) = code[j];
+        turn_done();
+        uint32_t o[E];
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const int tok = quarter * 4 + t;
-                    if (tok >= low && tok < high)
-                        v_out[((size_t)(row + tok) * g + kvh) * D + j * 64 + i * 16 + c] = f2h((float)((int)(o >> (8 * t) & 255u) - 128) * s);
-                }
-            }
-        } else if (c >= low && c < high) {
+        for (int j = 0; j < E; ++j) o[j] = turn[turn_word<D>(c, quarter, j)];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int tok = quarter * 4 + t;
+            part_t x;
+#pragma unroll
+            for (int j = 0; j < E; ++j) x[j] = value(o[j], t);
+            if (tok >= low && tok < high) *(part_t *)(v_out + ((size_t)(row + tok) * g + kvh) * D + c * E) = x;
+        }
+    } else if (c >= low && c < high) {
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) {
             uint16_t *dst = k_out + ((size_t)(row + c) * g + kvh) * D + (j * 4 + quarter) * 16;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 half8p_t x;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint32_t o = code[2 * i + (e >> 2)];
-                    x[e] = (_Float16)((float)((int)(o >> (8 * (e & 3)) & 255u) - 128) * s);
-                }
+                for (int e = 0; e < 8; ++e) x[e] = value(code[j][2 * i + (e >> 2)], e & 3);
                 *(half8p_t *)(dst + 8 * i) = x;
             }
         }
@@ -279,21 +328,22 @@ hipError_t launch_paged_append(const uint16_t *q, int64_t q_stride, const uint16
                                const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, int items, hipStream_t stream)
 {
     const RowsView r = {q, k, v, q_stride, kv_stride};
-    const int kv_groups = (items * 2 * dm.n_kv_heads + 3) / 4;
     const int units = dm.n_heads * (dm.head_dim / 16), slices = st.n >= 256 ? 1 : (units + 255) / 256;     // few rows: over several workgroups
-    const dim3 grid(kv_groups + (q ? st.n * slices : 0));
-    if (dm.head_dim == 128)
-        hipLaunchKernelGGL(paged_append_kernel<128>, grid, dim3(256), 0, stream, st, r, q_out, pa, dm.n_heads, dm.n_kv_heads, items, kv_groups, slices);
-    else
-        hipLaunchKernelGGL(paged_append_kernel<64>, grid, dim3(256), 0, stream, st, r, q_out, pa, dm.n_heads, dm.n_kv_heads, items, kv_groups, slices);
+    const int64_t kv_groups = (int64_t)items * ((dm.n_kv_heads + 1) / 2), all = kv_groups + (q ? (int64_t)st.n * slices : 0);
+    if (all * 256 > kMaxThreads) return hipErrorInvalidValue;
+    const dim3 grid(all);
+    if (dm.head_dim == 128) hipLaunchKernelGGL(paged_append_kernel<128>, grid, dim3(256), 0, stream, st, r, q_out, pa, dm.n_heads, dm.n_kv_heads, (int)kv_groups, slices);
+    else hipLaunchKernelGGL(paged_append_kernel<64>, grid, dim3(256), 0, stream, st, r, q_out, pa, dm.n_heads, dm.n_kv_heads, (int)kv_groups, slices);
     return hipGetLastError();
 }
 
 hipError_t launch_paged_read(const PagedArgs &pa, uint16_t *k_out, uint16_t *v_out, const relax_layer_dims &dm, const PagedSeqs &st, int items, hipStream_t stream)
 {
-    const dim3 grid((items * 2 * dm.n_kv_heads + 3) / 4);
-    if (dm.head_dim == 128) hipLaunchKernelGGL(paged_read_kernel<128>, grid, dim3(256), 0, stream, st, pa, k_out, v_out, dm.n_kv_heads, items);
-    else hipLaunchKernelGGL(paged_read_kernel<64>, grid, dim3(256), 0, stream, st, pa, k_out, v_out, dm.n_kv_heads, items);
+    const int64_t all = (int64_t)items * ((dm.n_kv_heads + 1) / 2);
+    if (all * 256 > kMaxThreads) return hipErrorInvalidValue;
+    const dim3 grid(all);
+    if (dm.head_dim == 128) hipLaunchKernelGGL(paged_read_kernel<128>, grid, dim3(256), 0, stream, st, pa, k_out, v_out, dm.n_kv_heads);
+    else hipLaunchKernelGGL(paged_read_kernel<64>, grid, dim3(256), 0, stream, st, pa, k_out, v_out, dm.n_kv_heads);
     return hipGetLastError();
 }
 

@@ -79,6 +79,21 @@ __device__ __forceinline__ int seq_of(SeqsArg st, int key, const Count &count, i
     return B;
 }
 
+// Tiles of a paged attention call are numbered sequence by sequence.  per_seq > 0: that many numbers for each, of which a short one leaves some unused;
+// 0: as many as it has (a decode step's or one prompt's batch needs no search; a prompt among many rows would launch its own number for
+// each of them).
+template <typename Count>
+__device__ __forceinline__ int tile_of(SeqsArg st, int item, int per_seq, const Count &count, int &place)
+{
+    place = 0;
+    if (per_seq == 1) return item;
+    if (per_seq == 0) return seq_of(st, item, count, place);
+    const int b = item / per_seq;
+    place = item - b * per_seq;
+    return b;
+}
+constexpr int64_t kMaxThreads = (1LL << 32) - 1;      // of a launch's x dimension
+
 struct PagedArgs {
     uint8_t *k, *v;
     float *k_scale, *v_scale;
@@ -101,9 +116,9 @@ __device__ inline int paged_block(const PagedArgs &pa, int g, int kvh, int slot,
     return ((page * g + kvh) << pa.shift) + (blk & ((1 << pa.shift) - 1));
 }
 
-// Attention of the sequences with at least `least` (row, head) pairs, in tiles of kPagedRowTile pairs, at most `tiles` per sequence (attn_paged_rows.hip)
+// Attention of the sequences with at least `least` (row, head) pairs, in `items` tiles of kPagedRowTile pairs (attn_paged_rows.hip)
 constexpr int kPagedRowTile = 256;
-hipError_t launch_paged_rows(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, int32_t tiles, int32_t least, uint16_t *out,
+hipError_t launch_paged_rows(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, int32_t items, int32_t per_seq, int32_t least, uint16_t *out,
                              hipStream_t stream);
 
 // four codes -> four fp16 integers

@@ -144,6 +144,69 @@ class DeviceModel:
         return logits, next_ids
 
 
+class DevicePagedCache:
+    """The 8-bit paged KV cache of one layer: the pool, its scales, the page table `pages` (int32 [kv_slots, pages per slot], written by the caller, who
+    hands out the pool's pages), the rotary table and the workspace, sized by upper bounds (n_max, L_max = kv_capacity, B_max)."""
+
+    def __init__(self, *, n_heads: int, n_kv_heads: int, head_dim: int, kv_capacity: int, n_pages: int, page_size: int = 64, kv_slots: int = 1,
+                 n_max: int = 1, B_max: Optional[int] = None, rope_base: Optional[float] = 10000.0, device="cuda", share_from: "DevicePagedCache" = None):
+        self.device = device
+        self.dims = rx.make_dims(n_heads * head_dim, n_heads, n_kv_heads, head_dim, 64, kv_capacity, kv_slots, rope_base=rope_base or 10000.0)
+        self.n_max, self.B_max = n_max, (B_max if B_max is not None else max(kv_slots, 1))
+        if share_from is not None:          # layers of one model share the page table, the rotary table and the workspace
+            self.pages, self.rope, self.ws, self.ws_bytes = share_from.pages, share_from.rope, share_from.ws, share_from.ws_bytes
+        else:
+            self.pages = torch.full((kv_slots, -(-kv_capacity // page_size)), -1, dtype=torch.int32, device=device)
+            self.rope = None
+            if rope_base is not None:
+                self.rope = torch.empty(rx.relax_rope_table_bytes(self.dims) // 4, dtype=torch.float32, device=device)
+                rx.check(rx.relax_rope_table_init(self.dims, self.rope), "relax_rope_table_init")
+            self.ws_bytes = rx.relax_paged_workspace_bytes(self.dims, n_max, kv_capacity, self.B_max)
+            self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
+            rx.check(rx.relax_workspace_init(self.dims, self.ws, self.ws_bytes), "relax_workspace_init")
+        shape = (n_pages, n_kv_heads, page_size // rx.RELAX_PAGED_BLOCK, rx.RELAX_PAGED_BLOCK * head_dim)
+        self.k, self.v = (torch.empty(shape, dtype=torch.uint8, device=device) for _ in "kv")
+        self.k_scale, self.v_scale = (torch.empty(shape[:3], dtype=torch.float32, device=device) for _ in "kv")
+        self.cache = rx.PagedCache(self.k, self.v, self.k_scale, self.v_scale, self.pages, self.rope, n_pages, page_size, self.pages.shape[1])
+
+    def append(self, qkv: torch.Tensor, seqs: "rx.Seqs", q_out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """qkv: fp16 [n, (h + 2 g) d], rows contiguous (any stride between them).  Returns q, rotated, fp16 [n, h, d]."""
+        h, g, d = self.dims.n_heads, self.dims.n_kv_heads, self.dims.head_dim
+        n, at = qkv.shape[0], qkv.data_ptr()
+        if qkv.dtype != torch.float16 or qkv.shape[1] != (h + 2 * g) * d or qkv.stride(1) != 1:
+            raise ValueError("qkv is fp16 [n, (h + 2 g) d] with contiguous rows")
+        if q_out is None:
+            q_out = torch.empty((n, h, d), dtype=torch.float16, device=self.device)
+        rx.check(rx.relax_paged_append(at, qkv.stride(0), at + 2 * h * d, at + 2 * (h + g) * d, qkv.stride(0), q_out, self.cache, seqs, self.dims, n,
+                                       self.ws, self.ws_bytes, stream), "relax_paged_append")
+        return q_out
+
+    def attention(self, q: torch.Tensor, seqs: "rx.Seqs", out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        out = torch.empty_like(q) if out is None else out
+        rx.check(rx.relax_paged_attention(q, self.cache, seqs, self.dims, out, q.shape[0], self.ws, self.ws_bytes, stream), "relax_paged_attention")
+        return out
+
+    def read(self, seqs: "rx.Seqs", n: int, stream=None):
+        """(k, v) of the call's n rows as fp16 [n, g, d]."""
+        k, v = (torch.empty((n, self.dims.n_kv_heads, self.dims.head_dim), dtype=torch.float16, device=self.device) for _ in "kv")
+        rx.check(rx.relax_paged_read(self.cache, seqs, self.dims, k, v, n, self.ws, self.ws_bytes, stream), "relax_paged_read")
+        return k, v
+
+
+def token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None, top: int = 0, entropy: bool = False, ws: Optional[torch.Tensor] = None, stream=None):
+    """relax_token_logprobs on fp16 logits [n, V]: (logprobs, entropy, top_ids, top_logprobs), None where not asked for.  ws: uint8, else made here."""
+    n, vocab = logits.shape
+    if logits.dtype != torch.float16 or (vocab > 1 and logits.stride(1) != 1):
+        raise ValueError("logits are fp16 [n, V] with contiguous rows")
+    new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=logits.device)
+    if ws is None:
+        ws = new(rx.relax_token_logprobs_workspace_bytes(n, vocab, top), dtype=torch.uint8)
+    lp, ent = new(n) if targets is not None else None, new(n) if entropy else None
+    ids, tops = (new(n, top, dtype=torch.int32), new(n, top)) if top else (None, None)
+    rx.check(rx.relax_token_logprobs(logits, logits.stride(0) if n > 1 else vocab, targets, lp, ent, ids, tops, n, vocab, top, ws, ws.numel(), stream), "relax_token_logprobs")
+    return lp, ent, ids, tops
+
+
 class DeviceLayerQ3:
     """One decoder layer on 3-bit weights resident on the GPU: the canonical matrices are uploaded, repacked once into the
     GPU-native layout (relax_repack_q3) and dropped; cache, rotary table and workspace as in DeviceLayer."""

@@ -521,3 +521,77 @@ def test_two_streams_with_workspaces_of_their_own(rx):
     torch.cuda.synchronize()
     for i in (0, 1):
         assert np.array_equal(out[i].cpu().numpy(), alone[i])
+
+
+@pytest.mark.parametrize("shape,q_lens,heads", [((16, 1, 64), [1500] + [1] * 299, [0, 15]), ((64, 8, 64), [1] * 150 + [700] + [1] * 150, [0, 63]),
+                                                ((8, 2, 64), [2, 31, 1, 1, 3] * 40, None)], ids=["small_tiles", "large_tiles", "ragged"])
+@pytest.mark.parametrize("device_table", [False, True])
+def test_one_prompt_among_many_sequences(rx, shape, q_lens, heads, device_table):
+    """As many tiles for every sequence as the prompt has would be 450 000; and sequences that begin and end inside the search's groups of 64."""
+    rng = np.random.default_rng(71)
+    attention_case(rx, rng, shape, 16, q_lens, [q + int(rng.integers(0, 60)) for q in q_lens], device_table=device_table, heads=heads)
+
+
+def test_queries_in_place(rx):
+    rng = np.random.default_rng(72)
+    b = Bench(rx, rng, 4, 2, 64, 16, [5, 1], [20, 3])
+    x = torch.from_numpy(half(rng, (b.n, 8 * 64))).cuda()
+    q, kv = x[:, :256].contiguous(), x[:, 256:].contiguous()
+    at = kv.data_ptr()
+    args = lambda q_ptr, stride, out: rx.relax_paged_append(q_ptr, stride, at, at + 256, 256, out, b.cache, b.seqs(), b.dims, b.n, *b.workspace())
+    out = torch.empty_like(q)
+    rx.check(args(q, 256, out))
+    rx.check(args(q, 256, q))
+    torch.cuda.synchronize()
+    assert torch.equal(q, out)
+
+
+def test_a_model_of_one_layer_from_prompt_to_log_probabilities(rx):
+    """Matrices, append, attention, the head and the log probabilities as a program strings them together: three requests of different ages,
+    a prompt scored token by token, then tokens picked with alternatives.  Attention against float64 on what the cache reads back as,
+    log probabilities against float64 on the logits; the first alternative is the next token."""
+    from paper_2311_02103_amd import runtime
+    rng = np.random.default_rng(73)
+    h, g, d, V, H = 8, 2, 64, 1000, 256
+    mat = lambda m, k: torch.from_numpy(half(rng, (m, k), k ** -0.5)).cuda()
+    emb, wqkv, wo, head = torch.from_numpy(half(rng, (V, H))).cuda(), mat((h + 2 * g) * d, H), mat(H, h * d), mat(V, H) * 4
+    cache = runtime.DevicePagedCache(n_heads=h, n_kv_heads=g, head_dim=d, kv_capacity=160, n_pages=30, page_size=16, kv_slots=3, n_max=200)
+    cache.pages.copy_(torch.from_numpy(rng.permutation(30).reshape(3, 10).astype(np.int32)))
+
+    def product(x, w):
+        y = torch.empty((x.shape[0], w.shape[0]), dtype=torch.float16, device="cuda")
+        rx.check(rx.relax_half_matmul(x, w, y, x.shape[0], w.shape[0], w.shape[1]))
+        return y
+    held = [0, 0, 0]
+    texts = [rng.integers(0, V, 120).astype(np.int32) for _ in range(3)]
+    for slots, lens in (([1], [97]), ([2, 0, 1], [33, 60, 1]), ([0, 1, 2], [1, 1, 1]), ([2, 0], [1, 4]), ([1, 2, 0], [1, 1, 1])):
+        for s, ln in zip(slots, lens):
+            held[s] += ln
+        ids = np.concatenate([texts[s][held[s] - ln:held[s]] for s, ln in zip(slots, lens)])
+        targets = np.concatenate([texts[s][held[s] - ln + 1:held[s] + 1] for s, ln in zip(slots, lens)])
+        kv_lens = [held[s] for s in slots]
+        seqs = rx.Seqs(lens, kv_lens, slots)
+        x = emb[torch.from_numpy(ids).cuda()]
+        q = cache.append(product(x, wqkv), seqs)
+        o = cache.attention(q, seqs)
+        y = x + product(o.view(-1, h * d), wo)
+        logits = product(y, head)
+        lp, ent, top_ids, tops = runtime.token_logprobs(logits, torch.from_numpy(targets).cuda(), 5, True)
+        pool = {key: t.cpu().numpy() for key, t in (("k", cache.k), ("v", cache.v), ("ks", cache.k_scale), ("vs", cache.v_scale))}
+        want, tol = po.attention(q.cpu().numpy().astype(np.float64), pool, cache.pages.cpu().numpy(), 16, lens, kv_lens, slots, g, d)
+        assert (np.abs(o.cpu().numpy() - want) <= tol).all()
+        k, v = cache.read(seqs, len(ids))
+        for row, ql, L, slot in po.sequences(lens, kv_lens, slots):
+            for name, got in (("k", k), ("v", v)):
+                vals = po.values(pool, name, cache.pages.cpu().numpy(), 16, slot, np.arange(L - ql, L), d)
+                assert np.array_equal(got[row:row + ql].cpu().numpy(), vals.astype(np.float32).astype(np.float16))
+        l64 = logits.cpu().numpy().astype(np.float64)
+        wlp, went, wids, wtops = po.token_logprobs(l64, targets, 5)
+        # a term e^z is off by 2^-23 |z| log2(e) and 2^-22, |z| weighted by e^z averages below log V + 1: log S by 2^-22 (log V + 4) = 2^-22 11, the entropy by log V + 2 < 9
+        # times that, and the results' own rounding 2^-22 of less than 20: below 2^-22 128 together
+        assert np.array_equal(top_ids.cpu().numpy(), wids)
+        for got, ref in ((lp, wlp), (tops, wtops), (ent, went)):
+            assert np.abs(got.cpu().numpy() - ref).max() <= 2.0 ** -15
+        for s, row in zip(slots, np.cumsum(lens) - 1):
+            texts[s][held[s]] = top_ids[row, 0].item()
+    assert rx.relax_workspace_error(cache.dims, cache.ws) == 0

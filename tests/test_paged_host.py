@@ -63,6 +63,8 @@ def test_what_single_calls_refuse():
     put = lambda q=P, qs=256, k=P, v=P, kvs=256, out=P: rx.relax_paged_append(q, qs, k, v, kvs, out, c, s, d, 2, P, BIG)
     assert {put(k=None), put(v=None), put(q=None), put(out=None)} == {rx.ERR_NULL}
     assert {put(q=P + 2), put(k=P + 8), put(v=P + 4), put(out=P + 8), put(qs=257), put(kvs=260), put(qs=248), put(kvs=248), put(kvs=-256)} == {rx.ERR_SHAPE}
+    wide = lambda q_out, n: rx.relax_paged_append(P, 512, 2 * P, 2 * P, 512, q_out, c, rx.Seqs([n], [5]), d, n, P, BIG)
+    assert wide(P, 2) == rx.ERR_SHAPE                                                  # in place with rows of another pitch: row 1 would land in row 0's keys
     assert rx.relax_paged_attention(None, c, s, d, P, 2, P, BIG) == rx.ERR_NULL
     assert rx.relax_paged_attention(P, c, s, d, None, 2, P, BIG) == rx.ERR_NULL
     assert rx.relax_paged_attention(P + 8, c, s, d, P, 2, P, BIG) == rx.ERR_SHAPE
