@@ -422,8 +422,7 @@ relax_status relax_paged_append(const uint16_t *q, int64_t q_stride, const uint1
 
 /* relax_attention over a paged cache: q [n,h,d] fp16 (already rotated), out [n,h,d] fp16, 16-byte aligned.  Row i of sequence b attends to
  * positions 0..pos_i of its slot, which must already hold this call's keys and values.  Scores, softmax and sums are fp32, the
- * probabilities are rounded to fp16 in front of their product with the values, and so, in calls of many rows (tiles of 256 rows times heads), are
- * the values.  A row that no token is left for (every page of its
+ * probabilities (times the scale of their values) are rounded to fp16 in front of their product with the codes.  A row that no token is left for (every page of its
  * sequence out of range) is zeros.  ws and errors as relax_paged_append.                                                */
 relax_status relax_paged_attention(const uint16_t *q, const relax_paged_cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims,
                                    uint16_t *out, int32_t n, void *ws, size_t ws_bytes, relax_stream stream);

@@ -13,9 +13,10 @@
 // four wavefronts per workgroup left to themselves, scores and exponentials in one stream of instructions, 170 (the matrix pipe busy 34 % of the time).
 // A turn takes about 1000 cycles at 2 GHz where 544 of the matrix pipe would do: next to the other half's vector work its 34 MFMAs take 970, alone 660.
 //
-// The value scale of a block, relative to the largest so far, multiplies its codes on their way into LDS here, one more rounding to fp16 (2^-11 of the value;
-// below 2^-32 of the largest value of the split it is coarser): the weights then need no scale of their own, and their sum is one more MFMA
-// with a tile of ones, of the weights as they are rounded for the products.
+// The value scale of a block, relative to the largest so far, is 2^E mu with 1 <= mu < 2.  The power of two multiplies the codes on their way into LDS, which is
+// exact down to 2^-24; mu is in the weights, as an addend of their exponent, so that the one rounding to fp16 stays that of the weights (with the whole
+// scale on the codes outputs were off by 3.2e-4 instead of 2.8e-4, 2.0e-4 of it their own rounding).  The sums of the weights are one more MFMA: its other operand is
+// 1 / mu of the token's block, as two halves in alternate rows, whose results add up to 1 / mu within 2^-22.
 #include <type_traits>
 
 #include "paged_device.h"
@@ -24,7 +25,8 @@ namespace relax {
 
 namespace {
 
-constexpr float kBias = 11.0f, kMost = 32768.0f; // as in attn_paged.hip: log2 of the weight at the reference; the largest weight before that moves
+constexpr float kBias = 11.0f, kMost = 65000.0f; // as in attn_paged.hip: log2 of the weight at the reference; the largest packed weight before that moves (at 32768
+                                                 // it moves more often: 4096 tokens of 32 / 8 heads 170 us for 159)
 constexpr float kUnset = -1e30f;                 // reference of a row that has met no token: below every score, and finite
 
 // LDS-only workgroup barrier: global loads stay in flight across it
@@ -39,7 +41,7 @@ constexpr int CT = 2;                            // column tiles of 16 pairs per
 constexpr int kThreads = 512;
 constexpr int kSegment = kThreads;               // blocks whose numbers and scales are in LDS at a time
 
-// What a block needs: c k_scale, v_scale relative to the reference, number in the pool (as bits)
+// What a block needs: c k_scale, log2 mu + kBias, number in the pool (as bits), 2^E as two halves to multiply (as bits)
 typedef float4p_t Block;
 
 // grid: x = tile * g + KV head (the last tile of a sequence, with the longest prefix, first)
@@ -56,6 +58,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_paged_rows_kernel(PagedSeqs,
     constexpr int kTileBytes = 64 * D * 2;
     __shared__ __align__(16) unsigned char lds[4 * kTileBytes];        // keys: two buffers, values: two
     __shared__ __align__(16) Block blocks[kSegment];
+    __shared__ __align__(8) uint32_t unscales[2][kSegment];            // 1 / mu: the two halves to add, each twice in a word
     __shared__ float v_tops[8];
     __shared__ int bad_s;
 
@@ -91,7 +94,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_paged_rows_kernel(PagedSeqs,
 
     float4p_t O[NT][CT];
     float m[CT];
-    float4p_t l[CT];                                                   // sums of the weights, in every row of a tile
+    float4p_t l[CT];                                                   // sums of the weights: the first two together
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
         m[ct] = kUnset, l[ct] = float4p_t{0.0f, 0.0f, 0.0f, 0.0f};
@@ -101,12 +104,10 @@ __global__ __launch_bounds__(kThreads, 2) void attn_paged_rows_kernel(PagedSeqs,
 
     float v_ref = 0.0f;
     u32x4p_t rk[2], rv[2];                                             // of the next two tiles, by their parity
-    float vr[2];                                                       // value scales of what is in rv
+    float vr[2];                                                       // 2^E of what is in rv
 #pragma unroll
     for (int i = 0; i < 2; ++i) rk[i] = rv[i] = u32x4p_t{0, 0, 0, 0}, vr[i] = 0.0f;
     half8p_t ring[PD], pf[CT];
-    const _Float16 one = (_Float16)1.0f;
-    const half8p_t ones = {one, one, one, one, one, one, one, one};
 
     // ---- staging: a tile is 4 J loads of keys and as many of values; with heads of 128 a wavefront brings one of each, with heads of 64 one ----
     const bool brings_keys = J == 2 || wave < 4, brings_values = J == 2 || wave >= 4;
@@ -120,7 +121,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_paged_rows_kernel(PagedSeqs,
         rk[parity] = packet(pa.k, info);
     };
     auto load_values = [&](int parity, const Block &info) {
-        rv[parity] = packet(pa.v, info), vr[parity] = info[1];
+        rv[parity] = packet(pa.v, info), vr[parity] = info[3];
     };
     auto store_key = [&](int kb, int i) {                              // half i of the load; the buffer is the tile's parity
         if (!brings_keys) return;
@@ -129,11 +130,10 @@ __global__ __launch_bounds__(kThreads, 2) void attn_paged_rows_kernel(PagedSeqs,
     };
     auto store_value = [&](int vb, int i) {                            // the four tokens of element i of the load
         if (!brings_values) return;
-        // (u - 128) r to fp16 in one rounding: 128 r is exact, the multiply-add rounds once in fp32
-        const uint32_t w = rv[vb][i];
-        const float r = vr[vb], off = -128.0f * r;
-        const half2p_t lo = {(_Float16)fmaf((float)(w & 255u), r, off), (_Float16)fmaf((float)(w >> 8 & 255u), r, off)};
-        const half2p_t hi = {(_Float16)fmaf((float)(w >> 16 & 255u), r, off), (_Float16)fmaf((float)(w >> 24), r, off)};
+        const half2p_t f = __builtin_bit_cast(half2p_t, vr[vb]);       // (the second factor rounds, where values below 2^-31 of the largest leave fp16's range)
+        half2p_t lo, hi;
+        codes_to_half(rv[vb][i], lo, hi);
+        lo = lo * half2p_t{f.x, f.x} * half2p_t{f.y, f.y}, hi = hi * half2p_t{f.x, f.x} * half2p_t{f.y, f.y};
         *(u32x2p_t *)(lds + (2 + vb) * kTileBytes + (((blk_w >> 1) * NT + 4 * load_w + i) * 64 + lane) * 16 + (blk_w & 1) * 8) =
             u32x2p_t{__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi)};
     };
@@ -156,14 +156,16 @@ __global__ __launch_bounds__(kThreads, 2) void attn_paged_rows_kernel(PagedSeqs,
     };
     auto weights = [&](const Scores &S, const Block (&bl)[2]) {
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-            const float off = kBias - m[ct];
+        for (int u = 0; u < 2; ++u) {
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int ct = 0; ct < CT; ++ct) {
+                const float off = bl[u][1] - m[ct];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) pf[ct][4 * u + i] = (_Float16)__builtin_amdgcn_exp2f(fmaf(S.s[u][ct][i], bl[u][0], off));
+            }
         }
     };
+    auto unscale_of = [&](int at) { return *(const u32x2p_t *)&unscales[lane & 1][min(at, kSegment - 2)]; };
     auto mask = [&](Scores &S, int at, int t0, bool bad) {             // at: the first of the two blocks in the segment
         if (t0 + 31 > wave_min || bad) {                               // uniform
 #pragma unroll
@@ -177,7 +179,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_paged_rows_kernel(PagedSeqs,
             }
         }
     };
-    // The weights were computed against the reference as it was.  Where one has left fp16's range behind 2^15 (or every column is new), the reference
+    // The weights were computed against the reference as it was.  Where one is about to leave fp16's range (or every column is new), the reference
     // moves to the maximum of these scores, what was summed against the old one is rescaled and the weights are computed again: rare behind the first
     // tiles of a row, and a look at the packed weights costs a quarter of the maxima of the scores.
     auto settle = [&](const Scores &S, const Block (&bl)[2]) {
@@ -229,7 +231,13 @@ __global__ __launch_bounds__(kThreads, 2) void attn_paged_rows_kernel(PagedSeqs,
         for (int w = 0; w < 8; ++w) ref = fmaxf(ref, v_tops[w]);
         if (pool < 0 && seg + tid < b_end) bad_s = 1;
         // (codes of a zero scale are zero; -inf times its factor has to stay -inf)
-        blocks[tid] = Block{fmaxf(ks * c, 0x1p-100f), ref > 0.0f ? vs / ref : 0.0f, __builtin_bit_cast(float, pool), 0.0f};
+        const float scale = fmaxf(ref > 0.0f ? __builtin_amdgcn_logf(vs / ref) : 0.0f, -40.0f);       // (2^-40: codes of a zero scale, which become zeros in fp16)
+        const float mu = __builtin_amdgcn_fractf(scale), inv = __builtin_amdgcn_exp2f(-mu);
+        const int e = (int)(scale - mu), e1 = max(e, -14);
+        const _Float16 inv_hi = (_Float16)inv, inv_lo = (_Float16)(inv - (float)inv_hi);
+        blocks[tid] = Block{fmaxf(ks * c, 0x1p-100f), mu + kBias, __builtin_bit_cast(float, pool),
+                            __builtin_bit_cast(float, half2p_t{(_Float16)ldexpf(1.0f, e1), (_Float16)ldexpf(1.0f, e - e1)})};
+        unscales[0][tid] = __builtin_bit_cast(uint32_t, half2p_t{inv_hi, inv_hi}), unscales[1][tid] = __builtin_bit_cast(uint32_t, half2p_t{inv_lo, inv_lo});
         if (v_ref > 0.0f && ref > v_ref) {                             // O is in units of the largest value scale so far
             const float f = v_ref / ref;
 #pragma unroll
@@ -263,6 +271,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_paged_rows_kernel(PagedSeqs,
             if (i + PD < G) ring[i % PD] = read_key(0, 0, i + PD);
         }
         Block bl[2] = {blocks[0], blocks[1]};
+        u32x2p_t un = unscale_of(0);
         __builtin_amdgcn_sched_barrier(0);
         lds_barrier();
         // two turns of either kind per tile; PARITY: its buffers and registers
@@ -293,8 +302,10 @@ __global__ __launch_bounds__(kThreads, 2) void attn_paged_rows_kernel(PagedSeqs,
                     if (sub == 1 && i >= 1 && i < 3) store_key(kb, i - 1);
                     __builtin_amdgcn_sched_barrier(0);
                 }
+                const half8p_t unscale = __builtin_bit_cast(half8p_t, u32x4p_t{un.x, un.x, un.y, un.y});
 #pragma unroll
-                for (int ct = 0; ct < CT; ++ct) l[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, pf[ct], l[ct], 0, 0, 0);
+                for (int ct = 0; ct < CT; ++ct) l[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(unscale, pf[ct], l[ct], 0, 0, 0);
+                un = unscale_of(t * 4 + 2 * sub + 2);
                 if (sub == 0) load_values(kb ^ 1, info_ahead);
                 if (sub == 1) load_keys(kb, info_ahead);
 #pragma unroll
@@ -317,7 +328,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_paged_rows_kernel(PagedSeqs,
     // ---- results: lane holds elements 16 i + 4 quarter .. + 3 of its columns ----
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-        const float den = l[ct][0];
+        const float den = l[ct][0] + l[ct][1];
         const int place = (wave * CT + ct) * 16 + col;
         if (place >= n_pairs) continue;
         const int pair = p0 + place, row = pair / rep;

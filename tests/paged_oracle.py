@@ -86,7 +86,7 @@ def attention(q, pool, pages, page_size, q_lens, kv_lens, slots, g, d, heads=Non
       the output to fp16                                                       2^-11 |o|, 2^-25 below fp16's normal range
       the probabilities to fp16, p (1 + e), |e| <= 2^-11, with a sum of the rounded ones: o becomes sum p (1 + e) v / sum p (1 + e), which is off by
       sum p (e - mean of e) v                                                  2^-11 (sum p |v| + |o|)
-      the values, scaled, to fp16                                              2^-11 sum p |v|, and 2^-32 of the largest |v| below fp16's normal range
+      values below 2^-31 of the largest                                        2^-32 of the largest |v|
       scores in fp32, whose sum of d products and scaling is off by (d + 8) 2^-24 of the sum of magnitudes, which changes a probability by
       that factor, at once in numerator and denominator                        2 (d + 8) 2^-24 |q| |k| sum p |v|
       sums of probabilities and of O in fp32, 2^6 roundings in a row           2^-18 sum p |v|
@@ -112,7 +112,7 @@ def attention(q, pool, pages, page_size, q_lens, kv_lens, slots, g, d, heads=Non
             o, mean = p @ vh, p @ np.abs(vh)
             delta = ((d + 8) * 2.0 ** -24 * mag.max(axis=1))[:, None]
             out[row:row + ql, head] = o
-            tol[row:row + ql, head] = np.where(some[:, None], 2.0 ** -10 * np.abs(o) + (2.0 ** -10 + 2 * delta + 2.0 ** -18) * mean + 2.0 ** -25 +
+            tol[row:row + ql, head] = np.where(some[:, None], 2.0 ** -10 * np.abs(o) + (2.0 ** -11 + 2 * delta + 2.0 ** -18) * mean + 2.0 ** -25 +
                                                (len(t) * 2.0 ** -36 + 2.0 ** -32) * np.abs(vh).max(), 0.0)
     return out, tol
 
