@@ -278,7 +278,7 @@ struct Plan {
 };
 
 // Tiles are searched for where a fixed number per sequence would launch more than twice as many (us: 300 rows on 1201 tokens beside 20 decode rows of 32 / 32 heads,
-// 399 tiles numbered as 6300, 46.8; searched for, 42.0.  One search is a load and a scan over 64 lengths, 0.3 us)
+// 39 tiles per KV head numbered as 399, 46.8; searched for, 42.0)
 void numbering(long long all, long long most, int32_t B, int32_t &items, int32_t &per_seq)
 {
     const bool search = most * B > 2 * all;

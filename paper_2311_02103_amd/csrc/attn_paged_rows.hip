@@ -9,7 +9,7 @@
 // Per 32 tokens a wavefront has 34 MFMAs of 16 cycles and about 75 vector instructions and 16 exponentials: some 500 cycles of the matrix pipe and as many of
 // the vector unit.  Two wavefronts share a SIMD, one of each half of the workgroup, and the halves
 // take turns: while wavefronts 0 .. 3 multiply (this step's weights with V, the next step's keys with Q), wavefronts 4 .. 7 compute weights and stage their
-// part of the next tile, then the other way round, with a barrier between the turns.  4096 tokens, 32 / 8 heads of 128: 149 us (0.92 PFLOP/s of the causal half); with
+// part of the next tile, then the other way round, with a barrier between the turns.  4096 tokens, 32 / 8 heads of 128: 147 us (0.93 PFLOP/s of the causal half); with
 // four wavefronts per workgroup left to themselves, scores and exponentials in one stream of instructions, 170 (the matrix pipe busy 34 % of the time).
 // A turn takes about 1000 cycles at 2 GHz where 544 of the matrix pipe would do: next to the other half's vector work its 34 MFMAs take 970, alone 660.
 //

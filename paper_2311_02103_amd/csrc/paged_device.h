@@ -25,7 +25,8 @@ typedef uint32_t u32x4p_t __attribute__((ext_vector_type(4)));
 // The ragged batch of a paged call, the FIRST argument of each of its kernels: they read it through the kernel argument segment with a
 // uniform index, one scalar load per field.  (A struct of arrays in a parameter that is indexed with a variable is copied to scratch
 // memory first, 264 bytes per lane for 16 sequences.)  Batches of up to kPagedInline sequences need no table in memory, and so no launch that writes
-// one.  Both together: the append of 64 rows of the 70B heads and its read-back went from 26.6 us of kernels to 13.5.
+// one.  Both together: the append of 64 rows of the 70B heads and its read-back went from 26.6 us of kernels to 13.5
+// (9.4 with what paged_append.hip describes).
 constexpr int kPagedInline = 128;
 struct PagedSeqs {
     const int32_t *dev;              // [4][B]: q_start, q_len, kv_len, slot; nullptr -> the arrays

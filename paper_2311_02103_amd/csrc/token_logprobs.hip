@@ -16,7 +16,7 @@
 // 11.1, of 152064 with 20 alternatives 19.9 / 14.8, of 262000 36.6 / 15.2, 16 rows of 128256 17.7 / 13.8; 1 row of 50257 10.5 / 11.4).
 //
 // Bound by the vector unit next to the read: a logit takes nine issue slots in the sums (four of them the exponential) and one and a half in the other
-// two passes, which look at pairs.  2047 rows of 32000 logits: 32 us without alternatives (4.1 TB/s), 46 with 20; 1 row 7.9.
+// two passes, which look at pairs.  2047 rows of 32000 logits: 32 us without alternatives (4.1 TB/s), 43 to 46 with 20; 1 row 7.8.
 #include <limits.h>
 
 #include <algorithm>
