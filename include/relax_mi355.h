@@ -388,7 +388,7 @@ relax_status relax_decoder_layer_f16(const relax_layer_dims *dims, const relax_l
  * (fragments of the matrix products that read them).  Codes and scales behind a sequence's last token have no meaning and need no
  * initialisation.  Several rows of the page table may name one page (a shared beginning) as long as no call appends to it
  * through two of them.  The page table is device data and is read at run time: a call captured in a graph follows it.  A block whose page
- * number is outside [0, n_pages) has no page: an append drops its tokens, attention leaves them out, a read gives zeros, and
+ * number is outside [0, n_pages), or whose sequence a device table gives more than kv_capacity positions, has no page: an append drops its tokens, attention leaves them out, a read gives zeros, and
  * each raises bit 2 of the flag that relax_workspace_error reports for the call's workspace.
  * The descriptor of a call is relax_seqs: slots are rows of the page table, dims.kv_slots their number, and dims.kv_capacity
  * (the positions the rotary table covers) bounds every length.  Of dims the calls use n_heads, n_kv_heads, head_dim, kv_capacity and kv_slots.  */
@@ -444,7 +444,7 @@ relax_status relax_paged_read(const relax_paged_cache *cache, const relax_seqs *
  * nothing else gives -inf and entropy 0.  A row that holds a NaN or +inf gives NaN log probabilities and entropy (a token at
  * -inf aside, unless NaN is in the row); its ids are those of the largest logits all the same, NaNs behind -inf.
  * ws (may be NULL): with relax_token_logprobs_workspace_bytes(n, vocab, top) bytes, 256-byte aligned, few rows are spread over more of the chip; without them
- * the call gives the same.  Errors: NULL (no output wanted either), SHAPE, UNSUPPORTED (top > 32).                         */
+ * the call gives the same.  Errors: NULL (no output wanted either), SHAPE, UNSUPPORTED (top > 32, vocab > 2^30).                         */
 size_t       relax_token_logprobs_workspace_bytes(int32_t n_max, int32_t vocab, int32_t top);
 relax_status relax_token_logprobs(const uint16_t *logits, int64_t stride, const int32_t *targets, float *logprobs, float *entropy, int32_t *top_ids,
                                   float *top_logprobs, int32_t n, int32_t vocab, int32_t top, void *ws, size_t ws_bytes, relax_stream stream);

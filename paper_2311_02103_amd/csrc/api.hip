@@ -1412,6 +1412,7 @@ PagedWs paged_ws(const relax_layer_dims &dm, int32_t n, int32_t L, int32_t B)
     return p;
 }
 
+constexpr int32_t kMaxVocab = 1 << 30;       // logits of a row: places in it are 32-bit numbers
 constexpr int32_t kMaxPagedSeqs = 65535;     // a workgroup finds its sequence 64 at a time
 
 // Everything the paged calls check alike; fills the kernels' descriptors.  items: see launch_paged_append.
@@ -1523,7 +1524,7 @@ relax_status relax_paged_read(const relax_paged_cache *cache, const relax_seqs *
 
 size_t relax_token_logprobs_workspace_bytes(int32_t n_max, int32_t vocab, int32_t top)
 {
-    if (n_max < 1 || vocab < 1 || top < 0 || top > 32) return 0;
+    if (n_max < 1 || vocab < 1 || vocab > kMaxVocab || top < 0 || top > 32) return 0;
     return align256(std::max<size_t>(token_logprobs_partial_bytes(n_max, vocab), 1));
 }
 
@@ -1534,7 +1535,7 @@ relax_status relax_token_logprobs(const uint16_t *logits, int64_t stride, const 
     if (n < 1 || vocab < 1 || stride < vocab || top < 0 || top > vocab || !aligned(logits, 2) || !aligned(targets, 4) || !aligned(logprobs, 4) ||
         !aligned(entropy, 4) || !aligned(top_ids, 4) || !aligned(top_logprobs, 4))
         return RELAX_ERR_SHAPE;
-    if (top > 32) return RELAX_ERR_UNSUPPORTED;
+    if (top > 32 || vocab > kMaxVocab) return RELAX_ERR_UNSUPPORTED;
     if (top > 0 ? !top_ids || !top_logprobs : !targets && !entropy) return RELAX_ERR_NULL;
     void *partials = ws && aligned(ws, 256) && ws_bytes >= token_logprobs_partial_bytes(n, vocab) ? ws : nullptr;
     return hip_status(launch_token_logprobs(logits, stride, targets, logprobs, entropy, top_ids, top_logprobs, n, vocab, top, partials, static_cast<hipStream_t>(stream)));

@@ -229,8 +229,12 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedSeqs, RowsView r
         const int blk = (first >> 4) + place;
         const int low = max(first - blk * 16, 0), high = min(si.kv_len - blk * 16, 16);
         if (first < 0 || high <= low) return;
+        if (si.kv_len > pa.cap) {                              // (a length from device memory: no page, and no row of the rotary table)
+            if (lane == 0) atomicOr(pa.err, kBadPage);
+            return;
+        }
         const int row = si.q_start + blk * 16 - first;
-        const auto find = [&] { return si.kv_len <= pa.cap ? paged_block(pa, g, kvh, si.slot, blk) : -1; };
+        const auto find = [&] { return paged_block(pa, g, kvh, si.slot, blk); };
         if (!(part & 1 ? put_values<D>(r, pa, find, kvh, lane, low, high, row, turn[wave])
                        : put_keys<D>(r, pa, find, kvh, lane, low, high, row, blk * 16)) && lane == 0) atomicOr(pa.err, kBadPage);
         return;

@@ -175,13 +175,16 @@ class DevicePagedCache:
         n, at = qkv.shape[0], qkv.data_ptr()
         if qkv.dtype != torch.float16 or qkv.shape[1] != (h + 2 * g) * d or qkv.stride(1) != 1:
             raise ValueError("qkv is fp16 [n, (h + 2 g) d] with contiguous rows")
+        pitch = qkv.stride(0) if n > 1 else qkv.shape[1]
         if q_out is None:
             q_out = torch.empty((n, h, d), dtype=torch.float16, device=self.device)
-        rx.check(rx.relax_paged_append(at, qkv.stride(0), at + 2 * h * d, at + 2 * (h + g) * d, qkv.stride(0), q_out, self.cache, seqs, self.dims, n,
+        rx.check(rx.relax_paged_append(at, pitch, at + 2 * h * d, at + 2 * (h + g) * d, pitch, q_out, self.cache, seqs, self.dims, n,
                                        self.ws, self.ws_bytes, stream), "relax_paged_append")
         return q_out
 
     def attention(self, q: torch.Tensor, seqs: "rx.Seqs", out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        if q.dtype != torch.float16 or not q.is_contiguous():
+            raise ValueError("q is fp16 [n, h, d], contiguous")
         out = torch.empty_like(q) if out is None else out
         rx.check(rx.relax_paged_attention(q, self.cache, seqs, self.dims, out, q.shape[0], self.ws, self.ws_bytes, stream), "relax_paged_attention")
         return out
@@ -194,10 +197,12 @@ class DevicePagedCache:
 
 
 def token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None, top: int = 0, entropy: bool = False, ws: Optional[torch.Tensor] = None, stream=None):
-    """relax_token_logprobs on fp16 logits [n, V]: (logprobs, entropy, top_ids, top_logprobs), None where not asked for.  ws: uint8, else made here."""
+    """relax_token_logprobs on fp16 logits [n, V], targets int32 [n]: (logprobs, entropy, top_ids, top_logprobs), None where not asked for.  ws: uint8, else made here."""
     n, vocab = logits.shape
     if logits.dtype != torch.float16 or (vocab > 1 and logits.stride(1) != 1):
         raise ValueError("logits are fp16 [n, V] with contiguous rows")
+    if targets is not None and (targets.dtype != torch.int32 or targets.shape != (n,) or not targets.is_contiguous()):
+        raise ValueError("targets are int32 [n]")
     new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=logits.device)
     if ws is None:
         ws = new(rx.relax_token_logprobs_workspace_bytes(n, vocab, top), dtype=torch.uint8)

@@ -53,7 +53,7 @@ int main(void)
     EXPECT(relax_paged_attention(DEV, &c, &s, &d, DEV, 1, DEV, 256, NULL), RELAX_ERR_WORKSPACE);
     c.n_pages = INT32_MAX;
     EXPECT(relax_paged_attention(DEV, &c, &s, &d, DEV, 1, DEV, 256, NULL), RELAX_ERR_UNSUPPORTED);
-    if (relax_token_logprobs_workspace_bytes(INT32_MAX, INT32_MAX, 32) == 0) ++failures;
+    if (relax_token_logprobs_workspace_bytes(INT32_MAX, 1 << 20, 32) == 0 || relax_token_logprobs_workspace_bytes(1, INT32_MAX, 32) != 0) ++failures;
     EXPECT(relax_token_logprobs(DEV, 99, DEV, DEV, NULL, NULL, NULL, 1, 100, 0, NULL, 0, NULL), RELAX_ERR_SHAPE);
     EXPECT(relax_token_logprobs(DEV, 100, NULL, NULL, NULL, NULL, NULL, 1, 100, 0, NULL, 0, NULL), RELAX_ERR_NULL);
     if (failures == 0) printf("paged driver ok\n");

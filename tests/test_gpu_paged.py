@@ -595,3 +595,21 @@ def test_a_model_of_one_layer_from_prompt_to_log_probabilities(rx):
         for s, row in zip(slots, np.cumsum(lens) - 1):
             texts[s][held[s]] = top_ids[row, 0].item()
     assert rx.relax_workspace_error(cache.dims, cache.ws) == 0
+
+
+def test_lengths_of_a_device_table_beyond_the_capacity(rx):
+    """Known on the device only: such a sequence has no pages, and the rotary table no rows for it."""
+    rng = np.random.default_rng(74)
+    b = Bench(rx, rng, 4, 2, 64, 16, [3, 20, 1], [20, 32, 9], device_table=True)
+    b.dev_table[2, 1] = b.cap + 500
+    qkv = half(rng, (b.n, 8 * 64))
+    b.append(qkv)
+    assert b.error() == 4
+    got, blocks = b.host_pool(), b.pages[1][b.pages[1] >= 0]
+    for key in got:                                            # nothing of its pages was touched, the others' rows are in
+        assert np.array_equal(got[key][blocks].view(np.uint8), b.pool[key][blocks].view(np.uint8)), key
+    others = np.r_[0:3, 23:24]
+    k, v = b.read()
+    assert (k[3:23] == 0).all() and (v[3:23] == 0).all()
+    x = qkv.astype(np.float64).reshape(b.n, 8, 64)
+    assert np.abs(v[others] - x[others, 6:]).max() <= np.abs(x).max() / 127 + 2.0 ** -9

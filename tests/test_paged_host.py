@@ -89,7 +89,7 @@ def test_what_token_logprobs_refuses():
     f = lambda x=P, st=100, t=P, lp=P, e=P, i=P, tp=P, n=2, V=100, k=5: rx.relax_token_logprobs(x, st, t, lp, e, i, tp, n, V, k)
     assert {f(x=None), f(t=None), f(lp=None), f(i=None), f(tp=None), f(t=None, lp=None, e=None, k=0)} == {rx.ERR_NULL}
     assert {f(n=0), f(V=0, k=0), f(st=99), f(k=-1), f(V=4), f(x=P + 1), f(t=P + 2), f(lp=P + 2), f(e=P + 1), f(i=P + 2), f(tp=P + 2)} == {rx.ERR_SHAPE}
-    assert f(k=33) == rx.ERR_UNSUPPORTED
+    assert {f(k=33), f(V=(1 << 30) + 1, st=1 << 31)} == {rx.ERR_UNSUPPORTED}
     assert rx.relax_token_logprobs_workspace_bytes(0, 10, 1) == 0 and rx.relax_token_logprobs_workspace_bytes(1, 10, 33) == 0
 
 
