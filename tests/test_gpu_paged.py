@@ -613,3 +613,34 @@ def test_lengths_of_a_device_table_beyond_the_capacity(rx):
     assert (k[3:23] == 0).all() and (v[3:23] == 0).all()
     x = qkv.astype(np.float64).reshape(b.n, 8, 64)
     assert np.abs(v[others] - x[others, 6:]).max() <= np.abs(x).max() / 127 + 2.0 ** -9
+
+
+def test_python_side_checks_and_layers_that_share_a_workspace(rx):
+    from paper_2311_02103_amd import runtime
+    rng = np.random.default_rng(75)
+    first = runtime.DevicePagedCache(n_heads=4, n_kv_heads=2, head_dim=64, kv_capacity=64, n_pages=4, page_size=16, n_max=40, rope_base=None)
+    second = runtime.DevicePagedCache(n_heads=4, n_kv_heads=2, head_dim=64, kv_capacity=64, n_pages=4, page_size=16, n_max=40, share_from=first)
+    first.pages.copy_(torch.tensor([[2, 0, 3, 1]], dtype=torch.int32))
+    seqs, x = rx.Seqs([40], [40]), [torch.from_numpy(half(rng, (40, 8 * 64))).cuda() for _ in range(2)]
+    for layer, rows in zip((first, second), x):
+        q = layer.append(rows, seqs)
+        assert torch.equal(q.view(40, 256), rows[:, :256])                             # no rotary table: q as it is
+    for layer, rows in zip((first, second), x):
+        k, v = layer.read(seqs, 40)
+        off = (torch.stack([k, v], 1) - rows[:, 256:].view(40, 2, 2, 64)).abs().max().item()
+        assert off <= rows.abs().max().item() * (0.5 / 127 + 2.0 ** -10)               # half a step of a block's scale, and the rounding to fp16
+        one = layer.append(rows[39:, :].as_strided((1, 512), (1, 1)), rx.Seqs([1], [41]))      # one row: any stride
+        assert torch.equal(one.view(-1), rows[39, :256])
+    with pytest.raises(ValueError):
+        first.append(x[0].float(), seqs)
+    with pytest.raises(ValueError):
+        first.append(x[0][:, :-8], seqs)
+    with pytest.raises(ValueError):
+        first.attention(torch.empty((40, 64, 4), dtype=torch.float16, device="cuda").transpose(1, 2), seqs)
+    with pytest.raises(rx.RelaxError):
+        first.append(torch.empty((41, 512), dtype=torch.float16, device="cuda"), rx.Seqs([41], [64 + 1]))
+    with pytest.raises(ValueError):
+        runtime.token_logprobs(x[0], torch.zeros(40, dtype=torch.int64, device="cuda"))
+    with pytest.raises(ValueError):
+        runtime.token_logprobs(x[0].float())
+    assert rx.relax_workspace_error(first.dims, first.ws) == 0
