@@ -16,8 +16,8 @@
 // 11.1, of 152064 with 20 alternatives 19.9 / 14.8, of 262000 36.6 / 15.2, 16 rows of 128256 17.7 / 13.8; 1 row of 50257 10.5 / 11.4; both sides are some
 // 7 % faster now that a packet's candidates are found as bits first).
 //
-// Bound by the vector unit next to the read: a logit takes nine issue slots in the sums (four of them the exponential) and one and a half in the other
-// two passes, which look at pairs.  2047 rows of 32000 logits: 32 us without alternatives (4.1 TB/s), 42 with 20; 1 row 7.5.
+// Bound by the passes of a row one after the other, between the other rows' reads: a logit takes nine issue slots in the sums (four of them the exponential) and one and
+// a half in the other two passes, which look at pairs; eight instead of nine changed nothing.  2047 rows of 32000 logits: 32 us without alternatives (4.1 TB/s), 42 with 20; 1 row 7.5.
 #include <limits.h>
 
 #include <algorithm>
