@@ -48,7 +48,7 @@ __global__ __launch_bounds__(64 * W, 4) void attn_paged_kernel(PagedSeqs, const 
     const int pos_min = past + p0 / rep, vis = min(past + (p0 + n_pairs - 1) / rep + 1, pa.cap);      // tokens that any of the pairs attends to
     const int t_begin = split * chunk;
     if (split > 0 && t_begin >= vis) return;
-    const int t_end = min(vis, t_begin + chunk);
+    const int t_end = split + 1 == splits ? vis : min(vis, t_begin + chunk);      // the last split takes what a device table holds beyond the host's bound
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, quarter = lane >> 4;
 
@@ -218,7 +218,7 @@ __global__ __launch_bounds__(256) void attn_paged_merge_kernel(PagedSeqs, const 
     // the splits that the tile of this pair had: those of its last pair
     const int pairs = si.q_len * rep, pair = place * rep + hd % rep, last = min(pair | 15, pairs - 1) / rep;
     if (pairs >= least) return;                                // (not split: the other kernel's)
-    const int vis = min(si.kv_len - si.q_len + last + 1, cap), used = max((vis + chunk - 1) / chunk, 1);
+    const int vis = min(si.kv_len - si.q_len + last + 1, cap), used = min(max((vis + chunk - 1) / chunk, 1), splits);
     const float *src = part + (size_t)i * splits * (D + 2);
     float mm = -INFINITY, den = 0.0f;
     float4p_t num = {0.0f, 0.0f, 0.0f, 0.0f};

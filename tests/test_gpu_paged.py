@@ -644,3 +644,20 @@ def test_python_side_checks_and_layers_that_share_a_workspace(rx):
     with pytest.raises(ValueError):
         runtime.token_logprobs(x[0].float())
     assert rx.relax_workspace_error(first.dims, first.ws) == 0
+
+
+@pytest.mark.parametrize("bound", [2, 130, 700])
+def test_a_device_table_beyond_the_bounds_of_the_call(rx, bound):
+    """Lengths of the table that the bounds of the host fall short of, within the capacity: all their tokens count."""
+    q_lens, kv_lens, shape = [1, 2], [3000, 41], (8, 2, 64)
+    b = Bench(rx, np.random.default_rng(78), *shape, 32, q_lens, kv_lens, device_table=True)
+    q = half(np.random.default_rng(79), (b.n, 8, 64))
+    dev = torch.from_numpy(q).cuda()
+    out = torch.empty_like(dev)
+    ws_bytes = rx.relax_paged_workspace_bytes(b.dims, b.n, bound, 2)
+    ws = torch.empty(ws_bytes, dtype=torch.uint8, device="cuda")
+    rx.check(rx.relax_workspace_init(b.dims, ws, ws_bytes))
+    rx.check(rx.relax_paged_attention(dev, b.cache, rx.Seqs(q_lens, [bound, 41 if bound > 41 else 2], None, b.dev_table), b.dims, out, b.n, ws, ws_bytes))
+    want, tol = po.attention(q.astype(np.float64), b.pool, b.pages, 32, q_lens, kv_lens, None, 2, 64)
+    assert (np.abs(out.cpu().numpy().astype(np.float64) - want) <= tol).all()
+    assert rx.relax_workspace_error(b.dims, ws) == 0
