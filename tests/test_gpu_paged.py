@@ -646,6 +646,41 @@ def test_python_side_checks_and_layers_that_share_a_workspace(rx):
     assert rx.relax_workspace_error(first.dims, first.ws) == 0
 
 
+# (heads, KV heads, d), page, q_lens, kv_lens: calls of tiles of 16 pairs in several splits, in one, and of tiles of 256 pairs
+DEVICE_LENGTHS = {"splits": ((4, 2, 64), 16, [1, 2, 1], [1100, 1500, 40]), "splits_128": ((8, 2, 128), 64, [3, 1], [900, 2000]),
+                  "one_split": ((32, 32, 64), 16, [1] * 9, [30, 200, 77, 16, 100, 5, 64, 33, 90]), "rows": ((80, 80, 64), 16, [300, 270], [300, 296]),
+                  "both_kernels": ((40, 40, 128), 16, [400, 2, 260, 300], [408, 70, 360, 300])}
+
+
+@pytest.mark.parametrize("kind", sorted(DEVICE_LENGTHS))
+def test_attention_on_lengths_of_a_device_table_beyond_the_capacity(rx, kind):
+    """Known on the device only: such a sequence has no token, which gives zeros and the flag, and the others are what they are without it; with host
+    bounds at the capacity and far below it."""
+    shape, page, q_lens, kv_lens = DEVICE_LENGTHS[kind]
+    b = Bench(rx, np.random.default_rng(76), *shape, page, q_lens, kv_lens, device_table=True)
+    q = half(np.random.default_rng(77), (b.n, b.h, b.d))
+    dev, (ws, ws_bytes) = torch.from_numpy(q).cuda(), b.workspace()
+    starts = np.concatenate([[0], np.cumsum(q_lens)])
+    for bounds in ([b.cap] * len(q_lens), kv_lens):
+        out = torch.empty_like(dev)
+        call = lambda: rx.check(rx.relax_paged_attention(dev, b.cache, rx.Seqs(q_lens, bounds, None, b.dev_table), b.dims, out, b.n, ws, ws_bytes))
+        rx.check(rx.relax_workspace_init(b.dims, ws, ws_bytes))
+        b.dev_table[2] = torch.tensor(kv_lens, dtype=torch.int32)
+        call()
+        clean = out.clone()
+        assert b.error() == 0
+        for lost in {0, len(q_lens) - 1}:
+            for length in (b.cap + 1, b.cap + 500, 2 ** 31 - 1):
+                b.dev_table[2, lost] = length
+                out.fill_(float("nan"))
+                call()
+                rows = slice(int(starts[lost]), int(starts[lost + 1]))
+                want = clean.clone()
+                want[rows] = 0
+                assert torch.equal(out, want) and b.error() == 4, (lost, length)
+            b.dev_table[2] = torch.tensor(kv_lens, dtype=torch.int32)
+
+
 @pytest.mark.parametrize("bound", [2, 130, 700])
 def test_a_device_table_beyond_the_bounds_of_the_call(rx, bound):
     """Lengths of the table that the bounds of the host fall short of, within the capacity: all their tokens count."""
