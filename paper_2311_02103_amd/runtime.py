@@ -144,21 +144,28 @@ class DeviceModel:
         return logits, next_ids
 
 
+_NOT_GIVEN = object()
+
+
 class DevicePagedCache:
     """The 8-bit paged KV cache of one layer: the pool, its scales, the page table `pages` (int32 [kv_slots, pages per slot], written by the caller, who
-    hands out the pool's pages), the rotary table and the workspace, sized by upper bounds (n_max, L_max = kv_capacity, B_max)."""
+    hands out the pool's pages), the rotary table and the workspace, sized by upper bounds (n_max, L_max = kv_capacity, B_max).  rope_base: 10000 if not
+    given, None: no rotation.  share_from: another layer's page table, rotary table and workspace, which have to cover this one's slots and positions;
+    rope_base is then the other layer's."""
 
     def __init__(self, *, n_heads: int, n_kv_heads: int, head_dim: int, kv_capacity: int, n_pages: int, page_size: int = 64, kv_slots: int = 1,
-                 n_max: int = 1, B_max: Optional[int] = None, rope_base: Optional[float] = 10000.0, device="cuda", share_from: "DevicePagedCache" = None):
-        self.device = device
-        self.dims = rx.make_dims(n_heads * head_dim, n_heads, n_kv_heads, head_dim, 64, kv_capacity, kv_slots, rope_base=rope_base or 10000.0)
+                 n_max: int = 1, B_max: Optional[int] = None, rope_base: Optional[float] = _NOT_GIVEN, device="cuda", share_from: "DevicePagedCache" = None):
+        self.device, self.page_size = device, page_size
+        self.rope_base = rope_base if rope_base is not _NOT_GIVEN else 10000.0 if share_from is None else share_from.rope_base
+        self.dims = rx.make_dims(n_heads * head_dim, n_heads, n_kv_heads, head_dim, 64, kv_capacity, kv_slots, rope_base=self.rope_base or 10000.0)
         self.n_max, self.B_max = n_max, (B_max if B_max is not None else max(kv_slots, 1))
         if share_from is not None:          # layers of one model share the page table, the rotary table and the workspace
+            self._check_shared(share_from)
             self.pages, self.rope, self.ws, self.ws_bytes = share_from.pages, share_from.rope, share_from.ws, share_from.ws_bytes
         else:
             self.pages = torch.full((kv_slots, -(-kv_capacity // page_size)), -1, dtype=torch.int32, device=device)
             self.rope = None
-            if rope_base is not None:
+            if self.rope_base is not None:
                 self.rope = torch.empty(rx.relax_rope_table_bytes(self.dims) // 4, dtype=torch.float32, device=device)
                 rx.check(rx.relax_rope_table_init(self.dims, self.rope), "relax_rope_table_init")
             self.ws_bytes = rx.relax_paged_workspace_bytes(self.dims, n_max, kv_capacity, self.B_max)
@@ -168,6 +175,20 @@ class DevicePagedCache:
         self.k, self.v = (torch.empty(shape, dtype=torch.uint8, device=device) for _ in "kv")
         self.k_scale, self.v_scale = (torch.empty(shape[:3], dtype=torch.float32, device=device) for _ in "kv")
         self.cache = rx.PagedCache(self.k, self.v, self.k_scale, self.v_scale, self.pages, self.rope, n_pages, page_size, self.pages.shape[1])
+
+    def _check_shared(self, other: "DevicePagedCache") -> None:
+        """The kernels index the shared tables by this layer's sizes, which the C calls cannot compare with the tables'."""
+        slots, positions = other.pages.shape[0], other.pages.shape[1] * other.page_size
+        if other.rope is not None:          # [kv_capacity, d / 2, 2]
+            positions = min(positions, other.rope.numel() // other.dims.head_dim)
+        if self.page_size != other.page_size:
+            raise ValueError("share_from: pages of %d tokens, the table's are of %d" % (self.page_size, other.page_size))
+        if self.dims.kv_slots > slots or self.dims.kv_capacity > positions:
+            raise ValueError("share_from: %d slots of %d positions on tables for %d of %d" % (self.dims.kv_slots, self.dims.kv_capacity, slots, positions))
+        if self.rope_base != other.rope_base or (other.rope is not None and self.dims.head_dim != other.dims.head_dim):
+            raise ValueError("share_from: the rotary table has another base or head_dim")
+        if torch.empty(0, device=self.device).device != other.pages.device:
+            raise ValueError("share_from: the tables are on another device")
 
     def append(self, qkv: torch.Tensor, seqs: "rx.Seqs", q_out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """qkv: fp16 [n, (h + 2 g) d], rows contiguous (any stride between them).  Returns q, rotated, fp16 [n, h, d]."""

@@ -1,0 +1,49 @@
+"""What the Python side of the paged cache and of the log probabilities refuses before it reaches the library, and where it allocates.  Tensors are
+on the CPU and the calls that would enqueue work are replaced: nothing runs on a GPU."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2311_02103_amd import binding as rx
+from paper_2311_02103_amd import runtime
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The library calls that were made, as (name, arguments); they succeed and do nothing."""
+    made = []
+    for name in ("relax_workspace_init", "relax_rope_table_init", "relax_paged_append", "relax_paged_attention", "relax_paged_read", "relax_token_logprobs"):
+        monkeypatch.setattr(rx, name, lambda *args, name=name: made.append((name, args)) or 0)
+    return made
+
+
+def cache(**kw):
+    base = dict(n_heads=4, n_kv_heads=2, head_dim=64, kv_capacity=100, n_pages=4, page_size=64, kv_slots=2, n_max=8, device="cpu")
+    base.update(kw)
+    return runtime.DevicePagedCache(**base)
+
+
+@pytest.mark.parametrize("other", [dict(kv_slots=3), dict(kv_capacity=101), dict(kv_capacity=128), dict(page_size=32), dict(page_size=128, kv_capacity=100),
+                                   dict(head_dim=128), dict(rope_base=None), dict(rope_base=500000.0), dict(kv_capacity=128, page_size=32)], ids=str)
+def test_layers_share_only_tables_that_cover_them(calls, other):
+    first = cache()
+    with pytest.raises(ValueError):
+        cache(share_from=first, **other)
+
+
+def test_a_rotary_base_where_the_other_layer_has_none(calls):
+    first = cache(rope_base=None)
+    with pytest.raises(ValueError):
+        cache(share_from=first, rope_base=10000.0)
+    assert cache(share_from=first).rope is None and cache(share_from=first, head_dim=128, rope_base=None).rope is None
+
+
+def test_tables_that_are_shared(calls):
+    first = cache(rope_base=500000.0)
+    for kw in (dict(), dict(kv_slots=1), dict(kv_capacity=64), dict(rope_base=500000.0), dict(n_pages=9), dict(n_kv_heads=4)):
+        second = cache(share_from=first, **kw)
+        assert second.pages is first.pages and second.rope is first.rope and second.ws is first.ws
+        assert second.rope_base == 500000.0 and second.dims.rope_base == 500000.0 and second.cache.c().pages_per_slot == first.pages.shape[1]
+    assert cache().rope_base == 10000.0
+    assert cache(share_from=cache(share_from=first, kv_slots=1, kv_capacity=64)).pages is first.pages      # what counts is the tables' size
+    assert cache(share_from=cache(rope_base=None), kv_capacity=128).rope is None
