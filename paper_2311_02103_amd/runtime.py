@@ -2,6 +2,7 @@
 the rotary table and the workspace of one layer.  Allocation and host->device copies only."""
 from __future__ import annotations
 
+import contextlib
 from typing import Dict, Optional, Sequence
 
 import numpy as np
@@ -144,6 +145,16 @@ class DeviceModel:
         return logits, next_ids
 
 
+def _allocating_for(stream):
+    """Context in which torch's new tensors belong to `stream` (as the calls take it: None, a torch stream or its address).  Memory of another stream
+    could be handed out again while the kernels on this one still use it, or still be in use there."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if isinstance(stream, int):
+        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    return torch.cuda.stream(stream)
+
+
 _NOT_GIVEN = object()
 
 
@@ -151,7 +162,7 @@ class DevicePagedCache:
     """The 8-bit paged KV cache of one layer: the pool, its scales, the page table `pages` (int32 [kv_slots, pages per slot], written by the caller, who
     hands out the pool's pages), the rotary table and the workspace, sized by upper bounds (n_max, L_max = kv_capacity, B_max).  rope_base: 10000 if not
     given, None: no rotation.  share_from: another layer's page table, rotary table and workspace, which have to cover this one's slots and positions;
-    rope_base is then the other layer's."""
+    rope_base is then the other layer's.  Tensors that a call with `stream` returns belong to that stream, as under torch.cuda.stream."""
 
     def __init__(self, *, n_heads: int, n_kv_heads: int, head_dim: int, kv_capacity: int, n_pages: int, page_size: int = 64, kv_slots: int = 1,
                  n_max: int = 1, B_max: Optional[int] = None, rope_base: Optional[float] = _NOT_GIVEN, device="cuda", share_from: "DevicePagedCache" = None):
@@ -198,7 +209,8 @@ class DevicePagedCache:
             raise ValueError("qkv is fp16 [n, (h + 2 g) d] with contiguous rows")
         pitch = qkv.stride(0) if n > 1 else qkv.shape[1]
         if q_out is None:
-            q_out = torch.empty((n, h, d), dtype=torch.float16, device=self.device)
+            with _allocating_for(stream):
+                q_out = torch.empty((n, h, d), dtype=torch.float16, device=self.device)
         rx.check(rx.relax_paged_append(at, pitch, at + 2 * h * d, at + 2 * (h + g) * d, pitch, q_out, self.cache, seqs, self.dims, n,
                                        self.ws, self.ws_bytes, stream), "relax_paged_append")
         return q_out
@@ -206,29 +218,34 @@ class DevicePagedCache:
     def attention(self, q: torch.Tensor, seqs: "rx.Seqs", out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         if q.dtype != torch.float16 or not q.is_contiguous():
             raise ValueError("q is fp16 [n, h, d], contiguous")
-        out = torch.empty_like(q) if out is None else out
+        if out is None:
+            with _allocating_for(stream):
+                out = torch.empty_like(q)
         rx.check(rx.relax_paged_attention(q, self.cache, seqs, self.dims, out, q.shape[0], self.ws, self.ws_bytes, stream), "relax_paged_attention")
         return out
 
     def read(self, seqs: "rx.Seqs", n: int, stream=None):
         """(k, v) of the call's n rows as fp16 [n, g, d]."""
-        k, v = (torch.empty((n, self.dims.n_kv_heads, self.dims.head_dim), dtype=torch.float16, device=self.device) for _ in "kv")
+        with _allocating_for(stream):
+            k, v = (torch.empty((n, self.dims.n_kv_heads, self.dims.head_dim), dtype=torch.float16, device=self.device) for _ in "kv")
         rx.check(rx.relax_paged_read(self.cache, seqs, self.dims, k, v, n, self.ws, self.ws_bytes, stream), "relax_paged_read")
         return k, v
 
 
 def token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None, top: int = 0, entropy: bool = False, ws: Optional[torch.Tensor] = None, stream=None):
-    """relax_token_logprobs on fp16 logits [n, V], targets int32 [n]: (logprobs, entropy, top_ids, top_logprobs), None where not asked for.  ws: uint8, else made here."""
+    """relax_token_logprobs on fp16 logits [n, V], targets int32 [n]: (logprobs, entropy, top_ids, top_logprobs), None where not asked for.  ws: uint8, else made here.
+    What is made here belongs to `stream`, as under torch.cuda.stream."""
     n, vocab = logits.shape
     if logits.dtype != torch.float16 or (vocab > 1 and logits.stride(1) != 1):
         raise ValueError("logits are fp16 [n, V] with contiguous rows")
     if targets is not None and (targets.dtype != torch.int32 or targets.shape != (n,) or not targets.is_contiguous()):
         raise ValueError("targets are int32 [n]")
     new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=logits.device)
-    if ws is None:
-        ws = new(rx.relax_token_logprobs_workspace_bytes(n, vocab, top), dtype=torch.uint8)
-    lp, ent = new(n) if targets is not None else None, new(n) if entropy else None
-    ids, tops = (new(n, top, dtype=torch.int32), new(n, top)) if top else (None, None)
+    with _allocating_for(stream):
+        if ws is None:
+            ws = new(rx.relax_token_logprobs_workspace_bytes(n, vocab, top), dtype=torch.uint8)
+        lp, ent = new(n) if targets is not None else None, new(n) if entropy else None
+        ids, tops = (new(n, top, dtype=torch.int32), new(n, top)) if top else (None, None)
     rx.check(rx.relax_token_logprobs(logits, logits.stride(0) if n > 1 else vocab, targets, lp, ent, ids, tops, n, vocab, top, ws, ws.numel(), stream), "relax_token_logprobs")
     return lp, ent, ids, tops
 

@@ -696,3 +696,35 @@ def test_a_device_table_beyond_the_bounds_of_the_call(rx, bound):
     want, tol = po.attention(q.astype(np.float64), b.pool, b.pages, 32, q_lens, kv_lens, None, 2, 64)
     assert (np.abs(out.cpu().numpy().astype(np.float64) - want) <= tol).all()
     assert rx.relax_workspace_error(b.dims, ws) == 0
+
+
+@pytest.mark.parametrize("by_address", [False, True])
+def test_python_calls_on_a_stream_of_their_own(rx, by_address):
+    """Append, attention, read and log probabilities on a side stream that starts late, with nothing but what the calls allocate, against the same on
+    the current stream; the current stream allocates and writes in between."""
+    from paper_2311_02103_amd import runtime
+    rng = np.random.default_rng(80)
+    make = lambda: runtime.DevicePagedCache(n_heads=8, n_kv_heads=2, head_dim=64, kv_capacity=512, n_pages=16, page_size=32, n_max=500)
+    here, there = make(), make()
+    for layer in (here, there):
+        layer.pages.copy_(torch.arange(16, dtype=torch.int32).view(1, 16))
+    x = torch.from_numpy(half(rng, (500, 12 * 64))).cuda()
+    logits, targets = torch.from_numpy(half(rng, (3, 70001), 3)).cuda(), torch.tensor([5, 70000, 12345], dtype=torch.int32, device="cuda")
+    seqs = rx.Seqs([500], [500])
+
+    def run(layer, stream):
+        q = layer.append(x, seqs, stream=stream)
+        return (q, layer.attention(q, seqs, stream=stream), *layer.read(seqs, 500, stream=stream), *runtime.token_logprobs(logits, targets, 7, True, stream=stream))
+    want = run(here, None)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            late = torch.randn(2048, 2048, device="cuda") @ torch.randn(2048, 2048, device="cuda")
+    for _ in range(3):
+        got = run(there, side.cuda_stream if by_address else side)
+        noise = [torch.full((size,), 255, dtype=torch.uint8, device="cuda") for size in (512, 4096, 65536, 1 << 20) for _ in range(4)]
+    torch.cuda.synchronize()
+    assert len(noise) == 16 and late.shape == (2048, 2048)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)

@@ -47,3 +47,42 @@ def test_tables_that_are_shared(calls):
     assert cache().rope_base == 10000.0
     assert cache(share_from=cache(share_from=first, kv_slots=1, kv_capacity=64)).pages is first.pages      # what counts is the tables' size
     assert cache(share_from=cache(rope_base=None), kv_capacity=128).rope is None
+
+
+class FakeStream:
+    cuda_stream = 0x5000
+
+
+@pytest.mark.parametrize("by_address", [False, True])
+def test_what_a_call_on_a_stream_allocates_belongs_to_it(calls, monkeypatch, by_address):
+    """Memory of the current stream would be handed out again there while the call's kernels run."""
+    seqs, here, made = rx.Seqs([3], [3]), [], []
+    layer = cache()
+
+    class On:
+        def __init__(self, stream):
+            self.stream = stream
+
+        def __enter__(self):
+            here.append(self.stream.cuda_stream)
+
+        def __exit__(self, *_):
+            here.pop()
+
+    class ExternalStream(FakeStream):
+        def __init__(self, address):
+            self.cuda_stream = address
+    monkeypatch.setattr(torch.cuda, "stream", On)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", ExternalStream)
+    for name in ("empty", "empty_like"):
+        plain = getattr(torch, name)
+        monkeypatch.setattr(torch, name, lambda *a, plain=plain, **kw: made.append(here[-1] if here else None) or plain(*a, **kw))
+    stream = FakeStream.cuda_stream if by_address else FakeStream()
+    x, logits = torch.zeros((3, 8 * 64), dtype=torch.float16), torch.zeros((2, 70000), dtype=torch.float16)
+    for stream, want in ((stream, FakeStream.cuda_stream), (None, None)):
+        for call, count in ((lambda: layer.append(x, seqs, stream=stream), 1), (lambda: layer.attention(x[:, :256].contiguous(), seqs, stream=stream), 1),
+                            (lambda: layer.read(seqs, 3, stream=stream), 2),
+                            (lambda: runtime.token_logprobs(logits, torch.zeros(2, dtype=torch.int32), 4, True, stream=stream), 5)):
+            made.clear(), calls.clear()
+            call()
+            assert made == [want] * count and len(calls) == 1 and calls[0][1][-1] is stream and not here
