@@ -155,6 +155,12 @@ def _allocating_for(stream):
     return torch.cuda.stream(stream)
 
 
+def _check_tensor(t: torch.Tensor, dtype, count: int, device, what: str) -> None:
+    """The calls take an address and count elements from there."""
+    if t.dtype != dtype or t.numel() != count or not t.is_contiguous() or t.device != device:
+        raise ValueError("%s: %d elements of %s, contiguous, on %s" % (what, count, dtype, device))
+
+
 _NOT_GIVEN = object()
 
 
@@ -204,11 +210,13 @@ class DevicePagedCache:
     def append(self, qkv: torch.Tensor, seqs: "rx.Seqs", q_out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """qkv: fp16 [n, (h + 2 g) d], rows contiguous (any stride between them).  Returns q, rotated, fp16 [n, h, d]."""
         h, g, d = self.dims.n_heads, self.dims.n_kv_heads, self.dims.head_dim
+        if qkv.dtype != torch.float16 or qkv.dim() != 2 or qkv.shape[1] != (h + 2 * g) * d or qkv.stride(1) != 1 or qkv.device != self.pages.device:
+            raise ValueError("qkv is fp16 [n, (h + 2 g) d] with contiguous rows, on the cache's device")
         n, at = qkv.shape[0], qkv.data_ptr()
-        if qkv.dtype != torch.float16 or qkv.shape[1] != (h + 2 * g) * d or qkv.stride(1) != 1:
-            raise ValueError("qkv is fp16 [n, (h + 2 g) d] with contiguous rows")
         pitch = qkv.stride(0) if n > 1 else qkv.shape[1]
-        if q_out is None:
+        if q_out is not None:
+            _check_tensor(q_out, torch.float16, n * h * d, self.pages.device, "q_out [n, h, d]")
+        else:
             with _allocating_for(stream):
                 q_out = torch.empty((n, h, d), dtype=torch.float16, device=self.device)
         rx.check(rx.relax_paged_append(at, pitch, at + 2 * h * d, at + 2 * (h + g) * d, pitch, q_out, self.cache, seqs, self.dims, n,
@@ -216,9 +224,11 @@ class DevicePagedCache:
         return q_out
 
     def attention(self, q: torch.Tensor, seqs: "rx.Seqs", out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
-        if q.dtype != torch.float16 or not q.is_contiguous():
-            raise ValueError("q is fp16 [n, h, d], contiguous")
-        if out is None:
+        count = q.shape[0] * self.dims.n_heads * self.dims.head_dim
+        _check_tensor(q, torch.float16, count, self.pages.device, "q [n, h, d]")
+        if out is not None:
+            _check_tensor(out, torch.float16, count, self.pages.device, "out [n, h, d]")
+        else:
             with _allocating_for(stream):
                 out = torch.empty_like(q)
         rx.check(rx.relax_paged_attention(q, self.cache, seqs, self.dims, out, q.shape[0], self.ws, self.ws_bytes, stream), "relax_paged_attention")
@@ -238,8 +248,10 @@ def token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None,
     n, vocab = logits.shape
     if logits.dtype != torch.float16 or (vocab > 1 and logits.stride(1) != 1):
         raise ValueError("logits are fp16 [n, V] with contiguous rows")
-    if targets is not None and (targets.dtype != torch.int32 or targets.shape != (n,) or not targets.is_contiguous()):
-        raise ValueError("targets are int32 [n]")
+    if targets is not None:
+        _check_tensor(targets, torch.int32, n, logits.device, "targets [n]")
+    if ws is not None:
+        _check_tensor(ws, torch.uint8, ws.numel(), logits.device, "ws")
     new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=logits.device)
     with _allocating_for(stream):
         if ws is None:

@@ -86,3 +86,29 @@ def test_what_a_call_on_a_stream_allocates_belongs_to_it(calls, monkeypatch, by_
             made.clear(), calls.clear()
             call()
             assert made == [want] * count and len(calls) == 1 and calls[0][1][-1] is stream and not here
+
+
+def test_tensors_that_do_not_fit(calls):
+    """Each would be read or written past its end, or from another device's address."""
+    layer, seqs = cache(), rx.Seqs([3], [3])
+    new = lambda *shape, dtype=torch.float16, device="cpu": torch.zeros(shape, dtype=dtype, device=device)
+    calls.clear()
+    for qkv, q_out in ((new(3, 512, device="meta"), None), (new(3, 8, 64), None), (new(1536), None), (new(3, 520), None), (new(512, 3).t(), None), (new(3, 512, dtype=torch.bfloat16), None),
+                       (new(3, 512), new(2, 4, 64)), (new(3, 512), new(3, 4, 64, dtype=torch.float32)), (new(3, 512), new(3, 64, 4).transpose(1, 2)),
+                       (new(3, 512), new(3, 4, 64, device="meta")), (new(3, 512), new(3, 4, 128))):
+        with pytest.raises(ValueError):
+            layer.append(qkv, seqs, q_out)
+    for q, out in ((new(3, 2, 64), None), (new(3, 4, 32), None), (new(3, 8, 64), None), (new(3, 4, 64, device="meta"), None), (new(3, 4, 64), new(3, 4, 32)),
+                   (new(3, 4, 64), new(3, 4, 64, dtype=torch.float32)), (new(3, 4, 64), new(3, 4, 64, device="meta")), (new(3, 4, 64), new(3, 8, 64)[:, :4])):
+        with pytest.raises(ValueError):
+            layer.attention(q, seqs, out)
+    logits = new(3, 100)
+    for targets, ws in ((new(2, dtype=torch.int32), None), (new(3, dtype=torch.int64), None), (new(3, dtype=torch.int32, device="meta"), None),
+                        (new(6, dtype=torch.int32)[::2], None), (None, new(64, dtype=torch.float32)), (None, new(64, dtype=torch.uint8, device="meta")),
+                        (None, new(128, dtype=torch.uint8)[::2])):
+        with pytest.raises(ValueError):
+            runtime.token_logprobs(logits, targets, 3, ws=ws)
+    assert not calls
+    layer.append(new(3, 520)[:, :512], seqs, new(3, 256)), layer.attention(new(3, 256), seqs, new(3, 4, 64))
+    runtime.token_logprobs(logits, new(3, dtype=torch.int32), 3, ws=new(512, dtype=torch.uint8))
+    assert [name for name, _ in calls] == ["relax_paged_append", "relax_paged_attention", "relax_token_logprobs"]
