@@ -436,7 +436,7 @@ relax_status relax_paged_read(const relax_paged_cache *cache, const relax_seqs *
 /* ---- Log probabilities of tokens ------------------------------------------------------------------------------------
  * What a serving program returns beside the picked token, or scores a given text with, from rows of logits (those of relax_model_step, or
  * of relax_half_matmul with the head on every row): with log p = x - log(sum e^x) per row
- *   logprobs[i]                log p of token targets[i]; -inf for an id outside [0, vocab)     (both NULL: not wanted)
+ *   logprobs[i]                log p of token targets[i]; -inf for an id outside [0, vocab) (as for a token at -inf)     (both NULL: not wanted)
  *   entropy[i]                 -sum p log p                                                     (NULL: not wanted)
  *   top_ids, top_logprobs      [n,top]: the `top` most likely tokens, most likely first, equal logits in order of their ids, and their
  *                              log p; 0 <= top <= 32, top <= vocab (top == 0: both unused)

@@ -87,16 +87,19 @@ struct Outputs {
     SliceList *slices;               // PART: [n][slices]
 };
 
-// The end of a row: `rest` is the sum without one maximum, both sums relative to m (0 where that is -inf); target: its logit, -inf outside the vocabulary
+// What the logits of a row are taken relative to: its maximum, 0 where that is infinite.  The sum of a row with a +inf then is +inf, of one with a NaN it is NaN.
+__device__ __forceinline__ float base_of(float m) { return fabsf(m) == INFINITY ? 0.0f : m; }
+
+// The end of a row: `rest` is the sum without one maximum, both sums relative to base_of(m); target: its logit, -inf outside the vocabulary
 struct RowEnd {
     float base, rest, log_s;
     bool empty;
     __device__ __forceinline__ RowEnd(float m, float rest_, int tops)
     {
-        base = m == -INFINITY ? 0.0f : m;
+        base = base_of(m);
         empty = m == -INFINITY && rest_ == 0.0f;               // no logit above -inf, and no NaN
         rest = rest_ + (float)(tops - 1);
-        log_s = log1pf(rest);
+        log_s = log1pf(fmaf(0.0f, rest, rest));                // (NaN where a +inf is in the row: only a token at -inf has a log probability then)
     }
     __device__ __forceinline__ float logp(float x) const { return empty || x == -INFINITY ? (rest == rest ? -INFINITY : rest) : x - base - log_s; }
     __device__ __forceinline__ float entropy(float t) const { return empty ? 0.0f : log_s - t * kLn2 / (1.0f + rest); }
@@ -197,7 +200,7 @@ __global__ __launch_bounds__(NT) void token_logprobs_kernel(const uint16_t *__re
     }
 
     // ---- sums: exponents in units of log 2; the maxima themselves, in the wavefronts that hold one, are counted instead ----
-    const float base = m == -INFINITY ? 0.0f : m;
+    const float base = base_of(m);
     float rest = 0.0f, t = 0.0f;
     int tops = 0;
     auto add = [&](const u32x4l_t &w, bool count) __attribute__((always_inline)) {

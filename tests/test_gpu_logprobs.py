@@ -159,3 +159,19 @@ def test_behind_a_head_and_in_a_graph(rx):
         torch.cuda.synchronize()
         for a, o in zip(got, out):
             assert np.array_equal(a, o.cpu().numpy())
+
+
+@pytest.mark.parametrize("ws", [True, False])
+@pytest.mark.parametrize("V,top", [(9, 9), (40, 32), (32000, 20), (152064, 32), (200000, 5)])
+def test_infinite_rows_with_masked_tokens(rx, V, top, ws):
+    """A +inf leaves no log probability but that of a token at -inf, in the vocabulary or outside; a NaN leaves none."""
+    rng = np.random.default_rng(9)
+    x = (rng.standard_normal((12, V)) * 2.5).astype(np.float16)
+    x[:, V // 4], x[:, V // 2], x[:, 0] = -np.inf, np.inf, 0.0
+    x[4:8, 1:] = np.where(rng.integers(0, 3, (4, V - 1)) == 0, np.inf, -np.inf)
+    x[8:, V - 1] = np.nan
+    t = np.array([V // 4, V // 2, 0, V] * 3)
+    x[4, t[4]], x[5, t[5]] = -np.inf, np.inf
+    got = call(rx, x, t, top, ws=ws)
+    check(x, t, top, got)
+    assert got[0][0] == got[0][3] == got[0][4] == got[0][7] == -np.inf and np.isnan(np.r_[got[0][1:3], got[0][5:7], got[0][8:], got[1]]).all()
