@@ -412,7 +412,7 @@ size_t relax_paged_workspace_bytes(const relax_layer_dims *dims, int32_t n_max, 
  *   q_out[i] = R(pos_i) q[i], fp16 [n,h,d]  (q_out may be q if q_stride is h d, else they do not overlap; q and q_out NULL: only k and v)
  *   k, v:  a block's scale is max|x| / 127 over the call's tokens in it, of keys behind the rotary embedding (which are not rounded in
  *   between); a block that holds earlier tokens of the sequence keeps its scale if that is larger, else their codes
- *   become round((u - 128) * old / new) + 128.  u = 128 + round(x / scale).  Infinite values count as +-65504, NaNs as 0.
+ *   become round((u - 128) * old / new) + 128.  u = 128 + round(x / scale).  Infinite inputs count as +-65504, NaNs as 0, in front of the rotation.
  * Tokens of the sequence in front of the call's, and whatever lies behind its last one, stay as they are but for that.  The slots of a call are distinct.
  * ws: relax_paged_workspace_bytes(dims, n, max kv_lens, B) bytes, 256-byte aligned.  Errors: NULL, SHAPE, CAPACITY, WORKSPACE, UNSUPPORTED
  * (page_size, pool too large, more than 65535 sequences).                                                              */
@@ -429,6 +429,7 @@ relax_status relax_paged_attention(const uint16_t *q, const relax_paged_cache *c
 
 /* What the cache stands for, as fp16: row i of sequence b is position kv_lens[b] - q_lens[b] + i, k_out and v_out [n,g,d], 16-byte aligned,
  * either may be NULL.  Keys come out as they are held, rotated: rows of a relax_kv_cache, or of an append without a rotary table.
+ * (A rotated key may be held up to 65504 * sqrt 2: beyond fp16's range it comes out infinite.)
  * ws and errors as relax_paged_append.                                                                                   */
 relax_status relax_paged_read(const relax_paged_cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims, uint16_t *k_out,
                               uint16_t *v_out, int32_t n, void *ws, size_t ws_bytes, relax_stream stream);

@@ -28,7 +28,8 @@ __device__ __forceinline__ void load8p(const uint16_t *p, float *v)
     for (int e = 0; e < 8; ++e) v[e] = (float)x[e];
 }
 
-// what a value is quantised from: fp16's range, a NaN is 0
+// what of an input is quantised: the ends of fp16's range for infinities, 0 for a NaN.  In front of the rotation: inf * 0 would be a NaN in both elements of the pair,
+// and a finite pair may leave that range behind it, which an fp32 scale holds
 __device__ __forceinline__ float storable(float x) { return x == x ? fminf(fmaxf(x, -65504.0f), 65504.0f) : 0.0f; }
 
 // pairs (a[e], b[e]) at the angles cs[2 e], cs[2 e + 1]
@@ -84,6 +85,8 @@ __device__ __forceinline__ bool put_keys(const RowsView &r, const PagedArgs &pa,
         const int e = (quarter + 4 * i) * 8;
         load8p(x + e, a[i]);
         load8p(x + e + D / 2, b[i]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) a[i][j] = storable(a[i][j]), b[i][j] = storable(b[i][j]);
         if (pa.rope) rotate8(a[i], b[i], pa.rope + ((size_t)(pos + src) * (D / 2) + e) * 2);
     }
     const int pool = find();
@@ -91,10 +94,7 @@ __device__ __forceinline__ bool put_keys(const RowsView &r, const PagedArgs &pa,
 #pragma unroll
     for (int i = 0; i < U; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            a[i][j] = storable(a[i][j]), b[i][j] = storable(b[i][j]);
-            amax = fmaxf(amax, fmaxf(fabsf(a[i][j]), fabsf(b[i][j])));
-        }
+        for (int j = 0; j < 8; ++j) amax = fmaxf(amax, fmaxf(fabsf(a[i][j]), fabsf(b[i][j])));
     amax = wave_max(amax);
     if (pool < 0) return false;
     // unit (i, half): elements (quarter + 4 i) * 8 + half * D / 2 of the lane's token

@@ -728,3 +728,36 @@ def test_python_calls_on_a_stream_of_their_own(rx, by_address):
     assert len(noise) == 16 and late.shape == (2048, 2048)
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("shape", [(4, 2, 64), (8, 4, 128)], ids=str)
+def test_rotated_keys_that_are_not_finite_or_near_the_limit(rx, shape):
+    """Infinities and NaNs are replaced in the inputs, so that a pair's other element is what its finite input gives, at position 0 too; a pair near
+    fp16's limit is held as it is behind the rotation, up to 65504 * sqrt 2."""
+    rng = np.random.default_rng(81)
+    h, g, d = shape
+    b = Bench(rx, rng, h, g, d, 16, [40], [40])
+    qkv = half(rng, (40, (h + 2 * g) * d))
+    k = qkv[:, h * d:(h + g) * d].reshape(40, g, d)
+    k[0, 0, 3], k[0, 0, 5 + d // 2], k[0, 1, 7], k[17, 1, 2], k[18, 0, 9] = np.inf, -np.inf, np.nan, np.nan, -np.inf
+    k[32:, 0, 1], k[32:, 0, 1 + d // 2] = 65504, -65504
+    qkv[:, h * d:(h + g) * d] = k.reshape(40, g * d)
+    b.append(qkv)
+    pool = b.host_pool()
+    want = np.stack([po.rotate(po.storable(k[t].astype(np.float64)), t, d) for t in range(40)])
+    assert np.abs(want[32:]).max() > 80000
+    index = po.code_index("k", d)
+    for first in (0, 16, 32):
+        page, block = b.pages[0, first // 16], want[first:first + 16]
+        for head in range(g):
+            s = pool["ks"][page, head, 0]
+            # as check_append: the scale within 2^-21, a code within half a step and 1e-4, since |a| + |b| of a pair is at most twice the block's maximum
+            assert abs(s - np.abs(block[:, head]).max() / 127) <= 2.0 ** -21 * s
+            codes = pool["k"][page, head, 0][index].astype(np.float64) - 128
+            assert np.abs(codes[:len(block)] - block[:, head] / np.abs(block[:, head]).max() * 127).max() <= 0.5 + 1e-4
+    out, tol = po.attention(half(np.random.default_rng(82), (40, h, d)).astype(np.float64), pool, b.pages, 16, [40], [40], None, g, d)
+    got = b.attention(half(np.random.default_rng(82), (40, h, d)))
+    assert (np.abs(got - out) <= tol).all()
+    back, vals = b.read()[0], po.values(pool, "k", b.pages, 16, 0, np.arange(40), d)
+    with np.errstate(over="ignore"):
+        assert np.array_equal(back, vals.astype(np.float32).astype(np.float16))
