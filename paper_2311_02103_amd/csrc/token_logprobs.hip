@@ -382,11 +382,22 @@ __global__ __launch_bounds__(256) void token_logprobs_join_kernel(const uint16_t
     }
 }
 
+// A launch has fewer than 2^32 threads: rows beyond kLaunchThreads / NT follow in further ones
+constexpr int64_t kLaunchThreads = 1LL << 31;
 template <int NT, int NP, bool RESIDENT>
 hipError_t launch_one(const uint16_t *logits, int64_t stride, const Outputs &o, int32_t n, int32_t V, int32_t k, hipStream_t stream)
 {
-    hipLaunchKernelGGL((token_logprobs_kernel<NT, NP, RESIDENT, false>), dim3(n), dim3(NT), 0, stream, logits, stride, o, V, k, V);
-    return hipGetLastError();
+    for (int64_t row = 0; row < n; row += kLaunchThreads / NT) {
+        Outputs at = o;
+        if (at.targets) at.targets += row, at.logprobs += row;
+        if (at.entropy) at.entropy += row;
+        if (k > 0) at.top_ids += row * k, at.top_logprobs += row * k;
+        const dim3 rows((uint32_t)std::min(n - row, kLaunchThreads / NT));
+        hipLaunchKernelGGL((token_logprobs_kernel<NT, NP, RESIDENT, false>), rows, dim3(NT), 0, stream, logits + row * stride, stride, at, V, k, V);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 // Slices of a row, as few as hold it: from 65530 logits on, where one workgroup takes longer than two kernels, and only while all slices run at once

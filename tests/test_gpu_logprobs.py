@@ -175,3 +175,20 @@ def test_infinite_rows_with_masked_tokens(rx, V, top, ws):
     got = call(rx, x, t, top, ws=ws)
     check(x, t, top, got)
     assert got[0][0] == got[0][3] == got[0][4] == got[0][7] == -np.inf and np.isnan(np.r_[got[0][1:3], got[0][5:7], got[0][8:], got[1]]).all()
+
+
+def test_more_rows_than_a_launch_has_threads_for(rx):
+    """2^24 + 300 rows of two logits, a workgroup of 256 threads each; closed form in 64 bits, tolerances as in check()."""
+    n, V = (1 << 24) + 300, 2
+    x = torch.randn((n, V), device="cuda", generator=torch.Generator(device="cuda").manual_seed(10)).half()
+    t = torch.randint(0, V, (n,), dtype=torch.int32, device="cuda", generator=torch.Generator(device="cuda").manual_seed(11))
+    lp, ent, tops = (torch.full((n,), 7.0, device="cuda") for _ in range(3))
+    ids = torch.full((n,), -5, dtype=torch.int32, device="cuda")
+    rx.check(rx.relax_token_logprobs(x, V, t, lp, ent, ids, tops, n, V, 1))
+    d = x.double()
+    d = d[:, 1] - d[:, 0]
+    want = torch.stack([-torch.log1p(torch.exp(d)), -torch.log1p(torch.exp(-d))], 1)
+    slack = 2.0 ** -22 * (np.log(V) + 4)
+    assert torch.equal(ids, (d > 0).to(torch.int32))
+    for got, ref, tol in ((lp, want.gather(1, t.long()[:, None])[:, 0], slack), (tops, want.max(1).values, slack), (ent, -(want.exp() * want).sum(1), slack * (np.log(V) + 2))):
+        assert bool(((got.double() - ref).abs() <= tol + 2.0 ** -22 * ref.abs()).all())
