@@ -415,7 +415,7 @@ size_t relax_paged_workspace_bytes(const relax_layer_dims *dims, int32_t n_max, 
  *   become round((u - 128) * old / new) + 128.  u = 128 + round(x / scale).  Infinite inputs count as +-65504, NaNs as 0, in front of the rotation.
  * Tokens of the sequence in front of the call's, and whatever lies behind its last one, stay as they are but for that.  The slots of a call are distinct.
  * ws: relax_paged_workspace_bytes(dims, n, max kv_lens, B) bytes, 256-byte aligned.  Errors: NULL, SHAPE, CAPACITY, WORKSPACE, UNSUPPORTED
- * (page_size, pool too large, more than 65535 sequences).                                                              */
+ * (page_size, pool too large, more than 65535 sequences, kv_capacity > 2^30).                                                              */
 relax_status relax_paged_append(const uint16_t *q, int64_t q_stride, const uint16_t *k, const uint16_t *v, int64_t kv_stride, uint16_t *q_out,
                                 const relax_paged_cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims, int32_t n,
                                 void *ws, size_t ws_bytes, relax_stream stream);

@@ -1414,6 +1414,7 @@ PagedWs paged_ws(const relax_layer_dims &dm, int32_t n, int32_t L, int32_t B)
 
 constexpr int32_t kMaxVocab = 1 << 30;       // logits of a row: places in it are 32-bit numbers
 constexpr int32_t kMaxPagedSeqs = 65535;     // a workgroup finds its sequence 64 at a time
+constexpr int32_t kMaxPagedCapacity = 1 << 30;       // positions are 32-bit numbers, also rounded up to a split and added to one
 
 // Everything the paged calls check alike; fills the kernels' descriptors.  items: see launch_paged_append.
 relax_status paged_begin(const relax_paged_cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims, int32_t n, void *ws, size_t ws_bytes,
@@ -1438,6 +1439,7 @@ relax_status paged_begin(const relax_paged_cache *cache, const relax_seqs *seqs,
     if (seqs->B > kMaxPagedSeqs) return RELAX_ERR_UNSUPPORTED;
     const PagedWs pl = paged_ws(*dims, n, L_max, seqs->B);
     if (ws_bytes < pl.total || !aligned(ws, 256)) return RELAX_ERR_WORKSPACE;
+    if (dims->kv_capacity > kMaxPagedCapacity) return RELAX_ERR_UNSUPPORTED;
     const bool inlined = !seqs->device_table && seqs->B <= kPagedInline;
     st.B = seqs->B, st.n = n, st.q_max = checked.q_max, st.dev = seqs->device_table, st.pad = 0;
     items = 0;

@@ -339,7 +339,7 @@ hipError_t launch_d(const uint16_t *q, const PagedArgs &pa, const relax_layer_di
 // more than one split leaves n * heads * splits <= kPartials, no split but the last is shorter than 128 tokens
 size_t paged_partial_floats(const relax_layer_dims &dm, int32_t n, int32_t L)
 {
-    const size_t most = kPartials, mine = (size_t)n * dm.n_heads * (size_t)((L + 127) / 128);
+    const size_t most = kPartials, mine = (size_t)n * dm.n_heads * (((size_t)L + 127) / 128);
     return (mine < most ? mine : most) * (dm.head_dim + 2);
 }
 

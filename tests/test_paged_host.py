@@ -109,3 +109,14 @@ def test_plain_token_logprobs():
     assert np.allclose(lp[0], np.log(0.25)) and lp[1] == -np.inf
     assert np.allclose(ent[0], 1.75 * np.log(2))
     assert ids.tolist() == [[0, 1, 2, 3], [2, 3, 0, 1]] and np.allclose(np.exp(tops[1]), [0.5, 0.375, 0.0625, 0.0625])
+
+
+def test_capacities_beyond_the_arithmetic_of_positions():
+    """2^31 - 1 positions, rounded up to a split, are no 32-bit number: refused by every call, behind the workspace."""
+    for cap in ((1 << 30) + 1, (1 << 31) - 1):
+        d, c = dims(kv_capacity=cap), cache(rope=None, page_size=256, pages_per_slot=1 << 23)
+        for L in (5, cap):
+            assert calls(c, rx.Seqs([2], [L]), d, 2) == {rx.ERR_UNSUPPORTED}, (cap, L)
+        assert calls(c, rx.Seqs([2], [cap]), d, 2, ws_bytes=256) == {rx.ERR_WORKSPACE}
+    at = [rx.relax_paged_workspace_bytes(dims(kv_capacity=(1 << 31) - 1, n_heads=1, n_kv_heads=1), 1, L, 1) for L in (1, 128, 4096, 1 << 22, (1 << 23) + 1, 1 << 30, (1 << 31) - 1)]
+    assert at == sorted(at) and at[0] > 0
