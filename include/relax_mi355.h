@@ -422,8 +422,10 @@ relax_status relax_paged_append(const uint16_t *q, int64_t q_stride, const uint1
 
 /* relax_attention over a paged cache: q [n,h,d] fp16 (already rotated), out [n,h,d] fp16, 16-byte aligned.  Row i of sequence b attends to
  * positions 0..pos_i of its slot, which must already hold this call's keys and values.  Scores, softmax and sums are fp32, the
- * probabilities (times the scale of their values) are rounded to fp16 in front of their product with the codes.  A row that no token is left for (every page of its
- * sequence out of range) is zeros.  ws and errors as relax_paged_append.                                                */
+ * probabilities (times the scale of their values) are rounded to fp16 in front of their product with the codes: 2^-11 of each.  Blocks of values
+ * whose scale is below 2^-24 of the largest one that the row, or a row of the same tile of the call, can see keep fewer bits: an error of up to 2^-31 of that largest
+ * |v|, and 2^-36 of it per token.  A row that no token is left for (every page of its
+ * sequence out of range, or a device length beyond kv_capacity) is zeros.  ws and errors as relax_paged_append.                                                */
 relax_status relax_paged_attention(const uint16_t *q, const relax_paged_cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims,
                                    uint16_t *out, int32_t n, void *ws, size_t ws_bytes, relax_stream stream);
 
@@ -444,8 +446,8 @@ relax_status relax_paged_read(const relax_paged_cache *cache, const relax_seqs *
  * logits: device fp16, row i at logits + i * stride, stride >= vocab (any alignment).  fp32 throughout.  A logit of -inf has probability 0; a row of
  * nothing else gives -inf and entropy 0.  A row that holds a NaN or +inf gives NaN log probabilities and entropy (a token at
  * -inf aside, unless NaN is in the row); its ids are those of the largest logits all the same, NaNs behind -inf.
- * ws (may be NULL): with relax_token_logprobs_workspace_bytes(n, vocab, top) bytes, 256-byte aligned, few rows are spread over more of the chip; without them
- * the call gives the same.  Errors: NULL (no output wanted either), SHAPE, UNSUPPORTED (top > 32, vocab > 2^30).                         */
+ * ws (may be NULL): with relax_token_logprobs_workspace_bytes(n, vocab, top) bytes, 256-byte aligned, few rows are spread over more of the chip.  The ids are
+ * the same with and without them; the fp32 results agree within rounding, since the order of the sums depends on n, on the row's alignment and on ws.  Errors: NULL (no output wanted either), SHAPE, UNSUPPORTED (top > 32, vocab > 2^30).                         */
 size_t       relax_token_logprobs_workspace_bytes(int32_t n_max, int32_t vocab, int32_t top);
 relax_status relax_token_logprobs(const uint16_t *logits, int64_t stride, const int32_t *targets, float *logprobs, float *entropy, int32_t *top_ids,
                                   float *top_logprobs, int32_t n, int32_t vocab, int32_t top, void *ws, size_t ws_bytes, relax_stream stream);

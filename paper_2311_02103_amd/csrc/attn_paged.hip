@@ -259,8 +259,8 @@ __global__ __launch_bounds__(256) void attn_paged_merge_kernel(PagedSeqs, const 
     *(u32x2p_t *)(out + (size_t)i * D + e) = u32x2p_t{lo, hi};
 }
 
-// Splits of a launch with `small` workgroups per split: from kUnsplit workgroups on none, below it as many as bring it to kPagedGroups workgroups, none but the last
-// shorter than 128 tokens, and no more than kPartials partial results (row, head, split).  The workgroups of a split launch have eight
+// Splits of a launch with `small` workgroups per split: from kUnsplit workgroups on none, below it as many as bring it to kPagedGroups workgroups, at most one
+// per 128 tokens of the longest sequence (rounded up to 32 tokens, a split has 96 at least), and no more than kPartials partial results (row, head, split).  The workgroups of a split launch have eight
 // wavefronts where a split has 256 tokens and more, as many tokens in flight with half the partial results.
 // us, unsplit / split: 16 x 3 rows of 64 / 8 heads (256 workgroups) 18.5 / 23, 4 x 17 rows of them (288) 20 / 25, 16 x 16 rows of 32 / 32 (512) 28 / 38.  16 decode rows
 // of 64 / 8 heads with 768 workgroups 31.6, with 512 35.8, with 1024 32.7, with four wavefronts 36.
@@ -336,7 +336,7 @@ hipError_t launch_d(const uint16_t *q, const PagedArgs &pa, const relax_layer_di
 
 }  // namespace
 
-// more than one split leaves n * heads * splits <= kPartials, no split but the last is shorter than 128 tokens
+// plan() has splits <= ceil(L / 128) and, where it has more than one, n * heads * splits <= kPartials
 size_t paged_partial_floats(const relax_layer_dims &dm, int32_t n, int32_t L)
 {
     const size_t most = kPartials, mine = (size_t)n * dm.n_heads * (((size_t)L + 127) / 128);

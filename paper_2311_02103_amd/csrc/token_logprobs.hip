@@ -17,7 +17,7 @@
 // 7 % faster now that a packet's candidates are found as bits first).
 //
 // Bound by the passes of a row one after the other, between the other rows' reads: a logit takes nine issue slots in the sums (four of them the exponential) and one and
-// a half in the other two passes, which look at pairs; eight instead of nine changed nothing.  2047 rows of 32000 logits: 32 us without alternatives (4.1 TB/s), 42 with 20; 1 row 7.5.
+// a half in the other two passes, which look at pairs; eight instead of nine changed nothing.  2047 rows of 32000 logits: 32 us without alternatives (4.1 TB/s), 39 to 43 with 20; 1 row 7.2.
 #include <limits.h>
 
 #include <algorithm>
@@ -400,7 +400,8 @@ hipError_t launch_one(const uint16_t *logits, int64_t stride, const Outputs &o, 
     return hipSuccess;
 }
 
-// Slices of a row, as few as hold it: from 65530 logits on, where one workgroup takes longer than two kernels, and only while all slices run at once
+// Slices of a row, as few as hold it: from 65530 logits on, where one workgroup takes longer than two kernels, and up to one slice per CU (more have not been
+// measured; several fit on one)
 constexpr int kUncut = 65529;
 int slices_of(int32_t n, int32_t V)
 {
