@@ -45,7 +45,7 @@ __global__ __launch_bounds__(64 * W, 4) void attn_paged_kernel(PagedSeqs, const 
     if (pairs >= least || p0 >= pairs) return;
     const int past = si.kv_len - si.q_len;
     const int n_pairs = min(16, pairs - p0);
-    const bool beyond = si.kv_len > pa.cap;      // (a length from device memory: no page, and so no token)
+    const bool beyond = beyond_capacity(si, pa.cap);
     const int pos_min = past + p0 / rep, vis = beyond ? 0 : past + (p0 + n_pairs - 1) / rep + 1;      // tokens that any of the pairs attends to
     const int t_begin = split * chunk;
     if (split > 0 && t_begin >= vis) return;
@@ -220,7 +220,7 @@ __global__ __launch_bounds__(256) void attn_paged_merge_kernel(PagedSeqs, const 
     // the splits that the tile of this pair had: those of its last pair
     const int pairs = si.q_len * rep, pair = place * rep + hd % rep, last = min(pair | 15, pairs - 1) / rep;
     if (pairs >= least) return;                                // (not split: the other kernel's)
-    const int vis = si.kv_len > cap ? 0 : si.kv_len - si.q_len + last + 1, used = min(max((vis + chunk - 1) / chunk, 1), splits);
+    const int vis = beyond_capacity(si, cap) ? 0 : si.kv_len - si.q_len + last + 1, used = min(max((vis + chunk - 1) / chunk, 1), splits);
     const float *src = part + (size_t)i * splits * (D + 2);
     float mm = -INFINITY, den = 0.0f;
     float4p_t num = {0.0f, 0.0f, 0.0f, 0.0f};

@@ -73,7 +73,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_paged_rows_kernel(PagedSeqs,
     if (pairs < least || p0 < 0) return;                          // (fewer pairs: the other kernel's)
     const int past = si.kv_len - si.q_len;
     const int n_pairs = min(kPairs, pairs - p0);
-    const bool beyond = si.kv_len > pa.cap;                       // (a length from device memory: no page, and so no token)
+    const bool beyond = beyond_capacity(si, pa.cap);
     const int vis = beyond ? 0 : past + (p0 + n_pairs - 1) / rep + 1;
     if (beyond && threadIdx.x == 0) atomicOr(pa.err, kBadPage);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);

@@ -226,14 +226,14 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedSeqs, RowsView r
         if (b >= st->B) return;
         const SeqSpan si = seq_span(st, b);
         const int first = si.kv_len - si.q_len;                // position of the sequence's first row
-        const int blk = (first >> 4) + place;
-        const int low = max(first - blk * 16, 0), high = min(si.kv_len - blk * 16, 16);
+        const int blk = (first >> 4) + place, lead = (first & 15) - place * 16;      // (no position of the block itself: a device table's length may be any number)
+        const int low = max(lead, 0), high = min(lead + si.q_len, 16);
         if (first < 0 || high <= low) return;
-        if (si.kv_len > pa.cap) {                              // (a length from device memory: no page, and no row of the rotary table)
+        if (beyond_capacity(si, pa.cap)) {
             if (lane == 0) atomicOr(pa.err, kBadPage);
             return;
         }
-        const int row = si.q_start + blk * 16 - first;
+        const int row = si.q_start - lead;
         const auto find = [&] { return paged_block(pa, g, kvh, si.slot, blk); };
         if (!(part & 1 ? put_values<D>(r, pa, find, kvh, lane, low, high, row, turn[wave])
                        : put_keys<D>(r, pa, find, kvh, lane, low, high, row, blk * 16)) && lane == 0) atomicOr(pa.err, kBadPage);
@@ -277,12 +277,12 @@ __global__ __launch_bounds__(256) void paged_read_kernel(PagedSeqs, PagedArgs pa
     else b = seq_of(st, item, [](int q_len) { return paged_blocks_of(q_len); }, place);
     if (b >= st->B) return;
     const SeqSpan si = seq_span(st, b);
-    const int first = si.kv_len - si.q_len, blk = (first >> 4) + place;
-    const int low = max(first - blk * 16, 0), high = min(si.kv_len - blk * 16, 16);
+    const int first = si.kv_len - si.q_len, blk = (first >> 4) + place, lead = (first & 15) - place * 16;
+    const int low = max(lead, 0), high = min(lead + si.q_len, 16);
     if (first < 0 || high <= low) return;
-    const int pool = si.kv_len <= pa.cap ? paged_block(pa, g, kvh, si.slot, blk) : -1;
+    const int pool = beyond_capacity(si, pa.cap) ? -1 : paged_block(pa, g, kvh, si.slot, blk);
     if (pool < 0 && lane == 0) atomicOr(pa.err, kBadPage);
-    const int row = si.q_start + blk * 16 - first, at = max(pool, 0);
+    const int row = si.q_start - lead, at = max(pool, 0);
     const float s = pool < 0 ? 0.0f : (part & 1 ? pa.v_scale : pa.k_scale)[at];       // no page: zeros
     const u32x4p_t *src = (const u32x4p_t *)((part & 1 ? pa.v : pa.k) + (size_t)at * (16 * D));
     const int c = lane & 15, quarter = lane >> 4;

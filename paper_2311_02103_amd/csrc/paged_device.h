@@ -47,6 +47,10 @@ __device__ __forceinline__ SeqSpan seq_span(SeqsArg st, int b)      // b: unifor
     return {st->q_start[b], st->q_len[b], st->kv_len[b], st->slot[b]};
 }
 
+// A length from device memory that the capacity does not cover: the sequence has no page, no row of the rotary table and no token.  (As unsigned numbers: one below
+// zero is none either.)
+__device__ __forceinline__ bool beyond_capacity(const SeqSpan &si, int cap) { return (uint32_t)si.kv_len > (uint32_t)cap; }
+
 // Blocks of 16 tokens that a sequence's q_len rows can touch, wherever they begin
 __host__ __device__ inline int paged_blocks_of(int q_len) { return (q_len + 30) >> 4; }
 

@@ -761,3 +761,47 @@ def test_rotated_keys_that_are_not_finite_or_near_the_limit(rx, shape):
     back, vals = b.read()[0], po.values(pool, "k", b.pages, 16, 0, np.arange(40), d)
     with np.errstate(over="ignore"):
         assert np.array_equal(back, vals.astype(np.float32).astype(np.float16))
+
+
+def test_append_and_read_on_device_lengths_next_to_the_end_of_their_type(rx):
+    """Lengths whose last block ends behind 2^31: no page, no row of another sequence touched."""
+    rng = np.random.default_rng(83)
+    b = Bench(rx, rng, 4, 2, 64, 16, [3, 20, 1], [20, 32, 9], device_table=True)
+    qkv = half(rng, (b.n, 8 * 64))
+    for length in (2 ** 31 - 1, 2 ** 31 - 5, 2 ** 31 - 16, 2 ** 31 - 17):
+        for lost, rows in ((0, slice(0, 3)), (1, slice(3, 23))):
+            b.dev_table[2] = torch.tensor([20, 32, 9], dtype=torch.int32)
+            rx.check(rx.relax_workspace_init(b.dims, b.ws, b.ws_bytes))
+            b.append(qkv)
+            k, v = b.read()
+            assert b.error() == 0
+            b.dev_table[2, lost] = length
+            held = b.host_pool()
+            b.append(qkv)
+            assert b.error() == 4
+            again = b.host_pool()
+            for key in held:
+                assert np.array_equal(held[key].view(np.uint8), again[key].view(np.uint8)), (length, lost, key)
+            got = b.read()
+            assert (got[:, rows] == 0).all()
+            keep = np.ones(b.n, bool)
+            keep[rows] = False
+            assert np.array_equal(got[0][keep], k[keep]) and np.array_equal(got[1][keep], v[keep])
+
+
+@pytest.mark.parametrize("kind", ["splits", "rows"])
+def test_device_lengths_below_zero(rx, kind):
+    """Not a length: nothing is read or written for it, whatever the other sequences do."""
+    shape, page, q_lens, kv_lens = DEVICE_LENGTHS[kind]
+    b = Bench(rx, np.random.default_rng(84), *shape, page, q_lens, kv_lens, device_table=True)
+    qkv = half(np.random.default_rng(85), (b.n, (b.h + 2 * b.g) * b.d))
+    q = b.append(qkv)
+    clean, held = b.attention(q), b.host_pool()
+    first = q_lens[0]
+    for length in (-1, -1000, -2 ** 31, -2 ** 31 + 2):
+        b.dev_table[2, 0] = length
+        assert np.array_equal(b.append(qkv)[first:], q[first:])
+        out, again = b.attention(q), b.host_pool()
+        assert (out[:first] == 0).all() and np.array_equal(out[first:], clean[first:]), length
+        for key in held:
+            assert np.array_equal(held[key].view(np.uint8), again[key].view(np.uint8)), (length, key)
