@@ -436,6 +436,98 @@ relax_status relax_paged_attention(const uint16_t *q, const relax_paged_cache *c
 relax_status relax_paged_read(const relax_paged_cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims, uint16_t *k_out,
                               uint16_t *v_out, int32_t n, void *ws, size_t ws_bytes, relax_stream stream);
 
+/* ---- Heads before attention: norms, rotary layouts, scaled positions --------------------------------------------------------
+ * How a model prepares the queries and keys of its heads, where it does more than relax_rmsnorm_rope: an RMSNorm of every head, a rotation of part
+ * of the head, pairs that are neighbours, positions stretched for long contexts.
+ *   x'   = x * w / sqrt(mean(x^2) + eps)                             over the d elements of a head; w fp16 [d], one for all heads of q and one for those of k
+ *   pair t < rotary_dim / 2 of x':  (a, b) -> (a cos - b sin, a sin + b cos)   with (cos, sin) = rope[pos][t];  a, b are
+ *     RELAX_ROPE_HALVES   elements t and t + rotary_dim / 2
+ *     RELAX_ROPE_PAIRS    elements 2 t and 2 t + 1
+ *   elements from rotary_dim on stay x'.
+ * In fp32: each product and sum is rounded once, (x * r) * w with r = fp32(1 / sqrt(..)), the sum of squares fp64; r = 0 where mean + eps is 0.     */
+enum { RELAX_ROPE_HALVES = 0, RELAX_ROPE_PAIRS = 1 };
+typedef struct {
+    const uint16_t *q_norm, *k_norm;  /* device fp16 [d], 16-byte aligned, or NULL: no norm of these heads                        */
+    float eps;                        /* >= 0; used with a norm                                                                   */
+    const float *rope;                /* device [kv_capacity, rotary_dim / 2, 2], 16-byte aligned (relax_rope_table_scaled, or with rotary_dim = d
+                                         relax_rope_table_init), or NULL: no rotation                                              */
+    int32_t rotary_dim;               /* multiple of 16 up to d (0 reads as d); others: RELAX_ERR_UNSUPPORTED                      */
+    int32_t layout;                   /* RELAX_ROPE_HALVES or RELAX_ROPE_PAIRS                                                    */
+} relax_head_prep;
+
+/* Rotary table of scaled positions: table[p][t] = amplitude * (cos, sin)(p * f'_t), p = 0 .. positions - 1, t < rotary_dim / 2, fp64 rounded to fp32, with
+ *   f_t = base^(-2 t / rotary_dim),  f'_t = f_t * (w_t + (1 - w_t) / factor)
+ *     RELAX_ROPE_PLAIN             w = 1
+ *     RELAX_ROPE_LINEAR            w = 0: every position divided by factor
+ *     RELAX_ROPE_INDEX_RAMP        w falls with the index t from 1 at floor(i(fast)), at least 0, to 0 at ceil(i(slow)), at most rotary_dim - 1, where
+ *                                  i(b) = rotary_dim * ln(trained / (2 pi b)) / (2 ln base) is the index whose pair makes b turns within `trained` positions
+ *                                  (the two meet: a ramp of 0.001)
+ *     RELAX_ROPE_WAVELENGTH_RAMP   w = (turns_t - slow) / (fast - slow), kept in 0..1, turns_t = trained * f_t / (2 pi)
+ * amplitude is 1 unless the model scales its angles' entries (0 reads as 1).  base > 1, factor > 0, for ramps trained >= 1 and 0 < slow < fast, all finite:
+ * else RELAX_ERR_SHAPE.  rotary_dim even, 2 .. 256, positions 1 .. 2^30: else RELAX_ERR_UNSUPPORTED (RELAX_ERR_SHAPE below 1).                        */
+enum { RELAX_ROPE_PLAIN = 0, RELAX_ROPE_LINEAR = 1, RELAX_ROPE_INDEX_RAMP = 2, RELAX_ROPE_WAVELENGTH_RAMP = 3 };
+typedef struct {
+    int32_t scaling;                  /* RELAX_ROPE_PLAIN .. RELAX_ROPE_WAVELENGTH_RAMP                                           */
+    int32_t rotary_dim;
+    double base, factor, trained, slow, fast, amplitude;
+} relax_rope_scaling;
+size_t       relax_rope_scaled_bytes(const relax_rope_scaling *scaling, int32_t positions);      /* 0 for invalid arguments */
+relax_status relax_rope_table_scaled(const relax_rope_scaling *scaling, int32_t positions, float *table, relax_stream stream);
+
+/* q_out[i] = the heads of row i's q prepared as above, k_out[i] those of its k, at the positions of the descriptor; fp16 [h,d] and [g,d] in rows
+ * of the given strides (elements, multiples of 8; 16-byte aligned).  q with q_out, or k with k_out, may be NULL; an output may be its
+ * input if the strides agree, else they do not overlap.  IEEE arithmetic: a NaN or an infinity stays in its head (in its pair, without a norm).
+ * A row whose position a device table puts outside [0, kv_capacity) is turned by the nearest one's angles and raises bit 2 of the flag.  Of dims the call
+ * uses what the paged calls use.  ws: relax_head_workspace_bytes(dims, B) bytes, 256-byte aligned (0 for invalid arguments).
+ * Errors: NULL, SHAPE, CAPACITY, WORKSPACE, UNSUPPORTED.                                                                         */
+size_t       relax_head_workspace_bytes(const relax_layer_dims *dims, int32_t B_max);
+relax_status relax_head_norm_rope(const uint16_t *q, int64_t q_stride, const uint16_t *k, int64_t k_stride, uint16_t *q_out, int64_t q_out_stride,
+                                  uint16_t *k_out, int64_t k_out_stride, const relax_head_prep *prep, const relax_seqs *seqs,
+                                  const relax_layer_dims *dims, int32_t n, void *ws, size_t ws_bytes, relax_stream stream);
+
+/* ---- Paged KV cache in 4 bits ------------------------------------------------------------------------------------------------
+ * relax_paged_cache with half its bytes: pages, blocks of RELAX_PAGED_BLOCK tokens, page table and descriptor are the same.  Every RELAX_PAGED4_GROUP elements of a token and
+ * KV head have a scale of their own and codes u in 0..15 that stand for (u - 8) * scale:
+ *   scale = round8(x* / -8), x* the element of the largest magnitude (the positive one of two), round8 to eight significant bits, at most 8160 in size
+ *   u     = 8 + round(x / scale), kept in 0..15 (8 where the scale is 0)
+ * Eight bits times a code is exact in fp16, so no call rounds what the cache holds, and tokens share nothing, so an append touches no other token.
+ * 32 bits, four bytes b, of a block of one KV head hold
+ *   k  word [e / 8 % 4][t][e / 32]:          element e % 8 = 4 (b % 2) + b / 2 in the low half of byte b, that + 2 in its high half
+ *   v  word [t / 4][e % 16][e / 32]:         token t % 4 = 2 (b % 2) + b / 2 in byte b; e / 16 % 2 = 0 in its low half, 1 in its high half
+ *   scales at  [page][head][block][t / 4][e / 32][t % 4], fp16
+ * (fragments of the matrix products that read them).  Codes and scales behind a sequence's last token, blocks without a page and lengths beyond the capacity: as relax_paged_cache.
+ * An element that is infinite counts as +-65504 and a NaN as 0, in front of norm and rotation; values beyond 65280 are held as 65280 or, where the scale's sign
+ * gives them code 15, as 57120; a group whose largest magnitude is below 2^-22 is held as zeros.                                  */
+#define RELAX_PAGED4_GROUP 32
+typedef struct {
+    uint8_t *k, *v;                   /* codes, [n_pages][g][page_size / 16][8 * d] bytes each, 16-byte aligned                    */
+    uint16_t *k_scale, *v_scale;      /* fp16 [n_pages][g][page_size / 16][d / 2], 16-byte aligned                                 */
+    const int32_t *pages;             /* [kv_slots][pages_per_slot]                                                               */
+    int32_t n_pages;                  /* n_pages * g * page_size / 16 < 2^31                                                      */
+    int32_t page_size;                /* 16, 32, 64, 128 or 256 tokens                                                            */
+    int32_t pages_per_slot;           /* kv_capacity <= pages_per_slot * page_size                                                */
+} relax_paged4_cache;
+
+/* As relax_paged_workspace_bytes, for the calls below. */
+size_t relax_paged4_workspace_bytes(const relax_layer_dims *dims, int32_t n_max, int32_t L_max, int32_t B_max);
+
+/* Puts the rows of a call into the cache: keys prepared as relax_head_norm_rope does (not rounded before they are quantised), values as they are, and
+ * q_out[i], fp16 [n,h,d], the prepared queries (q and q_out NULL: only k and v; q_out may be q if q_stride is h d).  prep NULL: neither norm nor rotation.
+ * Arguments, strides, workspace and errors as relax_paged_append and relax_head_norm_rope.                                        */
+relax_status relax_paged4_append(const uint16_t *q, int64_t q_stride, const uint16_t *k, const uint16_t *v, int64_t kv_stride, uint16_t *q_out,
+                                 const relax_head_prep *prep, const relax_paged4_cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims,
+                                 int32_t n, void *ws, size_t ws_bytes, relax_stream stream);
+
+/* relax_paged_attention over the 4-bit cache.  Scores, softmax and sums are fp32; the one rounding between what the cache holds and the result is that of the
+ * probabilities, or in rows of few (row, head) pairs of the probabilities times their values' scale, to fp16: 2^-11 of each, and below fp16's normal range
+ * 2^-26 of the largest probability (times the scale's code, at most 8).  A row that no token is left for is zeros.                 */
+relax_status relax_paged4_attention(const uint16_t *q, const relax_paged4_cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims,
+                                    uint16_t *out, int32_t n, void *ws, size_t ws_bytes, relax_stream stream);
+
+/* What the cache holds, exactly, as fp16: as relax_paged_read.  Blocks without a page give zeros and raise the flag.               */
+relax_status relax_paged4_read(const relax_paged4_cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims, uint16_t *k_out, uint16_t *v_out,
+                               int32_t n, void *ws, size_t ws_bytes, relax_stream stream);
+
 /* ---- Log probabilities of tokens ------------------------------------------------------------------------------------
  * What a serving program returns beside the picked token, or scores a given text with, from rows of logits (those of relax_model_step, or
  * of relax_half_matmul with the head on every row): with log p = x - log(sum e^x) per row

@@ -69,6 +69,21 @@ class PagedCacheC(C.Structure):
                 ("rope", C.c_void_p), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("pages_per_slot", C.c_int32)]
 
 
+class Paged4CacheC(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("pages", C.c_void_p),
+                ("n_pages", C.c_int32), ("page_size", C.c_int32), ("pages_per_slot", C.c_int32)]
+
+
+class HeadPrepC(C.Structure):
+    _fields_ = [("q_norm", C.c_void_p), ("k_norm", C.c_void_p), ("eps", C.c_float), ("rope", C.c_void_p), ("rotary_dim", C.c_int32), ("layout", C.c_int32)]
+
+
+class RopeScaling(C.Structure):
+    """relax_rope_scaling; amplitude 0 reads as 1."""
+    _fields_ = [("scaling", C.c_int32), ("rotary_dim", C.c_int32), ("base", C.c_double), ("factor", C.c_double), ("trained", C.c_double),
+                ("slow", C.c_double), ("fast", C.c_double), ("amplitude", C.c_double)]
+
+
 class PlanEntryC(C.Structure):
     _fields_ = [("name", C.c_char * 24), ("first_op", C.c_int32), ("last_op", C.c_int32), ("storage", C.c_int32), ("pinned", C.c_int32),
                 ("offset", C.c_uint64), ("bytes", C.c_uint64), ("storage_bytes", C.c_uint64)]
@@ -84,6 +99,9 @@ class MatmulPlanC(C.Structure):
 
 
 RELAX_PAGED_BLOCK = 16
+RELAX_PAGED4_GROUP = 32
+ROPE_HALVES, ROPE_PAIRS = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_INDEX_RAMP, ROPE_WAVELENGTH_RAMP = range(4)
 KERNEL_MATVEC, KERNEL_STREAM, KERNEL_SPLIT_K, KERNEL_TILED = range(4)
 
 _lib = None
@@ -133,6 +151,18 @@ _SIGNATURES = {
                                           C.c_size_t, C.c_void_p]),
     "relax_paged_read": (C.c_int32, [C.POINTER(PagedCacheC), C.POINTER(SeqsC), C.POINTER(LayerDims), C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p,
                                      C.c_size_t, C.c_void_p]),
+    "relax_rope_scaled_bytes": (C.c_size_t, [C.POINTER(RopeScaling), C.c_int32]),
+    "relax_rope_table_scaled": (C.c_int32, [C.POINTER(RopeScaling), C.c_int32, C.c_void_p, C.c_void_p]),
+    "relax_head_workspace_bytes": (C.c_size_t, [C.POINTER(LayerDims), C.c_int32]),
+    "relax_head_norm_rope": (C.c_int32, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.POINTER(HeadPrepC),
+                                         C.POINTER(SeqsC), C.POINTER(LayerDims), C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "relax_paged4_workspace_bytes": (C.c_size_t, [C.POINTER(LayerDims), C.c_int32, C.c_int32, C.c_int32]),
+    "relax_paged4_append": (C.c_int32, [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.POINTER(HeadPrepC), C.POINTER(Paged4CacheC),
+                                        C.POINTER(SeqsC), C.POINTER(LayerDims), C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]),
+    "relax_paged4_attention": (C.c_int32, [C.c_void_p, C.POINTER(Paged4CacheC), C.POINTER(SeqsC), C.POINTER(LayerDims), C.c_void_p, C.c_int32, C.c_void_p,
+                                           C.c_size_t, C.c_void_p]),
+    "relax_paged4_read": (C.c_int32, [C.POINTER(Paged4CacheC), C.POINTER(SeqsC), C.POINTER(LayerDims), C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p,
+                                      C.c_size_t, C.c_void_p]),
     "relax_token_logprobs_workspace_bytes": (C.c_size_t, [C.c_int32, C.c_int32, C.c_int32]),
     "relax_token_logprobs": (C.c_int32, [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
                                          C.c_void_p, C.c_size_t, C.c_void_p]),
@@ -272,6 +302,30 @@ class PagedCache:
         return self._c
 
 
+class Paged4Cache:
+    """relax_paged4_cache: codes k, v uint8 and scales k_scale, v_scale fp16 of the pool and the page table int32 [kv_slots, pages_per_slot], all on the
+    device.  The C struct is made once; the tensors are kept alive with it."""
+
+    def __init__(self, k: Ptr, v: Ptr, k_scale: Ptr, v_scale: Ptr, pages: Ptr, n_pages: int, page_size: int, pages_per_slot: int):
+        self._keep = (k, v, k_scale, v_scale, pages)
+        self._c = Paged4CacheC(*map(_ptr, self._keep), n_pages, page_size, pages_per_slot)
+
+    def c(self) -> Paged4CacheC:
+        return self._c
+
+
+class HeadPrep:
+    """relax_head_prep: norm weights fp16 [d] or None, the rotary table fp32 [kv_capacity, rotary_dim / 2, 2] or None.  Made once per layer; the tensors are kept
+    alive with it."""
+
+    def __init__(self, q_norm: Ptr = None, k_norm: Ptr = None, eps: float = 1e-6, rope: Ptr = None, rotary_dim: int = 0, layout: int = ROPE_HALVES):
+        self._keep = (q_norm, k_norm, rope)
+        self._c = HeadPrepC(_ptr(q_norm), _ptr(k_norm), eps, _ptr(rope), rotary_dim, layout)
+
+    def c(self) -> HeadPrepC:
+        return self._c
+
+
 class Seqs:
     """Host-side ragged descriptor; kv_lens are lengths AFTER this call's rows are appended.  device_table: optional
     device int32 [4][B] (q_start, q_len, kv_len, slot) that the kernels read instead; kv_lens are then upper bounds."""
@@ -390,6 +444,55 @@ def relax_paged_read(cache: Optional[PagedCache], seqs: Optional[Seqs], dims: Op
     cc = None if cache is None else cache.c()
     sc = None if seqs is None else seqs.c()
     return lib().relax_paged_read(_ref(cc), _ref(sc), _ref(dims), _ptr(k_out), _ptr(v_out), n, _ptr(ws), ws_bytes, _stream(stream))
+
+
+def relax_rope_scaled_bytes(scaling: Optional[RopeScaling], positions: int) -> int:
+    return int(lib().relax_rope_scaled_bytes(_ref(scaling), positions))
+
+
+def relax_rope_table_scaled(scaling: Optional[RopeScaling], positions: int, table: Ptr, stream=None) -> int:
+    return lib().relax_rope_table_scaled(_ref(scaling), positions, _ptr(table), _stream(stream))
+
+
+def relax_head_workspace_bytes(dims: Optional[LayerDims], B_max: int) -> int:
+    return int(lib().relax_head_workspace_bytes(_ref(dims), B_max))
+
+
+def relax_head_norm_rope(q: Ptr, q_stride: int, k: Ptr, k_stride: int, q_out: Ptr, q_out_stride: int, k_out: Ptr, k_out_stride: int, prep: Optional[HeadPrep],
+                         seqs: Optional[Seqs], dims: Optional[LayerDims], n: int, ws: Ptr, ws_bytes: int, stream=None) -> int:
+    """q and k may be parts of one matrix: their addresses as integers, the strides in elements."""
+    pc = None if prep is None else prep.c()
+    sc = None if seqs is None else seqs.c()
+    return lib().relax_head_norm_rope(_ptr(q), q_stride, _ptr(k), k_stride, _ptr(q_out), q_out_stride, _ptr(k_out), k_out_stride, _ref(pc), _ref(sc), _ref(dims), n,
+                                      _ptr(ws), ws_bytes, _stream(stream))
+
+
+def relax_paged4_workspace_bytes(dims: Optional[LayerDims], n_max: int, L_max: int, B_max: int) -> int:
+    return int(lib().relax_paged4_workspace_bytes(_ref(dims), n_max, L_max, B_max))
+
+
+def relax_paged4_append(q: Ptr, q_stride: int, k: Ptr, v: Ptr, kv_stride: int, q_out: Ptr, prep: Optional[HeadPrep], cache: Optional[Paged4Cache],
+                        seqs: Optional[Seqs], dims: Optional[LayerDims], n: int, ws: Ptr, ws_bytes: int, stream=None) -> int:
+    """q, k, v may be parts of one matrix: their addresses as integers, the strides in elements."""
+    pc = None if prep is None else prep.c()
+    cc = None if cache is None else cache.c()
+    sc = None if seqs is None else seqs.c()
+    return lib().relax_paged4_append(_ptr(q), q_stride, _ptr(k), _ptr(v), kv_stride, _ptr(q_out), _ref(pc), _ref(cc), _ref(sc), _ref(dims), n, _ptr(ws), ws_bytes,
+                                     _stream(stream))
+
+
+def relax_paged4_attention(q: Ptr, cache: Optional[Paged4Cache], seqs: Optional[Seqs], dims: Optional[LayerDims], out: Ptr, n: int, ws: Ptr, ws_bytes: int,
+                           stream=None) -> int:
+    cc = None if cache is None else cache.c()
+    sc = None if seqs is None else seqs.c()
+    return lib().relax_paged4_attention(_ptr(q), _ref(cc), _ref(sc), _ref(dims), _ptr(out), n, _ptr(ws), ws_bytes, _stream(stream))
+
+
+def relax_paged4_read(cache: Optional[Paged4Cache], seqs: Optional[Seqs], dims: Optional[LayerDims], k_out: Ptr, v_out: Ptr, n: int, ws: Ptr, ws_bytes: int,
+                      stream=None) -> int:
+    cc = None if cache is None else cache.c()
+    sc = None if seqs is None else seqs.c()
+    return lib().relax_paged4_read(_ref(cc), _ref(sc), _ref(dims), _ptr(k_out), _ptr(v_out), n, _ptr(ws), ws_bytes, _stream(stream))
 
 
 def relax_token_logprobs_workspace_bytes(n_max: int, vocab: int, top: int) -> int:

@@ -2,9 +2,12 @@
 // the workspace plan, and the launch sequence of each exported call.  See include/relax_mi355.h
 // for the contract and for the passages of the paper each rule comes from.
 #include <atomic>
+#include <cmath>
 #include <cstring>
 #include <mutex>
 
+#include "heads_device.h"
+#include "paged4_device.h"
 #include "paged_device.h"
 #include "relax_common.h"
 
@@ -1416,17 +1419,47 @@ constexpr int32_t kMaxVocab = 1 << 30;       // logits of a row: places in it ar
 constexpr int32_t kMaxPagedSeqs = 65535;     // a workgroup finds its sequence 64 at a time
 constexpr int32_t kMaxPagedCapacity = 1 << 30;       // positions are 32-bit numbers, also rounded up to a split and added to one
 
+// The kernels' form of a descriptor that build_seqs has accepted: in the arguments, the caller's table, or one in the workspace
+relax_status paged_seqs(const relax_seqs *seqs, SeqTable &checked, bool need_table, int32_t n, void *ws, size_t table, hipStream_t stream, PagedSeqs &st, int &items)
+{
+    const bool inlined = !seqs->device_table && seqs->B <= kPagedInline;
+    st.B = seqs->B, st.n = n, st.q_max = checked.q_max, st.dev = seqs->device_table, st.pad = 0;
+    items = 0;
+    int32_t start = 0;
+    for (int b = 0; b < seqs->B; ++b) {
+        items += paged_blocks_of(seqs->q_lens[b]);
+        if (inlined) st.q_start[b] = start, st.q_len[b] = seqs->q_lens[b], st.kv_len[b] = seqs->kv_lens[b], st.slot[b] = seqs->slots ? seqs->slots[b] : b;
+        start += seqs->q_lens[b];
+    }
+    if (inlined || seqs->device_table) return RELAX_OK;
+    WsPlan front = {};
+    front.table = table;
+    const relax_status rc = upload_table(checked, seqs, need_table, ws, front, stream);
+    st.dev = checked.dev;
+    return rc;
+}
+
+bool scales_aligned(const relax_paged_cache *c) { return aligned(c->k_scale, 4) && aligned(c->v_scale, 4) && aligned(c->rope, 16); }
+bool scales_aligned(const relax_paged4_cache *c) { return aligned(c->k_scale, 16) && aligned(c->v_scale, 16); }
+PagedArgs paged_args(const relax_paged_cache *c, const relax_layer_dims *dims, void *ws, int shift)
+{
+    return {c->k, c->v, c->k_scale, c->v_scale, c->pages, c->rope, static_cast<uint32_t *>(ws), c->n_pages, c->pages_per_slot, dims->kv_slots, dims->kv_capacity, shift};
+}
+Paged4Args paged_args(const relax_paged4_cache *c, const relax_layer_dims *dims, void *ws, int shift)
+{
+    return {c->k, c->v, c->k_scale, c->v_scale, c->pages, static_cast<uint32_t *>(ws), c->n_pages, c->pages_per_slot, dims->kv_slots, dims->kv_capacity, shift};
+}
+
 // Everything the paged calls check alike; fills the kernels' descriptors.  items: see launch_paged_append.
-relax_status paged_begin(const relax_paged_cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims, int32_t n, void *ws, size_t ws_bytes,
-                         hipStream_t stream, PagedArgs &pa, PagedSeqs &st, int32_t &L_max, int &items, float **partials)
+template <typename Cache, typename Args>
+relax_status paged_begin(const Cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims, int32_t n, void *ws, size_t ws_bytes,
+                         hipStream_t stream, Args &pa, PagedSeqs &st, int32_t &L_max, int &items, float **partials)
 {
     relax_status rc = check_dims(dims);
     if (rc != RELAX_OK) return rc;
     if (!cache || !cache->k || !cache->v || !cache->k_scale || !cache->v_scale || !cache->pages || !ws) return RELAX_ERR_NULL;
     if (cache->n_pages < 1 || cache->pages_per_slot < 1) return RELAX_ERR_SHAPE;
-    if (!aligned(cache->k, 16) || !aligned(cache->v, 16) || !aligned(cache->k_scale, 4) || !aligned(cache->v_scale, 4) || !aligned(cache->pages, 4) ||
-        !aligned(cache->rope, 16))
-        return RELAX_ERR_SHAPE;
+    if (!aligned(cache->k, 16) || !aligned(cache->v, 16) || !scales_aligned(cache) || !aligned(cache->pages, 4)) return RELAX_ERR_SHAPE;
     int shift = 0;
     while (shift < 4 && (RELAX_PAGED_BLOCK << shift) != cache->page_size) ++shift;
     if ((RELAX_PAGED_BLOCK << shift) != cache->page_size) return RELAX_ERR_UNSUPPORTED;
@@ -1440,26 +1473,43 @@ relax_status paged_begin(const relax_paged_cache *cache, const relax_seqs *seqs,
     const PagedWs pl = paged_ws(*dims, n, L_max, seqs->B);
     if (ws_bytes < pl.total || !aligned(ws, 256)) return RELAX_ERR_WORKSPACE;
     if (dims->kv_capacity > kMaxPagedCapacity) return RELAX_ERR_UNSUPPORTED;
-    const bool inlined = !seqs->device_table && seqs->B <= kPagedInline;
-    st.B = seqs->B, st.n = n, st.q_max = checked.q_max, st.dev = seqs->device_table, st.pad = 0;
-    items = 0;
-    int32_t start = 0;
-    for (int b = 0; b < seqs->B; ++b) {
-        items += paged_blocks_of(seqs->q_lens[b]);
-        if (inlined) st.q_start[b] = start, st.q_len[b] = seqs->q_lens[b], st.kv_len[b] = seqs->kv_lens[b], st.slot[b] = seqs->slots ? seqs->slots[b] : b;
-        start += seqs->q_lens[b];
-    }
-    pa = {cache->k, cache->v, cache->k_scale, cache->v_scale, cache->pages, cache->rope, static_cast<uint32_t *>(ws), cache->n_pages, cache->pages_per_slot,
-          dims->kv_slots, dims->kv_capacity, shift};
+    pa = paged_args(cache, dims, ws, shift);
     *partials = reinterpret_cast<float *>(static_cast<char *>(ws) + pl.partials);
-    if (!inlined && !seqs->device_table) {
-        WsPlan front = {};
-        front.table = pl.table;
-        rc = upload_table(checked, seqs, need_table, ws, front, stream);
-        st.dev = checked.dev;
-    }
-    return rc;
+    return paged_seqs(seqs, checked, need_table, n, ws, pl.table, stream, st, items);
 }
+
+// relax_head_prep as the kernels take it (nullptr: neither norm nor rotation)
+relax_status head_prep(const relax_head_prep *prep, const relax_layer_dims &dm, HeadPrep &p)
+{
+    p = {nullptr, nullptr, nullptr, 0.0f, 0, 0};
+    if (!prep) return RELAX_OK;
+    if (!aligned(prep->q_norm, 16) || !aligned(prep->k_norm, 16) || !aligned(prep->rope, 16)) return RELAX_ERR_SHAPE;
+    if ((prep->q_norm || prep->k_norm) && !(prep->eps >= 0.0f && std::isfinite(prep->eps))) return RELAX_ERR_SHAPE;
+    if (prep->rope) {
+        const int32_t rot = prep->rotary_dim == 0 ? dm.head_dim : prep->rotary_dim;
+        if (rot < 0 || rot > dm.head_dim || rot % 16 != 0 || (prep->layout != RELAX_ROPE_HALVES && prep->layout != RELAX_ROPE_PAIRS)) return RELAX_ERR_UNSUPPORTED;
+        p.rot = rot, p.pairs = prep->layout == RELAX_ROPE_PAIRS;
+    }
+    p.q_norm = prep->q_norm, p.k_norm = prep->k_norm, p.rope = prep->rope, p.eps = prep->eps;
+    return RELAX_OK;
+}
+
+relax_status check_scaling(const relax_rope_scaling *sc, int32_t positions)
+{
+    if (!sc) return RELAX_ERR_NULL;
+    if (positions < 1 || sc->rotary_dim < 1) return RELAX_ERR_SHAPE;
+    if (sc->scaling < RELAX_ROPE_PLAIN || sc->scaling > RELAX_ROPE_WAVELENGTH_RAMP || positions > kMaxPagedCapacity || sc->rotary_dim > 256 || sc->rotary_dim % 2 != 0)
+        return RELAX_ERR_UNSUPPORTED;
+    if (!std::isfinite(sc->base) || !(sc->base > 1.0) || !std::isfinite(sc->amplitude)) return RELAX_ERR_SHAPE;
+    if (sc->scaling != RELAX_ROPE_PLAIN && (!std::isfinite(sc->factor) || !(sc->factor > 0.0))) return RELAX_ERR_SHAPE;
+    if (sc->scaling >= RELAX_ROPE_INDEX_RAMP &&
+        (!std::isfinite(sc->trained) || !std::isfinite(sc->fast) || !(sc->trained >= 1.0) || !(sc->slow > 0.0) || !(sc->fast > sc->slow)))
+        return RELAX_ERR_SHAPE;
+    return RELAX_OK;
+}
+
+// rows [heads, d] of a strided matrix: 16-byte packets, at least the heads' width apart
+bool rows_fit(int64_t stride, int32_t heads, int32_t d) { return stride % 8 == 0 && stride >= (int64_t)heads * d; }
 
 }  // namespace
 
@@ -1522,6 +1572,120 @@ relax_status relax_paged_read(const relax_paged_cache *cache, const relax_seqs *
     const relax_status rc = paged_begin(cache, seqs, dims, n, ws, ws_bytes, st_, pa, st, L_max, items, &partials);
     if (rc != RELAX_OK) return rc;
     return hip_status(launch_paged_read(pa, k_out, v_out, *dims, st, items, st_));
+}
+
+size_t relax_rope_scaled_bytes(const relax_rope_scaling *scaling, int32_t positions)
+{
+    return check_scaling(scaling, positions) != RELAX_OK ? 0 : sizeof(float) * (size_t)positions * (size_t)scaling->rotary_dim;
+}
+
+relax_status relax_rope_table_scaled(const relax_rope_scaling *scaling, int32_t positions, float *table, relax_stream stream)
+{
+    const relax_status rc = check_scaling(scaling, positions);
+    if (rc != RELAX_OK) return rc;
+    if (!table) return RELAX_ERR_NULL;
+    if (!aligned(table, 16)) return RELAX_ERR_SHAPE;
+    return hip_status(launch_rope_scaled(*scaling, positions, table, static_cast<hipStream_t>(stream)));
+}
+
+size_t relax_head_workspace_bytes(const relax_layer_dims *dims, int32_t B_max)
+{
+    if (check_dims(dims) != RELAX_OK || B_max < 1) return 0;
+    return kWsFlagBytes + align256(sizeof(int32_t) * 4 * (size_t)B_max);
+}
+
+relax_status relax_head_norm_rope(const uint16_t *q, int64_t q_stride, const uint16_t *k, int64_t k_stride, uint16_t *q_out, int64_t q_out_stride, uint16_t *k_out,
+                                  int64_t k_out_stride, const relax_head_prep *prep, const relax_seqs *seqs, const relax_layer_dims *dims, int32_t n, void *ws,
+                                  size_t ws_bytes, relax_stream stream)
+{
+    if (!q != !q_out || !k != !k_out || (!q && !k) || !prep || !ws) return RELAX_ERR_NULL;
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(q_out, 16) || !aligned(k_out, 16)) return RELAX_ERR_SHAPE;
+    relax_status rc = check_dims(dims);
+    if (rc != RELAX_OK) return rc;
+    if (q && (!rows_fit(q_stride, dims->n_heads, dims->head_dim) || !rows_fit(q_out_stride, dims->n_heads, dims->head_dim))) return RELAX_ERR_SHAPE;
+    if (k && (!rows_fit(k_stride, dims->n_kv_heads, dims->head_dim) || !rows_fit(k_out_stride, dims->n_kv_heads, dims->head_dim))) return RELAX_ERR_SHAPE;
+    if (n > 1 && ((q && q == q_out && q_stride != q_out_stride) || (k && k == k_out && k_stride != k_out_stride))) return RELAX_ERR_SHAPE;
+    HeadPrep p;
+    rc = head_prep(prep, *dims, p);
+    if (rc != RELAX_OK) return rc;
+    SeqTable checked = {};
+    bool need_table = false;
+    int32_t L_max = 0;
+    rc = build_seqs(seqs, *dims, n, checked, L_max, need_table);
+    if (rc != RELAX_OK) return rc;
+    if (seqs->B > kMaxPagedSeqs) return RELAX_ERR_UNSUPPORTED;
+    if (ws_bytes < relax_head_workspace_bytes(dims, seqs->B) || !aligned(ws, 256)) return RELAX_ERR_WORKSPACE;
+    if (dims->kv_capacity > kMaxPagedCapacity) return RELAX_ERR_UNSUPPORTED;
+    hipStream_t st_ = static_cast<hipStream_t>(stream);
+    PagedSeqs st;
+    int items = 0;
+    rc = paged_seqs(seqs, checked, need_table, n, ws, kWsFlagBytes, st_, st, items);
+    if (rc != RELAX_OK) return rc;
+    const HeadRows r = {q, k, q_out, k_out, q_stride, k_stride, q_out_stride, k_out_stride};
+    return hip_status(launch_head_norm_rope(r, p, *dims, st, static_cast<uint32_t *>(ws), st_));
+}
+
+size_t relax_paged4_workspace_bytes(const relax_layer_dims *dims, int32_t n_max, int32_t L_max, int32_t B_max)
+{
+    return relax_paged_workspace_bytes(dims, n_max, L_max, B_max);
+}
+
+relax_status relax_paged4_append(const uint16_t *q, int64_t q_stride, const uint16_t *k, const uint16_t *v, int64_t kv_stride, uint16_t *q_out,
+                                 const relax_head_prep *prep, const relax_paged4_cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims, int32_t n,
+                                 void *ws, size_t ws_bytes, relax_stream stream)
+{
+    if (!k || !v || !q != !q_out) return RELAX_ERR_NULL;
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(q_out, 16)) return RELAX_ERR_SHAPE;
+    relax_status rc = check_dims(dims);
+    if (rc != RELAX_OK) return rc;
+    const int64_t width = (int64_t)dims->n_heads * dims->head_dim;
+    if (!rows_fit(kv_stride, dims->n_kv_heads, dims->head_dim) || (q && !rows_fit(q_stride, dims->n_heads, dims->head_dim))) return RELAX_ERR_SHAPE;
+    if (q && q == q_out && n > 1 && q_stride != width) return RELAX_ERR_SHAPE;      // row i would overwrite what row j has not read
+    HeadPrep p;
+    rc = head_prep(prep, *dims, p);
+    if (rc != RELAX_OK) return rc;
+    hipStream_t st_ = static_cast<hipStream_t>(stream);
+    Paged4Args pa;
+    PagedSeqs st;
+    int32_t L_max = 0;
+    int items = 0;
+    float *partials = nullptr;
+    rc = paged_begin(cache, seqs, dims, n, ws, ws_bytes, st_, pa, st, L_max, items, &partials);
+    if (rc != RELAX_OK) return rc;
+    const HeadRows hr = {q, nullptr, q_out, nullptr, q_stride, 0, width, 0};
+    return hip_status(launch_paged4_append(hr, k, v, kv_stride, p, pa, *dims, st, *seqs, st_));
+}
+
+relax_status relax_paged4_attention(const uint16_t *q, const relax_paged4_cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims, uint16_t *out,
+                                    int32_t n, void *ws, size_t ws_bytes, relax_stream stream)
+{
+    if (!q || !out) return RELAX_ERR_NULL;
+    if (!aligned(q, 16) || !aligned(out, 16)) return RELAX_ERR_SHAPE;
+    hipStream_t st_ = static_cast<hipStream_t>(stream);
+    Paged4Args pa;
+    PagedSeqs st;
+    int32_t L_max = 0;
+    int items = 0;
+    float *partials = nullptr;
+    const relax_status rc = paged_begin(cache, seqs, dims, n, ws, ws_bytes, st_, pa, st, L_max, items, &partials);
+    if (rc != RELAX_OK) return rc;
+    return hip_status(launch_paged4_attention(q, pa, *dims, st, *seqs, L_max, out, partials, st_));
+}
+
+relax_status relax_paged4_read(const relax_paged4_cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims, uint16_t *k_out, uint16_t *v_out,
+                               int32_t n, void *ws, size_t ws_bytes, relax_stream stream)
+{
+    if (!k_out && !v_out) return RELAX_ERR_NULL;
+    if (!aligned(k_out, 16) || !aligned(v_out, 16)) return RELAX_ERR_SHAPE;
+    hipStream_t st_ = static_cast<hipStream_t>(stream);
+    Paged4Args pa;
+    PagedSeqs st;
+    int32_t L_max = 0;
+    int items = 0;
+    float *partials = nullptr;
+    const relax_status rc = paged_begin(cache, seqs, dims, n, ws, ws_bytes, st_, pa, st, L_max, items, &partials);
+    if (rc != RELAX_OK) return rc;
+    return hip_status(launch_paged4_read(pa, k_out, v_out, *dims, st, items, st_));
 }
 
 size_t relax_token_logprobs_workspace_bytes(int32_t n_max, int32_t vocab, int32_t top)

@@ -272,13 +272,6 @@ constexpr int kUnsplit = 256, kPagedGroups = 768, kPartials = 65536;
 // 600 rows on 500 tokens of 16 / 2 heads of 64 (38) 14.5 / 24.
 constexpr int kRowTiles = 160;
 
-struct Plan {
-    int32_t least;                   // pairs from which a sequence is the other kernel's
-    int32_t row_items, items;        // tiles of 256 and of 16 pairs that are launched
-    int32_t row_per_seq, per_seq;    // as tile_of takes them
-    int32_t chunk, splits, waves;    // wavefronts per workgroup of 16-pair tiles
-};
-
 // Tiles are searched for where a fixed number per sequence would launch more than twice as many (us: 300 rows on 1201 tokens beside 20 decode rows of 32 / 32 heads,
 // 39 tiles per KV head numbered as 399, 46.8; searched for, 42.0)
 void numbering(long long all, long long most, int32_t B, int32_t &items, int32_t &per_seq)
@@ -288,15 +281,31 @@ void numbering(long long all, long long most, int32_t B, int32_t &items, int32_t
     per_seq = (int32_t)(search ? 0 : most);
 }
 
-Plan plan(const relax_layer_dims &dm, const relax_seqs &sq, int32_t n, int32_t L_max)
+template <int D>
+hipError_t launch_d(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, const PagedPlan &pl, uint16_t *out, float *partials,
+                    hipStream_t stream)
+{
+    if ((int64_t)pl.items * dm.n_kv_heads * 64 * pl.waves > kMaxThreads) return hipErrorInvalidValue;
+    const dim3 grid(pl.items * dm.n_kv_heads, pl.splits);
+    if (pl.waves == 8)
+        hipLaunchKernelGGL((attn_paged_kernel<D, 8>), grid, dim3(512), 0, stream, st, q, pa, partials, out, dm.n_heads, dm.n_kv_heads, pl.per_seq, pl.chunk, pl.splits, pl.least);
+    else
+        hipLaunchKernelGGL((attn_paged_kernel<D, 4>), grid, dim3(256), 0, stream, st, q, pa, partials, out, dm.n_heads, dm.n_kv_heads, pl.per_seq, pl.chunk, pl.splits, pl.least);
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess || pl.splits == 1 ? e : launch_paged_merge(pl, partials, out, dm, pa.cap, st, stream);
+}
+
+}  // namespace
+
+PagedPlan paged_plan(const relax_layer_dims &dm, const relax_seqs &sq, int32_t n, int32_t L_max, bool rows)
 {
     const int rep = dm.n_heads / dm.n_kv_heads;
     auto pairs_of = [&](int b) { return (long long)sq.q_lens[b] * rep; };
     long long large = 0;
     for (int b = 0; b < sq.B; ++b)
         if (pairs_of(b) >= kPagedRowTile) large += (pairs_of(b) + kPagedRowTile - 1) / kPagedRowTile;
-    Plan p;
-    p.least = large * dm.n_kv_heads >= kRowTiles ? kPagedRowTile : INT32_MAX;
+    PagedPlan p;
+    p.least = rows && large * dm.n_kv_heads >= kRowTiles ? kPagedRowTile : INT32_MAX;
     long long small = 0, most_small = 0, most_large = 0;
     for (int b = 0; b < sq.B; ++b) {
         const long long pairs = pairs_of(b);
@@ -316,27 +325,18 @@ Plan plan(const relax_layer_dims &dm, const relax_seqs &sq, int32_t n, int32_t L
     return p;
 }
 
-template <int D>
-hipError_t launch_d(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, const Plan &pl, uint16_t *out, float *partials,
-                    hipStream_t stream)
+hipError_t launch_paged_merge(const PagedPlan &pl, const float *partials, uint16_t *out, const relax_layer_dims &dm, int32_t cap, const PagedSeqs &st, hipStream_t stream)
 {
-    if ((int64_t)pl.items * dm.n_kv_heads * 64 * pl.waves > kMaxThreads) return hipErrorInvalidValue;
-    const dim3 grid(pl.items * dm.n_kv_heads, pl.splits);
-    if (pl.waves == 8)
-        hipLaunchKernelGGL((attn_paged_kernel<D, 8>), grid, dim3(512), 0, stream, st, q, pa, partials, out, dm.n_heads, dm.n_kv_heads, pl.per_seq, pl.chunk, pl.splits, pl.least);
+    const int threads = pl.splits > 4 * 64 / (dm.head_dim / 4) ? 256 : 64;      // one round of four splits per group of threads, if that is enough
+    const dim3 grid(st.n * dm.n_heads);
+    if (dm.head_dim == 128)
+        hipLaunchKernelGGL(attn_paged_merge_kernel<128>, grid, dim3(threads), 0, stream, st, partials, out, dm.n_heads, dm.n_kv_heads, cap, pl.chunk, pl.splits, pl.least);
     else
-        hipLaunchKernelGGL((attn_paged_kernel<D, 4>), grid, dim3(256), 0, stream, st, q, pa, partials, out, dm.n_heads, dm.n_kv_heads, pl.per_seq, pl.chunk, pl.splits, pl.least);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || pl.splits == 1) return e;
-    const int threads = pl.splits > 4 * 64 / (D / 4) ? 256 : 64;      // one round of four splits per group of threads, if that is enough
-    hipLaunchKernelGGL(attn_paged_merge_kernel<D>, dim3(st.n * dm.n_heads), dim3(threads), 0, stream, st, partials, out, dm.n_heads, dm.n_kv_heads, pa.cap,
-                       pl.chunk, pl.splits, pl.least);
+        hipLaunchKernelGGL(attn_paged_merge_kernel<64>, grid, dim3(threads), 0, stream, st, partials, out, dm.n_heads, dm.n_kv_heads, cap, pl.chunk, pl.splits, pl.least);
     return hipGetLastError();
 }
 
-}  // namespace
-
-// plan() has splits <= ceil(L / 128) and, where it has more than one, n * heads * splits <= kPartials
+// paged_plan() has splits <= ceil(L / 128) and, where it has more than one, n * heads * splits <= kPartials
 size_t paged_partial_floats(const relax_layer_dims &dm, int32_t n, int32_t L)
 {
     const size_t most = kPartials, mine = (size_t)n * dm.n_heads * (((size_t)L + 127) / 128);
@@ -346,7 +346,7 @@ size_t paged_partial_floats(const relax_layer_dims &dm, int32_t n, int32_t L)
 hipError_t launch_paged_attention(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, const relax_seqs &sq, int32_t L_max,
                                   uint16_t *out, float *partials, hipStream_t stream)
 {
-    const Plan pl = plan(dm, sq, st.n, L_max);
+    const PagedPlan pl = paged_plan(dm, sq, st.n, L_max);
     if (pl.row_items > 0) {
         const hipError_t e = launch_paged_rows(q, pa, dm, st, pl.row_items, pl.row_per_seq, pl.least, out, stream);
         if (e != hipSuccess || pl.items == 0) return e;

@@ -112,7 +112,8 @@ constexpr uint32_t kBadPage = 4u;    // bit 2 of the flag word: a block had no p
 
 // Number of a sequence's block `blk` in the pool for KV head kvh, -1 if its slot, its place in the slot's row of the page table or the page is
 // out of range: the table is device data, so what it says is checked here and not on the host.
-__device__ inline int paged_block(const PagedArgs &pa, int g, int kvh, int slot, int blk)
+template <typename Args>
+__device__ inline int paged_block(const Args &pa, int g, int kvh, int slot, int blk)
 {
     const int at = blk >> pa.shift;
     if ((unsigned)slot >= (unsigned)pa.slots || blk < 0 || at >= pa.per_slot) return -1;
@@ -120,6 +121,17 @@ __device__ inline int paged_block(const PagedArgs &pa, int g, int kvh, int slot,
     if ((unsigned)page >= (unsigned)pa.n_pages) return -1;
     return ((page * g + kvh) << pa.shift) + (blk & ((1 << pa.shift) - 1));
 }
+
+// How a paged attention call is cut (attn_paged.hip)
+struct PagedPlan {
+    int32_t least;                   // pairs from which a sequence is the other kernel's
+    int32_t row_items, items;        // tiles of 256 and of 16 pairs that are launched
+    int32_t row_per_seq, per_seq;    // as tile_of takes them
+    int32_t chunk, splits, waves;    // wavefronts per workgroup of 16-pair tiles
+};
+PagedPlan paged_plan(const relax_layer_dims &dm, const relax_seqs &sq, int32_t n, int32_t L_max, bool rows = true);      // rows: there are tiles of 256 pairs
+// out of the partial results [row][head][splits][d + 2] of the 16-pair tiles: d sums, the reference of the weights (log2), the sum of the weights
+hipError_t launch_paged_merge(const PagedPlan &pl, const float *partials, uint16_t *out, const relax_layer_dims &dm, int32_t cap, const PagedSeqs &st, hipStream_t stream);
 
 // Attention of the sequences with at least `least` (row, head) pairs, in `items` tiles of kPagedRowTile pairs (attn_paged_rows.hip)
 constexpr int kPagedRowTile = 256;

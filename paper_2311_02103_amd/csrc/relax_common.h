@@ -508,6 +508,20 @@ size_t paged_partial_floats(const relax_layer_dims &dm, int32_t n, int32_t L);
 hipError_t launch_paged_attention(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, const relax_seqs &sq, int32_t L_max,
                                   uint16_t *out, float *partials, hipStream_t stream);
 
+// Heads before attention (heads.hip, rope_scaled.hip; HeadRows, HeadPrep: heads_device.h)
+struct HeadRows;
+struct HeadPrep;
+hipError_t launch_head_norm_rope(const HeadRows &r, const HeadPrep &p, const relax_layer_dims &dm, const PagedSeqs &st, uint32_t *err, hipStream_t stream);
+hipError_t launch_rope_scaled(const relax_rope_scaling &sc, int32_t positions, float *table, hipStream_t stream);
+
+// Paged 4-bit KV cache (paged4_append.hip, attn_paged4.hip; Paged4Args: paged4_device.h).  hr: queries, q and q_out NULL for none
+struct Paged4Args;
+hipError_t launch_paged4_append(const HeadRows &hr, const uint16_t *k, const uint16_t *v, int64_t kv_stride, const HeadPrep &p, const Paged4Args &pa,
+                                const relax_layer_dims &dm, const PagedSeqs &st, const relax_seqs &sq, hipStream_t stream);
+hipError_t launch_paged4_read(const Paged4Args &pa, uint16_t *k_out, uint16_t *v_out, const relax_layer_dims &dm, const PagedSeqs &st, int items, hipStream_t stream);
+hipError_t launch_paged4_attention(const uint16_t *q, const Paged4Args &pa, const relax_layer_dims &dm, const PagedSeqs &st, const relax_seqs &sq, int32_t L_max,
+                                   uint16_t *out, float *partials, hipStream_t stream);
+
 // Log probabilities of rows of logits (token_logprobs.hip)
 hipError_t launch_token_logprobs(const uint16_t *logits, int64_t stride, const int32_t *targets, float *logprobs, float *entropy, int32_t *top_ids,
                                  float *top_logprobs, int32_t n, int32_t V, int32_t k, void *partials, hipStream_t stream);
