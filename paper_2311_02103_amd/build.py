@@ -33,7 +33,7 @@ NO_SCRATCH = {"gemv_q4_reg.hip": "gemv_q4_reg_kernel", "gemv_reg_f16.hip": "gemv
               "gemv_q3.hip": "gemv_q3", "fewrow_q4g32.hip": "fewrow_kernel", "fewrow_q4g64.hip": "fewrow_kernel",
               "fewrow_q4g128.hip": "fewrow_kernel", "fewrow_q3.hip": "fewrow_kernel", "fewrow_f16.hip": "fewrow_kernel", "attn_decode.hip": "attn_",
               "attn_paged.hip": "attn_paged", "attn_paged_rows.hip": "attn_paged", "paged_append.hip": "paged_",
-              "heads.hip": "head_norm_rope", "paged4_append.hip": "paged4_", "attn_paged4.hip": "attn_paged4"}
+              "heads.hip": "head_norm_rope", "paged4_append.hip": "paged4_", "attn_paged4.hip": "attn_paged4", "attn_paged4_rows.hip": "attn_paged4"}
 REMARK = "-Rpass-analysis=kernel-resource-usage"
 
 

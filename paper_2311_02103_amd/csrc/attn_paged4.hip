@@ -247,7 +247,11 @@ hipError_t launch_d(const uint16_t *q, const Paged4Args &pa, const relax_layer_d
 hipError_t launch_paged4_attention(const uint16_t *q, const Paged4Args &pa, const relax_layer_dims &dm, const PagedSeqs &st, const relax_seqs &sq, int32_t L_max,
                                    uint16_t *out, float *partials, hipStream_t stream)
 {
-    const PagedPlan pl = paged_plan(dm, sq, st.n, L_max, false);
+    const PagedPlan pl = paged_plan(dm, sq, st.n, L_max);
+    if (pl.row_items > 0) {
+        const hipError_t e = launch_paged4_rows(q, pa, dm, st, pl, out, stream);
+        if (e != hipSuccess || pl.items == 0) return e;
+    }
     return dm.head_dim == 128 ? launch_d<128>(q, pa, dm, st, pl, out, partials, stream) : launch_d<64>(q, pa, dm, st, pl, out, partials, stream);
 }
 

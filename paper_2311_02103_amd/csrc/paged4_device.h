@@ -25,6 +25,9 @@ struct Paged4Args {
     int32_t shift;                   // log2 of the blocks per page
 };
 
+// Attention of the sequences with at least pl.least (row, head) pairs, in tiles of kPagedRowTile pairs (attn_paged4_rows.hip)
+hipError_t launch_paged4_rows(const uint16_t *q, const Paged4Args &pa, const relax_layer_dims &dm, const PagedSeqs &st, const PagedPlan &pl, uint16_t *out, hipStream_t stream);
+
 // The eight codes of a word as fp16 numbers 0..15: the low halves of its bytes 0 .. 3, then the high ones
 __device__ __forceinline__ void word_codes(uint32_t w, half2p_t (&u)[4])
 {
