@@ -1,4 +1,5 @@
 // Rotary tables of scaled positions: table[p][t] = amplitude (cos, sin)(p f'_t), fp64 rounded to fp32 (frequencies: relax_rope_scaling in relax_mi355.h).
+#include <algorithm>
 #include <cmath>
 
 #include "heads_device.h"
@@ -7,15 +8,26 @@ namespace relax {
 
 namespace {
 
-// one thread per entry
-__global__ __launch_bounds__(256) void rope_scaled_kernel(float *table, RopeFrequency f, int64_t total, int half)
+constexpr int64_t kThreadsWanted = 1 << 17;
+
+// Thread i has pair i % half at positions i / half, + rows, + 2 rows ..: two sines and cosines, and a rotation by the angle of `rows` positions for each further entry (four multiply-adds in
+// 64 bits, off by 2^-52 each; a sine and cosine is some fifty instructions).
+__global__ __launch_bounds__(256) void rope_scaled_kernel(float *table, RopeFrequency f, int rows, int positions, int half)
 {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= total) return;
-    const int64_t p = i / half;
-    double s, c;
-    sincos((double)p * rope_frequency(f, (int)(i - p * half)), &s, &c);
-    ((float2 *)table)[i] = make_float2((float)(f.amplitude * c), (float)(f.amplitude * s));
+    if (i >= (int64_t)rows * half) return;
+    const int p0 = (int)(i / half), t = (int)(i - (int64_t)p0 * half);
+    const double w = rope_frequency(f, t);
+    double s, c, ds, dc;
+    sincos((double)p0 * w, &s, &c);
+    sincos((double)rows * w, &ds, &dc);
+    s *= f.amplitude, c *= f.amplitude;
+    float2 *dst = (float2 *)table + i;
+    for (int64_t p = p0; p < positions; p += rows, dst += (int64_t)rows * half) {
+        *dst = make_float2((float)c, (float)s);
+        const double turned = c * dc - s * ds;
+        s = c * ds + s * dc, c = turned;
+    }
 }
 
 }  // namespace
@@ -23,9 +35,12 @@ __global__ __launch_bounds__(256) void rope_scaled_kernel(float *table, RopeFreq
 hipError_t launch_rope_scaled(const relax_rope_scaling &sc, int32_t positions, float *table, hipStream_t stream)
 {
     const int half = sc.rotary_dim / 2;
+    // up to 16 entries per thread where that leaves kThreadsWanted of them
     const int64_t total = (int64_t)positions * half;
-    const RopeFrequency f = rope_frequencies(sc);
-    hipLaunchKernelGGL(rope_scaled_kernel, dim3((total + 255) / 256), dim3(256), 0, stream, table, f, total, half);
+    const int per = (int)std::min<int64_t>(16, std::max<int64_t>(1, total / kThreadsWanted)), rows = (positions + per - 1) / per;
+    const int64_t groups = ((int64_t)rows * half + 255) / 256;
+    if (groups * 256 > kMaxThreads) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(rope_scaled_kernel, dim3(groups), dim3(256), 0, stream, table, rope_frequencies(sc), rows, positions, half);
     return hipGetLastError();
 }
 
