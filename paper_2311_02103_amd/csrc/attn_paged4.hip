@@ -33,13 +33,14 @@ __device__ __forceinline__ float column_max(float v)
 }
 
 // grid: x = tile * g + KV head, y = split.  part: [row][head][splits][D + 2] when splits > 1.
-template <int D, int W>
-__global__ __launch_bounds__(64 * W, 2) void attn_paged4_kernel(PagedSeqs, const uint16_t *__restrict__ q, Paged4Args pa, float *__restrict__ part,
+template <int D, int W, bool FOLD>
+__global__ __launch_bounds__(64 * W, FOLD ? 3 : 2) void attn_paged4_kernel(PagedSeqs, const uint16_t *__restrict__ q, Paged4Args pa, float *__restrict__ part,
                                                              uint16_t *__restrict__ out, int h, int g, int per_seq, int chunk, int splits, int least)
 {
     constexpr int J = D / 32;                    // k steps, words of a lane per block, scales of a token
     constexpr int NT = D / 16;                   // 16-element tiles of O^T
     constexpr int P = D + 4;                     // pitch of a state in LDS
+    constexpr int SB = FOLD ? 1 : 2;             // blocks of a step whose scores a lane holds
     typedef uint32_t words_t __attribute__((ext_vector_type(J)));
     typedef _Float16 scales_t __attribute__((ext_vector_type(4 * J)));
     __shared__ __align__(16) float states[W * 16 * P];
@@ -70,7 +71,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_paged4_kernel(PagedSeqs, const
     const int w_begin = b_begin + wave * per, w_end = min(b_end, w_begin + per);
 
     // ---- queries: lane holds pair `col`; k step j takes elements 32 j + 8 quarter .. + 7, in the order of the codes ----
-    const int pair = p0 + min(col, n_pairs - 1), row = pair / rep, head = kvh * rep + pair - row * rep, pos = past + row;
+    const int pair = p0 + min(FOLD ? col & 7 : col, n_pairs - 1), row = pair / rep, head = kvh * rep + pair - row * rep, pos = past + row;
     half8p_t qf[J];
     float qs[J];                                 // -8 sum q of a step
     const float c = 1.44269504088896340736f / sqrtf((float)D);
@@ -103,50 +104,59 @@ __global__ __launch_bounds__(64 * W, 2) void attn_paged4_kernel(PagedSeqs, const
         }
         const int ns = (min(w_end - seg, kWave) + 1) >> 1;
         words_t kreg[2], vreg[2];                              // one step: two blocks
-        scales_t ks[2], vs[2];
-        auto load = [&](words_t (&reg)[2], scales_t (&sc)[2], const uint8_t *codes, const uint16_t *scales, int s) {
+        scales_t ks[SB], vs[SB];                               // (FOLD: of the lane's block)
+        auto load = [&](words_t (&reg)[2], scales_t (&sc)[SB], const uint8_t *codes, const uint16_t *scales, int s) __attribute__((always_inline)) {
+            size_t at[2];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const size_t at = max(__builtin_amdgcn_readlane(pool, min(2 * s + t, 63)), 0);       // no such block: any that can be read
-                reg[t] = stream_load((const words_t *)(codes + at * block4_codes(D)) + lane);
-                sc[t] = *((const scales_t *)(scales + at * block4_scales(D)) + quarter);
+                at[t] = max(__builtin_amdgcn_readlane(pool, min(2 * s + t, 63)), 0);       // no such block: any that can be read
+                reg[t] = stream_load((const words_t *)(codes + at[t] * block4_codes(D)) + lane);
             }
+#pragma unroll
+            for (int t = 0; t < SB; ++t) sc[t] = *((const scales_t *)(scales + (FOLD ? (col < 8 ? at[0] : at[1]) : at[t]) * block4_scales(D)) + quarter);
         };
         load(kreg, ks, pa.k, pa.k_scale, 0), load(vreg, vs, pa.v, pa.v_scale, 0);
         // a step's keys make room for the next one's as soon as the scores are there, its values when they are summed: one step is in flight all the time
         auto step = [&](int s, auto MORE) __attribute__((always_inline)) {
-            float x[8];
-            bool gone = false;                                 // uniform: some of the tokens are masked
-            float mx = -INFINITY;
+            float x[4 * SB];                                   // scores over c
+            float4p_t S[2][J];
+            const int t0 = (seg + 2 * s) * 16;                 // first token of the step
+            const bool there0 = __builtin_amdgcn_readlane(pool, min(2 * s, 63)) >= 0, there1 = __builtin_amdgcn_readlane(pool, min(2 * s + 1, 63)) >= 0;
+            const bool gone = !there0 || !there1 || t0 + 31 > pos_min;      // uniform: some of the tokens are masked
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                float4p_t S[J];
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
                     half2p_t p[4];
                     word_codes(kreg[t][j], p);
-                    S[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(p[0], p[1], p[2], p[3]), qf[j], float4p_t{qs[j], qs[j], qs[j], qs[j]}, 0, 0, 0);
+                    S[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(p[0], p[1], p[2], p[3]), qf[j], float4p_t{qs[j], qs[j], qs[j], qs[j]}, 0, 0, 0);
                 }
+#pragma unroll
+            for (int t = 0; t < SB; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    float sum = S[0][i] * (float)ks[t][i];
+                    const auto score = [&](int j) { return FOLD ? (col < 8 ? S[0][j][i] : S[1][j][i]) : S[t][j][i]; };
+                    float sum = score(0) * (float)ks[t][i];
 #pragma unroll
-                    for (int j = 1; j < J; ++j) sum = fmaf(S[j][i], (float)ks[t][4 * j + i], sum);
-                    x[4 * t + i] = sum * c;
+                    for (int j = 1; j < J; ++j) sum = fmaf(score(j), (float)ks[t][4 * j + i], sum);
+                    x[4 * t + i] = sum;
                 }
-                const bool there = __builtin_amdgcn_readlane(pool, min(2 * s + t, 63)) >= 0;
-                const int t0 = (seg + 2 * s + t) * 16;
-                if (!there || t0 + 15 > pos_min) {             // uniform
-                    gone = true;
+            if (gone) {
+#pragma unroll
+                for (int t = 0; t < SB; ++t) {
+                    const bool there = FOLD ? (col < 8 ? there0 : there1) : (t ? there1 : there0);
+                    const int first = t0 + 16 * (FOLD ? col >> 3 : t) + 4 * quarter;
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (!there || t0 + 4 * quarter + i > pos) x[4 * t + i] = -INFINITY;
+                        if (!there || first + i > pos) x[4 * t + i] = -INFINITY;
                 }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) mx = fmaxf(mx, x[4 * t + i]);
             }
+            float mx = x[0];
+#pragma unroll
+            for (int i = 1; i < 4 * SB; ++i) mx = fmaxf(mx, x[i]);
             if constexpr (MORE) load(kreg, ks, pa.k, pa.k_scale, s + 1);
-            mx = column_max(mx);
+            if constexpr (FOLD) mx = fmaxf(mx, lane_xor<8>(mx));
+            mx = column_max(mx) * c;
             const bool move = mx > m_run + kLag;               // the first visible tokens: m_run = -inf
             if (__any(move)) {
                 const float m_new = move ? mx : m_run, alpha = move ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.0f;
@@ -158,15 +168,15 @@ __global__ __launch_bounds__(64 * W, 2) void attn_paged4_kernel(PagedSeqs, const
                 for (int j = 0; j < J; ++j) off[j] *= alpha;
             }
             const float m_ref = m_run == -INFINITY ? 0.0f : m_run - kBias;      // nothing visible yet: every weight is exp2(-inf)
-            float w[8];
+            float w[4 * SB];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                w[i] = __builtin_amdgcn_exp2f(x[i] - m_ref);
+            for (int i = 0; i < 4 * SB; ++i) {
+                w[i] = __builtin_amdgcn_exp2f(fmaf(x[i], c, -m_ref));
                 l_run += w[i];
             }
             if (gone) {                                        // a scale behind the last token is anything
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                for (int t = 0; t < SB; ++t)
 #pragma unroll
                     for (int j = 0; j < J; ++j)
 #pragma unroll
@@ -174,11 +184,17 @@ __global__ __launch_bounds__(64 * W, 2) void attn_paged4_kernel(PagedSeqs, const
             }
 #pragma unroll
             for (int j = 0; j < J; ++j) {
-                half8p_t pf;
+                half2p_t pw[4];                                // the weights of both blocks, tokens 0 2 | 1 3
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
+                for (int t = 0; t < SB; ++t)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) pf[4 * t + (i & 1) * 2 + (i >> 1)] = (_Float16)(w[4 * t + i] * (float)vs[t][4 * j + i]);
+                    for (int i = 0; i < 2; ++i)
+                        pw[2 * t + i] = half2p_t{(_Float16)(w[4 * t + i] * (float)vs[t][4 * j + i]), (_Float16)(w[4 * t + i + 2] * (float)vs[t][4 * j + i + 2])};
+                if constexpr (FOLD) {                          // (columns from 8 on have the blocks the other way round, and no pair)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) pw[2 + i] = __builtin_bit_cast(half2p_t, lane_xor<8>(__builtin_bit_cast(float, pw[i])));
+                }
+                const half8p_t pf = operand(pw[0], pw[1], pw[2], pw[3]);
                 half2p_t a[4], e[4];
                 word_codes(vreg[0][j], a);
                 word_codes(vreg[1][j], e);
@@ -195,6 +211,7 @@ __global__ __launch_bounds__(64 * W, 2) void attn_paged4_kernel(PagedSeqs, const
     }
 
     // ---- the wavefronts' states meet in LDS ----
+    if constexpr (FOLD) l_run += lane_xor<8>(l_run);
     l_run = xor32_sum(xor16_sum(l_run));
 #pragma unroll
     for (int i = 0; i < NT; ++i)
@@ -229,15 +246,19 @@ __global__ __launch_bounds__(64 * W, 2) void attn_paged4_kernel(PagedSeqs, const
 }
 
 template <int D>
-hipError_t launch_d(const uint16_t *q, const Paged4Args &pa, const relax_layer_dims &dm, const PagedSeqs &st, const PagedPlan &pl, uint16_t *out, float *partials,
+hipError_t launch_d(const uint16_t *q, const Paged4Args &pa, const relax_layer_dims &dm, const PagedSeqs &st, const PagedPlan &pl, bool few, uint16_t *out, float *partials,
                     hipStream_t stream)
 {
     if ((int64_t)pl.items * dm.n_kv_heads * 64 * pl.waves > kMaxThreads) return hipErrorInvalidValue;
     const dim3 grid(pl.items * dm.n_kv_heads, pl.splits);
-    if (pl.waves == 8)
-        hipLaunchKernelGGL((attn_paged4_kernel<D, 8>), grid, dim3(512), 0, stream, st, q, pa, partials, out, dm.n_heads, dm.n_kv_heads, pl.per_seq, pl.chunk, pl.splits, pl.least);
-    else
-        hipLaunchKernelGGL((attn_paged4_kernel<D, 4>), grid, dim3(256), 0, stream, st, q, pa, partials, out, dm.n_heads, dm.n_kv_heads, pl.per_seq, pl.chunk, pl.splits, pl.least);
+    const auto launch = [&](auto W, auto FOLD) {
+        hipLaunchKernelGGL((attn_paged4_kernel<D, W, FOLD>), grid, dim3(64 * W), 0, stream, st, q, pa, partials, out, dm.n_heads, dm.n_kv_heads, pl.per_seq, pl.chunk, pl.splits,
+                           pl.least);
+    };
+    using four = std::integral_constant<int, 4>;
+    using eight = std::integral_constant<int, 8>;
+    if (pl.waves == 8) few ? launch(eight{}, std::true_type{}) : launch(eight{}, std::false_type{});
+    else few ? launch(four{}, std::true_type{}) : launch(four{}, std::false_type{});
     const hipError_t e = hipGetLastError();
     return e != hipSuccess || pl.splits == 1 ? e : launch_paged_merge(pl, partials, out, dm, pa.cap, st, stream);
 }
@@ -252,7 +273,8 @@ hipError_t launch_paged4_attention(const uint16_t *q, const Paged4Args &pa, cons
         const hipError_t e = launch_paged4_rows(q, pa, dm, st, pl, out, stream);
         if (e != hipSuccess || pl.items == 0) return e;
     }
-    return dm.head_dim == 128 ? launch_d<128>(q, pa, dm, st, pl, out, partials, stream) : launch_d<64>(q, pa, dm, st, pl, out, partials, stream);
+    const bool few = (int64_t)st.q_max * (dm.n_heads / dm.n_kv_heads) <= 8;
+    return dm.head_dim == 128 ? launch_d<128>(q, pa, dm, st, pl, few, out, partials, stream) : launch_d<64>(q, pa, dm, st, pl, few, out, partials, stream);
 }
 
 }  // namespace relax
