@@ -12,6 +12,7 @@
 // Values.  The weight of a token times its value scale, w s_j, is rounded to fp16 once per group of 32 elements and is the operand; -8 sum (w s_j), from one more product
 // per group, goes to the result.  Weights are exp2(score - reference + 1) with a reference that trails the maximum by at most 2: at most 8, and times 8160,
 // the largest scale, an fp16 number.  The smallest ones lose bits: 2^-25 absolute, at most 2^-26 of the largest weight, per code.
+#include <algorithm>
 #include <type_traits>
 
 #include "paged4_device.h"
@@ -32,235 +33,477 @@ __device__ __forceinline__ float column_max(float v)
     return fmaxf(both.x, both.y);
 }
 
-// grid: x = tile * g + KV head, y = split.  part: [row][head][splits][D + 2] when splits > 1.
-template <int D, int W, bool FOLD>
-__global__ __launch_bounds__(64 * W, FOLD ? 3 : 2) void attn_paged4_kernel(PagedSeqs, const uint16_t *__restrict__ q, Paged4Args pa, float *__restrict__ part,
-                                                             uint16_t *__restrict__ out, int h, int g, int per_seq, int chunk, int splits, int least)
+// n / d for 0 <= n < 2^31 by a product: with s = ceil(log2 d) and m = floor(2^(31 + s) / d) + 1 the error n (m d - 2^(31 + s)) is below 2^(31 + s)
+struct Divisor {
+    uint32_t m, shift;
+};
+Divisor divisor(uint32_t d)
+{
+    uint32_t s = 0;
+    while (s < 31 && (1u << s) < d) ++s;
+    return {(uint32_t)((1ull << (31 + s)) / d + 1), 31 + s};
+}
+__device__ __forceinline__ int quotient(int n, const Divisor &d) { return (int)((uint64_t)(uint32_t)n * d.m >> d.shift); }
+
+constexpr int kTile = 32;                        // (row, head) pairs of a tile at most
+template <int D, int TILE, int W>
+struct States {                                  // of the wavefronts, in LDS
+    static constexpr int kPairs = TILE, kWaves = W, kPitch = D + 4;
+    float o[W * TILE * kPitch], m[W * TILE], l[W * TILE];
+};
+
+// What a workgroup has to do: pairs p0 .. p0 + n_pairs - 1 of a sequence against tokens t_begin .. t_end - 1 and one KV head
+struct Task {
+    int q_start, slot, past, kvh, p0, n_pairs, t_begin, t_end;
+    int rep;
+    Divisor by_rep;
+    int used, split, splits;         // parts of the sequence, this one, the partial results per row
+};
+
+// The workgroup's part of a tile, its wavefronts a share of the tokens each.  CT: column tiles of 16 pairs.  FOLD: up to eight pairs, every column twice; a lane of the columns from 8 on
+// takes the second block of a step (the products with keys meet queries in one half of the columns and zeros in the other), so that scores, exponentials and weights of two blocks are those of one.  With two column tiles the codes are worth
+// the subtraction of their offset, which otherwise goes through the accumulators of the products.
+template <int D, int CT, bool FOLD, typename Lds>
+__device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *__restrict__ q, const Paged4Args &pa, float *__restrict__ part, uint16_t *__restrict__ out, int h,
+                                       int g)
 {
     constexpr int J = D / 32;                    // k steps, words of a lane per block, scales of a token
     constexpr int NT = D / 16;                   // 16-element tiles of O^T
-    constexpr int P = D + 4;                     // pitch of a state in LDS
     constexpr int SB = FOLD ? 1 : 2;             // blocks of a step whose scores a lane holds
+    constexpr bool EXACT = CT > 1;               // codes as u - 8
+    constexpr int W = Lds::kWaves;
+    static_assert(!FOLD || CT == 1, "eight pairs are one column tile");
     typedef uint32_t words_t __attribute__((ext_vector_type(J)));
     typedef _Float16 scales_t __attribute__((ext_vector_type(4 * J)));
-    __shared__ __align__(16) float states[W * 16 * P];
-    __shared__ float sm_m[W * 16], sm_l[W * 16];
-
-    const int rep = h / g, item = (int)blockIdx.x / g, kvh = (int)blockIdx.x - item * g, split = blockIdx.y;
-    const SeqsArg st = seqs_arg();
-    int tile;
-    const int b = tile_of(st, item, per_seq, [&](int q_len) { return q_len * rep < least ? (q_len * rep + 15) >> 4 : 0; }, tile);
-    if (b >= st->B) return;
-    const SeqSpan si = seq_span(st, __builtin_amdgcn_readfirstlane(b));
-    const int pairs = si.q_len * rep, p0 = tile * 16;
-    if (pairs >= least || p0 >= pairs) return;
-    const int n_pairs = min(16, pairs - p0);
-    const bool beyond = beyond_capacity(si, pa.cap);
-    const int past = beyond ? 0 : si.kv_len - si.q_len;
-    const int pos_min = past + p0 / rep, vis = beyond ? 0 : past + (p0 + n_pairs - 1) / rep + 1;      // tokens that any of the pairs attends to
-    const int t_begin = split * chunk;
-    if (split > 0 && t_begin >= vis) return;
-    if (beyond && threadIdx.x == 0) atomicOr(pa.err, kBadPage);
-    const int t_end = split + 1 == splits ? vis : min(vis, t_begin + chunk);      // the last split takes what a device table holds beyond the host's bound
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, quarter = lane >> 4;
+    const half2p_t eight = {(_Float16)-8.0f, (_Float16)-8.0f};
 
-    // ---- this wavefront's blocks: its share of the split, in pairs ----
-    const int b_begin = t_begin >> 4, b_end = t_end > t_begin ? (t_end + 15) >> 4 : b_begin;
+    // ---- this wavefront's blocks: its share of the part, in pairs ----
+    const int b_begin = (k.t_begin + 15) >> 4, b_end = k.t_end > k.t_begin ? (k.t_end + 15) >> 4 : b_begin;
     const int per = ((b_end - b_begin + 1) / 2 + W - 1) / W * 2;
     const int w_begin = b_begin + wave * per, w_end = min(b_end, w_begin + per);
+    const int pos_min = k.past + quotient(k.p0, k.by_rep);
 
-    // ---- queries: lane holds pair `col`; k step j takes elements 32 j + 8 quarter .. + 7, in the order of the codes ----
-    const int pair = p0 + min(FOLD ? col & 7 : col, n_pairs - 1), row = pair / rep, head = kvh * rep + pair - row * rep, pos = past + row;
-    half8p_t qf[J];
-    float qs[J];                                 // -8 sum q of a step
-    const float c = 1.44269504088896340736f / sqrtf((float)D);
-    {
-        const uint16_t *src = q + ((size_t)(si.q_start + row) * h + head) * D + quarter * 8;
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const half8p_t x = *(const half8p_t *)(src + j * 32);
-            qf[j] = half8p_t{x[0], x[4], x[1], x[5], x[2], x[6], x[3], x[7]};
-            float sum = 0.0f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum += (float)x[e];
-            qs[j] = xor32_sum(xor16_sum(sum)) * -8.0f;
-        }
-    }
-
-    float4p_t O[NT], off[J];                     // off: -8 times the sums of a group's operands
-#pragma unroll
-    for (int i = 0; i < NT; ++i) O[i] = float4p_t{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int j = 0; j < J; ++j) off[j] = float4p_t{0.0f, 0.0f, 0.0f, 0.0f};
-    float m_run = -INFINITY, l_run = 0.0f;
-
-    for (int seg = w_begin; seg < w_end; seg += kWave) {
-        // ---- lane j: number in the pool of block seg + j ----
+    // ---- lane j: number in the pool of the wavefront's block j; the next 64 when those are done ----
+    auto lookup = [&](int seg) __attribute__((always_inline)) {
         int pool = -1;
         if (seg + lane < w_end) {
-            pool = paged_block(pa, g, kvh, si.slot, seg + lane);
+            pool = paged_block(pa, g, k.kvh, k.slot, seg + lane);
             if (pool < 0) atomicOr(pa.err, kBadPage);
         }
-        const int ns = (min(w_end - seg, kWave) + 1) >> 1;
-        words_t kreg[2], vreg[2];                              // one step: two blocks
-        scales_t ks[SB], vs[SB];                               // (FOLD: of the lane's block)
-        auto load = [&](words_t (&reg)[2], scales_t (&sc)[SB], const uint8_t *codes, const uint16_t *scales, int s) __attribute__((always_inline)) {
-            size_t at[2];
+        return pool;
+    };
+    int pool = lookup(w_begin);
+
+    // ---- queries: lane holds pair `col` of each column tile; k step j takes elements 32 j + 8 quarter .. + 7, in the order of the codes ----
+    int pos[CT];
+    half8p_t qf[CT][J];                          // FOLD: of the columns below 8, zeros in the others; qg: the other way round
+    half8p_t qg[FOLD ? J : 1];
+    float qs[CT][J];                             // -8 sum q of a step
+    const float c = 1.44269504088896340736f / sqrtf((float)D);
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                at[t] = max(__builtin_amdgcn_readlane(pool, min(2 * s + t, 63)), 0);       // no such block: any that can be read
-                reg[t] = stream_load((const words_t *)(codes + at[t] * block4_codes(D)) + lane);
+    for (int ct = 0; ct < CT; ++ct) {
+        const int pair = k.p0 + min(FOLD ? col & 7 : ct * 16 + col, k.n_pairs - 1), row = quotient(pair, k.by_rep), head = k.kvh * k.rep + pair - row * k.rep;
+        pos[ct] = k.past + row;
+        const uint16_t *src = q + ((size_t)(k.q_start + row) * h + head) * D + quarter * 8;
+#pragma unroll
+        for (int j = 0; j < J; ++j) qf[ct][j] = *(const half8p_t *)(src + j * 32);
+    }
+    auto order_queries = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const half8p_t x = qf[ct][j];
+                qf[ct][j] = half8p_t{x[0], x[4], x[1], x[5], x[2], x[6], x[3], x[7]};
+                if constexpr (!EXACT) {
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum += (float)x[e];
+                    qs[ct][j] = xor32_sum(xor16_sum(sum)) * -8.0f;
+                }
+                if constexpr (FOLD) {
+                    const half8p_t zero = {};
+                    const u32x4p_t raw = __builtin_bit_cast(u32x4p_t, qf[ct][j]), none = __builtin_bit_cast(u32x4p_t, zero);
+                    qg[j] = __builtin_bit_cast(half8p_t, col < 8 ? none : raw), qf[ct][j] = __builtin_bit_cast(half8p_t, col < 8 ? raw : none);
+                }
             }
+    };
+
+    float4p_t O[CT][NT], off[J];                 // off: -8 times the sums of a group's operands
+    float m_run[CT], l_run[CT];
 #pragma unroll
-            for (int t = 0; t < SB; ++t) sc[t] = *((const scales_t *)(scales + (FOLD ? (col < 8 ? at[0] : at[1]) : at[t]) * block4_scales(D)) + quarter);
-        };
+    for (int ct = 0; ct < CT; ++ct) {
+        m_run[ct] = -INFINITY, l_run[ct] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) O[ct][i] = float4p_t{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+#pragma unroll
+    for (int j = 0; j < J; ++j) off[j] = float4p_t{0.0f, 0.0f, 0.0f, 0.0f};
+
+    words_t kreg[2], vreg[2];                                  // a step: two blocks
+    scales_t ks[SB], vs[SB];                                   // (FOLD: of the lane's block)
+    auto load = [&](words_t (&reg)[2], scales_t (&sc)[SB], const uint8_t *codes, const uint16_t *scales, int s) __attribute__((always_inline)) {
+        size_t at[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            at[t] = max(__builtin_amdgcn_readlane(pool, min(2 * s + t, 63)), 0);       // no such block: any that can be read
+            reg[t] = stream_load((const words_t *)(codes + at[t] * block4_codes(D)) + lane);
+        }
+#pragma unroll
+        for (int t = 0; t < SB; ++t) sc[t] = *((const scales_t *)(scales + (FOLD ? (col < 8 ? at[0] : at[1]) : at[t]) * block4_scales(D)) + quarter);
+    };
+    bool ordered = false;
+    for (int seg = w_begin; seg < w_end; seg += kWave) {
+        if (seg != w_begin) pool = lookup(seg);
+        const int ns = (min(w_end - seg, kWave) + 1) >> 1;
+        // loads are issued without a condition, behind the last step the last one's again: behind a branch their number at a wait is not known
         load(kreg, ks, pa.k, pa.k_scale, 0), load(vreg, vs, pa.v, pa.v_scale, 0);
+        if (!ordered) order_queries(), ordered = true;
         // a step's keys make room for the next one's as soon as the scores are there, its values when they are summed: one step is in flight all the time
-        auto step = [&](int s, auto MORE) __attribute__((always_inline)) {
-            float x[4 * SB];                                   // scores over c
-            float4p_t S[2][J];
+        // (two in flight take 40 registers more and lose: 120001 tokens 30.6 us for 29.1)
+#pragma unroll 1
+        for (int s = 0; s < ns; ++s) {
+            float x[CT][4 * SB];                               // scores over c
             const int t0 = (seg + 2 * s) * 16;                 // first token of the step
             const bool there0 = __builtin_amdgcn_readlane(pool, min(2 * s, 63)) >= 0, there1 = __builtin_amdgcn_readlane(pool, min(2 * s + 1, 63)) >= 0;
             const bool gone = !there0 || !there1 || t0 + 31 > pos_min;      // uniform: some of the tokens are masked
+            float4p_t S[CT][J];
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+            for (int t = 0; t < 2; ++t) {
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
                     half2p_t p[4];
                     word_codes(kreg[t][j], p);
-                    S[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(p[0], p[1], p[2], p[3]), qf[j], float4p_t{qs[j], qs[j], qs[j], qs[j]}, 0, 0, 0);
+                    if constexpr (EXACT) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) p[e] += eight;
+                    }
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) {
+                        const float start = EXACT ? 0.0f : qs[ct][j];
+                        S[ct][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(p[0], p[1], p[2], p[3]), FOLD && t ? qg[FOLD ? j : 0] : qf[ct][j],
+                                                                          FOLD && t ? S[ct][j] : float4p_t{start, start, start, start}, 0, 0, 0);
+                    }
                 }
+                if (FOLD && t == 0) continue;
 #pragma unroll
-            for (int t = 0; t < SB; ++t)
+                for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const auto score = [&](int j) { return FOLD ? (col < 8 ? S[0][j][i] : S[1][j][i]) : S[t][j][i]; };
-                    float sum = score(0) * (float)ks[t][i];
+                    for (int i = 0; i < 4; ++i) {
+                        const int u = FOLD ? 0 : t;
+                        float sum = fmaf(S[ct][0][i], (float)ks[u][i], 0.0f);      // (as a multiply-add of mixed types: a product would convert its scale first)
 #pragma unroll
-                    for (int j = 1; j < J; ++j) sum = fmaf(score(j), (float)ks[t][4 * j + i], sum);
-                    x[4 * t + i] = sum;
-                }
+                        for (int j = 1; j < J; ++j) sum = fmaf(S[ct][j][i], (float)ks[u][4 * j + i], sum);
+                        x[ct][4 * u + i] = sum;
+                    }
+            }
             if (gone) {
 #pragma unroll
                 for (int t = 0; t < SB; ++t) {
                     const bool there = FOLD ? (col < 8 ? there0 : there1) : (t ? there1 : there0);
                     const int first = t0 + 16 * (FOLD ? col >> 3 : t) + 4 * quarter;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (!there || first + i > pos) x[4 * t + i] = -INFINITY;
+                    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (!there || first + i > pos[ct]) x[ct][4 * t + i] = -INFINITY;
                 }
             }
-            float mx = x[0];
+            load(kreg, ks, pa.k, pa.k_scale, min(s + 1, ns - 1));
+            bool move[CT], any = false;
+            float mx[CT];
 #pragma unroll
-            for (int i = 1; i < 4 * SB; ++i) mx = fmaxf(mx, x[i]);
-            if constexpr (MORE) load(kreg, ks, pa.k, pa.k_scale, s + 1);
-            if constexpr (FOLD) mx = fmaxf(mx, lane_xor<8>(mx));
-            mx = column_max(mx) * c;
-            const bool move = mx > m_run + kLag;               // the first visible tokens: m_run = -inf
-            if (__any(move)) {
-                const float m_new = move ? mx : m_run, alpha = move ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.0f;
-                l_run *= alpha;
-                m_run = m_new;
+            for (int ct = 0; ct < CT; ++ct) {
+                mx[ct] = x[ct][0];
 #pragma unroll
-                for (int i = 0; i < NT; ++i) O[i] *= alpha;
-#pragma unroll
-                for (int j = 0; j < J; ++j) off[j] *= alpha;
+                for (int i = 1; i < 4 * SB; ++i) mx[ct] = fmaxf(mx[ct], x[ct][i]);
+                if constexpr (FOLD) mx[ct] = fmaxf(mx[ct], lane_xor<8>(mx[ct]));
+                mx[ct] = column_max(mx[ct]) * c;
+                move[ct] = mx[ct] > m_run[ct] + kLag;          // the first visible tokens: m_run = -inf
+                any = any || move[ct];
             }
-            const float m_ref = m_run == -INFINITY ? 0.0f : m_run - kBias;      // nothing visible yet: every weight is exp2(-inf)
-            float w[4 * SB];
+            if (__any(any)) {
 #pragma unroll
-            for (int i = 0; i < 4 * SB; ++i) {
-                w[i] = __builtin_amdgcn_exp2f(fmaf(x[i], c, -m_ref));
-                l_run += w[i];
+                for (int ct = 0; ct < CT; ++ct) {
+                    const float m_new = move[ct] ? mx[ct] : m_run[ct], alpha = move[ct] ? __builtin_amdgcn_exp2f(m_run[ct] - m_new) : 1.0f;
+                    l_run[ct] *= alpha;
+                    m_run[ct] = m_new;
+#pragma unroll
+                    for (int i = 0; i < NT; ++i) O[ct][i] *= alpha;
+                    if constexpr (!EXACT) {
+#pragma unroll
+                        for (int j = 0; j < J; ++j) off[j] *= alpha;
+                    }
+                }
             }
-            if (gone) {                                        // a scale behind the last token is anything
+            float w[CT][4 * SB];
 #pragma unroll
-                for (int t = 0; t < SB; ++t)
+            for (int ct = 0; ct < CT; ++ct) {
+                const float m_ref = m_run[ct] == -INFINITY ? 0.0f : m_run[ct] - kBias;      // nothing visible yet: every weight is exp2(-inf)
 #pragma unroll
-                    for (int j = 0; j < J; ++j)
+                for (int i = 0; i < 4 * SB; ++i) {
+                    w[ct][i] = __builtin_amdgcn_exp2f(fmaf(x[ct][i], c, -m_ref));
+                    l_run[ct] += w[ct][i];
+                }
+            }
+            if (gone) {                                        // a scale behind the last token, or of no block, is anything
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) vs[t][4 * j + i] = x[4 * t + i] == -INFINITY ? (_Float16)0.0f : vs[t][4 * j + i];
+                for (int t = 0; t < SB; ++t) {
+                    const bool there = FOLD ? (col < 8 ? there0 : there1) : (t ? there1 : there0);
+                    const int first = t0 + 16 * (FOLD ? col >> 3 : t) + 4 * quarter;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (!there || first + i >= k.t_end)
+#pragma unroll
+                            for (int j = 0; j < J; ++j) vs[t][4 * j + i] = (_Float16)0.0f;
+                }
             }
 #pragma unroll
             for (int j = 0; j < J; ++j) {
-                half2p_t pw[4];                                // the weights of both blocks, tokens 0 2 | 1 3
-#pragma unroll
-                for (int t = 0; t < SB; ++t)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        pw[2 * t + i] = half2p_t{(_Float16)(w[4 * t + i] * (float)vs[t][4 * j + i]), (_Float16)(w[4 * t + i + 2] * (float)vs[t][4 * j + i + 2])};
-                if constexpr (FOLD) {                          // (columns from 8 on have the blocks the other way round, and no pair)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) pw[2 + i] = __builtin_bit_cast(half2p_t, lane_xor<8>(__builtin_bit_cast(float, pw[i])));
-                }
-                const half8p_t pf = operand(pw[0], pw[1], pw[2], pw[3]);
                 half2p_t a[4], e[4];
                 word_codes(vreg[0][j], a);
                 word_codes(vreg[1][j], e);
-                O[2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(a[0], a[1], e[0], e[1]), pf, O[2 * j], 0, 0, 0);
-                O[2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(a[2], a[3], e[2], e[3]), pf, O[2 * j + 1], 0, 0, 0);
-                const half2p_t eight = {(_Float16)-8.0f, (_Float16)-8.0f};
-                off[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(eight, eight, eight, eight), pf, off[j], 0, 0, 0);
+                if constexpr (EXACT) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) a[i] += eight, e[i] += eight;
+                }
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) {
+                    half2p_t pw[4];                            // the weights of both blocks, tokens 0 2 | 1 3
+#pragma unroll
+                    for (int t = 0; t < SB; ++t)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            float lo = fmaf(w[ct][4 * t + i], (float)vs[t][4 * j + i], 0.0f), hi = fmaf(w[ct][4 * t + i + 2], (float)vs[t][4 * j + i + 2], 0.0f);
+                            asm("" : "+v"(lo), "+v"(hi));      // (the products in fp32 and one conversion of both: multiply-adds that write a half take twice the time)
+                            pw[2 * t + i] = half2p_t{(_Float16)lo, (_Float16)hi};
+                        }
+                    if constexpr (FOLD) {                      // (columns from 8 on have the blocks the other way round, and no pair)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) pw[2 + i] = __builtin_bit_cast(half2p_t, lane_xor<8>(__builtin_bit_cast(float, pw[i])));
+                    }
+                    const half8p_t pf = operand(pw[0], pw[1], pw[2], pw[3]);
+                    O[ct][2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(a[0], a[1], e[0], e[1]), pf, O[ct][2 * j], 0, 0, 0);
+                    O[ct][2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(a[2], a[3], e[2], e[3]), pf, O[ct][2 * j + 1], 0, 0, 0);
+                    if constexpr (!EXACT) off[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(eight, eight, eight, eight), pf, off[j], 0, 0, 0);
+                }
             }
-            if constexpr (MORE) load(vreg, vs, pa.v, pa.v_scale, s + 1);
-        };
-#pragma unroll 1
-        for (int s = 0; s + 1 < ns; ++s) step(s, std::true_type{});
-        step(ns - 1, std::false_type{});
+            load(vreg, vs, pa.v, pa.v_scale, min(s + 1, ns - 1));
+        }
     }
 
-    // ---- the wavefronts' states meet in LDS ----
-    if constexpr (FOLD) l_run += lane_xor<8>(l_run);
-    l_run = xor32_sum(xor16_sum(l_run));
 #pragma unroll
-    for (int i = 0; i < NT; ++i)
-        *(float4p_t *)(states + (wave * 16 + col) * P + i * 16 + quarter * 4) = O[i] + off[i >> 1];
-    if (quarter == 0) sm_m[wave * 16 + col] = m_run, sm_l[wave * 16 + col] = l_run;
+    for (int ct = 0; ct < CT; ++ct) {
+        const int at = wave * Lds::kPairs + (FOLD ? col & 7 : ct * 16 + col);
+        if constexpr (FOLD) l_run[ct] += lane_xor<8>(l_run[ct]);
+        l_run[ct] = xor32_sum(xor16_sum(l_run[ct]));
+        if (FOLD && col >= 8) continue;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) *(float4p_t *)(lds.o + at * Lds::kPitch + i * 16 + quarter * 4) = EXACT ? O[ct][i] : O[ct][i] + off[i >> 1];
+        if (quarter == 0) lds.m[at] = m_run[ct], lds.l[at] = l_run[ct];
+    }
+
+    // ---- the wavefronts' states meet: T threads per pair, E times four elements each ----
     __syncthreads();
-    for (int u = tid; u < n_pairs * (D / 4); u += 64 * W) {
-        const int pc = u / (D / 4), e = u % (D / 4) * 4;
-        float mm = -INFINITY;
+    constexpr int TW = FOLD ? 8 : 16 * CT, T = 64 * W / TW, E = D / 4 / T > 0 ? D / 4 / T : 1;
+    const int pc = tid / T, e0 = tid % T * 4;
+    if (pc >= k.n_pairs || e0 >= D) return;
+    float mw[W], lw[W], mm = -INFINITY, den = 0.0f;
+    float4p_t num[E], o[W][E];
 #pragma unroll
-        for (int w = 0; w < W; ++w) mm = fmaxf(mm, sm_m[w * 16 + pc]);
-        float4p_t num = {0.0f, 0.0f, 0.0f, 0.0f};
-        float den = 0.0f;
+    for (int w = 0; w < W; ++w) {
+        mw[w] = lds.m[w * Lds::kPairs + pc], lw[w] = lds.l[w * Lds::kPairs + pc];
 #pragma unroll
-        for (int w = 0; w < W; ++w) {
-            const float mw = sm_m[w * 16 + pc], fw = mw == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mw - mm);
-            num += *(const float4p_t *)(states + (w * 16 + pc) * P + e) * fw;
-            den += sm_l[w * 16 + pc] * fw;
+        for (int i = 0; i < E; ++i) o[w][i] = *(const float4p_t *)(lds.o + (w * Lds::kPairs + pc) * Lds::kPitch + e0 + i * 4 * T);
+    }
+#pragma unroll
+    for (int w = 0; w < W; ++w) mm = fmaxf(mm, mw[w]);
+#pragma unroll
+    for (int i = 0; i < E; ++i) num[i] = float4p_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        const float f = mw[w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mw[w] - mm);
+        den += lw[w] * f;
+#pragma unroll
+        for (int i = 0; i < E; ++i) num[i] += o[w][i] * f;
+    }
+    const int pr = quotient(k.p0 + pc, k.by_rep);
+    const size_t at = (size_t)(k.q_start + pr) * h + k.kvh * k.rep + k.p0 + pc - pr * k.rep;
+    if (k.used > 1) {
+        float *dst = part + (at * k.splits + k.split) * (D + 2);
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            float2 *d2 = (float2 *)(dst + e0 + i * 4 * T);
+            d2[0] = make_float2(num[i].x, num[i].y), d2[1] = make_float2(num[i].z, num[i].w);
         }
-        const int pr = (p0 + pc) / rep, ph = kvh * rep + p0 + pc - pr * rep;
-        const size_t at = (size_t)(si.q_start + pr) * h + ph;
-        if (splits > 1) {
-            float *dst = part + (at * splits + split) * (D + 2);
-            dst[e] = num.x, dst[e + 1] = num.y, dst[e + 2] = num.z, dst[e + 3] = num.w;
-            if (e == 0) dst[D] = mm, dst[D + 1] = den;
-        } else {
-            const float inv = den > 0.0f ? 1.0f / den : den;   // a row that no token is left for is zeros; a NaN stays one
-            const uint32_t lo = f2h(num.x * inv) | (uint32_t)f2h(num.y * inv) << 16, hi = f2h(num.z * inv) | (uint32_t)f2h(num.w * inv) << 16;
-            *(u32x2p_t *)(out + at * D + e) = u32x2p_t{lo, hi};
+        if (e0 == 0) *(float2 *)(dst + D) = make_float2(mm, den);
+    } else {
+        const float inv = den > 0.0f ? 1.0f / den : den;       // a row that no token is left for is zeros; a NaN stays one
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            const float4p_t r = num[i] * inv;
+            *(u32x2p_t *)(out + at * D + e0 + i * 4 * T) = u32x2p_t{f2h(r.x) | (uint32_t)f2h(r.y) << 16, f2h(r.z) | (uint32_t)f2h(r.w) << 16};
         }
     }
 }
 
+// grid: item * g + KV head, an item being a part of a tile (the tiles of a part side by side: they read the same tokens).  per_seq: as tile_of takes it.  part: [row][head][splits][D + 2], of
+// rows that have more than one part.  FEW: no sequence has more than eight pairs.
+struct Grid {
+    int h, g, rep, per_seq, chunk, splits, least;
+    Divisor by_g, by_rep, by_per_seq, by_chunk;
+};
+template <int D, bool FEW, int W>
+__global__ __launch_bounds__(64 * W, 2) void attn_paged4_kernel(PagedSeqs, const uint16_t *__restrict__ q, Paged4Args pa, float *__restrict__ part, uint16_t *__restrict__ out, Grid gr)
+{
+    __shared__ __align__(16) States<D, FEW ? 8 : kTile, W> lds;
+    const int rep = gr.rep, item = quotient(blockIdx.x, gr.by_g), kvh = (int)blockIdx.x - item * gr.g;
+    const SeqsArg st = seqs_arg();
+    const auto tiles_of = [&](int q_len) { return q_len * rep < gr.least ? (q_len * rep + kTile - 1) / kTile : 0; };
+    const auto parts_of = [&](int kv_len) { return min(max(quotient(kv_len + gr.chunk - 1, gr.by_chunk), 1), gr.splits); };
+    int place = item, b = 0;
+    if (gr.per_seq > 0) b = quotient(item, gr.by_per_seq), place = item - b * gr.per_seq;
+    else b = seq_at(st, item, [&](int j) { return st->dev ? tiles_of(st->dev[st->B + j]) * gr.splits : tiles_of(st->q_len[j]) * parts_of(st->kv_len[j]); }, place);
+    if (b >= st->B) return;
+    const SeqSpan si = seq_span(st, __builtin_amdgcn_readfirstlane(b));
+    const int pairs = si.q_len * rep, tiles = tiles_of(si.q_len), split = tiles > 1 ? place / tiles : place, p0 = (tiles > 1 ? place - split * tiles : 0) * kTile;
+    if (tiles == 0) return;
+    const int n_pairs = min(kTile, pairs - p0);
+    const bool beyond = beyond_capacity(si, pa.cap);
+    const int past = beyond ? 0 : si.kv_len - si.q_len;
+    const int vis = beyond ? 0 : past + quotient(p0 + n_pairs - 1, gr.by_rep) + 1;      // tokens that any of the pairs attends to
+    // the tile's tokens in equal parts, as many as the sequence has chunks (more than the host's bound gives makes them longer)
+    const int used = beyond ? 1 : parts_of(si.kv_len);
+    if (split >= used) return;
+    const int share = used == 1 ? vis : ((vis + used - 1) / used + 31) & ~31, t_begin = min(split * share, vis), t_end = min(vis, t_begin + share);
+    if (beyond && threadIdx.x == 0) atomicOr(pa.err, kBadPage);
+    const Task task = {si.q_start, si.slot, past, kvh, p0, n_pairs, t_begin, t_end, rep, gr.by_rep, used, split, gr.splits};
+    if (FEW || n_pairs <= 8) attend<D, 1, true>(lds, task, q, pa, part, out, gr.h, gr.g);
+    else if constexpr (!FEW) n_pairs <= 16 ? attend<D, 1, false>(lds, task, q, pa, part, out, gr.h, gr.g) : attend<D, 2, false>(lds, task, q, pa, part, out, gr.h, gr.g);
+}
+
+// Estimated times, us, fitted to 19 calls with 10 to 20 cuts each, of which they choose one that is 1 % behind the best in the mean and 10 % at most: a workgroup's beginning and end, with four and with
+// eight wavefronts; a step of 32 tokens with up to 16 pairs and with 32, alone on a SIMD and beside another wavefront (heads of 64: times kHalfHead); the share of the longest workgroup that
+// comes on top when there are more of them than at a time; a merge, and each of its partial results; the cache's bytes
+constexpr float kGroupUs[2] = {3.8f, 5.8f}, kStepUs[2][2] = {{0.96f, 1.17f}, {1.35f, 2.4f}}, kHalfHead = 0.71f, kTail = 0.14f, kMergeUs = 2.9f, kMergeResultUs = 4.1e-4f, kBytesUs = 5.1f,
+                kBytesPerUs = 6.15e6f;
+constexpr int kLeast = 128, kPartials4 = 65536;  // tokens of a part, and partial results (row, head, part), at least and at most
+
+// How the tiles are cut: a sequence of L tokens into ceil(L / chunk) equal parts
+struct Cut {
+    int64_t items;                   // parts of tiles
+    int32_t chunk, splits;           // splits: the most parts of a sequence
+    int32_t per_seq;                 // parts of every sequence, 0: not alike
+    int32_t rows;                    // rows of sequences that have more than one part
+    int32_t waves;                   // wavefronts per workgroup
+    bool few;                        // no sequence has more than eight pairs
+};
+Cut cut(const PagedPlan &pl, const relax_layer_dims &dm, const PagedSeqs &st, const relax_seqs &sq, int32_t L_max)
+{
+    const int rep = dm.n_heads / dm.n_kv_heads, g = dm.n_kv_heads;
+    const auto tiles_of = [&](int b) {
+        const int64_t pairs = (int64_t)sq.q_lens[b] * rep;
+        return pairs < pl.least ? (pairs + kTile - 1) / kTile : 0;
+    };
+    int64_t tiles = 0, tokens = 0, most = 0;
+    float unique = 0.0f;
+    for (int b = 0; b < sq.B; ++b) {
+        const int64_t t = tiles_of(b);
+        tiles += t, tokens += t * sq.kv_lens[b];
+        if (t) most = std::max(most, (int64_t)sq.q_lens[b] * rep), unique += (float)sq.kv_lens[b];
+    }
+    const float bytes_us = kBytesUs + unique * (float)(g * 2 * (block4_codes(dm.head_dim) + 2 * block4_scales(dm.head_dim)) / 16) / kBytesPerUs;
+    const float head = dm.head_dim == 64 ? kHalfHead : 1.0f;
+    int32_t waves = 4;
+    int64_t chunk = std::max<int64_t>(32, ((int64_t)L_max + 31) & ~31);
+    float best = INFINITY;
+    // takes parts of up to c tokens if they are estimated to be faster than what was considered before.  Two wavefronts per SIMD: 512 workgroups of four at a time, 256 of eight
+    const auto consider = [&](int64_t c) {
+        const float by_c = 1.0f / (float)c;
+        float groups = 0.0f, merged = 0.0f, total[2] = {0.0f, 0.0f}, longest[2][2] = {{0.0f, 0.0f}, {0.0f, 0.0f}};
+        for (int b = 0; b < sq.B; ++b) {
+            const float t = (float)tiles_of(b), L = (float)sq.kv_lens[b];
+            if (t == 0.0f) continue;
+            const float parts = ceilf(L * by_c), share = parts == 1.0f ? L : L / parts;
+            const float *step = kStepUs[(int64_t)sq.q_lens[b] * rep > 16];
+            for (int w = 0; w < 2; ++w) {
+                const float steps = ceilf(share * (w ? 1.0f / 256 : 1.0f / 128)) * head, beside = kGroupUs[w] + steps * step[1];
+                longest[w][0] = std::max(longest[w][0], kGroupUs[w] + steps * step[0]), longest[w][1] = std::max(longest[w][1], beside);
+                total[w] += beside * t * parts;
+            }
+            groups += t * parts;
+            if (parts > 1.0f) merged += (float)sq.q_lens[b] * parts;
+        }
+        groups *= (float)g;
+        for (int w = 0; w < 2; ++w) {
+            const float slots = w ? 256.0f : 512.0f;
+            float us = groups <= slots ? longest[w][groups * (w ? 8.0f : 4.0f) > 1024.0f] : total[w] * (float)g / slots + kTail * longest[w][1];
+            us = std::max(us, bytes_us) + (merged > 0.0f ? kMergeUs + kMergeResultUs * merged * (float)dm.n_heads : 0.0f);
+            if (us < best) best = us, chunk = c, waves = w ? 8 : 4;
+        }
+    };
+    if (tiles * g < 2048) {
+        consider(chunk);
+        const int64_t most_parts = std::max<int64_t>(1, kPartials4 / ((int64_t)st.n * dm.n_heads)), least = (std::max<int64_t>(kLeast, L_max / most_parts + 1) + 31) & ~31;
+        for (int parts = 2; parts <= (sq.B <= 4 ? 64 : sq.B <= 24 ? 16 : 4); parts += parts < 4 ? 1 : parts / 2) {
+            const int64_t c = (L_max / parts + 32) & ~31;
+            if (c >= least) consider(c);
+        }
+        const int64_t even = (tokens * g / 512 + 32) & ~31;    // as many parts as workgroups at a time, for sequences alike
+        if (even >= least && even < L_max) consider(even);
+    }
+    Cut c = {0, (int32_t)chunk, (int32_t)((L_max + chunk - 1) / chunk), -1, 0, waves, most <= 8};
+    for (int b = 0; b < sq.B; ++b) {
+        const int64_t parts = st.dev ? c.splits : (sq.kv_lens[b] + chunk - 1) / chunk, items = tiles_of(b) * parts;
+        c.items += items;
+        if (parts > 1) c.rows += sq.q_lens[b];
+        if (c.per_seq < 0) c.per_seq = (int32_t)std::min<int64_t>(items, INT32_MAX);
+        else if (c.per_seq != items) c.per_seq = 0;
+    }
+    return c;
+}
+
+// The sequences in order of their lengths, longest first, where they are in the arguments: the workgroups that take longest begin first
+void longest_first(PagedSeqs &st)
+{
+    if (st.dev || st.B < 2) return;
+    struct Entry {
+        int32_t kv_len, b;
+    } order[kPagedInline];
+    bool sorted = true;
+    for (int b = 0; b < st.B; ++b) order[b] = {st.kv_len[b], b}, sorted = sorted && (b == 0 || st.kv_len[b] <= st.kv_len[b - 1]);
+    if (sorted) return;
+    std::sort(order, order + st.B, [](const Entry &x, const Entry &y) { return x.kv_len != y.kv_len ? x.kv_len > y.kv_len : x.b < y.b; });
+    int32_t from[3][kPagedInline];
+    for (int b = 0; b < st.B; ++b) from[0][b] = st.q_start[b], from[1][b] = st.q_len[b], from[2][b] = st.slot[b];
+    for (int b = 0; b < st.B; ++b) {
+        const int i = order[b].b;
+        st.q_start[b] = from[0][i], st.q_len[b] = from[1][i], st.slot[b] = from[2][i], st.kv_len[b] = order[b].kv_len;
+    }
+}
+
 template <int D>
-hipError_t launch_d(const uint16_t *q, const Paged4Args &pa, const relax_layer_dims &dm, const PagedSeqs &st, const PagedPlan &pl, bool few, uint16_t *out, float *partials,
+hipError_t launch_d(const uint16_t *q, const Paged4Args &pa, const relax_layer_dims &dm, const PagedSeqs &st, const PagedPlan &pl, const Cut &c, uint16_t *out, float *partials,
                     hipStream_t stream)
 {
-    if ((int64_t)pl.items * dm.n_kv_heads * 64 * pl.waves > kMaxThreads) return hipErrorInvalidValue;
-    const dim3 grid(pl.items * dm.n_kv_heads, pl.splits);
-    const auto launch = [&](auto W, auto FOLD) {
-        hipLaunchKernelGGL((attn_paged4_kernel<D, W, FOLD>), grid, dim3(64 * W), 0, stream, st, q, pa, partials, out, dm.n_heads, dm.n_kv_heads, pl.per_seq, pl.chunk, pl.splits,
-                           pl.least);
+    if (c.items * dm.n_kv_heads * 64 * c.waves > kMaxThreads) return hipErrorInvalidValue;
+    const dim3 grid(c.items * dm.n_kv_heads);
+    const int rep = dm.n_heads / dm.n_kv_heads;
+    const Grid gr = {dm.n_heads, dm.n_kv_heads, rep, c.per_seq, c.chunk, c.splits, pl.least, divisor(dm.n_kv_heads), divisor(rep), divisor(std::max(c.per_seq, 1)), divisor(c.chunk)};
+    const auto launch = [&](auto FEW, auto W) {
+        hipLaunchKernelGGL((attn_paged4_kernel<D, FEW, W>), grid, dim3(64 * W), 0, stream, st, q, pa, partials, out, gr);
     };
     using four = std::integral_constant<int, 4>;
     using eight = std::integral_constant<int, 8>;
-    if (pl.waves == 8) few ? launch(eight{}, std::true_type{}) : launch(eight{}, std::false_type{});
-    else few ? launch(four{}, std::true_type{}) : launch(four{}, std::false_type{});
+    if (c.waves == 8) c.few ? launch(std::true_type{}, eight{}) : launch(std::false_type{}, eight{});
+    else c.few ? launch(std::true_type{}, four{}) : launch(std::false_type{}, four{});
     const hipError_t e = hipGetLastError();
-    return e != hipSuccess || pl.splits == 1 ? e : launch_paged_merge(pl, partials, out, dm, pa.cap, st, stream);
+    if (e != hipSuccess || c.rows == 0) return e;
+    PagedPlan parts = pl;
+    parts.chunk = c.chunk, parts.splits = c.splits;
+    return launch_paged_merge(parts, partials, out, dm, pa.cap, st, stream, c.rows);
 }
 
 }  // namespace
@@ -273,8 +516,10 @@ hipError_t launch_paged4_attention(const uint16_t *q, const Paged4Args &pa, cons
         const hipError_t e = launch_paged4_rows(q, pa, dm, st, pl, out, stream);
         if (e != hipSuccess || pl.items == 0) return e;
     }
-    const bool few = (int64_t)st.q_max * (dm.n_heads / dm.n_kv_heads) <= 8;
-    return dm.head_dim == 128 ? launch_d<128>(q, pa, dm, st, pl, few, out, partials, stream) : launch_d<64>(q, pa, dm, st, pl, few, out, partials, stream);
+    const Cut c = cut(pl, dm, st, sq, L_max);
+    PagedSeqs by_length = st;
+    longest_first(by_length);
+    return dm.head_dim == 128 ? launch_d<128>(q, pa, dm, by_length, pl, c, out, partials, stream) : launch_d<64>(q, pa, dm, by_length, pl, c, out, partials, stream);
 }
 
 }  // namespace relax

@@ -54,19 +54,18 @@ __device__ __forceinline__ bool beyond_capacity(const SeqSpan &si, int cap) { re
 // Blocks of 16 tokens that a sequence's q_len rows can touch, wherever they begin
 __host__ __device__ inline int paged_blocks_of(int q_len) { return (q_len + 30) >> 4; }
 
-// Sequence b of the call that item `key` belongs to when sequence j brings count(q_len_j) items, and the item's place among its own.
+// Sequence b of the call that item `key` belongs to when sequence j brings count(j) items (seq_of: count(q_len_j)), and the item's place among its own.
 // key is the same in all lanes of the wavefront; b = B: behind the last one.  64 sequences at a time, one per lane.
 template <typename Count>
-__device__ __forceinline__ int seq_of(SeqsArg st, int key, const Count &count, int &place)
+__device__ __forceinline__ int seq_at(SeqsArg st, int key, const Count &count, int &place)
 {
     const int B = st->B;
     place = key;
     if (B == 1) return 0;                                      // (the caller finds a place behind the last one by the lengths)
     const int lane = threadIdx.x & 63;
-    const int32_t *dev = st->dev;
     int before = 0;
     for (int base = 0; base < B; base += kWave) {
-        const int own = base + lane < B ? count(dev ? dev[B + base + lane] : st->q_len[base + lane]) : 0;
+        const int own = base + lane < B ? count(base + lane) : 0;
         int sum = own;                                         // inclusive sum over the lanes up to this one
 #pragma unroll
         for (int off = 1; off < kWave; off <<= 1) {
@@ -82,6 +81,14 @@ __device__ __forceinline__ int seq_of(SeqsArg st, int key, const Count &count, i
         before += __builtin_amdgcn_readlane(sum, kWave - 1);
     }
     return B;
+}
+
+template <typename Count>
+__device__ __forceinline__ int seq_of(SeqsArg st, int key, const Count &count, int &place)
+{
+    const int32_t *dev = st->dev;
+    const int B = st->B;
+    return seq_at(st, key, [&](int j) { return count(dev ? dev[B + j] : st->q_len[j]); }, place);
 }
 
 // Tiles of a paged attention call are numbered sequence by sequence.  per_seq > 0: that many numbers for each, of which a short one leaves some unused;
@@ -131,7 +138,8 @@ struct PagedPlan {
 };
 PagedPlan paged_plan(const relax_layer_dims &dm, const relax_seqs &sq, int32_t n, int32_t L_max, bool rows = true);      // rows: there are tiles of 256 pairs
 // out of the partial results [row][head][splits][d + 2] of the 16-pair tiles: d sums, the reference of the weights (log2), the sum of the weights
-hipError_t launch_paged_merge(const PagedPlan &pl, const float *partials, uint16_t *out, const relax_layer_dims &dm, int32_t cap, const PagedSeqs &st, hipStream_t stream);
+// rows > 0: of the first `rows` rows of the call alone, in the order of st's sequences, and parts by the sequence's length, of which a single one has been written already
+hipError_t launch_paged_merge(const PagedPlan &pl, const float *partials, uint16_t *out, const relax_layer_dims &dm, int32_t cap, const PagedSeqs &st, hipStream_t stream, int32_t rows = 0);
 
 // Attention of the sequences with at least `least` (row, head) pairs, in `items` tiles of kPagedRowTile pairs (attn_paged_rows.hip)
 constexpr int kPagedRowTile = 256;
