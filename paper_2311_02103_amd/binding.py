@@ -16,6 +16,11 @@ from array import array
 from dataclasses import dataclass
 from typing import Optional, Sequence, Union
 
+try:                           # the same in C (csrc/marshal.c), for the calls whose host time counts; without it (not built yet) they are marshalled here
+    from . import _marshal
+except ImportError:
+    _marshal = None
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "librelax_mi355.so")
 
@@ -231,6 +236,8 @@ def _stream(stream) -> Optional[int]:
         if torch is None:
             import torch
         if torch.cuda.is_initialized() and _raw_stream(torch) is not None:      # 0.4 us instead of 2.9 for a Stream object, per call
+            if _marshal is not None:
+                _marshal.use_streams(torch._C._cuda_getDevice, _raw_stream(torch))
             return _raw_stream(torch)(torch._C._cuda_getDevice()) or None
         if torch.cuda.is_initialized() or torch.cuda.is_available():     # the first is a flag, the second asks the runtime
             return torch.cuda.current_stream().cuda_stream or None
@@ -242,6 +249,34 @@ def _stream(stream) -> Optional[int]:
 
 def _ref(obj):
     return None if obj is None else C.byref(obj)
+
+
+# Arguments of the calls that _call makes, a letter each: p device memory, i integer, r struct, s stream (csrc/marshal.c)
+_KINDS = {
+    "relax_rope_table_scaled": "rips",
+    "relax_head_norm_rope": "pipipipirrripis",
+    "relax_paged4_append": "pippiprrrripis",
+    "relax_paged4_attention": "prrrpipis",
+    "relax_paged4_read": "rrrppipis",
+}
+_bound = {}
+
+
+def _bind(name: str):
+    """The function of the library as one that takes tensors, objects of this module and streams; made at its first call."""
+    fn, kinds = getattr(lib(), name), _KINDS[name]
+    if _marshal is not None:
+        _marshal.slow_stream(_stream)
+        call = _marshal.Call(C.cast(fn, C.c_void_p).value, kinds)
+    else:
+        convert = {"p": _ptr, "i": lambda i: i, "r": lambda o: _ref(o.c() if hasattr(o, "c") else o), "s": _stream}
+
+        def call(*args):
+            if len(args) != len(kinds):
+                raise TypeError("%d positional arguments" % len(kinds))
+            return fn(*[convert[kind](arg) for kind, arg in zip(kinds, args)])
+    _bound[name] = call
+    return call
 
 
 @dataclass
@@ -309,6 +344,7 @@ class Paged4Cache:
     def __init__(self, k: Ptr, v: Ptr, k_scale: Ptr, v_scale: Ptr, pages: Ptr, n_pages: int, page_size: int, pages_per_slot: int):
         self._keep = (k, v, k_scale, v_scale, pages)
         self._c = Paged4CacheC(*map(_ptr, self._keep), n_pages, page_size, pages_per_slot)
+        self._at = C.addressof(self._c)
 
     def c(self) -> Paged4CacheC:
         return self._c
@@ -321,16 +357,16 @@ class HeadPrep:
     def __init__(self, q_norm: Ptr = None, k_norm: Ptr = None, eps: float = 1e-6, rope: Ptr = None, rotary_dim: int = 0, layout: int = ROPE_HALVES):
         self._keep = (q_norm, k_norm, rope)
         self._c = HeadPrepC(_ptr(q_norm), _ptr(k_norm), eps, _ptr(rope), rotary_dim, layout)
+        self._at = C.addressof(self._c)
 
     def c(self) -> HeadPrepC:
         return self._c
 
 
-class Seqs:
-    """Host-side ragged descriptor; kv_lens are lengths AFTER this call's rows are appended.  device_table: optional
-    device int32 [4][B] (q_start, q_len, kv_len, slot) that the kernels read instead; kv_lens are then upper bounds."""
-
-    def __init__(self, q_lens: Sequence[int], kv_lens: Sequence[int], slots: Optional[Sequence[int]] = None, device_table: Ptr = None):
+class _PySeqs:
+    def __init__(self, q_lens, kv_lens, slots=None, device_table=None):
+        if len(kv_lens) < len(q_lens) or (slots is not None and len(slots) < len(q_lens)):
+            raise ValueError("a length and a slot for each sequence")
         self.B = len(q_lens)
         self._q, self._kv = _int32s(q_lens), _int32s(kv_lens)
         self._sl = None if slots is None else _int32s(slots)
@@ -338,6 +374,18 @@ class Seqs:
 
     def c(self) -> SeqsC:
         return SeqsC(self.B, self._q, self._kv, self._sl, _ptr(self._table))       # arrays convert to pointers, and are kept alive by the struct
+
+
+class Seqs(_PySeqs if _marshal is None else _marshal.Seqs):
+    """Host-side ragged descriptor; kv_lens are lengths AFTER this call's rows are appended.  device_table: optional
+    device int32 [4][B] (q_start, q_len, kv_len, slot) that the kernels read instead; kv_lens are then upper bounds.
+    Seqs(q_lens, kv_lens, slots=None, device_table=None)."""
+
+    if _marshal is not None:
+        def c(self) -> SeqsC:
+            struct_ = SeqsC.from_address(self._at)
+            struct_._seqs = self               # its memory
+            return struct_
 
 
 def make_dims(hidden, n_heads, n_kv_heads, head_dim, ffn, kv_capacity, kv_slots=1, rms_eps=1e-5, rope_base=10000.0,
@@ -451,7 +499,7 @@ def relax_rope_scaled_bytes(scaling: Optional[RopeScaling], positions: int) -> i
 
 
 def relax_rope_table_scaled(scaling: Optional[RopeScaling], positions: int, table: Ptr, stream=None) -> int:
-    return lib().relax_rope_table_scaled(_ref(scaling), positions, _ptr(table), _stream(stream))
+    return (_bound.get("relax_rope_table_scaled") or _bind("relax_rope_table_scaled"))(scaling, positions, table, stream)
 
 
 def relax_head_workspace_bytes(dims: Optional[LayerDims], B_max: int) -> int:
@@ -461,10 +509,8 @@ def relax_head_workspace_bytes(dims: Optional[LayerDims], B_max: int) -> int:
 def relax_head_norm_rope(q: Ptr, q_stride: int, k: Ptr, k_stride: int, q_out: Ptr, q_out_stride: int, k_out: Ptr, k_out_stride: int, prep: Optional[HeadPrep],
                          seqs: Optional[Seqs], dims: Optional[LayerDims], n: int, ws: Ptr, ws_bytes: int, stream=None) -> int:
     """q and k may be parts of one matrix: their addresses as integers, the strides in elements."""
-    pc = None if prep is None else prep.c()
-    sc = None if seqs is None else seqs.c()
-    return lib().relax_head_norm_rope(_ptr(q), q_stride, _ptr(k), k_stride, _ptr(q_out), q_out_stride, _ptr(k_out), k_out_stride, _ref(pc), _ref(sc), _ref(dims), n,
-                                      _ptr(ws), ws_bytes, _stream(stream))
+    return (_bound.get("relax_head_norm_rope") or _bind("relax_head_norm_rope"))(q, q_stride, k, k_stride, q_out, q_out_stride, k_out, k_out_stride, prep, seqs, dims, n, ws,
+                                                                                 ws_bytes, stream)
 
 
 def relax_paged4_workspace_bytes(dims: Optional[LayerDims], n_max: int, L_max: int, B_max: int) -> int:
@@ -474,25 +520,17 @@ def relax_paged4_workspace_bytes(dims: Optional[LayerDims], n_max: int, L_max: i
 def relax_paged4_append(q: Ptr, q_stride: int, k: Ptr, v: Ptr, kv_stride: int, q_out: Ptr, prep: Optional[HeadPrep], cache: Optional[Paged4Cache],
                         seqs: Optional[Seqs], dims: Optional[LayerDims], n: int, ws: Ptr, ws_bytes: int, stream=None) -> int:
     """q, k, v may be parts of one matrix: their addresses as integers, the strides in elements."""
-    pc = None if prep is None else prep.c()
-    cc = None if cache is None else cache.c()
-    sc = None if seqs is None else seqs.c()
-    return lib().relax_paged4_append(_ptr(q), q_stride, _ptr(k), _ptr(v), kv_stride, _ptr(q_out), _ref(pc), _ref(cc), _ref(sc), _ref(dims), n, _ptr(ws), ws_bytes,
-                                     _stream(stream))
+    return (_bound.get("relax_paged4_append") or _bind("relax_paged4_append"))(q, q_stride, k, v, kv_stride, q_out, prep, cache, seqs, dims, n, ws, ws_bytes, stream)
 
 
 def relax_paged4_attention(q: Ptr, cache: Optional[Paged4Cache], seqs: Optional[Seqs], dims: Optional[LayerDims], out: Ptr, n: int, ws: Ptr, ws_bytes: int,
                            stream=None) -> int:
-    cc = None if cache is None else cache.c()
-    sc = None if seqs is None else seqs.c()
-    return lib().relax_paged4_attention(_ptr(q), _ref(cc), _ref(sc), _ref(dims), _ptr(out), n, _ptr(ws), ws_bytes, _stream(stream))
+    return (_bound.get("relax_paged4_attention") or _bind("relax_paged4_attention"))(q, cache, seqs, dims, out, n, ws, ws_bytes, stream)
 
 
 def relax_paged4_read(cache: Optional[Paged4Cache], seqs: Optional[Seqs], dims: Optional[LayerDims], k_out: Ptr, v_out: Ptr, n: int, ws: Ptr, ws_bytes: int,
                       stream=None) -> int:
-    cc = None if cache is None else cache.c()
-    sc = None if seqs is None else seqs.c()
-    return lib().relax_paged4_read(_ref(cc), _ref(sc), _ref(dims), _ptr(k_out), _ptr(v_out), n, _ptr(ws), ws_bytes, _stream(stream))
+    return (_bound.get("relax_paged4_read") or _bind("relax_paged4_read"))(cache, seqs, dims, k_out, v_out, n, ws, ws_bytes, stream)
 
 
 def relax_token_logprobs_workspace_bytes(n_max: int, vocab: int, top: int) -> int:

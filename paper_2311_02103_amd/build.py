@@ -6,6 +6,7 @@ import re
 import shutil
 import subprocess
 import sys
+import sysconfig
 import tempfile
 from concurrent.futures import ThreadPoolExecutor
 
@@ -14,6 +15,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "librelax_mi355.so")
+MARSHAL = os.path.join(HERE, "_marshal.so")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
@@ -178,8 +180,17 @@ def _compile(src: str) -> str:
     return obj
 
 
+def build_marshal() -> str:
+    """The Python extension of csrc/marshal.c (host code alone)."""
+    cmd = [os.environ.get("CC", "gcc"), "-O2", "-Wall", "-shared", "-fPIC", "-I" + sysconfig.get_paths()["include"], "-I" + os.path.join(ROOT, "include"),
+           "-o", MARSHAL, os.path.join(CSRC, "marshal.c")]
+    subprocess.run(cmd, check=True)
+    return MARSHAL
+
+
 def build(verbose: bool = True) -> str:
     os.makedirs(OBJ, exist_ok=True)
+    build_marshal()
     with ThreadPoolExecutor(max_workers=min(8, len(sources()))) as pool:
         objs = list(pool.map(_compile, sources()))
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + objs

@@ -1,0 +1,297 @@
+/* Argument marshalling of binding.py's calls, as a CPython extension: what ctypes does with a call of fifteen arguments, and building a descriptor, took longer than the library's own
+ * part of the call and the launch together.
+ *
+ *   Call(address, kinds)(*args) -> int      calls the C function at `address`, which takes integers and pointers alone and returns an int32; `kinds` has a letter per argument
+ *     p  a pointer to device memory: None, an address, or a tensor (contiguous: its data_ptr())
+ *     i  an integer
+ *     r  a pointer to a struct: None, a Seqs, a ctypes structure, or an object whose _at is an address
+ *     s  a stream: None (the current one), an address, or an object whose cuda_stream is one
+ *   Seqs(q_lens, kv_lens, slots, device_table)      relax_seqs with arrays of its own
+ */
+#define PY_SSIZE_T_CLEAN
+#include <Python.h>
+#include <stddef.h>
+#include <stdint.h>
+#include <structmember.h>
+
+#include "relax_mi355.h"
+
+#define MAX_ARGS 16
+
+static PyObject *str_data_ptr, *str_is_contiguous, *str_at, *str_cuda_stream;
+static PyObject *get_device, *get_stream;       /* torch's, once it has initialised a device */
+static PyObject *slow_stream;                   /* binding._stream */
+
+/* ---- descriptor -------------------------------------------------------------------------------------------------- */
+typedef struct {
+    PyObject_HEAD
+    relax_seqs c;
+    int32_t *lens;
+    PyObject *table;
+} Seqs;
+
+static int pointer_of(PyObject *o, void **out)
+{
+    if (o == Py_None) {
+        *out = NULL;
+        return 0;
+    }
+    if (PyLong_Check(o)) {
+        *out = PyLong_AsVoidPtr(o);
+        return *out == NULL && PyErr_Occurred() ? -1 : 0;
+    }
+    PyObject *r = PyObject_CallMethodNoArgs(o, str_is_contiguous);
+    if (!r) return -1;
+    const int yes = PyObject_IsTrue(r);
+    Py_DECREF(r);
+    if (yes < 0) return -1;
+    if (!yes) {
+        PyErr_SetString(PyExc_ValueError, "tensor must be contiguous");
+        return -1;
+    }
+    r = PyObject_CallMethodNoArgs(o, str_data_ptr);
+    if (!r) return -1;
+    *out = PyLong_AsVoidPtr(r);
+    Py_DECREF(r);
+    return *out == NULL && PyErr_Occurred() ? -1 : 0;
+}
+
+/* int32 of a number, wrapped as ctypes wraps it */
+static int int32_of(PyObject *o, int32_t *out)
+{
+    PyObject *i = PyLong_Check(o) ? Py_NewRef(o) : PyNumber_Long(o);
+    if (!i) return -1;
+    const unsigned long long v = PyLong_AsUnsignedLongLongMask(i);
+    Py_DECREF(i);
+    if (v == (unsigned long long)-1 && PyErr_Occurred()) return -1;
+    *out = (int32_t)v;
+    return 0;
+}
+
+static void seqs_clear(Seqs *s)
+{
+    PyMem_Free(s->lens);
+    s->lens = NULL;
+    Py_CLEAR(s->table);
+    s->c = (relax_seqs){0};
+}
+
+static int seqs_init(Seqs *s, PyObject *args, PyObject *kw)
+{
+    static char *names[] = {"q_lens", "kv_lens", "slots", "device_table", NULL};
+    PyObject *given[3] = {NULL, NULL, Py_None}, *table = Py_None, *list[3] = {NULL, NULL, NULL};
+    if (!PyArg_ParseTupleAndKeywords(args, kw, "OO|OO", names, &given[0], &given[1], &given[2], &table)) return -1;
+    int ok = 0;
+    Py_ssize_t n[3] = {0, 0, 0}, all = 0;
+    for (int k = 0; k < 3; ++k) {
+        if (k == 2 && given[k] == Py_None) continue;
+        list[k] = PySequence_Fast(given[k], "lengths and slots are sequences of integers");
+        if (!list[k]) goto done;
+        n[k] = PySequence_Fast_GET_SIZE(list[k]);
+        all += n[k];
+        if (n[k] > INT32_MAX || n[k] < n[0]) {
+            PyErr_SetString(PyExc_ValueError, "a length and a slot for each sequence");
+            goto done;
+        }
+    }
+    int32_t *lens = PyMem_Malloc((size_t)(all + 1) * sizeof(int32_t)), *at = lens;
+    if (!lens) {
+        PyErr_NoMemory();
+        goto done;
+    }
+    const int32_t *start[3] = {NULL, NULL, NULL};
+    for (int k = 0; k < 3; ++k) {
+        if (!list[k]) continue;
+        start[k] = at;
+        /* (the sequence is asked for its items one by one: converting one may change it) */
+        for (Py_ssize_t i = 0; i < n[k]; ++i) {
+            PyObject *item = i < PySequence_Fast_GET_SIZE(list[k]) ? Py_NewRef(PySequence_Fast_GET_ITEM(list[k], i)) : NULL;
+            const int bad = !item || int32_of(item, at++) < 0;
+            Py_XDECREF(item);
+            if (bad) {
+                if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, "the sequence changed");
+                PyMem_Free(lens);
+                goto done;
+            }
+        }
+    }
+    void *device = NULL;
+    if (pointer_of(table, &device) < 0) {
+        PyMem_Free(lens);
+        goto done;
+    }
+    seqs_clear(s);
+    s->lens = lens;
+    s->table = Py_NewRef(table);
+    s->c = (relax_seqs){(int32_t)n[0], start[0], start[1], start[2], device};
+    ok = 1;
+done:
+    for (int k = 0; k < 3; ++k) Py_XDECREF(list[k]);
+    return ok ? 0 : -1;
+}
+
+static void seqs_dealloc(Seqs *s)
+{
+    seqs_clear(s);
+    Py_TYPE(s)->tp_free((PyObject *)s);
+}
+
+static PyObject *seqs_at(Seqs *s, void *unused) { return PyLong_FromVoidPtr(&s->c); }
+static PyObject *seqs_B(Seqs *s, void *unused) { return PyLong_FromLong(s->c.B); }
+static PyGetSetDef seqs_get[] = {{"_at", (getter)seqs_at, NULL, "address of the struct", NULL}, {"B", (getter)seqs_B, NULL, "number of sequences", NULL}, {0}};
+static PyTypeObject SeqsType = {
+    PyVarObject_HEAD_INIT(NULL, 0).tp_name = "_marshal.Seqs",
+    .tp_basicsize = sizeof(Seqs),
+    .tp_flags = Py_TPFLAGS_DEFAULT | Py_TPFLAGS_BASETYPE,
+    .tp_new = PyType_GenericNew,
+    .tp_init = (initproc)seqs_init,
+    .tp_dealloc = (destructor)seqs_dealloc,
+    .tp_getset = seqs_get,
+};
+
+/* ---- calls ------------------------------------------------------------------------------------------------------- */
+typedef struct {
+    PyObject_HEAD
+    vectorcallfunc vectorcall;
+    void *fn;
+    int count;
+    char kinds[MAX_ARGS + 1];
+} Call;
+
+static int struct_of(PyObject *o, void **out)
+{
+    if (o == Py_None) {
+        *out = NULL;
+        return 0;
+    }
+    if (PyObject_TypeCheck(o, &SeqsType)) {
+        *out = &((Seqs *)o)->c;
+        return 0;
+    }
+    if (PyObject_CheckBuffer(o)) {              /* (its owner holds it for the length of the call) */
+        Py_buffer view;
+        if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) < 0) return -1;
+        *out = view.buf;
+        PyBuffer_Release(&view);
+        return 0;
+    }
+    PyObject *r = PyObject_GetAttr(o, str_at);
+    if (!r) return -1;
+    *out = PyLong_AsVoidPtr(r);
+    Py_DECREF(r);
+    return *out == NULL && PyErr_Occurred() ? -1 : 0;
+}
+
+static int stream_of(PyObject *o, void **out)
+{
+    PyObject *r;
+    if (PyLong_Check(o)) r = Py_NewRef(o);
+    else if (o != Py_None) r = PyObject_GetAttr(o, str_cuda_stream);
+    else if (get_stream) {
+        PyObject *device = PyObject_CallNoArgs(get_device);
+        r = device ? PyObject_CallOneArg(get_stream, device) : NULL;
+        Py_XDECREF(device);
+    } else r = PyObject_CallOneArg(slow_stream, Py_None);
+    if (!r) return -1;
+    *out = r == Py_None ? NULL : PyLong_AsVoidPtr(r);
+    Py_DECREF(r);
+    return *out == NULL && PyErr_Occurred() ? -1 : 0;
+}
+
+static PyObject *call_run(Call *self, PyObject *const *args, size_t flags, PyObject *names)
+{
+    if (PyVectorcall_NARGS(flags) != self->count || (names && PyTuple_GET_SIZE(names))) {
+        PyErr_Format(PyExc_TypeError, "%d positional arguments", self->count);
+        return NULL;
+    }
+    void *a[MAX_ARGS] = {0};
+    for (int i = 0; i < self->count; ++i) {
+        int bad = 0;
+        switch (self->kinds[i]) {
+        case 'p': bad = pointer_of(args[i], &a[i]); break;
+        case 'r': bad = struct_of(args[i], &a[i]); break;
+        case 's': bad = stream_of(args[i], &a[i]); break;
+        default: {
+            const long long v = PyLong_AsLongLong(args[i]);
+            bad = v == -1 && PyErr_Occurred() ? -1 : 0;
+            a[i] = (void *)(intptr_t)v;
+        }
+        }
+        if (bad < 0) return NULL;
+    }
+    int32_t rc;
+    /* arguments of this class are passed alike whatever their width, and a function does not look at those behind its last */
+    typedef int32_t (*fn_t)(void *, void *, void *, void *, void *, void *, void *, void *, void *, void *, void *, void *, void *, void *, void *, void *);
+    Py_BEGIN_ALLOW_THREADS
+    rc = ((fn_t)self->fn)(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[11], a[12], a[13], a[14], a[15]);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+static PyObject *call_new(PyTypeObject *type, PyObject *args, PyObject *kw)
+{
+    PyObject *address;
+    const char *kinds;
+    if (!PyArg_ParseTuple(args, "Os", &address, &kinds)) return NULL;
+    const size_t count = strlen(kinds);
+    void *fn = PyLong_AsVoidPtr(address);
+    if (PyErr_Occurred()) return NULL;
+    if (!fn || count > MAX_ARGS || strspn(kinds, "pirs") != count) {
+        PyErr_SetString(PyExc_ValueError, "an address and at most 16 of the letters p, i, r, s");
+        return NULL;
+    }
+    Call *self = (Call *)type->tp_alloc(type, 0);
+    if (!self) return NULL;
+    self->vectorcall = (vectorcallfunc)call_run;
+    self->fn = fn;
+    self->count = (int)count;
+    memcpy(self->kinds, kinds, count + 1);
+    return (PyObject *)self;
+}
+
+static PyTypeObject CallType = {
+    PyVarObject_HEAD_INIT(NULL, 0).tp_name = "_marshal.Call",
+    .tp_basicsize = sizeof(Call),
+    .tp_flags = Py_TPFLAGS_DEFAULT | Py_TPFLAGS_HAVE_VECTORCALL,
+    .tp_new = call_new,
+    .tp_call = PyVectorcall_Call,
+    .tp_vectorcall_offset = offsetof(Call, vectorcall),
+};
+
+static PyObject *use_streams(PyObject *module, PyObject *args)
+{
+    PyObject *device, *stream;
+    if (!PyArg_ParseTuple(args, "OO", &device, &stream)) return NULL;
+    Py_XSETREF(get_device, Py_NewRef(device));
+    Py_XSETREF(get_stream, Py_NewRef(stream));
+    Py_RETURN_NONE;
+}
+static PyObject *set_slow_stream(PyObject *module, PyObject *f)
+{
+    Py_XSETREF(slow_stream, Py_NewRef(f));
+    Py_RETURN_NONE;
+}
+
+static PyMethodDef methods[] = {
+    {"use_streams", use_streams, METH_VARARGS, "use_streams(current_device, current_raw_stream): what a stream of None asks"},
+    {"slow_stream", set_slow_stream, METH_O, "what a stream of None asks before use_streams"},
+    {0},
+};
+static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, .m_name = "_marshal", .m_size = -1, .m_methods = methods};
+
+PyMODINIT_FUNC PyInit__marshal(void)
+{
+    str_data_ptr = PyUnicode_InternFromString("data_ptr");
+    str_is_contiguous = PyUnicode_InternFromString("is_contiguous");
+    str_at = PyUnicode_InternFromString("_at");
+    str_cuda_stream = PyUnicode_InternFromString("cuda_stream");
+    slow_stream = Py_NewRef(Py_None);
+    if (!str_data_ptr || !str_is_contiguous || !str_at || !str_cuda_stream || PyType_Ready(&SeqsType) < 0 || PyType_Ready(&CallType) < 0) return NULL;
+    PyObject *m = PyModule_Create(&module);
+    if (!m) return NULL;
+    if (PyModule_AddObjectRef(m, "Seqs", (PyObject *)&SeqsType) < 0 || PyModule_AddObjectRef(m, "Call", (PyObject *)&CallType) < 0) {
+        Py_DECREF(m);
+        return NULL;
+    }
+    return m;
+}

@@ -1,0 +1,142 @@
+"""Argument marshalling in C (csrc/marshal.c) against a recording C function, and against the same in Python."""
+import ctypes as C
+import gc
+import sys
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2311_02103_amd import binding as rx
+
+marshal = pytest.importorskip("paper_2311_02103_amd._marshal")
+
+
+class Recorder:
+    def __init__(self, count, result=0):
+        self.got = []
+        self.fn = C.CFUNCTYPE(C.c_int32, *[C.c_int64] * count)(lambda *a: self.got.append(a) or result)
+        self.address = C.cast(self.fn, C.c_void_p).value
+
+
+class At:
+    def __init__(self, at):
+        self._at = at
+
+
+class Stream:
+    def __init__(self, address):
+        self.cuda_stream = address
+
+
+def descriptor(seqs):
+    c = seqs.c()
+    take = lambda p: None if not p else [p[i] for i in range(c.B)]
+    return c.B, take(c.q_lens), take(c.kv_lens), take(c.slots), c.device_table
+
+
+def test_every_kind_of_argument():
+    rec = Recorder(15, -3)
+    call = marshal.Call(rec.address, "ppppiiiirrrrsss")
+    t, seqs, dims = torch.zeros(7, dtype=torch.float16), rx.Seqs([1], [2]), rx.make_dims(64, 1, 1, 64, 64, 8)
+    cache = rx.Paged4Cache(1, 2, 3, 4, 5, 1, 16, 1)
+    args = (None, 0x7fffffff0000, t, 0, -5, 1 << 40, np.int64(7), True, None, seqs, dims, cache, 0x1230, Stream(0x4560), Stream(0))
+    assert call(*args) == -3
+    assert rec.got == [(0, 0x7fffffff0000, t.data_ptr(), 0, -5, 1 << 40, 7, 1, 0, seqs._at, C.addressof(dims), cache._at, 0x1230, 0x4560, 0)]
+    assert marshal.Call(Recorder(0, 9).address, "")() == 9
+
+
+def test_what_it_refuses():
+    rec = Recorder(3)
+    call = marshal.Call(rec.address, "pir")
+    for args, error in (((None, 1), TypeError), ((None, 1, None, None), TypeError), ((None, 1.5, None), TypeError), ((None, "1", None), TypeError),
+                        ((torch.zeros(4, 4)[:, :2], 1, None), ValueError), ((object(), 1, None), AttributeError), ((None, 1, object()), AttributeError),
+                        ((None, 1 << 70, None), OverflowError), ((1 << 70, 1, None), OverflowError), ((None, 1, At("x")), TypeError)):
+        with pytest.raises(error):
+            call(*args)
+    with pytest.raises(TypeError):
+        call(None, 1, None, stream=None)
+    assert not rec.got
+    for bad in ((0, "p"), (rec.address, "x"), (rec.address, "p" * 17)):
+        with pytest.raises(ValueError):
+            marshal.Call(*bad)
+
+
+def test_a_stream_of_none_asks_for_the_current_one():
+    rec = Recorder(1)
+    code = "import sys; sys.path.insert(0, %r)\nfrom paper_2311_02103_amd import _marshal as m\nimport ctypes as C\ngot = []\n" % rx._HERE.rsplit("/", 1)[0]
+    code += "f = C.CFUNCTYPE(C.c_int32, C.c_int64)(lambda a: got.append(a) or 0)\ncall = m.Call(C.cast(f, C.c_void_p).value, 's')\n"
+    code += "m.slow_stream(lambda s: 5 if s is None else 1)\ncall(None)\nm.slow_stream(lambda s: None)\ncall(None)\n"
+    code += "m.use_streams(lambda: 3, lambda d: d * 16)\ncall(None)\nm.use_streams(lambda: 3, lambda d: 0)\ncall(None)\nassert got == [5, 0, 48, 0], got\n"
+    import subprocess
+    subprocess.run([sys.executable, "-c", code], check=True, timeout=120)
+    del rec
+
+
+@pytest.mark.parametrize("kind", [rx._PySeqs, rx.Seqs])
+def test_descriptors(kind):
+    take = descriptor if kind is rx.Seqs else lambda s: (s.c().B, list(s._q), list(s._kv)[:s.B], None if s._sl is None else list(s._sl), s.c().device_table)
+    table = torch.zeros(8, dtype=torch.int32)
+    assert take(kind([3, 1], [3, 900])) == (2, [3, 1], [3, 900], None, None)
+    assert take(kind((3, 1), np.array([3, 900]), slots=[7, 2], device_table=table)) == (2, [3, 1], [3, 900], [7, 2], table.data_ptr())
+    assert take(kind([True], [(1 << 32) + 5], None, 0x1000)) == (1, [1], [5], None, 0x1000)
+    assert take(kind([], [])) == (0, [], [], None, None) and kind([1], [2]).B == 1
+    assert take(kind([1], [2, 3], [4, 5]))[:3] == (1, [1], [2])
+    for bad in (([1, 2], [1]), ([1, 2], [1, 2], [0])):
+        with pytest.raises(ValueError):
+            kind(*bad)
+    for bad in (([1], 5), (["x"], [1]), ([1], [None])):
+        with pytest.raises((TypeError, ValueError)):
+            kind(*bad)
+
+
+def test_descriptors_hold_their_memory_and_the_table():
+    table = torch.zeros(8, dtype=torch.int32)
+    before = sys.getrefcount(table)
+    seqs = rx.Seqs(list(range(1, 50)), list(range(100, 149)), device_table=table)
+    assert sys.getrefcount(table) == before + 1
+    c = seqs.c()
+    del seqs
+    gc.collect()
+    junk = [rx.Seqs([9] * 49, [9] * 49) for _ in range(100)]
+    assert [c.q_lens[i] for i in range(49)] == list(range(1, 50)) and [c.kv_lens[i] for i in range(49)] == list(range(100, 149))
+    del c, junk
+    gc.collect()
+    assert sys.getrefcount(table) == before
+    with pytest.raises(ValueError):
+        rx.Seqs([1], [1], None, torch.zeros(4, 4, dtype=torch.int32)[:, :2])
+    assert sys.getrefcount(table) == before
+
+
+def test_no_reference_is_lost():
+    rec = Recorder(4)
+    call = marshal.Call(rec.address, "ppsr")
+    t, at, stream = torch.zeros(3), At(123456789), Stream(987654321)
+    before = [sys.getrefcount(x) for x in (t, at, stream, None)]
+    for _ in range(1000):
+        call(t, t, stream, at)
+    rec.got.clear()
+    after = [sys.getrefcount(x) for x in (t, at, stream, None)]
+    assert after[:3] == before[:3] and abs(after[3] - before[3]) < 100
+
+
+def test_the_python_form_says_the_same(monkeypatch):
+    """The library's own refusals through both."""
+    dims, cache, prep, P = rx.make_dims(256, 4, 4, 64, 688, 64, 2), rx.Paged4Cache(*[0x10000] * 5, 10, 16, 4), rx.HeadPrep(0x10000, 0x10000, 1e-6, 0x10000), 0x10000
+    t = torch.zeros(512, dtype=torch.float16)
+
+    def codes():
+        out = []
+        for s in (rx.Seqs([2], [5]), rx.Seqs([2], [65]), None):
+            for d in (dims, None):
+                out += [rx.relax_paged4_append(P, 256, P, P, 256, P, prep, cache, s, d, 2, P, 8), rx.relax_paged4_attention(t.data_ptr() // 16 * 16, cache, s, d, P, 2, P, 8, stream=0),
+                        rx.relax_paged4_read(cache, s, d, P, None, 2, P, 8, stream=Stream(0)), rx.relax_head_norm_rope(P, 256, None, 0, P, 256, None, 0, prep, s, d, 2, P, 8)]
+        return out + [rx.relax_rope_table_scaled(rx.RopeScaling(7, 64), 4, P), rx.relax_rope_table_scaled(None, 4, P)]
+    monkeypatch.setattr(rx, "_bound", {})
+    fast = codes()
+    monkeypatch.setattr(rx, "_bound", {})
+    monkeypatch.setattr(rx, "_marshal", None)
+    assert codes() == fast and len(set(fast)) >= 4
+    with pytest.raises(TypeError):
+        rx._bound["relax_paged4_read"](1, 2)
