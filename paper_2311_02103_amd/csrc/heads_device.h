@@ -48,8 +48,21 @@ typedef half8p_t Unit;               // eight elements of a head
 template <int D>
 constexpr int kUnits = D / 8;        // lanes of a head
 
-// what of an input is quantised: the ends of fp16's range for infinities, 0 for a NaN
-__device__ __forceinline__ float storable4(float x) { return x == x ? fminf(fmaxf(x, -65504.0f), 65504.0f) : 0.0f; }
+// What of a unit is quantised: the ends of fp16's range for infinities, 0 for a NaN.  A look at all eight (x * 0 is a NaN for either) costs less than treating each
+__device__ __forceinline__ void to_storable(const Unit &in, float (&x)[8])
+{
+    const half2p_t zero = {(_Float16)0.0f, (_Float16)0.0f};
+    half2p_t t = zero;
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) t = __builtin_elementwise_fma(half2p_t{in[i], in[i + 1]}, zero, t);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = (float)in[i];
+    const float bad = (float)t.x + (float)t.y;
+    if (__any(bad != bad)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = x[i] == x[i] ? fminf(fmaxf(x[i], -65504.0f), 65504.0f) : 0.0f;
+    }
+}
 
 template <int OFF>
 __device__ __forceinline__ double lane_xor(double v)
@@ -57,6 +70,15 @@ __device__ __forceinline__ double lane_xor(double v)
     const uint64_t u = __builtin_bit_cast(uint64_t, v);
     const float lo = lane_xor<OFF>(__builtin_bit_cast(float, (uint32_t)u)), hi = lane_xor<OFF>(__builtin_bit_cast(float, (uint32_t)(u >> 32)));
     return __builtin_bit_cast(double, (uint64_t)__builtin_bit_cast(uint32_t, hi) << 32 | __builtin_bit_cast(uint32_t, lo));
+}
+
+// 1 / sqrt(ms) rounded once to fp32: the hardware's estimate (2^-23) and two steps of Newton's method in fp64 (2^-45, then fp64's own 2^-52), a sixth of the instructions of a square root and
+// a division.  0 for infinity and for 0
+__device__ __forceinline__ float rsqrt_once(double ms)
+{
+    const double r0 = (double)__builtin_amdgcn_rsqf((float)ms), half = 0.5 * ms;
+    const double r1 = r0 * __builtin_fma(-half * r0, r0, 1.5), r2 = r1 * __builtin_fma(-half * r1, r1, 1.5);
+    return ms > 0.0 && ms < __builtin_inf() ? (float)r2 : ms == ms ? 0.0f : __builtin_nanf("");
 }
 
 // x *= w / sqrt(mean square + eps) over the lanes of a head
@@ -71,8 +93,7 @@ __device__ __forceinline__ void normalise(float (&x)[8], const Unit &w, float ep
     sum += lane_xor<2>(sum);
     sum += lane_xor<4>(sum);
     if (D == 128) sum += lane_xor<8>(sum);
-    const double ms = sum * (1.0 / D) + (double)eps;
-    const float r = ms > 0.0 ? (float)(1.0 / __builtin_sqrt(ms)) : ms == 0.0 ? 0.0f : __builtin_nanf("");
+    const float r = rsqrt_once(sum * (1.0 / D) + (double)eps);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const float y = x[j] * r;
@@ -80,7 +101,8 @@ __device__ __forceinline__ void normalise(float (&x)[8], const Unit &w, float ep
     }
 }
 
-// The angles of a lane's unit at one position: (cos, sin) of the eight pairs that its elements belong to (halves), of its four pairs (neighbours)
+// The angles of a lane's unit at one position: (cos, sin) of its four pairs (neighbours), of the eight pairs that its elements belong to (halves; the sines of the first half's negated, so that
+// either element is x cos + other sin)
 struct Angles {
     float4p_t cs[4];
 };
@@ -94,6 +116,8 @@ __device__ __forceinline__ void load_angles(Angles &a, const HeadPrep &p, int po
     if (!p.pairs) {
 #pragma unroll
         for (int i = 2; i < 4; ++i) a.cs[i] = src[i];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a.cs[i].y = unit < low ? -a.cs[i].y : a.cs[i].y, a.cs[i].w = unit < low ? -a.cs[i].w : a.cs[i].w;
     }
 }
 
@@ -102,33 +126,36 @@ template <int D>
 __device__ __forceinline__ void rotate(float (&x)[8], const Angles &a, const HeadPrep &p, int unit, int lane)
 {
 #pragma clang fp contract(off)
-    const bool turns = unit * 8 < p.rot;
+    float z[8];
     if (p.pairs) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const float c = a.cs[j >> 1][(j & 1) * 2], s = a.cs[j >> 1][(j & 1) * 2 + 1];
             const float ac = x[2 * j] * c, bs = x[2 * j + 1] * s, as = x[2 * j] * s, bc = x[2 * j + 1] * c;
-            x[2 * j] = turns ? ac - bs : x[2 * j], x[2 * j + 1] = turns ? as + bc : x[2 * j + 1];
+            z[2 * j] = ac - bs, z[2 * j + 1] = as + bc;
         }
-        return;
-    }
-    const int low = p.rot >> 4;
-    const bool first = unit < low;
-    float y[8];
-    if (p.rot == D) {                                          // uniform
-#pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = lane_xor<D / 16>(x[j]);
     } else {
-        const int from = turns ? (first ? lane + low : lane - low) : lane;
+        float y[8];
+        if (p.rot == D) {                                      // uniform
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = __shfl(x[j], from, kWave);
+            for (int j = 0; j < 8; ++j) y[j] = lane_xor<D / 16>(x[j]);
+        } else {
+            const int low = p.rot >> 4, from = unit * 8 < p.rot ? (unit < low ? lane + low : lane - low) : lane;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) y[j] = __shfl(x[j], from, kWave);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float own = x[j] * a.cs[j >> 1][(j & 1) * 2], other = y[j] * a.cs[j >> 1][(j & 1) * 2 + 1];
+            z[j] = own + other;
+        }
     }
+    if (p.rot == D) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const float c = a.cs[j >> 1][(j & 1) * 2], s = a.cs[j >> 1][(j & 1) * 2 + 1];
-        const float own = x[j] * c, other = y[j] * s;
-        const float turned = first ? own - other : other + own;
-        x[j] = turns ? turned : x[j];
+        for (int j = 0; j < 8; ++j) x[j] = z[j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = unit * 8 < p.rot ? z[j] : x[j];
     }
 }
 
@@ -174,7 +201,8 @@ __device__ __forceinline__ void head_rows(SeqsArg st, const HeadRows &r, const H
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = (float)in[j];
         const bool isq = hd < h;
-        if (p.q_norm || p.k_norm) {
+        if (p.q_norm && p.k_norm) normalise<D>(x, isq ? wq : wk, p.eps);
+        else if (p.q_norm || p.k_norm) {
             float y[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[j] = x[j];
@@ -194,12 +222,13 @@ __device__ __forceinline__ void head_rows(SeqsArg st, const HeadRows &r, const H
     }
 }
 
-// wavefronts per row of head_rows: enough of them for few rows, few heads per wavefront never more than there are
+// wavefronts per row of head_rows: one per step of heads for few rows, few for many, whose angles and positions then serve more heads (us for 2043 rows of 32 / 8 heads with 2048, 4096 and
+// 8192 wavefronts wanted: 11.2, 11.5, 13.0)
 inline int head_slices(int heads, int n, int d)
 {
     const int steps = (heads * d / 8 + kWave - 1) / kWave;     // of one row
     int slices = 1;
-    while (slices < steps && (int64_t)n * slices < 8192) slices *= 2;
+    while (slices < steps && (int64_t)n * slices < 2048) slices *= 2;
     return slices < steps ? slices : steps;
 }
 

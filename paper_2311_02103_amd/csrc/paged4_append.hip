@@ -33,20 +33,30 @@ __device__ __forceinline__ _Float16 scale_of(float top, float low)
     const float r = __builtin_bit_cast(float, (u + 0x7fffu + (u >> 16 & 1u)) & 0xffff0000u);
     return (_Float16)fminf(fmaxf(r, -8160.0f), 8160.0f);
 }
-// rne(x / s) in -8..7 as 0..15, inv the reciprocal of s within 2^-23.  x - a s is exact (a has 24 bits, s eight), so q is the quotient rounded once, but for 2^-22 of its last bit;
-// and a quotient that is no tie is at least 0.501 of its last bit away from one, because s has eight bits: no value goes to the wrong side
-__device__ __forceinline__ uint32_t code4(float x, float s, float inv)
-{
-    const float a = x * inv, q = fmaf(fmaf(-a, s, x), inv, a);
-    return (uint32_t)((int)fminf(fmaxf(rintf(q), -8.0f), 7.0f) + 8);
-}
-__device__ __forceinline__ void codes_of(const float (&x)[8], float s, uint32_t (&u)[8])
+// rne(x / s) in -8..7 plus 8, of eight elements, four to a number: d0 = sum over j of the codes of elements i_j times 16^j, exact in fp32.
+// x - a s is exact (a has 24 bits, s eight), inv the reciprocal of s within 2^-23, so q is the quotient rounded once but for 2^-22 of its last bit; and a quotient that is no tie is at least
+// 0.501 of its last bit away from one, because s has eight bits: no value goes to the wrong side.  (The bounds are whole numbers: they may go in front of the rounding.)
+__device__ __forceinline__ void codes_of(const float (&x)[8], float s, float (&c)[8])
 {
     const float inv = s != 0.0f ? __builtin_amdgcn_rcpf(s) : 0.0f;      // (a scale of 0: all codes 8)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) u[j] = code4(x[j], s, inv);
+    for (int j = 0; j < 8; ++j) {
+        const float a = x[j] * inv, q = fmaf(fmaf(-a, s, x[j]), inv, a);
+        c[j] = rintf(__builtin_amdgcn_fmed3f(q, -8.0f, 7.0f));
+    }
+}
+__device__ __forceinline__ uint32_t digits(float a, float b, float c, float d)      // nibbles a b c d, each plus 8
+{
+    return (uint32_t)fmaf(fmaf(fmaf(d, 16.0f, c), 16.0f, b), 16.0f, a + (float)0x8888);
 }
 __device__ __forceinline__ uint32_t dword_dpp_xor2(uint32_t v) { return __builtin_bit_cast(uint32_t, lane_xor<2>(__builtin_bit_cast(float, v))); }
+
+// four nibbles to the low halves of four bytes
+__device__ __forceinline__ uint32_t spread(uint32_t v)
+{
+    const uint32_t w = (v | v << 8) & 0x00ff00ffu;
+    return (w | w << 4) & 0x0f0f0f0fu;
+}
 
 // the dwords that the lanes with the same l % 16 hold, by l / 16
 __device__ __forceinline__ void gather_quarters(uint32_t v, uint32_t (&w)[4])
@@ -109,8 +119,7 @@ __global__ __launch_bounds__(256) void paged4_append_kernel(PagedSeqs, HeadRows 
         Unit ahead = in;
         if (hd + HS < end) ahead = *(const Unit *)(src + min(hd + HS + sub, g - 1) * D);
         float x[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = storable4((float)in[i]);
+        to_storable(in, x);
         if (!values) {
             if (p.k_norm) normalise<D>(x, wk, p.eps);
             if (p.rope) rotate<D>(x, a, p, unit, lane);
@@ -121,20 +130,22 @@ __global__ __launch_bounds__(256) void paged4_append_kernel(PagedSeqs, HeadRows 
         top = fmaxf(top, lane_xor<1>(top)), bottom = fminf(bottom, lane_xor<1>(bottom));
         top = fmaxf(top, lane_xor<2>(top)), bottom = fminf(bottom, lane_xor<2>(bottom));
         const _Float16 s = scale_of(top, bottom);
-        uint32_t u[8];
-        codes_of(x, (float)s, u);
+        float c[8];
+        codes_of(x, (float)s, c);
         const int kvh = hd + sub;
         const bool there = kvh < g;
         const size_t blk = (size_t)pool + ((size_t)kvh << pa.shift);
         if (!values) {
-            const uint32_t w = u[0] | u[1] << 16 | u[2] << 4 | u[3] << 20 | u[4] << 8 | u[5] << 24 | u[6] << 12 | u[7] << 28;
+            const uint32_t w = digits(c[0], c[2], c[4], c[6]) | digits(c[1], c[3], c[5], c[7]) << 16;
             if (fresh && there) ((uint32_t *)(pa.k + blk * block4_codes(D)))[((unit & 3) * 16 + t16) * J + j] = w;
         } else {
             // lanes of elements below 16 of 32 and their partners above: bytes of elements 0 .. 3, resp. 4 .. 7, of the eight
-            const uint32_t mine = u[0] | u[1] << 8 | u[2] << 16 | u[3] << 24, rest = u[4] | u[5] << 8 | u[6] << 16 | u[7] << 24;
             const bool above = unit & 2;
-            const uint32_t given = dword_dpp_xor2(above ? mine : rest);
-            const uint32_t bytes = above ? given | rest << 4 : mine | given << 4;
+            const uint32_t mine = digits(c[0], c[1], c[2], c[3]), rest = digits(c[4], c[5], c[6], c[7]);
+            const uint32_t given = dword_dpp_xor2(above ? mine : rest), kept = above ? rest : mine;
+            // bytes of the four elements: the nibble of the lane below in the low half, of the lane above in the high one
+            const uint32_t lows = spread(above ? given : kept), highs = spread(above ? kept : given);
+            const uint32_t bytes = lows | highs << 4;
             uint32_t w4[4];
             gather_quarters(bytes, w4);
             const uint32_t sel = (uint32_t)quarter | (uint32_t)(quarter + 4) << 8;                     // byte `quarter` of either
@@ -227,8 +238,8 @@ hipError_t launch_paged4_append(const HeadRows &hr, const uint16_t *k, const uin
     int64_t quads = 0;
     for (int b = 0; b < sq.B; ++b) quads += st.q_max == 1 ? 1 : paged4_quads_of(sq.q_lens[b]);
     const int h = hr.q ? dm.n_heads : 0, g = dm.n_kv_heads, per_step = 16 * 8 / dm.head_dim, all_steps = (g + per_step - 1) / per_step;
-    int steps = 1;
-    while (steps < 4 && quads * (2 * ((all_steps + steps - 1) / steps)) > 16384) steps *= 2;
+    int steps = 1;                                             // of KV heads per wavefront (us, append and read-back of 2043 rows of 32 / 32 heads with 4096, 8192 and 16384 wavefronts: 25.6, 26.3, 29.5)
+    while (steps < 16 && quads * (2 * ((all_steps + steps - 1) / steps)) > 4096) steps *= 2;
     const int chunks = (all_steps + steps - 1) / steps, slices = h ? head_slices(h, st.n, dm.head_dim) : 1;
     const int64_t kv_groups = (quads * 2 * chunks + 3) / 4, q_groups = h ? ((int64_t)st.n * slices + 3) / 4 : 0;
     if ((kv_groups + q_groups) * 256 > kMaxThreads) return hipErrorInvalidValue;
