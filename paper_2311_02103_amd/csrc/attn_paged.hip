@@ -205,7 +205,7 @@ __global__ __launch_bounds__(64 * W, 4) void attn_paged_kernel(PagedSeqs, const 
 // groups of threads side by side and four of each in flight, and the groups' results meet in LDS
 template <int D>
 __global__ __launch_bounds__(256) void attn_paged_merge_kernel(PagedSeqs, const float *__restrict__ part, uint16_t *__restrict__ out, int h, int g, int cap,
-                                                               int chunk, int splits, int least, int direct)
+                                                               int chunk, int splits, int least)
 {
     constexpr int T = D / 4, F = 4;
     __shared__ __align__(16) float sums[256 / T][D];
@@ -220,10 +220,8 @@ __global__ __launch_bounds__(256) void attn_paged_merge_kernel(PagedSeqs, const 
     // the splits that the tile of this pair had: those of its last pair
     const int pairs = si.q_len * rep, pair = place * rep + hd % rep, last = min(pair | 15, pairs - 1) / rep;
     if (pairs >= least) return;                                // (not split: the other kernel's)
-    const int vis = beyond_capacity(si, cap) ? 0 : direct ? si.kv_len : si.kv_len - si.q_len + last + 1, used = min(max((vis + chunk - 1) / chunk, 1), splits);
-    if (used <= direct) return;                                // (written already)
-    const size_t at = direct ? (size_t)(si.q_start + place) * h + hd : i;
-    const float *src = part + at * splits * (D + 2);
+    const int vis = beyond_capacity(si, cap) ? 0 : si.kv_len - si.q_len + last + 1, used = min(max((vis + chunk - 1) / chunk, 1), splits);
+    const float *src = part + (size_t)i * splits * (D + 2);
     float mm = -INFINITY, den = 0.0f;
     float4p_t num = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int s0 = grp; s0 < used; s0 += groups * F) {
@@ -258,7 +256,7 @@ __global__ __launch_bounds__(256) void attn_paged_merge_kernel(PagedSeqs, const 
     }
     const float inv = den > 0.0f ? 1.0f / den : den;
     const uint32_t lo = f2h(num.x * inv) | (uint32_t)f2h(num.y * inv) << 16, hi = f2h(num.z * inv) | (uint32_t)f2h(num.w * inv) << 16;
-    *(u32x2p_t *)(out + at * D + e) = u32x2p_t{lo, hi};
+    *(u32x2p_t *)(out + (size_t)i * D + e) = u32x2p_t{lo, hi};
 }
 
 // Splits of a launch with `small` workgroups per split: from kUnsplit workgroups on none, below it as many as bring it to kPagedGroups workgroups, at most one
@@ -294,12 +292,16 @@ hipError_t launch_d(const uint16_t *q, const PagedArgs &pa, const relax_layer_di
     else
         hipLaunchKernelGGL((attn_paged_kernel<D, 4>), grid, dim3(256), 0, stream, st, q, pa, partials, out, dm.n_heads, dm.n_kv_heads, pl.per_seq, pl.chunk, pl.splits, pl.least);
     const hipError_t e = hipGetLastError();
-    return e != hipSuccess || pl.splits == 1 ? e : launch_paged_merge(pl, partials, out, dm, pa.cap, st, stream);
+    if (e != hipSuccess || pl.splits == 1) return e;
+    const int threads = pl.splits > 4 * 64 / (D / 4) ? 256 : 64;      // one round of four splits per group of threads, if that is enough
+    hipLaunchKernelGGL(attn_paged_merge_kernel<D>, dim3(st.n * dm.n_heads), dim3(threads), 0, stream, st, partials, out, dm.n_heads, dm.n_kv_heads, pa.cap,
+                       pl.chunk, pl.splits, pl.least);
+    return hipGetLastError();
 }
 
 }  // namespace
 
-PagedPlan paged_plan(const relax_layer_dims &dm, const relax_seqs &sq, int32_t n, int32_t L_max, bool rows)
+PagedPlan paged_plan(const relax_layer_dims &dm, const relax_seqs &sq, int32_t n, int32_t L_max)
 {
     const int rep = dm.n_heads / dm.n_kv_heads;
     auto pairs_of = [&](int b) { return (long long)sq.q_lens[b] * rep; };
@@ -307,7 +309,7 @@ PagedPlan paged_plan(const relax_layer_dims &dm, const relax_seqs &sq, int32_t n
     for (int b = 0; b < sq.B; ++b)
         if (pairs_of(b) >= kPagedRowTile) large += (pairs_of(b) + kPagedRowTile - 1) / kPagedRowTile;
     PagedPlan p;
-    p.least = rows && large * dm.n_kv_heads >= kRowTiles ? kPagedRowTile : INT32_MAX;
+    p.least = large * dm.n_kv_heads >= kRowTiles ? kPagedRowTile : INT32_MAX;
     long long small = 0, most_small = 0, most_large = 0;
     for (int b = 0; b < sq.B; ++b) {
         const long long pairs = pairs_of(b);
@@ -325,18 +327,6 @@ PagedPlan paged_plan(const relax_layer_dims &dm, const relax_seqs &sq, int32_t n
     p.splits = (L_max + p.chunk - 1) / p.chunk;
     p.waves = p.splits > 1 && p.chunk >= 256 ? 8 : 4;
     return p;
-}
-
-hipError_t launch_paged_merge(const PagedPlan &pl, const float *partials, uint16_t *out, const relax_layer_dims &dm, int32_t cap, const PagedSeqs &st, hipStream_t stream, int32_t rows)
-{
-    const int threads = pl.splits > 4 * 64 / (dm.head_dim / 4) ? 256 : 64;      // one round of four splits per group of threads, if that is enough
-    const dim3 grid((rows ? rows : st.n) * dm.n_heads);
-    const int direct = rows > 0;
-    if (dm.head_dim == 128)
-        hipLaunchKernelGGL(attn_paged_merge_kernel<128>, grid, dim3(threads), 0, stream, st, partials, out, dm.n_heads, dm.n_kv_heads, cap, pl.chunk, pl.splits, pl.least, direct);
-    else
-        hipLaunchKernelGGL(attn_paged_merge_kernel<64>, grid, dim3(threads), 0, stream, st, partials, out, dm.n_heads, dm.n_kv_heads, cap, pl.chunk, pl.splits, pl.least, direct);
-    return hipGetLastError();
 }
 
 // paged_plan() has splits <= ceil(L / 128) and, where it has more than one, n * heads * splits <= kPartials

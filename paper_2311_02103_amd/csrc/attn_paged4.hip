@@ -484,8 +484,77 @@ void longest_first(PagedSeqs &st)
     }
 }
 
+// out from the parts of the rows that have more than one: T * G threads per (row, head), a thread four elements of every G-th part.  The first F of them are asked for before the number of parts is
+// known (there is memory for all that a row could have), so that they do not wait for the descriptor.  all: every row of the call, in its order; else the first rows of st's sequences.
+template <int D, int G>
+__global__ __launch_bounds__(256) void attn_paged4_merge_kernel(PagedSeqs, const float *__restrict__ part, uint16_t *__restrict__ out, Grid gr, Divisor by_h, int count, int cap, int all)
+{
+    constexpr int T = D / 4, F = 4, P = 256 / (T * G);
+    __shared__ __align__(16) float sums[P][G][D];
+    __shared__ float sm_m[P][G], sm_l[P][G];
+    const SeqsArg st = seqs_arg();
+    const int tid = threadIdx.x, p = __builtin_amdgcn_readfirstlane(tid / (T * G)), grp = tid / T % G, e = tid % T * 4;
+    const int idx = min((int)blockIdx.x * P + p, count - 1), r = quotient(idx, by_h), hd = idx - r * gr.h;
+    float ms[F], ls[F];
+    float4p_t as[F];
+    const auto load = [&](const float *src, int s0, int most) {
+#pragma unroll
+        for (int j = 0; j < F; ++j) {
+            const float2 *q2 = (const float2 *)(src + (size_t)min(s0 + j * G, most) * (D + 2));
+            const float2 lo = q2[e / 2], hi = q2[e / 2 + 1], ml = q2[D / 2];
+            ms[j] = ml.x, ls[j] = ml.y, as[j] = float4p_t{lo.x, lo.y, hi.x, hi.y};
+        }
+    };
+    size_t at = idx;
+    if (all) load(part + at * gr.splits * (D + 2), grp, gr.splits - 1);
+    int place = 0, b = r;
+    if (st->q_max != 1) b = seq_of(st, r, [](int q_len) { return q_len; }, place);
+    const SeqSpan si = seq_span(st, __builtin_amdgcn_readfirstlane(min(b, st->B - 1)));
+    if (!all) {
+        at = (size_t)(si.q_start + place) * gr.h + hd;
+        load(part + at * gr.splits * (D + 2), grp, gr.splits - 1);
+    }
+    const int used = beyond_capacity(si, cap) || si.q_len * gr.rep >= gr.least ? 1 : min(max(quotient(si.kv_len + gr.chunk - 1, gr.by_chunk), 1), gr.splits);
+    float mm = -INFINITY, den = 0.0f;
+    float4p_t num = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s0 = grp;;) {
+        float mx = mm;
+#pragma unroll
+        for (int j = 0; j < F; ++j) mx = s0 + j * G < used ? fmaxf(mx, ms[j]) : mx;
+        const float ref = mx == -INFINITY ? 0.0f : mx, f0 = __builtin_amdgcn_exp2f(mm - ref);
+        den *= f0, num *= f0;
+#pragma unroll
+        for (int j = 0; j < F; ++j) {
+            const bool there = s0 + j * G < used;              // (memory that no part was written to may hold anything)
+            const float f = there ? __builtin_amdgcn_exp2f(ms[j] - ref) : 0.0f;
+            den += there ? ls[j] * f : 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) num[i] += there ? as[j][i] * f : 0.0f;
+        }
+        mm = mx;
+        s0 += G * F;
+        if (s0 - grp >= used) break;                           // uniform
+        load(part + at * gr.splits * (D + 2), s0, used - 1);
+    }
+    *(float4p_t *)&sums[p][grp][e] = num;
+    if (e == 0) sm_m[p][grp] = mm, sm_l[p][grp] = den;
+    __syncthreads();
+    if (grp > 0 || used <= 1 || (int)blockIdx.x * P + p >= count) return;      // (one part: written already)
+#pragma unroll
+    for (int w = 0; w < G; ++w) mm = fmaxf(mm, sm_m[p][w]);
+    num = float4p_t{0.0f, 0.0f, 0.0f, 0.0f}, den = 0.0f;
+#pragma unroll
+    for (int w = 0; w < G; ++w) {
+        const float f = sm_m[p][w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm_m[p][w] - mm);
+        num += *(const float4p_t *)&sums[p][w][e] * f, den += sm_l[p][w] * f;
+    }
+    const float inv = den > 0.0f ? 1.0f / den : den;
+    const uint32_t lo = f2h(num.x * inv) | (uint32_t)f2h(num.y * inv) << 16, hi = f2h(num.z * inv) | (uint32_t)f2h(num.w * inv) << 16;
+    *(u32x2p_t *)(out + at * D + e) = u32x2p_t{lo, hi};
+}
+
 template <int D>
-hipError_t launch_d(const uint16_t *q, const Paged4Args &pa, const relax_layer_dims &dm, const PagedSeqs &st, const PagedPlan &pl, const Cut &c, uint16_t *out, float *partials,
+hipError_t launch_d(const uint16_t *q, const Paged4Args &pa, const relax_layer_dims &dm, const PagedSeqs &call, const PagedSeqs &st, const PagedPlan &pl, const Cut &c, uint16_t *out, float *partials,
                     hipStream_t stream)
 {
     if (c.items * dm.n_kv_heads * 64 * c.waves > kMaxThreads) return hipErrorInvalidValue;
@@ -501,9 +570,15 @@ hipError_t launch_d(const uint16_t *q, const Paged4Args &pa, const relax_layer_d
     else c.few ? launch(std::true_type{}, four{}) : launch(std::false_type{}, four{});
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || c.rows == 0) return e;
-    PagedPlan parts = pl;
-    parts.chunk = c.chunk, parts.splits = c.splits;
-    return launch_paged_merge(parts, partials, out, dm, pa.cap, st, stream, c.rows);
+    const int all = c.rows == st.n, count = c.rows * dm.n_heads;
+    const PagedSeqs &rows = all ? call : st;
+    const auto merge = [&](auto G) {
+        constexpr int P = 256 / (D / 4 * G);
+        hipLaunchKernelGGL((attn_paged4_merge_kernel<D, G>), dim3((count + P - 1) / P), dim3(256), 0, stream, rows, partials, out, gr, divisor(dm.n_heads), count, pa.cap, all);
+    };
+    if (c.splits > 16) merge(std::integral_constant<int, 1024 / D>{});
+    else merge(std::integral_constant<int, 256 / D>{});
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -519,7 +594,7 @@ hipError_t launch_paged4_attention(const uint16_t *q, const Paged4Args &pa, cons
     const Cut c = cut(pl, dm, st, sq, L_max);
     PagedSeqs by_length = st;
     longest_first(by_length);
-    return dm.head_dim == 128 ? launch_d<128>(q, pa, dm, by_length, pl, c, out, partials, stream) : launch_d<64>(q, pa, dm, by_length, pl, c, out, partials, stream);
+    return dm.head_dim == 128 ? launch_d<128>(q, pa, dm, st, by_length, pl, c, out, partials, stream) : launch_d<64>(q, pa, dm, st, by_length, pl, c, out, partials, stream);
 }
 
 }  // namespace relax

@@ -136,10 +136,7 @@ struct PagedPlan {
     int32_t row_per_seq, per_seq;    // as tile_of takes them
     int32_t chunk, splits, waves;    // wavefronts per workgroup of 16-pair tiles
 };
-PagedPlan paged_plan(const relax_layer_dims &dm, const relax_seqs &sq, int32_t n, int32_t L_max, bool rows = true);      // rows: there are tiles of 256 pairs
-// out of the partial results [row][head][splits][d + 2] of the 16-pair tiles: d sums, the reference of the weights (log2), the sum of the weights
-// rows > 0: of the first `rows` rows of the call alone, in the order of st's sequences, and parts by the sequence's length, of which a single one has been written already
-hipError_t launch_paged_merge(const PagedPlan &pl, const float *partials, uint16_t *out, const relax_layer_dims &dm, int32_t cap, const PagedSeqs &st, hipStream_t stream, int32_t rows = 0);
+PagedPlan paged_plan(const relax_layer_dims &dm, const relax_seqs &sq, int32_t n, int32_t L_max);
 
 // Attention of the sequences with at least `least` (row, head) pairs, in `items` tiles of kPagedRowTile pairs (attn_paged_rows.hip)
 constexpr int kPagedRowTile = 256;
