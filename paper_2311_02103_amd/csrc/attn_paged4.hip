@@ -22,6 +22,8 @@ namespace relax {
 namespace {
 
 constexpr float kBias = 1.0f, kLag = 2.0f;       // log2: weight at the reference, and how far the reference may trail the maximum
+// with two column tiles: log2 of the weight at the reference, the largest weight before that moves, the reference of a column that has met no token
+constexpr float kPackedBias = 11.0f, kMost = 65000.0f, kUnset = -1e30f;
 
 typedef _Float16 half4p_t __attribute__((ext_vector_type(4)));
 
@@ -32,6 +34,10 @@ __device__ __forceinline__ float column_max(float v)
     both = pair_xor32(fmaxf(both.x, both.y));
     return fmaxf(both.x, both.y);
 }
+
+// elements i and i + 1 of a vector of halves
+template <typename V>
+__device__ __forceinline__ uint32_t pair_of(const V &v, int i) { return __builtin_bit_cast(uint32_t, half2p_t{v[i], v[i + 1]}); }
 
 // n / d for 0 <= n < 2^31 by a product: with s = ceil(log2 d) and m = floor(2^(31 + s) / d) + 1 the error n (m d - 2^(31 + s)) is below 2^(31 + s)
 struct Divisor {
@@ -70,14 +76,15 @@ __device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *
     constexpr int J = D / 32;                    // k steps, words of a lane per block, scales of a token
     constexpr int NT = D / 16;                   // 16-element tiles of O^T
     constexpr int SB = FOLD ? 1 : 2;             // blocks of a step whose scores a lane holds
-    constexpr bool EXACT = CT > 1;               // codes as u - 8
+    constexpr bool EXACT = CT > 1;               // operands are the numbers that the cache stands for
     constexpr int W = Lds::kWaves;
     static_assert(!FOLD || CT == 1, "eight pairs are one column tile");
     typedef uint32_t words_t __attribute__((ext_vector_type(J)));
     typedef _Float16 scales_t __attribute__((ext_vector_type(4 * J)));
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, quarter = lane >> 4;
-    const half2p_t eight = {(_Float16)-8.0f, (_Float16)-8.0f};
+    const half2p_t eight = {(_Float16)-8.0f, (_Float16)-8.0f}, one = {(_Float16)1.0f, (_Float16)1.0f};
+    const float4p_t none = {0.0f, 0.0f, 0.0f, 0.0f};
 
     // ---- this wavefront's blocks: its share of the part, in pairs ----
     const int b_begin = (k.t_begin + 15) >> 4, b_end = k.t_end > k.t_begin ? (k.t_end + 15) >> 4 : b_begin;
@@ -133,9 +140,11 @@ __device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *
 
     float4p_t O[CT][NT], off[J];                 // off: -8 times the sums of a group's operands
     float m_run[CT], l_run[CT];
+    float4p_t l_all[CT];                         // EXACT: sums of the weights, the same in all four
+    half8p_t pf[CT];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-        m_run[ct] = -INFINITY, l_run[ct] = 0.0f;
+        m_run[ct] = EXACT ? kUnset : -INFINITY, l_run[ct] = 0.0f, l_all[ct] = none;
 #pragma unroll
         for (int i = 0; i < NT; ++i) O[ct][i] = float4p_t{0.0f, 0.0f, 0.0f, 0.0f};
     }
@@ -144,7 +153,8 @@ __device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *
 
     words_t kreg[2], vreg[2];                                  // a step: two blocks
     scales_t ks[SB], vs[SB];                                   // (FOLD: of the lane's block)
-    auto load = [&](words_t (&reg)[2], scales_t (&sc)[SB], const uint8_t *codes, const uint16_t *scales, int s) __attribute__((always_inline)) {
+    const int k_four = EXACT ? col >> 2 : quarter;             // four tokens whose key scales the lane needs: those of its operand or those of its scores
+    auto load = [&](words_t (&reg)[2], scales_t (&sc)[SB], const uint8_t *codes, const uint16_t *scales, int four, int s) __attribute__((always_inline)) {
         size_t at[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -152,23 +162,115 @@ __device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *
             reg[t] = stream_load((const words_t *)(codes + at[t] * block4_codes(D)) + lane);
         }
 #pragma unroll
-        for (int t = 0; t < SB; ++t) sc[t] = *((const scales_t *)(scales + (FOLD ? (col < 8 ? at[0] : at[1]) : at[t]) * block4_scales(D)) + quarter);
+        for (int t = 0; t < SB; ++t) sc[t] = *((const scales_t *)(scales + (FOLD ? (col < 8 ? at[0] : at[1]) : at[t]) * block4_scales(D)) + four);
     };
     bool ordered = false;
     for (int seg = w_begin; seg < w_end; seg += kWave) {
         if (seg != w_begin) pool = lookup(seg);
         const int ns = (min(w_end - seg, kWave) + 1) >> 1;
         // loads are issued without a condition, behind the last step the last one's again: behind a branch their number at a wait is not known
-        load(kreg, ks, pa.k, pa.k_scale, 0), load(vreg, vs, pa.v, pa.v_scale, 0);
+        load(kreg, ks, pa.k, pa.k_scale, k_four, 0), load(vreg, vs, pa.v, pa.v_scale, quarter, 0);
         if (!ordered) order_queries(), ordered = true;
         // a step's keys make room for the next one's as soon as the scores are there, its values when they are summed: one step is in flight all the time
         // (two in flight take 40 registers more and lose: 120001 tokens 30.6 us for 29.1)
 #pragma unroll 1
         for (int s = 0; s < ns; ++s) {
-            float x[CT][4 * SB];                               // scores over c
             const int t0 = (seg + 2 * s) * 16;                 // first token of the step
             const bool there0 = __builtin_amdgcn_readlane(pool, min(2 * s, 63)) >= 0, there1 = __builtin_amdgcn_readlane(pool, min(2 * s + 1, 63)) >= 0;
             const bool gone = !there0 || !there1 || t0 + 31 > pos_min;      // uniform: some of the tokens are masked
+            if constexpr (EXACT) {
+                float4p_t S[2][CT];                            // scores over c
+                const uint32_t own = 0x01000100u + (lane & 1) * 0x02020202u + (lane & 2) * 0x02020202u;       // the lane's token of four, twice
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int j = 0; j < J; ++j) {
+                        const u32x2p_t four = {pair_of(ks[t], 4 * j), pair_of(ks[t], 4 * j + 2)};
+                        const half2p_t scale = __builtin_bit_cast(half2p_t, __builtin_amdgcn_perm(four.y, four.x, own)), off = scale * eight;
+                        half2p_t p[4];
+                        word_codes(kreg[t][j], p);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) p[e] = __builtin_elementwise_fma(p[e], scale, off);
+#pragma unroll
+                        for (int ct = 0; ct < CT; ++ct)
+                            S[t][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(p[0], p[1], p[2], p[3]), qf[ct][j], j ? S[t][ct] : none, 0, 0, 0);
+                    }
+                load(kreg, ks, pa.k, pa.k_scale, k_four, min(s + 1, ns - 1));
+                if (gone) {
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                if (!(t ? there1 : there0) || t0 + 16 * t + 4 * quarter + i > pos[ct]) S[t][ct][i] = -INFINITY;
+                }
+                const auto weights = [&]() __attribute__((always_inline)) {
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                        for (int t = 0; t < 2; ++t)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)        // tokens 0 2 1 3, as the values lie
+                                pf[ct][4 * t + (i & 1) * 2 + (i >> 1)] = (_Float16)__builtin_amdgcn_exp2f(fmaf(S[t][ct][i], c, kPackedBias - m_run[ct]));
+                };
+                weights();
+                // The weights were computed against the reference as it was.  Where one is about to leave fp16's range (or every column is new) the reference moves to the
+                // maximum of these scores: rare behind the first tokens, and a look at the packed weights costs a quarter of the maxima of the scores.
+                half2p_t top = {(_Float16)0.0f, (_Float16)0.0f};
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) top = __builtin_elementwise_max(top, half2p_t{pf[ct][2 * i], pf[ct][2 * i + 1]});
+                if (__any(fmaxf((float)top.x, (float)top.y) > kMost)) {
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) {
+                        float mx = -INFINITY, most = 0.0f;     // a column moves by itself: no row depends on the others of its tile
+#pragma unroll
+                        for (int t = 0; t < 2; ++t)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) mx = fmaxf(mx, S[t][ct][i] * c), most = fmaxf(most, (float)pf[ct][4 * t + i]);
+                        mx = column_max(mx), most = column_max(most);
+                        const float to = most > kMost && mx > m_run[ct] ? mx : m_run[ct], alpha = __builtin_amdgcn_exp2f(m_run[ct] - to);
+                        m_run[ct] = to, l_all[ct] *= alpha;
+#pragma unroll
+                        for (int i = 0; i < NT; ++i) O[ct][i] *= alpha;
+                    }
+                    weights();
+                }
+                if (gone) {                                    // a scale behind the last token, or of no block, is anything, and a weight of zero would not hide a NaN
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (!(t ? there1 : there0) || t0 + 16 * t + 4 * quarter + i >= k.t_end)
+#pragma unroll
+                                for (int j = 0; j < J; ++j) vs[t][4 * j + i] = (_Float16)0.0f;
+                }
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    half2p_t a[2][4];
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        word_codes(vreg[t][j], a[t]);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {          // tokens i and i + 2
+                            const half2p_t scale = {vs[t][4 * j + i], vs[t][4 * j + i + 2]}, off = scale * eight;
+                            a[t][i] = __builtin_elementwise_fma(a[t][i], scale, off), a[t][2 + i] = __builtin_elementwise_fma(a[t][2 + i], scale, off);
+                        }
+                    }
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) {
+                        O[ct][2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(a[0][0], a[0][1], a[1][0], a[1][1]), pf[ct], O[ct][2 * j], 0, 0, 0);
+                        O[ct][2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(a[0][2], a[0][3], a[1][2], a[1][3]), pf[ct], O[ct][2 * j + 1], 0, 0, 0);
+                    }
+                }
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) l_all[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(one, one, one, one), pf[ct], l_all[ct], 0, 0, 0);
+                load(vreg, vs, pa.v, pa.v_scale, quarter, min(s + 1, ns - 1));
+                continue;
+            } else {
+            float x[CT][4 * SB];                               // scores over c
             float4p_t S[CT][J];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
@@ -176,13 +278,9 @@ __device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *
                 for (int j = 0; j < J; ++j) {
                     half2p_t p[4];
                     word_codes(kreg[t][j], p);
-                    if constexpr (EXACT) {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) p[e] += eight;
-                    }
 #pragma unroll
                     for (int ct = 0; ct < CT; ++ct) {
-                        const float start = EXACT ? 0.0f : qs[ct][j];
+                        const float start = qs[ct][j];
                         S[ct][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(p[0], p[1], p[2], p[3]), FOLD && t ? qg[FOLD ? j : 0] : qf[ct][j],
                                                                           FOLD && t ? S[ct][j] : float4p_t{start, start, start, start}, 0, 0, 0);
                     }
@@ -211,7 +309,7 @@ __device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *
                             if (!there || first + i > pos[ct]) x[ct][4 * t + i] = -INFINITY;
                 }
             }
-            load(kreg, ks, pa.k, pa.k_scale, min(s + 1, ns - 1));
+            load(kreg, ks, pa.k, pa.k_scale, k_four, min(s + 1, ns - 1));
             bool move[CT], any = false;
             float mx[CT];
 #pragma unroll
@@ -232,10 +330,8 @@ __device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *
                     m_run[ct] = m_new;
 #pragma unroll
                     for (int i = 0; i < NT; ++i) O[ct][i] *= alpha;
-                    if constexpr (!EXACT) {
 #pragma unroll
-                        for (int j = 0; j < J; ++j) off[j] *= alpha;
-                    }
+                    for (int j = 0; j < J; ++j) off[j] *= alpha;
                 }
             }
             float w[CT][4 * SB];
@@ -265,10 +361,6 @@ __device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *
                 half2p_t a[4], e[4];
                 word_codes(vreg[0][j], a);
                 word_codes(vreg[1][j], e);
-                if constexpr (EXACT) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) a[i] += eight, e[i] += eight;
-                }
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
                     half2p_t pw[4];                            // the weights of both blocks, tokens 0 2 | 1 3
@@ -287,10 +379,11 @@ __device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *
                     const half8p_t pf = operand(pw[0], pw[1], pw[2], pw[3]);
                     O[ct][2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(a[0], a[1], e[0], e[1]), pf, O[ct][2 * j], 0, 0, 0);
                     O[ct][2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(a[2], a[3], e[2], e[3]), pf, O[ct][2 * j + 1], 0, 0, 0);
-                    if constexpr (!EXACT) off[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(eight, eight, eight, eight), pf, off[j], 0, 0, 0);
+                    off[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(eight, eight, eight, eight), pf, off[j], 0, 0, 0);
                 }
             }
-            load(vreg, vs, pa.v, pa.v_scale, min(s + 1, ns - 1));
+            load(vreg, vs, pa.v, pa.v_scale, quarter, min(s + 1, ns - 1));
+            }
         }
     }
 
@@ -298,7 +391,7 @@ __device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *
     for (int ct = 0; ct < CT; ++ct) {
         const int at = wave * Lds::kPairs + (FOLD ? col & 7 : ct * 16 + col);
         if constexpr (FOLD) l_run[ct] += lane_xor<8>(l_run[ct]);
-        l_run[ct] = xor32_sum(xor16_sum(l_run[ct]));
+        l_run[ct] = EXACT ? l_all[ct][0] : xor32_sum(xor16_sum(l_run[ct]));
         if (FOLD && col >= 8) continue;
 #pragma unroll
         for (int i = 0; i < NT; ++i) *(float4p_t *)(lds.o + at * Lds::kPitch + i * 16 + quarter * 4) = EXACT ? O[ct][i] : O[ct][i] + off[i >> 1];
