@@ -301,7 +301,7 @@ hipError_t launch_d(const uint16_t *q, const PagedArgs &pa, const relax_layer_di
 
 }  // namespace
 
-PagedPlan paged_plan(const relax_layer_dims &dm, const relax_seqs &sq, int32_t n, int32_t L_max)
+PagedPlan paged_plan(const relax_layer_dims &dm, const relax_seqs &sq, int32_t n, int32_t L_max, int32_t row_tiles)
 {
     const int rep = dm.n_heads / dm.n_kv_heads;
     auto pairs_of = [&](int b) { return (long long)sq.q_lens[b] * rep; };
@@ -309,7 +309,7 @@ PagedPlan paged_plan(const relax_layer_dims &dm, const relax_seqs &sq, int32_t n
     for (int b = 0; b < sq.B; ++b)
         if (pairs_of(b) >= kPagedRowTile) large += (pairs_of(b) + kPagedRowTile - 1) / kPagedRowTile;
     PagedPlan p;
-    p.least = large * dm.n_kv_heads >= kRowTiles ? kPagedRowTile : INT32_MAX;
+    p.least = large * dm.n_kv_heads >= row_tiles ? kPagedRowTile : INT32_MAX;
     long long small = 0, most_small = 0, most_large = 0;
     for (int b = 0; b < sq.B; ++b) {
         const long long pairs = pairs_of(b);
@@ -339,7 +339,7 @@ size_t paged_partial_floats(const relax_layer_dims &dm, int32_t n, int32_t L)
 hipError_t launch_paged_attention(const uint16_t *q, const PagedArgs &pa, const relax_layer_dims &dm, const PagedSeqs &st, const relax_seqs &sq, int32_t L_max,
                                   uint16_t *out, float *partials, hipStream_t stream)
 {
-    const PagedPlan pl = paged_plan(dm, sq, st.n, L_max);
+    const PagedPlan pl = paged_plan(dm, sq, st.n, L_max, kRowTiles);
     if (pl.row_items > 0) {
         const hipError_t e = launch_paged_rows(q, pa, dm, st, pl.row_items, pl.row_per_seq, pl.least, out, stream);
         if (e != hipSuccess || pl.items == 0) return e;

@@ -2,16 +2,19 @@
 //
 //   o[i] = sum_t p[i,t] v[t],   p[i,:] = softmax_t(q[i] . k[t] / sqrt d),  t = 0 .. pos_i,   k[t][e] = s_k[t][e / 32] (u_k[t][e] - 8), v likewise
 //
-// Tiles, splits and the merge of partial results are those of attn_paged.hip: 16 consecutive (row, head) pairs against one KV head and one split of the
-// tokens, S^T = K Q^T and O^T = V^T P^T, so that a pair is a column, a lane (quarter, column) of the scores holds tokens 4 quarter .. + 3 of a
-// block, and the lane's eight probabilities of two blocks are what the second product wants from it.
+// A tile is up to 32 consecutive (row, head) pairs against one KV head and one part of the tokens, S^T = K Q^T and O^T = V^T P^T, so that a pair is a column, a lane
+// (quarter, column) of the scores holds tokens 4 quarter .. + 3 of a block, and the lane's eight weights of two blocks are what the second product wants from it.
 //
-// Codes go into both products as fp16 integers 0..15 (paged4_device.h).
-// Scores.  A scale is constant over a k step of 32 elements, so a step is a product of its own, S_j = sum u q, and x = sum_j s_kj S_j.  The accumulator of S_j starts at
-// -8 sum q, which takes the codes' offset off.
-// Values.  The weight of a token times its value scale, w s_j, is rounded to fp16 once per group of 32 elements and is the operand; -8 sum (w s_j), from one more product
-// per group, goes to the result.  Weights are exp2(score - reference + 1) with a reference that trails the maximum by at most 2: at most 8, and times 8160,
-// the largest scale, an fp16 number.  The smallest ones lose bits: 2^-25 absolute, at most 2^-26 of the largest weight, per code.
+// Up to eight pairs (a decode step with grouped heads): bytes and vector instructions are near each other, and a column costs little, so codes go into both products as fp16 integers 0..15
+// (paged4_device.h) and the scales meet columns.  A scale is constant over a k step of 32 elements, so a step is a product of its own, S_j = sum u q, and x = sum_j s_kj S_j.  The
+// accumulator of S_j starts at -8 sum q, which takes the codes' offset off.  The weight of a token times its value scale, w s_j, is rounded to fp16 once per group of 32 elements and is
+// the operand; -8 sum (w s_j), from one more product per group, goes to the result.  Weights are exp2(score - reference + 1) with a reference that trails the
+// maximum by at most 2: at most 8, and times 8160, the largest scale, an fp16 number.  The smallest ones lose bits: 2^-25 absolute, at most 2^-26 of the largest weight, per code.
+// More pairs: the vector unit bounds it, and a column costs more than a token, so operands are the numbers that the cache stands for, (u - 8) s = u s + (-8 s), one multiply-add per two and
+// exact (eight and four bits).  The products need no factor; the weight is rounded to fp16 and its sum is that of the rounded ones, from a product with ones.
+// (300 rows of 32 / 8 heads on 1201 tokens beside eight sequences of five: 30.7 us; with codes and scales of columns as above 36.7.)
+//
+// us, and what the bytes alone take at 6.0 TB/s (heads of 128): 64 / 8 heads, 16 sequences of 100 to 8000 tokens 21.7 of 12.5; one of 120001 29.2 of 23.0.
 #include <algorithm>
 #include <type_traits>
 
@@ -21,9 +24,9 @@ namespace relax {
 
 namespace {
 
-constexpr float kBias = 1.0f, kLag = 2.0f;       // log2: weight at the reference, and how far the reference may trail the maximum
-// with two column tiles: log2 of the weight at the reference, the largest weight before that moves, the reference of a column that has met no token
-constexpr float kPackedBias = 11.0f, kMost = 65000.0f, kUnset = -1e30f;
+constexpr float kUnset = -1e30f;                 // reference of a column that has met no token: below every score, and finite
+constexpr float kBias = 1.0f, kLag = 2.0f;       // up to eight pairs, log2: weight at the reference, and how far that may trail the maximum
+constexpr float kPackedBias = 11.0f, kMost = 65000.0f;       // more: log2 of the weight at the reference, the largest weight before that moves
 
 typedef _Float16 half4p_t __attribute__((ext_vector_type(4)));
 
@@ -34,10 +37,6 @@ __device__ __forceinline__ float column_max(float v)
     both = pair_xor32(fmaxf(both.x, both.y));
     return fmaxf(both.x, both.y);
 }
-
-// elements i and i + 1 of a vector of halves
-template <typename V>
-__device__ __forceinline__ uint32_t pair_of(const V &v, int i) { return __builtin_bit_cast(uint32_t, half2p_t{v[i], v[i + 1]}); }
 
 // n / d for 0 <= n < 2^31 by a product: with s = ceil(log2 d) and m = floor(2^(31 + s) / d) + 1 the error n (m d - 2^(31 + s)) is below 2^(31 + s)
 struct Divisor {
@@ -66,17 +65,15 @@ struct Task {
     int used, split, splits;         // parts of the sequence, this one, the partial results per row
 };
 
-// The workgroup's part of a tile, its wavefronts a share of the tokens each.  CT: column tiles of 16 pairs.  FOLD: up to eight pairs, every column twice; a lane of the columns from 8 on
-// takes the second block of a step (the products with keys meet queries in one half of the columns and zeros in the other), so that scores, exponentials and weights of two blocks are those of one.  With two column tiles the codes are worth
-// the subtraction of their offset, which otherwise goes through the accumulators of the products.
+// The workgroup's part of a tile, its wavefronts a share of the tokens each, a step two blocks.  CT: column tiles of 16 pairs, with decoded operands.  FOLD: up to eight pairs, every column twice,
+// with codes as operands: a lane of the columns from 8 on takes the second block of a step (the products with keys meet queries in one half of the columns and zeros in the other), so
+// that scores, exponentials and weights of two blocks are those of one.
 template <int D, int CT, bool FOLD, typename Lds>
 __device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *__restrict__ q, const Paged4Args &pa, float *__restrict__ part, uint16_t *__restrict__ out, int h,
                                        int g)
 {
     constexpr int J = D / 32;                    // k steps, words of a lane per block, scales of a token
     constexpr int NT = D / 16;                   // 16-element tiles of O^T
-    constexpr int SB = FOLD ? 1 : 2;             // blocks of a step whose scores a lane holds
-    constexpr bool EXACT = CT > 1;               // operands are the numbers that the cache stands for
     constexpr int W = Lds::kWaves;
     static_assert(!FOLD || CT == 1, "eight pairs are one column tile");
     typedef uint32_t words_t __attribute__((ext_vector_type(J)));
@@ -107,7 +104,7 @@ __device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *
     int pos[CT];
     half8p_t qf[CT][J];                          // FOLD: of the columns below 8, zeros in the others; qg: the other way round
     half8p_t qg[FOLD ? J : 1];
-    float qs[CT][J];                             // -8 sum q of a step
+    float qs[FOLD ? J : 1];                      // -8 sum q of a step
     const float c = 1.44269504088896340736f / sqrtf((float)D);
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
@@ -124,37 +121,33 @@ __device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *
             for (int j = 0; j < J; ++j) {
                 const half8p_t x = qf[ct][j];
                 qf[ct][j] = half8p_t{x[0], x[4], x[1], x[5], x[2], x[6], x[3], x[7]};
-                if constexpr (!EXACT) {
+                if constexpr (FOLD) {
                     float sum = 0.0f;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) sum += (float)x[e];
-                    qs[ct][j] = xor32_sum(xor16_sum(sum)) * -8.0f;
-                }
-                if constexpr (FOLD) {
-                    const half8p_t zero = {};
-                    const u32x4p_t raw = __builtin_bit_cast(u32x4p_t, qf[ct][j]), none = __builtin_bit_cast(u32x4p_t, zero);
-                    qg[j] = __builtin_bit_cast(half8p_t, col < 8 ? none : raw), qf[ct][j] = __builtin_bit_cast(half8p_t, col < 8 ? raw : none);
+                    qs[j] = xor32_sum(xor16_sum(sum)) * -8.0f;
+                    const u32x4p_t raw = __builtin_bit_cast(u32x4p_t, qf[ct][j]), zero = {0, 0, 0, 0};
+                    qg[j] = __builtin_bit_cast(half8p_t, col < 8 ? zero : raw), qf[ct][j] = __builtin_bit_cast(half8p_t, col < 8 ? raw : zero);
                 }
             }
     };
 
-    float4p_t O[CT][NT], off[J];                 // off: -8 times the sums of a group's operands
-    float m_run[CT], l_run[CT];
-    float4p_t l_all[CT];                         // EXACT: sums of the weights, the same in all four
-    half8p_t pf[CT];
+    float4p_t O[CT][NT], off[FOLD ? J : 1];      // off: -8 times the sums of a group's operands
+    float m[CT];                                 // the columns' references
+    float4p_t l[CT];                             // sums of the weights: the same in all four, FOLD: the lane's own in the first
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-        m_run[ct] = EXACT ? kUnset : -INFINITY, l_run[ct] = 0.0f, l_all[ct] = none;
+        m[ct] = kUnset, l[ct] = none;
 #pragma unroll
-        for (int i = 0; i < NT; ++i) O[ct][i] = float4p_t{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int i = 0; i < NT; ++i) O[ct][i] = none;
     }
 #pragma unroll
-    for (int j = 0; j < J; ++j) off[j] = float4p_t{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int j = 0; j < (FOLD ? J : 1); ++j) off[j] = none;
 
-    words_t kreg[2], vreg[2];                                  // a step: two blocks
-    scales_t ks[SB], vs[SB];                                   // (FOLD: of the lane's block)
-    const int k_four = EXACT ? col >> 2 : quarter;             // four tokens whose key scales the lane needs: those of its operand or those of its scores
-    auto load = [&](words_t (&reg)[2], scales_t (&sc)[SB], const uint8_t *codes, const uint16_t *scales, int four, int s) __attribute__((always_inline)) {
+    words_t kreg[2], vreg[2];
+    scales_t ks[FOLD ? 1 : 2], vs[FOLD ? 1 : 2];               // (FOLD: of the lane's block)
+    const int k_four = FOLD ? quarter : col >> 2;              // four tokens whose key scales the lane needs: those of its scores or that of its operand
+    auto load = [&](words_t (&reg)[2], scales_t (&sc)[FOLD ? 1 : 2], const uint8_t *codes, const uint16_t *scales, int four, int s) __attribute__((always_inline)) {
         size_t at[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -162,7 +155,7 @@ __device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *
             reg[t] = stream_load((const words_t *)(codes + at[t] * block4_codes(D)) + lane);
         }
 #pragma unroll
-        for (int t = 0; t < SB; ++t) sc[t] = *((const scales_t *)(scales + (FOLD ? (col < 8 ? at[0] : at[1]) : at[t]) * block4_scales(D)) + four);
+        for (int t = 0; t < (FOLD ? 1 : 2); ++t) sc[t] = *((const scales_t *)(scales + (FOLD ? (col < 8 ? at[0] : at[1]) : at[t]) * block4_scales(D)) + four);
     };
     bool ordered = false;
     for (int seg = w_begin; seg < w_end; seg += kWave) {
@@ -176,21 +169,90 @@ __device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *
 #pragma unroll 1
         for (int s = 0; s < ns; ++s) {
             const int t0 = (seg + 2 * s) * 16;                 // first token of the step
-            const bool there0 = __builtin_amdgcn_readlane(pool, min(2 * s, 63)) >= 0, there1 = __builtin_amdgcn_readlane(pool, min(2 * s + 1, 63)) >= 0;
-            const bool gone = !there0 || !there1 || t0 + 31 > pos_min;      // uniform: some of the tokens are masked
-            if constexpr (EXACT) {
-                float4p_t S[2][CT];                            // scores over c
-                const uint32_t own = 0x01000100u + (lane & 1) * 0x02020202u + (lane & 2) * 0x02020202u;       // the lane's token of four, twice
+            const bool there[2] = {__builtin_amdgcn_readlane(pool, min(2 * s, 63)) >= 0, __builtin_amdgcn_readlane(pool, min(2 * s + 1, 63)) >= 0};
+            const bool gone = !there[0] || !there[1] || t0 + 31 > pos_min;      // uniform: some of the tokens are masked
+            // the first token that the lane has a score of in (its) block t, and whether there is the block
+            const auto first = [&](int t) { return t0 + 16 * (FOLD ? col >> 3 : t) + 4 * quarter; };
+            const auto have = [&](int t) { return FOLD ? (col < 8 ? there[0] : there[1]) : there[t]; };
+            const auto clean_scales = [&]() __attribute__((always_inline)) {    // a scale behind the last token, or of no block, is anything, and a weight of zero would not hide a NaN
+#pragma unroll
+                for (int t = 0; t < (FOLD ? 1 : 2); ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (!have(t) || first(t) + i >= k.t_end)
+#pragma unroll
+                            for (int j = 0; j < J; ++j) vs[t][4 * j + i] = (_Float16)0.0f;
+            };
+            if constexpr (FOLD) {
+                float4p_t S[J];
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int j = 0; j < J; ++j) {
-                        const u32x2p_t four = {pair_of(ks[t], 4 * j), pair_of(ks[t], 4 * j + 2)};
-                        const half2p_t scale = __builtin_bit_cast(half2p_t, __builtin_amdgcn_perm(four.y, four.x, own)), off = scale * eight;
+                        half2p_t p[4];
+                        word_codes(kreg[t][j], p);
+                        S[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(p[0], p[1], p[2], p[3]), t ? qg[j] : qf[0][j], t ? S[j] : float4p_t{qs[j], qs[j], qs[j], qs[j]}, 0, 0, 0);
+                    }
+                float x[4], w[4];                              // scores over c, weights
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    x[i] = fmaf(S[0][i], (float)ks[0][i], 0.0f);       // (as a multiply-add of mixed types: a product would convert its scale first)
+#pragma unroll
+                    for (int j = 1; j < J; ++j) x[i] = fmaf(S[j][i], (float)ks[0][4 * j + i], x[i]);
+                }
+                if (gone) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (!have(0) || first(0) + i > pos[0]) x[i] = -INFINITY;
+                }
+                load(kreg, ks, pa.k, pa.k_scale, k_four, min(s + 1, ns - 1));
+                float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
+                mx = column_max(fmaxf(mx, lane_xor<8>(mx))) * c;
+                const bool move = mx > m[0] + kLag;
+                if (__any(move)) {
+                    const float to = move ? mx : m[0], alpha = __builtin_amdgcn_exp2f(m[0] - to);
+                    m[0] = to, l[0][0] *= alpha;
+#pragma unroll
+                    for (int i = 0; i < NT; ++i) O[0][i] *= alpha;
+#pragma unroll
+                    for (int j = 0; j < J; ++j) off[j] *= alpha;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    w[i] = __builtin_amdgcn_exp2f(fmaf(x[i], c, kBias - m[0]));
+                    l[0][0] += w[i];
+                }
+                if (gone) clean_scales();
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    half2p_t a[4], e[4], pw[4];                // pw: the weights of both blocks times their scales, tokens 0 2 | 1 3
+                    word_codes(vreg[0][j], a);
+                    word_codes(vreg[1][j], e);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        float lo = fmaf(w[i], (float)vs[0][4 * j + i], 0.0f), hi = fmaf(w[i + 2], (float)vs[0][4 * j + i + 2], 0.0f);
+                        asm("" : "+v"(lo), "+v"(hi));          // (the products in fp32 and one conversion of both: multiply-adds that write a half take twice the time)
+                        pw[i] = half2p_t{(_Float16)lo, (_Float16)hi};
+                        pw[2 + i] = __builtin_bit_cast(half2p_t, lane_xor<8>(__builtin_bit_cast(float, pw[i])));      // (columns from 8 on have the blocks the other way round, and no pair)
+                    }
+                    const half8p_t pf = operand(pw[0], pw[1], pw[2], pw[3]);
+                    O[0][2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(a[0], a[1], e[0], e[1]), pf, O[0][2 * j], 0, 0, 0);
+                    O[0][2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(a[2], a[3], e[2], e[3]), pf, O[0][2 * j + 1], 0, 0, 0);
+                    off[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(eight, eight, eight, eight), pf, off[j], 0, 0, 0);
+                }
+            } else {
+                float4p_t S[2][CT];                            // scores over c
+                const uint32_t own = 0x01000100u + (lane & 3) * 0x02020202u;   // bytes of the lane's token of four, twice
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int j = 0; j < J; ++j) {
+                        const uint32_t lo = __builtin_bit_cast(uint32_t, half2p_t{ks[t][4 * j], ks[t][4 * j + 1]}), hi = __builtin_bit_cast(uint32_t, half2p_t{ks[t][4 * j + 2], ks[t][4 * j + 3]});
+                        const half2p_t scale = __builtin_bit_cast(half2p_t, __builtin_amdgcn_perm(hi, lo, own)), zero_point = scale * eight;
                         half2p_t p[4];
                         word_codes(kreg[t][j], p);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) p[e] = __builtin_elementwise_fma(p[e], scale, off);
+                        for (int e = 0; e < 4; ++e) p[e] = __builtin_elementwise_fma(p[e], scale, zero_point);
 #pragma unroll
                         for (int ct = 0; ct < CT; ++ct)
                             S[t][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(p[0], p[1], p[2], p[3]), qf[ct][j], j ? S[t][ct] : none, 0, 0, 0);
@@ -203,8 +265,9 @@ __device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *
                         for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
                             for (int i = 0; i < 4; ++i)
-                                if (!(t ? there1 : there0) || t0 + 16 * t + 4 * quarter + i > pos[ct]) S[t][ct][i] = -INFINITY;
+                                if (!have(t) || first(t) + i > pos[ct]) S[t][ct][i] = -INFINITY;
                 }
+                half8p_t pf[CT];
                 const auto weights = [&]() __attribute__((always_inline)) {
 #pragma unroll
                     for (int ct = 0; ct < CT; ++ct)
@@ -212,7 +275,7 @@ __device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *
                         for (int t = 0; t < 2; ++t)
 #pragma unroll
                             for (int i = 0; i < 4; ++i)        // tokens 0 2 1 3, as the values lie
-                                pf[ct][4 * t + (i & 1) * 2 + (i >> 1)] = (_Float16)__builtin_amdgcn_exp2f(fmaf(S[t][ct][i], c, kPackedBias - m_run[ct]));
+                                pf[ct][4 * t + (i & 1) * 2 + (i >> 1)] = (_Float16)__builtin_amdgcn_exp2f(fmaf(S[t][ct][i], c, kPackedBias - m[ct]));
                 };
                 weights();
                 // The weights were computed against the reference as it was.  Where one is about to leave fp16's range (or every column is new) the reference moves to the
@@ -231,22 +294,14 @@ __device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *
 #pragma unroll
                             for (int i = 0; i < 4; ++i) mx = fmaxf(mx, S[t][ct][i] * c), most = fmaxf(most, (float)pf[ct][4 * t + i]);
                         mx = column_max(mx), most = column_max(most);
-                        const float to = most > kMost && mx > m_run[ct] ? mx : m_run[ct], alpha = __builtin_amdgcn_exp2f(m_run[ct] - to);
-                        m_run[ct] = to, l_all[ct] *= alpha;
+                        const float to = most > kMost && mx > m[ct] ? mx : m[ct], alpha = __builtin_amdgcn_exp2f(m[ct] - to);
+                        m[ct] = to, l[ct] *= alpha;
 #pragma unroll
                         for (int i = 0; i < NT; ++i) O[ct][i] *= alpha;
                     }
                     weights();
                 }
-                if (gone) {                                    // a scale behind the last token, or of no block, is anything, and a weight of zero would not hide a NaN
-#pragma unroll
-                    for (int t = 0; t < 2; ++t)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (!(t ? there1 : there0) || t0 + 16 * t + 4 * quarter + i >= k.t_end)
-#pragma unroll
-                                for (int j = 0; j < J; ++j) vs[t][4 * j + i] = (_Float16)0.0f;
-                }
+                if (gone) clean_scales();
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
                     half2p_t a[2][4];
@@ -255,8 +310,8 @@ __device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *
                         word_codes(vreg[t][j], a[t]);
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {          // tokens i and i + 2
-                            const half2p_t scale = {vs[t][4 * j + i], vs[t][4 * j + i + 2]}, off = scale * eight;
-                            a[t][i] = __builtin_elementwise_fma(a[t][i], scale, off), a[t][2 + i] = __builtin_elementwise_fma(a[t][2 + i], scale, off);
+                            const half2p_t scale = {vs[t][4 * j + i], vs[t][4 * j + i + 2]}, zero_point = scale * eight;
+                            a[t][i] = __builtin_elementwise_fma(a[t][i], scale, zero_point), a[t][2 + i] = __builtin_elementwise_fma(a[t][2 + i], scale, zero_point);
                         }
                     }
 #pragma unroll
@@ -266,136 +321,21 @@ __device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *
                     }
                 }
 #pragma unroll
-                for (int ct = 0; ct < CT; ++ct) l_all[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(one, one, one, one), pf[ct], l_all[ct], 0, 0, 0);
-                load(vreg, vs, pa.v, pa.v_scale, quarter, min(s + 1, ns - 1));
-                continue;
-            } else {
-            float x[CT][4 * SB];                               // scores over c
-            float4p_t S[CT][J];
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-#pragma unroll
-                for (int j = 0; j < J; ++j) {
-                    half2p_t p[4];
-                    word_codes(kreg[t][j], p);
-#pragma unroll
-                    for (int ct = 0; ct < CT; ++ct) {
-                        const float start = qs[ct][j];
-                        S[ct][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(p[0], p[1], p[2], p[3]), FOLD && t ? qg[FOLD ? j : 0] : qf[ct][j],
-                                                                          FOLD && t ? S[ct][j] : float4p_t{start, start, start, start}, 0, 0, 0);
-                    }
-                }
-                if (FOLD && t == 0) continue;
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int u = FOLD ? 0 : t;
-                        float sum = fmaf(S[ct][0][i], (float)ks[u][i], 0.0f);      // (as a multiply-add of mixed types: a product would convert its scale first)
-#pragma unroll
-                        for (int j = 1; j < J; ++j) sum = fmaf(S[ct][j][i], (float)ks[u][4 * j + i], sum);
-                        x[ct][4 * u + i] = sum;
-                    }
-            }
-            if (gone) {
-#pragma unroll
-                for (int t = 0; t < SB; ++t) {
-                    const bool there = FOLD ? (col < 8 ? there0 : there1) : (t ? there1 : there0);
-                    const int first = t0 + 16 * (FOLD ? col >> 3 : t) + 4 * quarter;
-#pragma unroll
-                    for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (!there || first + i > pos[ct]) x[ct][4 * t + i] = -INFINITY;
-                }
-            }
-            load(kreg, ks, pa.k, pa.k_scale, k_four, min(s + 1, ns - 1));
-            bool move[CT], any = false;
-            float mx[CT];
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) {
-                mx[ct] = x[ct][0];
-#pragma unroll
-                for (int i = 1; i < 4 * SB; ++i) mx[ct] = fmaxf(mx[ct], x[ct][i]);
-                if constexpr (FOLD) mx[ct] = fmaxf(mx[ct], lane_xor<8>(mx[ct]));
-                mx[ct] = column_max(mx[ct]) * c;
-                move[ct] = mx[ct] > m_run[ct] + kLag;          // the first visible tokens: m_run = -inf
-                any = any || move[ct];
-            }
-            if (__any(any)) {
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct) {
-                    const float m_new = move[ct] ? mx[ct] : m_run[ct], alpha = move[ct] ? __builtin_amdgcn_exp2f(m_run[ct] - m_new) : 1.0f;
-                    l_run[ct] *= alpha;
-                    m_run[ct] = m_new;
-#pragma unroll
-                    for (int i = 0; i < NT; ++i) O[ct][i] *= alpha;
-#pragma unroll
-                    for (int j = 0; j < J; ++j) off[j] *= alpha;
-                }
-            }
-            float w[CT][4 * SB];
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) {
-                const float m_ref = m_run[ct] == -INFINITY ? 0.0f : m_run[ct] - kBias;      // nothing visible yet: every weight is exp2(-inf)
-#pragma unroll
-                for (int i = 0; i < 4 * SB; ++i) {
-                    w[ct][i] = __builtin_amdgcn_exp2f(fmaf(x[ct][i], c, -m_ref));
-                    l_run[ct] += w[ct][i];
-                }
-            }
-            if (gone) {                                        // a scale behind the last token, or of no block, is anything
-#pragma unroll
-                for (int t = 0; t < SB; ++t) {
-                    const bool there = FOLD ? (col < 8 ? there0 : there1) : (t ? there1 : there0);
-                    const int first = t0 + 16 * (FOLD ? col >> 3 : t) + 4 * quarter;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (!there || first + i >= k.t_end)
-#pragma unroll
-                            for (int j = 0; j < J; ++j) vs[t][4 * j + i] = (_Float16)0.0f;
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < J; ++j) {
-                half2p_t a[4], e[4];
-                word_codes(vreg[0][j], a);
-                word_codes(vreg[1][j], e);
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct) {
-                    half2p_t pw[4];                            // the weights of both blocks, tokens 0 2 | 1 3
-#pragma unroll
-                    for (int t = 0; t < SB; ++t)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            float lo = fmaf(w[ct][4 * t + i], (float)vs[t][4 * j + i], 0.0f), hi = fmaf(w[ct][4 * t + i + 2], (float)vs[t][4 * j + i + 2], 0.0f);
-                            asm("" : "+v"(lo), "+v"(hi));      // (the products in fp32 and one conversion of both: multiply-adds that write a half take twice the time)
-                            pw[2 * t + i] = half2p_t{(_Float16)lo, (_Float16)hi};
-                        }
-                    if constexpr (FOLD) {                      // (columns from 8 on have the blocks the other way round, and no pair)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) pw[2 + i] = __builtin_bit_cast(half2p_t, lane_xor<8>(__builtin_bit_cast(float, pw[i])));
-                    }
-                    const half8p_t pf = operand(pw[0], pw[1], pw[2], pw[3]);
-                    O[ct][2 * j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(a[0], a[1], e[0], e[1]), pf, O[ct][2 * j], 0, 0, 0);
-                    O[ct][2 * j + 1] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(a[2], a[3], e[2], e[3]), pf, O[ct][2 * j + 1], 0, 0, 0);
-                    off[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(eight, eight, eight, eight), pf, off[j], 0, 0, 0);
-                }
+                for (int ct = 0; ct < CT; ++ct) l[ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(operand(one, one, one, one), pf[ct], l[ct], 0, 0, 0);
             }
             load(vreg, vs, pa.v, pa.v_scale, quarter, min(s + 1, ns - 1));
-            }
         }
     }
 
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
         const int at = wave * Lds::kPairs + (FOLD ? col & 7 : ct * 16 + col);
-        if constexpr (FOLD) l_run[ct] += lane_xor<8>(l_run[ct]);
-        l_run[ct] = EXACT ? l_all[ct][0] : xor32_sum(xor16_sum(l_run[ct]));
+        float den = l[ct][0];
+        if constexpr (FOLD) den = xor32_sum(xor16_sum(den + lane_xor<8>(den)));
         if (FOLD && col >= 8) continue;
 #pragma unroll
-        for (int i = 0; i < NT; ++i) *(float4p_t *)(lds.o + at * Lds::kPitch + i * 16 + quarter * 4) = EXACT ? O[ct][i] : O[ct][i] + off[i >> 1];
-        if (quarter == 0) lds.m[at] = m_run[ct], lds.l[at] = l_run[ct];
+        for (int i = 0; i < NT; ++i) *(float4p_t *)(lds.o + at * Lds::kPitch + i * 16 + quarter * 4) = FOLD ? O[ct][i] + off[FOLD ? i >> 1 : 0] : O[ct][i];
+        if (quarter == 0) lds.m[at] = m[ct], lds.l[at] = den;
     }
 
     // ---- the wavefronts' states meet: T threads per pair, E times four elements each ----
@@ -417,7 +357,7 @@ __device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *
     for (int i = 0; i < E; ++i) num[i] = float4p_t{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-        const float f = mw[w] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mw[w] - mm);
+        const float f = __builtin_amdgcn_exp2f(mw[w] - mm);
         den += lw[w] * f;
 #pragma unroll
         for (int i = 0; i < E; ++i) num[i] += o[w][i] * f;
@@ -482,6 +422,9 @@ __global__ __launch_bounds__(64 * W, 2) void attn_paged4_kernel(PagedSeqs, const
 // comes on top when there are more of them than at a time; a merge, and each of its partial results; the cache's bytes
 constexpr float kGroupUs[2] = {3.8f, 5.8f}, kStepUs[2][2] = {{0.96f, 1.17f}, {1.35f, 2.4f}}, kHalfHead = 0.71f, kTail = 0.14f, kMergeUs = 2.9f, kMergeResultUs = 4.1e-4f, kBytesUs = 5.1f,
                 kBytesPerUs = 6.15e6f;
+// Tiles of 256 pairs over all KV heads from which the kernel of such tiles is faster: it has 256 workgroups at a time, each as slow alone as beside 255 others (us, these tiles / those: 1200 rows on 600
+// cached tokens of 32 / 8 heads, 150 tiles, 52.7 / 59.7; 1600 rows, 200, 51.7 / 54.4 and on 600 cached tokens 76.2 / 71.4; 2043 rows, 255, 71.6 / 66.0; 4096 rows, 512, 227 / 141)
+constexpr int kRowTiles = 200;
 constexpr int kLeast = 128, kPartials4 = 65536;  // tokens of a part, and partial results (row, head, part), at least and at most
 
 // How the tiles are cut: a sequence of L tokens into ceil(L / chunk) equal parts
@@ -679,7 +622,7 @@ hipError_t launch_d(const uint16_t *q, const Paged4Args &pa, const relax_layer_d
 hipError_t launch_paged4_attention(const uint16_t *q, const Paged4Args &pa, const relax_layer_dims &dm, const PagedSeqs &st, const relax_seqs &sq, int32_t L_max,
                                    uint16_t *out, float *partials, hipStream_t stream)
 {
-    const PagedPlan pl = paged_plan(dm, sq, st.n, L_max);
+    const PagedPlan pl = paged_plan(dm, sq, st.n, L_max, kRowTiles);
     if (pl.row_items > 0) {
         const hipError_t e = launch_paged4_rows(q, pa, dm, st, pl, out, stream);
         if (e != hipSuccess || pl.items == 0) return e;

@@ -129,14 +129,14 @@ __device__ inline int paged_block(const Args &pa, int g, int kvh, int slot, int 
     return ((page * g + kvh) << pa.shift) + (blk & ((1 << pa.shift) - 1));
 }
 
-// How a paged attention call is cut (attn_paged.hip)
+// How a paged attention call is cut (attn_paged.hip): sequences that fill a tile of 256 pairs go to such tiles if there are row_tiles of them over all KV heads
 struct PagedPlan {
     int32_t least;                   // pairs from which a sequence is the other kernel's
     int32_t row_items, items;        // tiles of 256 and of 16 pairs that are launched
     int32_t row_per_seq, per_seq;    // as tile_of takes them
     int32_t chunk, splits, waves;    // wavefronts per workgroup of 16-pair tiles
 };
-PagedPlan paged_plan(const relax_layer_dims &dm, const relax_seqs &sq, int32_t n, int32_t L_max);
+PagedPlan paged_plan(const relax_layer_dims &dm, const relax_seqs &sq, int32_t n, int32_t L_max, int32_t row_tiles);
 
 // Attention of the sequences with at least `least` (row, head) pairs, in `items` tiles of kPagedRowTile pairs (attn_paged_rows.hip)
 constexpr int kPagedRowTile = 256;
