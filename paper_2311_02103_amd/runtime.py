@@ -161,6 +161,14 @@ def _check_tensor(t: torch.Tensor, dtype, count: int, device, what: str) -> None
         raise ValueError("%s: %d elements of %s, contiguous, on %s" % (what, count, dtype, device))
 
 
+def _qkv_rows(qkv: torch.Tensor, dims, device):
+    """(rows, address, elements from one row to the next) of a projection's output."""
+    h, g, d = dims.n_heads, dims.n_kv_heads, dims.head_dim
+    if qkv.dtype != torch.float16 or qkv.dim() != 2 or qkv.shape[1] != (h + 2 * g) * d or qkv.stride(1) != 1 or qkv.device != device:
+        raise ValueError("qkv is fp16 [n, (h + 2 g) d] with contiguous rows, on the cache's device")
+    return qkv.shape[0], qkv.data_ptr(), qkv.stride(0) if qkv.shape[0] > 1 else qkv.shape[1]
+
+
 _NOT_GIVEN = object()
 
 
@@ -210,10 +218,7 @@ class DevicePagedCache:
     def append(self, qkv: torch.Tensor, seqs: "rx.Seqs", q_out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """qkv: fp16 [n, (h + 2 g) d], rows contiguous (any stride between them).  Returns q, rotated, fp16 [n, h, d]."""
         h, g, d = self.dims.n_heads, self.dims.n_kv_heads, self.dims.head_dim
-        if qkv.dtype != torch.float16 or qkv.dim() != 2 or qkv.shape[1] != (h + 2 * g) * d or qkv.stride(1) != 1 or qkv.device != self.pages.device:
-            raise ValueError("qkv is fp16 [n, (h + 2 g) d] with contiguous rows, on the cache's device")
-        n, at = qkv.shape[0], qkv.data_ptr()
-        pitch = qkv.stride(0) if n > 1 else qkv.shape[1]
+        n, at, pitch = _qkv_rows(qkv, self.dims, self.pages.device)
         if q_out is not None:
             _check_tensor(q_out, torch.float16, n * h * d, self.pages.device, "q_out [n, h, d]")
         else:
@@ -239,6 +244,106 @@ class DevicePagedCache:
         with _allocating_for(stream):
             k, v = (torch.empty((n, self.dims.n_kv_heads, self.dims.head_dim), dtype=torch.float16, device=self.device) for _ in "kv")
         rx.check(rx.relax_paged_read(self.cache, seqs, self.dims, k, v, n, self.ws, self.ws_bytes, stream), "relax_paged_read")
+        return k, v
+
+
+def rope_table(scaling: "rx.RopeScaling", positions: int, device="cuda", stream=None) -> torch.Tensor:
+    """The rotary table fp32 [positions, rotary_dim / 2, 2] of scaled positions (relax_rope_table_scaled)."""
+    nbytes = rx.relax_rope_scaled_bytes(scaling, positions)
+    if not nbytes:
+        raise ValueError("relax_rope_scaling or the number of positions is out of range")
+    with _allocating_for(stream):
+        table = torch.empty((positions, scaling.rotary_dim // 2, 2), dtype=torch.float32, device=device)
+    rx.check(rx.relax_rope_table_scaled(scaling, positions, table, stream), "relax_rope_table_scaled")
+    return table
+
+
+class DevicePaged4Cache:
+    """The 4-bit paged KV cache of one layer, and how the layer prepares its heads: norm weights q_norm and k_norm (fp16 [d], None: no norm of these heads), eps, the
+    rotary table of `rope` (None: no rotation; 10000 over the whole head if not given) and its layout.  Pool, page table, workspace and share_from as
+    DevicePagedCache; `rope` is then the other layer's, norms and layout are this one's."""
+
+    def __init__(self, *, n_heads: int, n_kv_heads: int, head_dim: int, kv_capacity: int, n_pages: int, page_size: int = 64, kv_slots: int = 1, n_max: int = 1,
+                 B_max: Optional[int] = None, q_norm: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                 rope: Optional["rx.RopeScaling"] = _NOT_GIVEN, layout: int = rx.ROPE_HALVES, device="cuda", share_from: "DevicePaged4Cache" = None):
+        self.device, self.page_size = device, page_size
+        self.dims = rx.make_dims(n_heads * head_dim, n_heads, n_kv_heads, head_dim, 64, kv_capacity, kv_slots)
+        self.n_max, self.B_max = n_max, (B_max if B_max is not None else max(kv_slots, 1))
+        where = torch.empty(0, device=device).device
+        for name, w in (("q_norm", q_norm), ("k_norm", k_norm)):
+            if w is not None:
+                _check_tensor(w, torch.float16, head_dim, where, name)
+        if share_from is not None:          # layers of one model share the page table, the rotary table and the workspace
+            self._check_shared(share_from, rope, where)
+            self.rotary, self.rope, self.pages, self.ws, self.ws_bytes = share_from.rotary, share_from.rope, share_from.pages, share_from.ws, share_from.ws_bytes
+        else:
+            self.rotary = rope if rope is not _NOT_GIVEN else rx.RopeScaling(rx.ROPE_PLAIN, head_dim, 10000.0, 1.0)
+            self.pages = torch.full((kv_slots, -(-kv_capacity // page_size)), -1, dtype=torch.int32, device=device)
+            self.rope = None if self.rotary is None else rope_table(self.rotary, kv_capacity, device)
+            self.ws_bytes = rx.relax_paged4_workspace_bytes(self.dims, n_max, kv_capacity, self.B_max)
+            self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
+            rx.check(rx.relax_workspace_init(self.dims, self.ws, self.ws_bytes), "relax_workspace_init")
+        blocks = (n_pages, n_kv_heads, page_size // rx.RELAX_PAGED_BLOCK)
+        self.k, self.v = (torch.empty(blocks + (rx.RELAX_PAGED_BLOCK * head_dim // 2,), dtype=torch.uint8, device=device) for _ in "kv")
+        self.k_scale, self.v_scale = (torch.empty(blocks + (rx.RELAX_PAGED_BLOCK * head_dim // rx.RELAX_PAGED4_GROUP,), dtype=torch.float16, device=device) for _ in "kv")
+        self.cache = rx.Paged4Cache(self.k, self.v, self.k_scale, self.v_scale, self.pages, n_pages, page_size, self.pages.shape[1])
+        self.prep = rx.HeadPrep(q_norm, k_norm, eps, self.rope, 0 if self.rotary is None else self.rotary.rotary_dim, layout)
+
+    def _check_shared(self, other: "DevicePaged4Cache", rope, device) -> None:
+        """The kernels index the shared tables by this layer's sizes, which the C calls cannot compare with the tables'."""
+        slots, positions = other.pages.shape[0], other.pages.shape[1] * other.page_size
+        if other.rope is not None:
+            positions = min(positions, other.rope.shape[0])
+        if self.page_size != other.page_size:
+            raise ValueError("share_from: pages of %d tokens, the table's are of %d" % (self.page_size, other.page_size))
+        if self.dims.kv_slots > slots or self.dims.kv_capacity > positions:
+            raise ValueError("share_from: %d slots of %d positions on tables for %d of %d" % (self.dims.kv_slots, self.dims.kv_capacity, slots, positions))
+        if rope is not _NOT_GIVEN and (rope is None) != (other.rotary is None) or rope not in (_NOT_GIVEN, None) and bytes(rope) != bytes(other.rotary):
+            raise ValueError("share_from: the rotary table is of another scaling")
+        if other.rotary is not None and other.rotary.rotary_dim > self.dims.head_dim:
+            raise ValueError("share_from: the rotary table turns %d elements of heads of %d" % (other.rotary.rotary_dim, self.dims.head_dim))
+        if device != other.pages.device:
+            raise ValueError("share_from: the tables are on another device")
+
+    def append(self, qkv: torch.Tensor, seqs: "rx.Seqs", q_out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """qkv: fp16 [n, (h + 2 g) d], rows contiguous (any stride between them).  Returns q, prepared, fp16 [n, h, d]."""
+        h, g, d = self.dims.n_heads, self.dims.n_kv_heads, self.dims.head_dim
+        n, at, pitch = _qkv_rows(qkv, self.dims, self.pages.device)
+        if q_out is not None:
+            _check_tensor(q_out, torch.float16, n * h * d, self.pages.device, "q_out [n, h, d]")
+        else:
+            with _allocating_for(stream):
+                q_out = torch.empty((n, h, d), dtype=torch.float16, device=self.device)
+        rx.check(rx.relax_paged4_append(at, pitch, at + 2 * h * d, at + 2 * (h + g) * d, pitch, q_out, self.prep, self.cache, seqs, self.dims, n, self.ws, self.ws_bytes,
+                                        stream), "relax_paged4_append")
+        return q_out
+
+    def heads(self, qkv: torch.Tensor, seqs: "rx.Seqs", stream=None):
+        """(q, k) of the rows, prepared as `append` does and rounded to fp16, [n, h, d] and [n, g, d]; nothing goes into the cache (relax_head_norm_rope)."""
+        h, g, d = self.dims.n_heads, self.dims.n_kv_heads, self.dims.head_dim
+        n, at, pitch = _qkv_rows(qkv, self.dims, self.pages.device)
+        with _allocating_for(stream):
+            q, k = (torch.empty((n, heads, d), dtype=torch.float16, device=self.device) for heads in (h, g))
+        rx.check(rx.relax_head_norm_rope(at, pitch, at + 2 * h * d, pitch, q, h * d, k, g * d, self.prep, seqs, self.dims, n, self.ws, self.ws_bytes, stream),
+                 "relax_head_norm_rope")
+        return q, k
+
+    def attention(self, q: torch.Tensor, seqs: "rx.Seqs", out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        count = q.shape[0] * self.dims.n_heads * self.dims.head_dim
+        _check_tensor(q, torch.float16, count, self.pages.device, "q [n, h, d]")
+        if out is not None:
+            _check_tensor(out, torch.float16, count, self.pages.device, "out [n, h, d]")
+        else:
+            with _allocating_for(stream):
+                out = torch.empty_like(q)
+        rx.check(rx.relax_paged4_attention(q, self.cache, seqs, self.dims, out, q.shape[0], self.ws, self.ws_bytes, stream), "relax_paged4_attention")
+        return out
+
+    def read(self, seqs: "rx.Seqs", n: int, stream=None):
+        """(k, v) of the call's n rows as fp16 [n, g, d]: exactly what the cache holds."""
+        with _allocating_for(stream):
+            k, v = (torch.empty((n, self.dims.n_kv_heads, self.dims.head_dim), dtype=torch.float16, device=self.device) for _ in "kv")
+        rx.check(rx.relax_paged4_read(self.cache, seqs, self.dims, k, v, n, self.ws, self.ws_bytes, stream), "relax_paged4_read")
         return k, v
 
 

@@ -491,7 +491,50 @@ def test_attention_on_queries_of_any_size(rx, std):
         assert (np.abs(got - want) <= tol).all()
 
 
-# Calls whose sequences fill tiles of 256 (row, head) pairs, 160 of them and more over all KV heads: (heads, KV heads, d), q_lens, kv_lens, heads to check
+@pytest.mark.parametrize("lead", [0, 45])
+@pytest.mark.parametrize("pairs", [1, 2, 7, 8, 9, 15, 16, 17, 31, 32, 33, 40, 41, 48, 49, 64, 65])
+def test_attention_at_every_width_of_a_tile(rx, pairs, lead):
+    """Rows whose last tile has that many (row, head) pairs, on as many tokens as rows and behind 45 more: plain, and with large scores, uneven scales, blocks of zeros and a hole."""
+    rng = np.random.default_rng(100 * pairs + lead)
+    for shape, rows in (((2, 2, 128), pairs), ((3, 1, 64), -(-pairs // 3))):
+        attention_case(rx, rng, shape, 16, [rows], [rows + lead])
+
+    def spoil(b):
+        scaled(lambda r, s: 10.0 ** r.uniform(-4, 2, s))(b)
+        for key in ("ks", "vs"):
+            b.pool[key][:, :, :, 5:9] = np.where(np.isnan(b.pool[key][:, :, :, 5:9]), np.nan, 0.0).astype(np.float16)
+            b.dev[key].copy_(torch.from_numpy(b.pool[key]))
+        b.pages[0, 1] = -1
+        b.dev_pages.copy_(torch.from_numpy(b.pages))
+    if pairs + lead > 16:
+        assert attention_case(rx, rng, (2, 2, 128), 16, [pairs], [pairs + lead], std=4.0, edit=spoil).error() == 4
+
+
+@pytest.mark.parametrize("rows,L", [(1, 900), (8, 1030), (12, 1003), (25, 2000)])
+def test_bad_rows_in_small_tiles_and_parts(rx, rows, L):
+    """A NaN or an infinity of a query stays in its row and head, also where a row's parts are merged."""
+    rng = np.random.default_rng(rows)
+    b = Bench(rx, rng, 6, 2, 64, 32, [rows], [L])
+    q = half(rng, (rows, 6, 64))
+    clean = b.attention(q)
+    same = np.ones((rows, 6), bool)
+    for row, head, value in ((0, 4, np.nan), (rows // 2, 1, np.inf), (rows - 1, 2, -np.inf)):
+        q[row, head, 7 * head] = value
+        same[row, head] = False
+    got = b.attention(q)
+    assert np.array_equal(got[same], clean[same]) and not np.isfinite(got[~same]).all(axis=1).any()
+
+
+def test_parts_of_many_lengths(rx):
+    """Sequences of one and of many parts in one call, in no order of length: those that are merged are the first in the order of lengths, and have rows of any number."""
+    rng = np.random.default_rng(81)
+    for shape, q_lens, kv_lens in (((16, 2, 64), [1, 1, 1, 1, 1, 1, 1], [40, 3000, 1, 700, 16, 9000, 129]), ((4, 2, 128), [3, 1, 20, 1, 2], [50, 6000, 2200, 1, 4000]),
+                                   ((8, 1, 128), [1, 1], [20000, 3])):
+        for device_table in (False, True):
+            attention_case(rx, rng, shape, 32, q_lens, kv_lens, list(range(len(q_lens)))[::-1], device_table=device_table)
+
+
+# Calls whose sequences fill tiles of 256 (row, head) pairs, 160 to 200 of them and more over all KV heads: (heads, KV heads, d), q_lens, kv_lens, heads to check
 MANY_ROWS = [
     ((80, 80, 64), [300], [300], [0, 41, 79]),
     ((80, 80, 128), [257], [1000], [0, 1, 40, 79]),
@@ -500,6 +543,13 @@ MANY_ROWS = [
     ((40, 8, 64), [1001], [1001], [0, 9, 39]),
     ((160, 160, 64), [256], [8200], [0, 77, 159]),                # more blocks than are in LDS at a time
     ((24, 8, 128), [2000], [2000], [2, 23]),
+    ((100, 100, 64), [300], [300], [0, 41, 99]),
+    ((100, 100, 128), [257], [1000], [0, 1, 99]),
+    ((64, 8, 128), [33, 60, 40, 32, 35, 47, 33, 64, 50, 45, 70, 66, 100], [33, 61, 300, 32, 99, 47, 700, 64, 1050, 45, 70, 90, 333], [0, 7, 8, 63]),
+    ((40, 8, 128), [300, 1, 450, 3, 260, 200], [310, 800, 450, 77, 900, 1200], [0, 5, 39]),
+    ((40, 8, 64), [1300], [1300], [0, 9, 39]),
+    ((200, 200, 64), [256], [8200], [0, 199]),                    # more blocks than are in LDS at a time
+    ((24, 8, 128), [2150], [2150], [2, 23]),
 ]
 
 
@@ -792,3 +842,53 @@ def test_calls_repeat_bit_by_bit(rx):
         first = b.attention(q)
         assert all(same_bits(first, b.attention(q)) for _ in range(3))
 
+
+def test_a_model_of_one_layer_with_normalised_heads(rx):
+    """The Python classes as a program strings them together: projection, append, attention, the output product; requests of different ages, normalised heads of which part is
+    turned at stretched positions.  Two layers share the tables.  Keys and values against the definition bit by bit, attention in 64 bits on what is held."""
+    from paper_2311_02103_amd import runtime
+    rng = np.random.default_rng(91)
+    h, g, d, H, page = 8, 2, 64, 256, 16
+    scaling = rx.RopeScaling(rx.ROPE_WAVELENGTH_RAMP, 32, 10000.0, 4.0, 64.0, 1.0, 4.0)
+    mat = lambda m, k: torch.from_numpy(half(rng, (m, k), k ** -0.5)).cuda()
+    norms = [torch.from_numpy(half(rng, d, 0.2) + np.float16(1)).cuda() for _ in "qk"]
+    made = dict(n_heads=h, n_kv_heads=g, head_dim=d, kv_capacity=160, n_pages=30, page_size=page, kv_slots=3, n_max=200, q_norm=norms[0], k_norm=norms[1], eps=EPS, layout=rx.ROPE_PAIRS)
+    first = runtime.DevicePaged4Cache(rope=scaling, **made)
+    layers = [first, runtime.DevicePaged4Cache(share_from=first, **made)]
+    first.pages.copy_(torch.from_numpy(rng.permutation(30).reshape(3, 10).astype(np.int32)))
+    pages, table = first.pages.cpu().numpy(), first.rope.cpu().numpy()
+    weights = [(mat((h + 2 * g) * d, H), mat(H, h * d)) for _ in layers]
+
+    def product(x, w):
+        y = torch.empty((x.shape[0], w.shape[0]), dtype=torch.float16, device="cuda")
+        rx.check(rx.relax_half_matmul(x, w, y, x.shape[0], w.shape[0], w.shape[1]))
+        return y
+    held = [0, 0, 0]
+    for slots, lens in (([1], [97]), ([2, 0, 1], [33, 60, 1]), ([0, 1, 2], [1, 1, 1]), ([2, 0], [1, 4])):
+        for s_, ln in zip(slots, lens):
+            held[s_] += ln
+        kv_lens, n = [held[s_] for s_ in slots], sum(lens)
+        seqs, pos = rx.Seqs(lens, kv_lens, slots), positions(lens, kv_lens)
+        x = torch.from_numpy(half(rng, (n, H))).cuda()
+        for layer, (wqkv, wo) in zip(layers, weights):
+            before = {key: t.cpu().numpy() for key, t in (("k", layer.k), ("v", layer.v), ("ks", layer.k_scale), ("vs", layer.v_scale))}
+            qkv = product(x, wqkv)
+            q = layer.append(qkv, seqs)
+            o = layer.attention(q, seqs)
+            alone_q, alone_k = layer.heads(qkv, seqs)
+            x = x + product(o.view(-1, h * d), wo)
+            rows = qkv.cpu().numpy().reshape(n, h + 2 * g, d).astype(np.float32)
+            w = [t.cpu().numpy().astype(np.float32) for t in norms]
+            want_q, want_k = (po.prepare(rows[:, a:b], w_, np.float32(EPS), table[pos][:, None], 32, True) for a, b, w_ in ((0, h, w[0]), (h, h + g, w[1])))
+            assert same_bits(q.cpu().numpy(), want_q.astype(np.float16)) and same_bits(alone_q.cpu().numpy(), want_q.astype(np.float16))
+            assert same_bits(alone_k.cpu().numpy(), want_k.astype(np.float16))
+            pool = po.append(before, pages, page, want_k, rows[:, h + g:], lens, kv_lens, slots)
+            for key, t in (("k", layer.k), ("v", layer.v), ("ks", layer.k_scale), ("vs", layer.v_scale)):
+                assert same_bits(t.cpu().numpy(), pool[key]), key
+            want, tol = po.attention(q.cpu().numpy().astype(np.float64), pool, pages, page, lens, kv_lens, slots, g, d)
+            assert (np.abs(o.cpu().numpy() - want) <= tol).all()
+            for name, got in zip("kv", layer.read(seqs, n)):
+                for row, ql, L, slot in po.sequences(lens, kv_lens, slots):
+                    c, s_ = po.values(pool, name, pages, page, slot, np.arange(L - ql, L), d)
+                    assert np.array_equal(got[row:row + ql].cpu().numpy().astype(np.float64), c * s_)
+    assert rx.relax_workspace_error(first.dims, first.ws) == 0
