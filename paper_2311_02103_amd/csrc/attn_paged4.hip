@@ -69,7 +69,7 @@ struct Task {
 // with codes as operands: a lane of the columns from 8 on takes the second block of a step (the products with keys meet queries in one half of the columns and zeros in the other), so
 // that scores, exponentials and weights of two blocks are those of one.
 template <int D, int CT, bool FOLD, typename Lds>
-__device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *__restrict__ q, const Paged4Args &pa, float *__restrict__ part, uint16_t *__restrict__ out, int h,
+__device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *q, const Paged4Args &pa, float *__restrict__ part, uint16_t *out, int h,
                                        int g)
 {
     constexpr int J = D / 32;                    // k steps, words of a lane per block, scales of a token
@@ -389,7 +389,7 @@ struct Grid {
     Divisor by_g, by_rep, by_per_seq, by_chunk;
 };
 template <int D, bool FEW, int W>
-__global__ __launch_bounds__(64 * W, 2) void attn_paged4_kernel(PagedSeqs, const uint16_t *__restrict__ q, Paged4Args pa, float *__restrict__ part, uint16_t *__restrict__ out, Grid gr)
+__global__ __launch_bounds__(64 * W, 2) void attn_paged4_kernel(PagedSeqs, const uint16_t *q, Paged4Args pa, float *__restrict__ part, uint16_t *out, Grid gr)
 {
     __shared__ __align__(16) States<D, FEW ? 8 : kTile, W> lds;
     const int rep = gr.rep, item = quotient(blockIdx.x, gr.by_g), kvh = (int)blockIdx.x - item * gr.g;
@@ -523,7 +523,7 @@ void longest_first(PagedSeqs &st)
 // out from the parts of the rows that have more than one: T * G threads per (row, head), a thread four elements of every G-th part.  The first F of them are asked for before the number of parts is
 // known (there is memory for all that a row could have), so that they do not wait for the descriptor.  all: every row of the call, in its order; else the first rows of st's sequences.
 template <int D, int G>
-__global__ __launch_bounds__(256) void attn_paged4_merge_kernel(PagedSeqs, const float *__restrict__ part, uint16_t *__restrict__ out, Grid gr, Divisor by_h, int count, int cap, int all)
+__global__ __launch_bounds__(256) void attn_paged4_merge_kernel(PagedSeqs, const float *__restrict__ part, uint16_t *out, Grid gr, Divisor by_h, int count, int cap, int all)
 {
     constexpr int T = D / 4, F = 4, P = 256 / (T * G);
     __shared__ __align__(16) float sums[P][G][D];

@@ -29,7 +29,7 @@ constexpr int kSegment = kThreads;               // blocks whose numbers are in 
 
 // grid: x = tile * g + KV head (the last tile of a sequence, with the longest prefix, first)
 template <int D>
-__global__ __launch_bounds__(kThreads, 2) void attn_paged4_rows_kernel(PagedSeqs, const uint16_t *__restrict__ q, Paged4Args pa, uint16_t *__restrict__ out, int h, int g, int per_seq,
+__global__ __launch_bounds__(kThreads, 2) void attn_paged4_rows_kernel(PagedSeqs, const uint16_t *q, Paged4Args pa, uint16_t *out, int h, int g, int per_seq,
                                                                        int least)
 {
     constexpr int J = D / 32, NT = D / 16;       // words of a lane per block, also k steps; 16-element tiles of O^T

@@ -525,6 +525,18 @@ def test_bad_rows_in_small_tiles_and_parts(rx, rows, L):
     assert np.array_equal(got[same], clean[same]) and not np.isfinite(got[~same]).all(axis=1).any()
 
 
+@pytest.mark.parametrize("shape,q_lens,kv_lens", [((8, 2, 64), [1, 3, 20], [3000, 50, 700]), ((64, 8, 128), [1], [40]), ((100, 100, 64), [300, 1], [300, 900])], ids=str)
+def test_attention_in_place(rx, shape, q_lens, kv_lens):
+    """out may be q: a tile reads its rows before it writes them, and no other reads them."""
+    rng = np.random.default_rng(17)
+    b = Bench(rx, rng, *shape, 16, q_lens, kv_lens)
+    q = half(rng, (b.n, b.h, b.d))
+    want, x = b.attention(q), torch.from_numpy(q).cuda()
+    rx.check(rx.relax_paged4_attention(x, b.cache, b.seqs(), b.dims, x, b.n, *b.workspace()))
+    torch.cuda.synchronize()
+    assert same_bits(x.cpu().numpy(), want)
+
+
 def test_parts_of_many_lengths(rx):
     """Sequences of one and of many parts in one call, in no order of length: those that are merged are the first in the order of lengths, and have rows of any number."""
     rng = np.random.default_rng(81)
