@@ -260,11 +260,11 @@ __global__ __launch_bounds__(256) void attn_paged_merge_kernel(PagedSeqs, const 
 }
 
 // Splits of a launch with `small` workgroups per split: from kUnsplit workgroups on none, below it as many as bring it to kPagedGroups workgroups, at most one
-// per 128 tokens of the longest sequence (rounded up to 32 tokens, a split has 96 at least), and no more than kPartials partial results (row, head, split).  The workgroups of a split launch have eight
+// per 128 tokens of the longest sequence (rounded up to 32 tokens, a split has 96 at least), and no more than kPagedPartials partial results (row, head, split).  The workgroups of a split launch have eight
 // wavefronts where a split has 256 tokens and more, as many tokens in flight with half the partial results.
 // us, unsplit / split: 16 x 3 rows of 64 / 8 heads (256 workgroups) 18.5 / 23, 4 x 17 rows of them (288) 20 / 25, 16 x 16 rows of 32 / 32 (512) 28 / 38.  16 decode rows
 // of 64 / 8 heads with 768 workgroups 31.6, with 512 35.8, with 1024 32.7, with four wavefronts 36.
-constexpr int kUnsplit = 256, kPagedGroups = 768, kPartials = 65536;
+constexpr int kUnsplit = 256, kPagedGroups = 768;
 
 // The kernel of 256-pair tiles takes the sequences that fill one, in calls that have kRowTiles such tiles over all KV heads: it halves the time of long prompts
 // and loses on the rest, where its workgroups are few and each waits 5 us for its first tile (us, tiles of 16 / of 256; heads of 128): 2048 rows of 32 / 32 heads
@@ -321,7 +321,7 @@ PagedPlan paged_plan(const relax_layer_dims &dm, const relax_seqs &sq, int32_t n
     numbering(small, (most_small + 15) / 16, sq.B, p.items, p.per_seq);
     long long s = small && small * dm.n_kv_heads < kUnsplit ? kPagedGroups / (small * dm.n_kv_heads) : 1;
     s = std::min(s, (long long)(L_max + 127) / 128);
-    s = std::min(s, (long long)kPartials / ((long long)n * dm.n_heads));
+    s = std::min(s, (long long)kPagedPartials / ((long long)n * dm.n_heads));
     s = std::max(s, 1LL);
     p.chunk = (int32_t)(((L_max + s - 1) / s + 31) / 32 * 32);
     p.splits = (L_max + p.chunk - 1) / p.chunk;
@@ -329,10 +329,10 @@ PagedPlan paged_plan(const relax_layer_dims &dm, const relax_seqs &sq, int32_t n
     return p;
 }
 
-// paged_plan() has splits <= ceil(L / 128) and, where it has more than one, n * heads * splits <= kPartials
+// paged_plan() has splits <= ceil(L / 128) and, where it has more than one, n * heads * splits <= kPagedPartials
 size_t paged_partial_floats(const relax_layer_dims &dm, int32_t n, int32_t L)
 {
-    const size_t most = kPartials, mine = (size_t)n * dm.n_heads * (((size_t)L + 127) / 128);
+    const size_t most = kPagedPartials, mine = (size_t)n * dm.n_heads * (((size_t)L + 127) / 128);
     return (mine < most ? mine : most) * (dm.head_dim + 2);
 }
 

@@ -14,7 +14,9 @@
 // exact (eight and four bits).  The products need no factor; the weight is rounded to fp16 and its sum is that of the rounded ones, from a product with ones.
 // (300 rows of 32 / 8 heads on 1201 tokens beside eight sequences of five: 30.7 us; with codes and scales of columns as above 36.7.)
 //
-// us, and what the bytes alone take at 6.0 TB/s (heads of 128): 64 / 8 heads, 16 sequences of 100 to 8000 tokens 21.7 of 12.5; one of 120001 29.2 of 23.0.
+// Few pairs are bound by bytes, with what a workgroup's beginning and end and the merge take on top (about 3.8 and 3.9 us): heads of 128, 64 / 8 heads, one sequence of 120001 tokens 28.7 us, 4.8 TB/s
+// (23.0 at a long stream's rate), 16 of 100 to 8000 tokens 21.3 (12.5).  17 to 32 pairs are bound by the vector unit beside the matrix pipe: some 270 instructions per 32 tokens and 34 products.
+// (Tiles of 48 pairs, queries in LDS: 29.2 us for 30.6 in the call above, but 38.2 for 34.9 with 1200 rows on nothing.)
 #include <algorithm>
 #include <type_traits>
 
@@ -425,7 +427,7 @@ constexpr float kGroupUs[2] = {3.8f, 5.8f}, kStepUs[2][2] = {{0.96f, 1.17f}, {1.
 // Tiles of 256 pairs over all KV heads from which the kernel of such tiles is faster: it has 256 workgroups at a time, each as slow alone as beside 255 others (us, these tiles / those: 1200 rows on 600
 // cached tokens of 32 / 8 heads, 150 tiles, 52.7 / 59.7; 1600 rows, 200, 51.7 / 54.4 and on 600 cached tokens 76.2 / 71.4; 2043 rows, 255, 71.6 / 66.0; 4096 rows, 512, 227 / 141)
 constexpr int kRowTiles = 200;
-constexpr int kLeast = 128, kPartials4 = 65536;  // tokens of a part, and partial results (row, head, part), at least and at most
+constexpr int kLeast = 128;                      // tokens of a part
 
 // How the tiles are cut: a sequence of L tokens into ceil(L / chunk) equal parts
 struct Cut {
@@ -482,7 +484,7 @@ Cut cut(const PagedPlan &pl, const relax_layer_dims &dm, const PagedSeqs &st, co
     };
     if (tiles * g < 2048) {
         consider(chunk);
-        const int64_t most_parts = std::max<int64_t>(1, kPartials4 / ((int64_t)st.n * dm.n_heads)), least = (std::max<int64_t>(kLeast, L_max / most_parts + 1) + 31) & ~31;
+        const int64_t most_parts = std::max<int64_t>(1, kPagedPartials / ((int64_t)st.n * dm.n_heads)), least = (std::max<int64_t>(kLeast, L_max / most_parts + 1) + 31) & ~31;
         for (int parts = 2; parts <= (sq.B <= 4 ? 64 : sq.B <= 24 ? 16 : 4); parts += parts < 4 ? 1 : parts / 2) {
             const int64_t c = (L_max / parts + 32) & ~31;
             if (c >= least) consider(c);

@@ -4,6 +4,9 @@
 // one KV head and all tokens they see, 32 of them per wavefront, every tile of 64 tokens in LDS as fp16 in the order of the fragments.  A scale belongs to 32
 // elements of one token here, so both operands are decoded to the numbers that the cache stands for, (u - 8) s = u s + (-8 s), one multiply-add per pair and exact
 // (eight and four bits): the products need no factor, and the one rounding is that of the weights.
+//
+// 4096 rows of 32 / 8 heads of 128: 139 us, 0.99 PFLOP/s of the causal half (a large fp16 product reaches 1.35 here: 102 us).  Bound by the two halves' turns: one takes about 1050 cycles, of which
+// its 34 matrix instructions need 571 alone; next to them a vector instruction of the other half takes 8.5 cycles instead of 5.4.
 #include <type_traits>
 
 #include "paged4_device.h"

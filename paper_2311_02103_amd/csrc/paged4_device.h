@@ -6,8 +6,8 @@
 // The order of the codes in a word is the one that brings them out as fragments:
 //   K  word [quarter = e / 8 % 4][t][e / 32]   lane (token = l % 16, quarter = l / 16): k step e / 32, elements 0 4 1 5 2 6 3 7 of its eight
 //   V  word [t / 4][e % 16][e / 32]            lane (e % 16 = l % 16, quarter = l / 16): its four tokens as 0 2 1 3, for the element below 16 of 32 and for the one above
-// A scale multiplies 32 products (K) or a probability (V): [t / 4][e / 32][t % 4], the four tokens that a lane of the result of K Q^T holds in eight bytes.
-// The offset of 8 comes off the sums: sum (u - 8) q = sum u q - 8 sum q.
+// Scales [t / 4][e / 32][t % 4]: the four tokens that a lane of the result of K Q^T, and of the operand V, holds in eight bytes.  The offset of 8 comes off the codes,
+// u s + (-8 s), exactly, or off the sums: sum (u - 8) q = sum u q - 8 sum q.
 #pragma once
 
 #include "paged_device.h"

@@ -129,6 +129,8 @@ __device__ inline int paged_block(const Args &pa, int g, int kvh, int slot, int 
     return ((page * g + kvh) << pa.shift) + (blk & ((1 << pa.shift) - 1));
 }
 
+constexpr int kPagedPartials = 65536;             // partial results (row, head, split) of a paged attention call at most
+
 // How a paged attention call is cut (attn_paged.hip): sequences that fill a tile of 256 pairs go to such tiles if there are row_tiles of them over all KV heads
 struct PagedPlan {
     int32_t least;                   // pairs from which a sequence is the other kernel's
