@@ -419,10 +419,10 @@ __global__ __launch_bounds__(64 * W, 2) void attn_paged4_kernel(PagedSeqs, const
     else if constexpr (!FEW) n_pairs <= 16 ? attend<D, 1, false>(lds, task, q, pa, part, out, gr.h, gr.g) : attend<D, 2, false>(lds, task, q, pa, part, out, gr.h, gr.g);
 }
 
-// Estimated times, us, fitted to 19 calls with 10 to 20 cuts each, of which they choose one that is 1 % behind the best in the mean and 10 % at most: a workgroup's beginning and end, with four and with
-// eight wavefronts; a step of 32 tokens with up to 16 pairs and with 32, alone on a SIMD and beside another wavefront (heads of 64: times kHalfHead); the share of the longest workgroup that
-// comes on top when there are more of them than at a time; a merge, and each of its partial results; the cache's bytes
-constexpr float kGroupUs[2] = {3.8f, 5.8f}, kStepUs[2][2] = {{0.96f, 1.17f}, {1.35f, 2.4f}}, kHalfHead = 0.71f, kTail = 0.14f, kMergeUs = 2.9f, kMergeResultUs = 4.1e-4f, kBytesUs = 5.1f,
+// Estimated times, us, fitted to 24 calls with 10 to 20 cuts each, of which they choose one that is 0.4 % behind the best in the mean and 10 % at most.  With up to 16 pairs and with more: a workgroup's
+// beginning and end, with four and with eight wavefronts; a step of 32 tokens, alone on a SIMD and beside another wavefront (heads of 64: times kHalfHead).  The share of the longest workgroup
+// that comes on top when there are more of them than at a time; a merge, and each of its partial results; the cache's bytes
+constexpr float kGroupUs[2][2] = {{3.8f, 5.8f}, {3.8f, 8.8f}}, kStepUs[2][2] = {{0.96f, 1.17f}, {1.1f, 1.8f}}, kHalfHead = 0.71f, kTail = 0.14f, kMergeUs = 2.9f, kMergeResultUs = 4.1e-4f, kBytesUs = 5.1f,
                 kBytesPerUs = 6.15e6f;
 // Tiles of 256 pairs over all KV heads from which the kernel of such tiles is faster: it has 256 workgroups at a time, each as slow alone as beside 255 others (us, these tiles / those: 1200 rows on 600
 // cached tokens of 32 / 8 heads, 150 tiles, 52.7 / 59.7; 1600 rows, 200, 51.7 / 54.4 and on 600 cached tokens 76.2 / 71.4; 2043 rows, 255, 71.6 / 66.0; 4096 rows, 512, 227 / 141)
@@ -457,6 +457,7 @@ Cut cut(const PagedPlan &pl, const relax_layer_dims &dm, const PagedSeqs &st, co
     int32_t waves = 4;
     int64_t chunk = std::max<int64_t>(32, ((int64_t)L_max + 31) & ~31);
     float best = INFINITY;
+    const auto up = [](float x) { return (float)(int32_t)(x + 0.9999f); };      // (ceilf is a function call here: 1 us of a call's host time with 64 sequences)
     // takes parts of up to c tokens if they are estimated to be faster than what was considered before.  Two wavefronts per SIMD: 512 workgroups of four at a time, 256 of eight
     const auto consider = [&](int64_t c) {
         const float by_c = 1.0f / (float)c;
@@ -464,11 +465,12 @@ Cut cut(const PagedPlan &pl, const relax_layer_dims &dm, const PagedSeqs &st, co
         for (int b = 0; b < sq.B; ++b) {
             const float t = (float)tiles_of(b), L = (float)sq.kv_lens[b];
             if (t == 0.0f) continue;
-            const float parts = ceilf(L * by_c), share = parts == 1.0f ? L : L / parts;
-            const float *step = kStepUs[(int64_t)sq.q_lens[b] * rep > 16];
+            const float parts = up(L * by_c), share = parts == 1.0f ? L : L / parts;
+            const bool wide = (int64_t)sq.q_lens[b] * rep > 16;
+            const float *step = kStepUs[wide], *group = kGroupUs[wide];
             for (int w = 0; w < 2; ++w) {
-                const float steps = ceilf(share * (w ? 1.0f / 256 : 1.0f / 128)) * head, beside = kGroupUs[w] + steps * step[1];
-                longest[w][0] = std::max(longest[w][0], kGroupUs[w] + steps * step[0]), longest[w][1] = std::max(longest[w][1], beside);
+                const float steps = up(share * (w ? 1.0f / 256 : 1.0f / 128)) * head, beside = group[w] + steps * step[1];
+                longest[w][0] = std::max(longest[w][0], group[w] + steps * step[0]), longest[w][1] = std::max(longest[w][1], beside);
                 total[w] += beside * t * parts;
             }
             groups += t * parts;
