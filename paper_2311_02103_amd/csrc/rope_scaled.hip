@@ -1,5 +1,5 @@
 // Rotary tables of scaled positions: table[p][t] = amplitude (cos, sin)(p f'_t), fp64 rounded to fp32 (frequencies: relax_rope_scaling in relax_mi355.h).
-// A sine and cosine per entry made it bound by fp64 instructions: 131071 positions of 128 elements 32.7 us.  Sixteen entries from one, by rotation: 13.3 us, 5.0 TB/s
+// A sine and cosine per entry made it bound by fp64 instructions: 131071 positions of 128 elements 32.7 us.  All entries of a thread from one, by rotation: 11.8 us, 5.7 TB/s
 // written (9.8 at the rate of a fill).
 #include <algorithm>
 #include <cmath>
@@ -10,10 +10,10 @@ namespace relax {
 
 namespace {
 
-constexpr int64_t kThreadsWanted = 1 << 17;
+constexpr int kThreads = 1 << 18;                // of a launch at most: four workgroups per CU, all at once (with up to 16 entries per thread, eight per CU and more: 14.3 us for 11.8)
 
 // Thread i has pair i % half at positions i / half, + rows, + 2 rows ..: two sines and cosines, and a rotation by the angle of `rows` positions for each further entry (four multiply-adds in
-// 64 bits, off by 2^-52 each; a sine and cosine is some fifty instructions).
+// 64 bits, off by 2^-52 each: 32 of them with 131072 positions of 128 elements; a sine and cosine is some fifty instructions).
 __global__ __launch_bounds__(256) void rope_scaled_kernel(float *table, RopeFrequency f, int rows, int positions, int half)
 {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -37,11 +37,8 @@ __global__ __launch_bounds__(256) void rope_scaled_kernel(float *table, RopeFreq
 hipError_t launch_rope_scaled(const relax_rope_scaling &sc, int32_t positions, float *table, hipStream_t stream)
 {
     const int half = sc.rotary_dim / 2;
-    // up to 16 entries per thread where that leaves kThreadsWanted of them
-    const int64_t total = (int64_t)positions * half;
-    const int per = (int)std::min<int64_t>(16, std::max<int64_t>(1, total / kThreadsWanted)), rows = (positions + per - 1) / per;
+    const int rows = std::min(positions, kThreads / half);
     const int64_t groups = ((int64_t)rows * half + 255) / 256;
-    if (groups * 256 > kMaxThreads) return hipErrorInvalidValue;
     hipLaunchKernelGGL(rope_scaled_kernel, dim3(groups), dim3(256), 0, stream, table, rope_frequencies(sc), rows, positions, half);
     return hipGetLastError();
 }
