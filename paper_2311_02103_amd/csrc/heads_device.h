@@ -72,11 +72,11 @@ __device__ __forceinline__ double lane_xor(double v)
     return __builtin_bit_cast(double, (uint64_t)__builtin_bit_cast(uint32_t, hi) << 32 | __builtin_bit_cast(uint32_t, lo));
 }
 
-// 1 / sqrt(ms) rounded once to fp32: the hardware's estimate (2^-23) and two steps of Newton's method in fp64 (2^-45, then fp64's own 2^-52), a sixth of the instructions of a square root and
-// a division.  0 for infinity and for 0
+// 1 / sqrt(ms) rounded once to fp32: the hardware's estimate in fp64 (2^-24; the one in fp32 has no estimate of a subnormal number, which eps may be) and two steps of Newton's method (2^-46,
+// then fp64's own 2^-52), a sixth of the instructions of a square root and a division.  0 for infinity and for 0
 __device__ __forceinline__ float rsqrt_once(double ms)
 {
-    const double r0 = (double)__builtin_amdgcn_rsqf((float)ms), half = 0.5 * ms;
+    const double r0 = __builtin_amdgcn_rsq(ms), half = 0.5 * ms;
     const double r1 = r0 * __builtin_fma(-half * r0, r0, 1.5), r2 = r1 * __builtin_fma(-half * r1, r1, 1.5);
     return ms > 0.0 && ms < __builtin_inf() ? (float)r2 : ms == ms ? 0.0f : __builtin_nanf("");
 }

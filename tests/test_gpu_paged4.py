@@ -296,6 +296,17 @@ def test_heads_that_are_not_finite_or_zero(rx):
         assert (got[0][0, :64] == 0).all()
 
 
+@pytest.mark.parametrize("eps", [1e-45, 1e-40, 1e-30, 1.0, 3.4e38])
+def test_heads_with_any_eps(rx, eps):
+    """Heads of zeros, whose factor is that of eps alone, and of ordinary and of the smallest numbers."""
+    rng = np.random.default_rng(14)
+    t = Heads(rx, rng, 4, 2, 128, [4], [9], dict(eps=eps))
+    x = half(rng, (4, 6 * 128))
+    x[0], x[1, :128], x[2, :256] = 0, 0, np.float16(6e-8)
+    for got, want in zip(t.run(x), t.want(x)):
+        assert same_bits(got, want)
+
+
 def test_heads_beyond_the_capacity(rx):
     """A device table's positions outside the table of angles: the nearest row, and the flag."""
     rng = np.random.default_rng(13)
