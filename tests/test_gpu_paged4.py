@@ -677,6 +677,114 @@ def test_lengths_beyond_the_bounds_of_a_captured_call(rx):
     assert (np.abs(got - want) <= tol).all()
 
 
+DEVICE_LENGTHS = {"parts": ((4, 2, 64), 16, [1, 2, 1], [1100, 1500, 40]), "parts_128": ((8, 2, 128), 64, [3, 1], [900, 2000]), "wide_parts": ((8, 2, 128), 32, [9, 1], [900, 2000]),
+                  "one_part": ((32, 32, 64), 16, [1] * 9, [30, 200, 77, 16, 100, 5, 64, 33, 90]), "rows": ((100, 100, 64), 16, [300, 270], [300, 296]),
+                  "both_kernels": ((40, 40, 128), 16, [400, 2, 260, 300], [408, 70, 360, 300])}
+
+
+@pytest.mark.parametrize("kind", sorted(DEVICE_LENGTHS))
+def test_attention_on_lengths_of_a_device_table_beyond_the_capacity(rx, kind):
+    """Known on the device only: such a sequence has no token, which gives zeros and the flag, and the others are what they are without it; with host bounds at the capacity and far
+    below it."""
+    shape, page, q_lens, kv_lens = DEVICE_LENGTHS[kind]
+    b = Bench(rx, np.random.default_rng(76), *shape, page, q_lens, kv_lens, device_table=True)
+    q = half(np.random.default_rng(77), (b.n, b.h, b.d))
+    dev, (ws, ws_bytes) = torch.from_numpy(q).cuda(), b.workspace()
+    starts = np.concatenate([[0], np.cumsum(q_lens)])
+    for bounds in ([b.cap] * len(q_lens), kv_lens):
+        out = torch.empty_like(dev)
+        call = lambda: rx.check(rx.relax_paged4_attention(dev, b.cache, rx.Seqs(q_lens, bounds, None, b.dev_table), b.dims, out, b.n, ws, ws_bytes))
+        rx.check(rx.relax_workspace_init(b.dims, ws, ws_bytes))
+        b.dev_table[2] = torch.tensor(kv_lens, dtype=torch.int32)
+        call()
+        clean = out.clone()
+        assert b.error() == 0
+        for lost in {0, len(q_lens) - 1}:
+            for length in (b.cap + 1, b.cap + 500, 2 ** 31 - 1, -1, -2 ** 31):
+                b.dev_table[2, lost] = length
+                out.fill_(float("nan"))
+                call()
+                rows = slice(int(starts[lost]), int(starts[lost + 1]))
+                want = clean.clone()
+                want[rows] = 0
+                assert torch.equal(out, want) and b.error() == 4, (lost, length)
+            b.dev_table[2] = torch.tensor(kv_lens, dtype=torch.int32)
+
+
+@pytest.mark.parametrize("bound", [2, 130, 700])
+def test_a_device_table_beyond_the_bounds_of_the_call(rx, bound):
+    """Lengths of the table that the bounds of the host fall short of, within the capacity: all their tokens count, with the workspace of the bounds."""
+    for q_lens, kv_lens, shape in (([1, 2], [3000, 41], (8, 2, 64)), ([1, 2], [3000, 41], (40, 2, 64))):
+        b = Bench(rx, np.random.default_rng(78), *shape, 32, q_lens, kv_lens, device_table=True)
+        q = half(np.random.default_rng(79), (b.n, b.h, 64))
+        dev = torch.from_numpy(q).cuda()
+        out = torch.empty_like(dev)
+        ws_bytes = rx.relax_paged4_workspace_bytes(b.dims, b.n, bound, 2)
+        ws = torch.empty(ws_bytes, dtype=torch.uint8, device="cuda")
+        rx.check(rx.relax_workspace_init(b.dims, ws, ws_bytes))
+        rx.check(rx.relax_paged4_attention(dev, b.cache, rx.Seqs(q_lens, [bound, 41 if bound > 41 else 2], None, b.dev_table), b.dims, out, b.n, ws, ws_bytes))
+        want, tol = po.attention(q.astype(np.float64), b.pool, b.pages, 32, q_lens, kv_lens, None, 2, 64)
+        assert (np.abs(out.cpu().numpy().astype(np.float64) - want) <= tol).all()
+        assert rx.relax_workspace_error(b.dims, ws) == 0
+
+
+def test_append_and_read_on_device_lengths_next_to_the_end_of_their_type(rx):
+    """Lengths whose last block ends behind 2^31, or below zero: no page, no row of another sequence touched."""
+    rng = np.random.default_rng(83)
+    b = Bench(rx, rng, 4, 2, 64, 16, [3, 20, 1], [20, 32, 9], device_table=True, prep=dict())
+    qkv = half(rng, (b.n, 8 * 64))
+    for length in (2 ** 31 - 1, 2 ** 31 - 5, 2 ** 31 - 16, 2 ** 31 - 17, -1, -1000, -2 ** 31 + 2, -2 ** 31):
+        for lost, rows in ((0, slice(0, 3)), (1, slice(3, 23))):
+            b.dev_table[2] = torch.tensor([20, 32, 9], dtype=torch.int32)
+            b.clear()
+            q = b.append(qkv)
+            b.read()
+            assert b.error() == 0
+            b.dev_table[2, lost] = length
+            held = b.host_pool()
+            again_q = b.append(qkv)
+            assert b.error() == 4
+            keep = np.ones(b.n, bool)
+            keep[rows] = False
+            assert same_bits(again_q[keep], q[keep])
+            again = b.host_pool()
+            for key in held:
+                assert same_bits(held[key], again[key]), (length, lost, key)
+            got = b.read()
+            assert (got[:, rows] == 0).all()
+
+
+@pytest.mark.parametrize("by_address", [False, True])
+def test_python_calls_on_a_stream_of_their_own(rx, by_address):
+    """Table, heads, append, attention and read on a side stream that starts late, with nothing but what the calls allocate, against the same on the current stream; the current
+    stream allocates and writes in between."""
+    from paper_2311_02103_amd import runtime
+    rng = np.random.default_rng(80)
+    make = lambda: runtime.DevicePaged4Cache(n_heads=8, n_kv_heads=2, head_dim=64, kv_capacity=512, n_pages=16, page_size=32, n_max=500)
+    here, there = make(), make()
+    for layer in (here, there):
+        layer.pages.copy_(torch.arange(16, dtype=torch.int32).view(1, 16))
+    x = torch.from_numpy(half(rng, (500, 12 * 64))).cuda()
+    seqs, scaling = rx.Seqs([500], [500]), rx.RopeScaling(rx.ROPE_LINEAR, 128, 10000.0, 2.0)
+
+    def run(layer, stream):
+        q = layer.append(x, seqs, stream=stream)
+        return (q, layer.attention(q, seqs, stream=stream), *layer.read(seqs, 500, stream=stream), *layer.heads(x, seqs, stream=stream), runtime.rope_table(scaling, 5000, stream=stream))
+    want = run(here, None)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            late = torch.randn(2048, 2048, device="cuda") @ torch.randn(2048, 2048, device="cuda")
+    for _ in range(3):
+        got = run(there, side.cuda_stream if by_address else side)
+        noise = [torch.full((size,), 255, dtype=torch.uint8, device="cuda") for size in (512, 4096, 65536, 1 << 20) for _ in range(4)]
+    torch.cuda.synchronize()
+    assert len(noise) == 16 and late.shape == (2048, 2048)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+
+
 def test_shared_pages(rx):
     """Two sequences on the same first pages."""
     def share(b):
