@@ -385,13 +385,14 @@ __device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *
 }
 
 // grid: item * g + KV head, an item being a part of a tile (the tiles of a part side by side: they read the same tokens).  per_seq: as tile_of takes it.  part: [row][head][splits][D + 2], of
-// rows that have more than one part.  FEW: no sequence has more than eight pairs.
+// rows that have more than one part.  FEW: no sequence has more than eight pairs; three wavefronts per SIMD (64 sequences of 100 to 730 tokens, 32 / 32 heads: 28.2 us for 31.2 with two; the fewest
+// sequences as before).
 struct Grid {
     int h, g, rep, per_seq, chunk, splits, least;
     Divisor by_g, by_rep, by_per_seq, by_chunk;
 };
 template <int D, bool FEW, int W>
-__global__ __launch_bounds__(64 * W, 2) void attn_paged4_kernel(PagedSeqs, const uint16_t *q, Paged4Args pa, float *__restrict__ part, uint16_t *out, Grid gr)
+__global__ __launch_bounds__(64 * W, FEW ? 3 : 2) void attn_paged4_kernel(PagedSeqs, const uint16_t *q, Paged4Args pa, float *__restrict__ part, uint16_t *out, Grid gr)
 {
     __shared__ __align__(16) States<D, FEW ? 8 : kTile, W> lds;
     const int rep = gr.rep, item = quotient(blockIdx.x, gr.by_g), kvh = (int)blockIdx.x - item * gr.g;
@@ -419,11 +420,15 @@ __global__ __launch_bounds__(64 * W, 2) void attn_paged4_kernel(PagedSeqs, const
     else if constexpr (!FEW) n_pairs <= 16 ? attend<D, 1, false>(lds, task, q, pa, part, out, gr.h, gr.g) : attend<D, 2, false>(lds, task, q, pa, part, out, gr.h, gr.g);
 }
 
-// Estimated times, us, fitted to 24 calls with 10 to 20 cuts each, of which they choose one that is 0.4 % behind the best in the mean and 10 % at most.  With up to 16 pairs and with more: a workgroup's
-// beginning and end, with four and with eight wavefronts; a step of 32 tokens, alone on a SIMD and beside another wavefront (heads of 64: times kHalfHead).  The share of the longest workgroup
-// that comes on top when there are more of them than at a time; a merge, and each of its partial results; the cache's bytes
-constexpr float kGroupUs[2][2] = {{3.8f, 5.8f}, {3.8f, 8.8f}}, kStepUs[2][2] = {{0.96f, 1.17f}, {1.1f, 1.8f}}, kHalfHead = 0.71f, kTail = 0.14f, kMergeUs = 2.9f, kMergeResultUs = 4.1e-4f, kBytesUs = 5.1f,
-                kBytesPerUs = 6.15e6f;
+// Estimated times, us, fitted to 46 calls with up to 40 cuts each, of which they choose one that is 0.7 % behind the best in the mean and 12 % at most.  kGroupUs: a workgroup's beginning and end, with
+// one, four and eight wavefronts (kWideGroupUs: with four and eight, where a sequence has more than 16 pairs); kStepUs: a step of 32 tokens with up to three wavefronts on a SIMD (kWideStepUs: up to
+// two); heads of 64: times kHalfHead.  kTail: the share of the longest workgroup that comes on top when there are more of them than at a time.  A merge, and each of its partial results; the
+// cache's bytes.
+// One wavefront alone has no states to merge and the shortest end, which counts when there are several rounds of workgroups: 128 sequences of 20 to 530 tokens, 32 / 32 heads, 39.4 us for 47.0 with four;
+// two are between them (never more than 12 % better than the best of the others) and are not built.
+constexpr int kWaves[3] = {1, 4, 8};
+constexpr float kGroupUs[3] = {3.0f, 3.5f, 5.4f}, kWideGroupUs[3] = {0.0f, 3.2f, 7.1f}, kStepUs[3] = {0.96f, 1.14f, 1.19f}, kWideStepUs[2] = {1.1f, 1.11f}, kHalfHead = 0.89f, kTail = 0.15f, kMergeUs = 3.45f,
+                kMergeResultUs = 3.2e-4f, kBytesUs = 5.9f, kBytesPerUs = 7.0e6f;
 // Tiles of 256 pairs over all KV heads from which the kernel of such tiles is faster: it has 256 workgroups at a time, each as slow alone as beside 255 others (us, these tiles / those: 1200 rows on 600
 // cached tokens of 32 / 8 heads, 150 tiles, 52.7 / 59.7; 1600 rows, 200, 51.7 / 54.4 and on 600 cached tokens 76.2 / 71.4; 2043 rows, 255, 71.6 / 66.0; 4096 rows, 512, 227 / 141)
 constexpr int kRowTiles = 200;
@@ -458,30 +463,38 @@ Cut cut(const PagedPlan &pl, const relax_layer_dims &dm, const PagedSeqs &st, co
     int64_t chunk = std::max<int64_t>(32, ((int64_t)L_max + 31) & ~31);
     float best = INFINITY;
     const auto up = [](float x) { return (float)(int32_t)(x + 0.9999f); };      // (ceilf is a function call here: 1 us of a call's host time with 64 sequences)
-    // takes parts of up to c tokens if they are estimated to be faster than what was considered before.  Two wavefronts per SIMD: 512 workgroups of four at a time, 256 of eight
+    // takes parts of up to c tokens if they are estimated to be faster than what was considered before.  Workgroups at a time: what three wavefronts per SIMD make of one and of four, two of eight;
+    // with more than eight pairs two wavefronts per SIMD, and not one alone
+    const bool few = most <= 8;
+    const float slots[3] = {12.0f * 256.0f, few ? 3.0f * 256.0f : 2.0f * 256.0f, 256.0f};
     const auto consider = [&](int64_t c) {
         const float by_c = 1.0f / (float)c;
-        float groups = 0.0f, merged = 0.0f, total[2] = {0.0f, 0.0f}, longest[2][2] = {{0.0f, 0.0f}, {0.0f, 0.0f}};
+        float groups = 0.0f, merged = 0.0f, wide_groups = 0.0f;
+        float steps[3] = {0.0f, 0.0f, 0.0f}, wide_steps[3] = {0.0f, 0.0f, 0.0f}, most_steps[3] = {0.0f, 0.0f, 0.0f}, most_wide[3] = {0.0f, 0.0f, 0.0f};
         for (int b = 0; b < sq.B; ++b) {
             const float t = (float)tiles_of(b), L = (float)sq.kv_lens[b];
             if (t == 0.0f) continue;
-            const float parts = up(L * by_c), share = parts == 1.0f ? L : L / parts;
+            const float parts = up(L * by_c), share = parts == 1.0f ? L : L / parts, k = t * parts;
             const bool wide = (int64_t)sq.q_lens[b] * rep > 16;
-            const float *step = kStepUs[wide], *group = kGroupUs[wide];
-            for (int w = 0; w < 2; ++w) {
-                const float steps = up(share * (w ? 1.0f / 256 : 1.0f / 128)) * head, beside = group[w] + steps * step[1];
-                longest[w][0] = std::max(longest[w][0], group[w] + steps * step[0]), longest[w][1] = std::max(longest[w][1], beside);
-                total[w] += beside * t * parts;
+            for (int w = few ? 0 : 1; w < 3; ++w) {
+                const float n = up(share * (1.0f / (float)(32 * kWaves[w])));
+                if (wide) wide_steps[w] += n * k, most_wide[w] = std::max(most_wide[w], n);
+                else steps[w] += n * k, most_steps[w] = std::max(most_steps[w], n);
             }
-            groups += t * parts;
+            groups += k;
+            if (wide) wide_groups += k;
             if (parts > 1.0f) merged += (float)sq.q_lens[b] * parts;
         }
-        groups *= (float)g;
-        for (int w = 0; w < 2; ++w) {
-            const float slots = w ? 256.0f : 512.0f;
-            float us = groups <= slots ? longest[w][groups * (w ? 8.0f : 4.0f) > 1024.0f] : total[w] * (float)g / slots + kTail * longest[w][1];
+        const float all = groups * (float)g;
+        for (int w = few ? 0 : 1; w < 3; ++w) {
+            const float on_simd = all * (float)kWaves[w] * (1.0f / 1024.0f);
+            const int n = on_simd <= 1.0f ? 0 : on_simd <= 2.0f || !few || w == 2 ? 1 : 2;
+            const float step = kStepUs[n] * head, wide_step = kWideStepUs[std::min(n, 1)] * head;
+            const float longest = std::max(most_steps[w] > 0.0f ? kGroupUs[w] + most_steps[w] * step : 0.0f, most_wide[w] > 0.0f ? kWideGroupUs[w] + most_wide[w] * wide_step : 0.0f);
+            const float total = (groups - wide_groups) * kGroupUs[w] + steps[w] * step + wide_groups * kWideGroupUs[w] + wide_steps[w] * wide_step;
+            float us = all <= slots[w] ? longest : total * (float)g / slots[w] + kTail * longest;
             us = std::max(us, bytes_us) + (merged > 0.0f ? kMergeUs + kMergeResultUs * merged * (float)dm.n_heads : 0.0f);
-            if (us < best) best = us, chunk = c, waves = w ? 8 : 4;
+            if (us < best) best = us, chunk = c, waves = kWaves[w];
         }
     };
     if (tiles * g < 2048) {
@@ -494,7 +507,7 @@ Cut cut(const PagedPlan &pl, const relax_layer_dims &dm, const PagedSeqs &st, co
         const int64_t even = (tokens * g / 512 + 32) & ~31;    // as many parts as workgroups at a time, for sequences alike
         if (even >= least && even < L_max) consider(even);
     }
-    Cut c = {0, (int32_t)chunk, (int32_t)((L_max + chunk - 1) / chunk), -1, 0, waves, most <= 8};
+    Cut c = {0, (int32_t)chunk, (int32_t)((L_max + chunk - 1) / chunk), -1, 0, waves, few};
     for (int b = 0; b < sq.B; ++b) {
         const int64_t parts = st.dev ? c.splits : (sq.kv_lens[b] + chunk - 1) / chunk, items = tiles_of(b) * parts;
         c.items += items;
@@ -606,7 +619,8 @@ hipError_t launch_d(const uint16_t *q, const Paged4Args &pa, const relax_layer_d
     };
     using four = std::integral_constant<int, 4>;
     using eight = std::integral_constant<int, 8>;
-    if (c.waves == 8) c.few ? launch(std::true_type{}, eight{}) : launch(std::false_type{}, eight{});
+    if (c.waves == 1) launch(std::true_type{}, std::integral_constant<int, 1>{});
+    else if (c.waves == 8) c.few ? launch(std::true_type{}, eight{}) : launch(std::false_type{}, eight{});
     else c.few ? launch(std::true_type{}, four{}) : launch(std::false_type{}, four{});
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || c.rows == 0) return e;

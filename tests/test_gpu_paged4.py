@@ -462,6 +462,23 @@ def test_attention_of_many_sequences(rx, q_most, device_table):
     attention_case(rx, rng, (8, 2, 64), 16, q_lens, kv_lens, slots, device_table=device_table)
 
 
+@pytest.mark.parametrize("device_table", [False, True])
+@pytest.mark.parametrize("shape,count,q_most", [((32, 32, 128), 100, 1), ((16, 16, 64), 200, 1), ((32, 4, 64), 300, 1), ((16, 16, 128), 128, 7)], ids=str)
+def test_attention_of_many_short_sequences(rx, shape, count, q_most, device_table):
+    """More tiles than wavefronts at a time, with holes in some page tables."""
+    rng = np.random.default_rng(count + q_most)
+    q_lens = [int(rng.integers(1, q_most + 1)) for _ in range(count)]
+    kv_lens = [q + int(rng.integers(0, 150)) for q in q_lens]
+    kv_lens[3] = q_lens[3]
+
+    def lose(b):
+        for i in (5, 50, count - 1):
+            b.pages[i, 0] = -1
+        b.dev_pages.copy_(torch.from_numpy(b.pages))
+    b = attention_case(rx, rng, shape, 16, q_lens, kv_lens, device_table=device_table, edit=lose, heads=[0, shape[0] - 1])
+    assert b.error() == 4
+
+
 def scaled(factors):
     """edit: scales times what factors(rng, shape) gives, still of eight bits."""
     def edit(b):
