@@ -424,7 +424,7 @@ __global__ __launch_bounds__(64 * W, FEW ? 3 : 2) void attn_paged4_kernel(PagedS
 // one, four and eight wavefronts (kWideGroupUs: with four and eight, where a sequence has more than 16 pairs); kStepUs: a step of 32 tokens with up to three wavefronts on a SIMD (kWideStepUs: up to
 // two); heads of 64: times kHalfHead.  kTail: the share of the longest workgroup that comes on top when there are more of them than at a time.  A merge, and each of its partial results; the
 // cache's bytes.
-// One wavefront alone has no states to merge and the shortest end, which counts when there are several rounds of workgroups: 128 sequences of 20 to 530 tokens, 32 / 32 heads, 39.4 us for 47.0 with four;
+// One wavefront alone has no states to merge and the shortest end, which counts when there are several rounds of workgroups: 128 sequences of 20 to 530 tokens, 32 / 32 heads, 33.0 us for 39.5 with four;
 // two are between them (never more than 12 % better than the best of the others) and are not built.
 constexpr int kWaves[3] = {1, 4, 8};
 constexpr float kGroupUs[3] = {3.0f, 3.5f, 5.4f}, kWideGroupUs[3] = {0.0f, 3.2f, 7.1f}, kStepUs[3] = {0.96f, 1.14f, 1.19f}, kWideStepUs[2] = {1.1f, 1.11f}, kHalfHead = 0.89f, kTail = 0.15f, kMergeUs = 3.45f,
@@ -497,8 +497,8 @@ Cut cut(const PagedPlan &pl, const relax_layer_dims &dm, const PagedSeqs &st, co
             if (us < best) best = us, chunk = c, waves = kWaves[w];
         }
     };
+    consider(chunk);
     if (tiles * g < 2048) {
-        consider(chunk);
         const int64_t most_parts = std::max<int64_t>(1, kPagedPartials / ((int64_t)st.n * dm.n_heads)), least = (std::max<int64_t>(kLeast, L_max / most_parts + 1) + 31) & ~31;
         for (int parts = 2; parts <= (sq.B <= 4 ? 64 : sq.B <= 24 ? 16 : 4); parts += parts < 4 ? 1 : parts / 2) {
             const int64_t c = (L_max / parts + 32) & ~31;
