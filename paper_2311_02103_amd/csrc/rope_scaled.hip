@@ -1,5 +1,5 @@
 // Rotary tables of scaled positions: table[p][t] = amplitude (cos, sin)(p f'_t), fp64 rounded to fp32 (frequencies: relax_rope_scaling in relax_mi355.h).
-// A sine and cosine per entry made it bound by fp64 instructions: 131071 positions of 128 elements 32.7 us.  All entries of a thread from one, by rotation: 11.8 us, 5.7 TB/s
+// A sine and cosine per entry made it bound by fp64 instructions: 131071 positions of 128 elements 32.7 us.  All entries of a thread from one, by rotation: 11.2 to 11.8 us, 5.7 to 6.0 TB/s
 // written (9.8 at the rate of a fill).
 #include <algorithm>
 #include <cmath>
