@@ -474,7 +474,7 @@ Cut cut(const PagedPlan &pl, const relax_layer_dims &dm, const PagedSeqs &st, co
         for (int b = 0; b < sq.B; ++b) {
             const float t = (float)tiles_of(b), L = (float)sq.kv_lens[b];
             if (t == 0.0f) continue;
-            const float parts = up(L * by_c), share = parts == 1.0f ? L : L / parts, k = t * parts;
+            const float parts = std::max(up(L * by_c), 1.0f), share = parts == 1.0f ? L : L / parts, k = t * parts;
             const bool wide = (int64_t)sq.q_lens[b] * rep > 16;
             for (int w = few ? 0 : 1; w < 3; ++w) {
                 const float n = up(share * (1.0f / (float)(32 * kWaves[w])));
