@@ -486,7 +486,7 @@ relax_status relax_head_norm_rope(const uint16_t *q, int64_t q_stride, const uin
                                   const relax_layer_dims *dims, int32_t n, void *ws, size_t ws_bytes, relax_stream stream);
 
 /* ---- Paged KV cache in 4 bits ------------------------------------------------------------------------------------------------
- * relax_paged_cache with half its bytes: pages, blocks of RELAX_PAGED_BLOCK tokens, page table and descriptor are the same.  Every RELAX_PAGED4_GROUP elements of a token and
+ * relax_paged_cache in little more than half its bytes: pages, blocks of RELAX_PAGED_BLOCK tokens, page table and descriptor are the same.  Every RELAX_PAGED4_GROUP elements of a token and
  * KV head have a scale of their own and codes u in 0..15 that stand for (u - 8) * scale:
  *   scale = round8(x* / -8), x* the element of the largest magnitude (the positive one of two), round8 to eight significant bits, at most 8160 in size
  *   u     = 8 + round(x / scale), kept in 0..15 (8 where the scale is 0)
