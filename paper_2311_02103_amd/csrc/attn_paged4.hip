@@ -8,8 +8,10 @@
 // Up to eight pairs (a decode step with grouped heads): bytes and vector instructions are near each other, and a column costs little, so codes go into both products as fp16 integers 0..15
 // (paged4_device.h) and the scales meet columns.  A scale is constant over a k step of 32 elements, so a step is a product of its own, S_j = sum u q, and x = sum_j s_kj S_j.  The
 // accumulator of S_j starts at -8 sum q, which takes the codes' offset off.  The weight of a token times its value scale, w s_j, is rounded to fp16 once per group of 32 elements and is
-// the operand; -8 sum (w s_j), from one more product per group, goes to the result.  Weights are exp2(score - reference + 1) with a reference that trails the
-// maximum by at most 2: at most 8, and times 8160, the largest scale, an fp16 number.  The smallest ones lose bits: 2^-25 absolute, at most 2^-26 of the largest weight, per code.
+// the operand; -8 sum (w s_j), from one more product per group, goes to the result.  The reference of a column, which the weights are exp2(score - reference) to, stands 12 below the
+// largest score + log2 s of a lane's four tokens, s the root of the sum of squares of their scales, and moves when w s is about to leave fp16's range: the largest of these products is
+// 2^12 .. 65000 whatever the size of the values, and an operand below fp16's normal range is off by 2^-37 of it.  (A reference that follows the score alone has to leave room for the
+// largest scale, 8160, and rounds the tails of ordinary values away.)
 // More pairs: the vector unit bounds it, and a column costs more than a token, so operands are the numbers that the cache stands for, (u - 8) s = u s + (-8 s), one multiply-add per two and
 // exact (eight and four bits).  The products need no factor; the weight is rounded to fp16 and its sum is that of the rounded ones, from a product with ones.
 // (300 rows of 32 / 8 heads on 1201 tokens beside eight sequences of five: 30.7 us; with codes and scales of columns as above 36.7.)
@@ -27,7 +29,8 @@ namespace relax {
 namespace {
 
 constexpr float kUnset = -1e30f;                 // reference of a column that has met no token: below every score, and finite
-constexpr float kBias = 1.0f, kLag = 2.0f;       // up to eight pairs, log2: weight at the reference, and how far that may trail the maximum
+constexpr float kBias = 12.0f, kHead = 15.9f;    // up to eight pairs: log2 of the largest weight times scale behind a move of the reference, and before the next one
+constexpr float kLeast2 = 0x1p-28f;              // square of the least scale that counts there: subnormal ones may be zeros in a product, and zeros leave the weights, up to 2^30, in fp32's range
 constexpr float kPackedBias = 11.0f, kMost = 65000.0f;       // more: log2 of the weight at the reference, the largest weight before that moves
 
 typedef _Float16 half4p_t __attribute__((ext_vector_type(4)));
@@ -208,11 +211,20 @@ __device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *
                         if (!have(0) || first(0) + i > pos[0]) x[i] = -INFINITY;
                 }
                 load(kreg, ks, pa.k, pa.k_scale, k_four, min(s + 1, ns - 1));
-                float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-                mx = column_max(fmaxf(mx, lane_xor<8>(mx))) * c;
-                const bool move = mx > m[0] + kLag;
-                if (__any(move)) {
-                    const float to = move ? mx : m[0], alpha = __builtin_amdgcn_exp2f(m[0] - to);
+                if (gone) clean_scales();
+                float square = kLeast2;                        // of the lane's scales: each is below the root
+#pragma unroll
+                for (int j = 0; j < J; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; i += 2) {
+                        const half2p_t two = {vs[0][4 * j + i], vs[0][4 * j + i + 1]};
+                        square = __builtin_amdgcn_fdot2(two, two, square, false);
+                    }
+                const float level = 0.5f * __builtin_amdgcn_logf(square), mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), top = fmaf(mx, c, -m[0]) + level;      // above log2 of weights times scales
+                if (__any(top > kHead)) {                      // rare behind the first tokens; every column is new there
+                    const float high = column_max(fmaxf(top, lane_xor<8>(top))), at = fmaf(mx, c, level), near = column_max(fmaxf(at, lane_xor<8>(at))) - kBias;
+                    // a column moves by itself: no row depends on the others of its tile.  (A little too far: by more than the rounding of a large reference, which would put it below)
+                    const float to = high > kHead ? fmaf(fabsf(near), 0x1p-22f, near) : m[0], alpha = __builtin_amdgcn_exp2f(m[0] - to);
                     m[0] = to, l[0][0] *= alpha;
 #pragma unroll
                     for (int i = 0; i < NT; ++i) O[0][i] *= alpha;
@@ -220,11 +232,7 @@ __device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *
                     for (int j = 0; j < J; ++j) off[j] *= alpha;
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    w[i] = __builtin_amdgcn_exp2f(fmaf(x[i], c, kBias - m[0]));
-                    l[0][0] += w[i];
-                }
-                if (gone) clean_scales();
+                for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_exp2f(fmaf(x[i], c, -m[0])), l[0][0] += w[i];
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
                     half2p_t a[4], e[4], pw[4];                // pw: the weights of both blocks times their scales, tokens 0 2 | 1 3
