@@ -6,9 +6,8 @@ import pytest
 import paged4_oracle as po
 from test_gpu_paged4 import Bench, half, rx, seed_of  # noqa: F401  (rx: the fixture)
 
-pytestmark = pytest.mark.gpu
-
 torch = pytest.importorskip("torch")
+gpu = pytest.mark.gpu
 
 
 def exact_scores(b, rng, v_scale):
@@ -48,6 +47,7 @@ def narrow(q, b):
     return out, tol
 
 
+@gpu
 @pytest.mark.parametrize("exponent,spread", [(-12, 0), (-15, 0), (-10, 8), (0, 0), (12, 0)])
 @pytest.mark.parametrize("shape,rows,L", [((8, 1, 128), 1, 20001), ((8, 1, 128), 1, 4099), ((8, 1, 128), 3, 4099), ((16, 2, 64), 1, 9000), ((2, 2, 64), 3, 2000), ((4, 4, 64), 1, 700)], ids=str)
 def test_values_of_any_size(rx, shape, rows, L, exponent, spread):  # noqa: F811
@@ -62,6 +62,7 @@ def test_values_of_any_size(rx, shape, rows, L, exponent, spread):  # noqa: F811
     assert (over <= 1).all(), (float(over.max()), np.sqrt((got - want).var() / want.var()))
 
 
+@gpu
 @pytest.mark.parametrize("at", [0, 0.5, 1])
 @pytest.mark.parametrize("exponent", [-13, -3])
 @pytest.mark.parametrize("shape,rows,L", [((8, 1, 128), 1, 20001), ((16, 2, 64), 1, 9000), ((2, 2, 128), 4, 3000), ((4, 4, 64), 1, 700), ((8, 2, 128), 9, 3000)], ids=str)
@@ -89,6 +90,7 @@ def test_a_tail_of_small_weights(rx, shape, rows, L, exponent, at):  # noqa: F81
     assert np.abs(want).min() > 2.0 ** -20 and (over <= 1).all(), (float(over.max()), float(np.abs(got).max()), float(np.abs(want).min()))
 
 
+@gpu
 @pytest.mark.parametrize("shape,rows", [((8, 1, 128), 1), ((4, 4, 64), 3), ((8, 2, 64), 5)], ids=str)
 def test_scores_far_from_zero(rx, shape, rows):  # noqa: F811
     """Every score of a row is far below or above zero, up to 2^25: whatever the weights are held against stays a number.  (Beyond that fp32 tells scores apart by four and more.)"""
@@ -106,3 +108,132 @@ def test_scores_far_from_zero(rx, shape, rows):  # noqa: F811
             got = b.attention(q).astype(np.float64)
             want, tol = narrow(q.astype(np.float64), b)
             assert (np.abs(got - want) <= tol).all(), (sign, size, key_scale)
+
+
+def held(b, name, slot, L):
+    """(values, scales) of one slot's first L tokens, float32 [g, L, d] on the GPU."""
+    byte, shift = (torch.from_numpy(x).cuda() for x in po.code_place(name, b.d))
+    pages = torch.from_numpy(b.pages[slot, :-(-L // b.page_size)]).cuda().long()
+    u = (b.dev[name][pages][..., byte.flatten()].int() >> shift.flatten().int()) & 15            # [pages, g, blocks, 16 d]
+    s = b.dev[name + "s"][pages][..., torch.from_numpy(po.scale_place(b.d)).cuda().flatten()]
+    lead = u.shape[:3]
+    s = s.view(*lead, 16, b.d // 32).repeat_interleave(32, dim=4).float()
+    x = (u.view(*lead, 16, b.d).float() - 8) * s
+    order = lambda y: y.permute(1, 0, 2, 3, 4).reshape(b.g, -1, b.d)[:, :L].contiguous()
+    return order(x), order(s)
+
+
+def misses(out, v, s, mass):
+    """Where an output is not the value it has to be.  One token has all the weight but `mass`: what is rounded is its weight, or weight times scale, and the output, 2^-11 each, 2^-25 below
+    fp16's normal range, sums in fp32 of few terms that are not zero, below 2^-17 of a scale; and the others' values, 8 scales at most, on either side."""
+    return (out - v).abs() > 2.0 ** -10 * v.abs() + 2.0 ** -25 + (2.0 ** -17 + 16.0 * mass) * s.amax()
+
+
+EVERY = {  # (heads, KV heads, d), q_lens, kv_lens
+    "long": ((64, 8, 128), [1], [120001]), "long_4": ((8, 2, 64), [2], [30011]), "drafts": ((64, 8, 128), [3], [30011]), "tiles": ((16, 2, 64), [7, 1], [9000, 700]),
+    "ungrouped": ((40, 40, 128), [1], [3001]), "ragged": ((16, 2, 64), [1] * 7, [40, 3000, 1, 700, 16, 9000, 129]), "chunk": ((8, 1, 128), [40, 3], [5000, 1030]),
+    "rows": ((200, 200, 64), [256], [8200]), "short": ((32, 32, 64), [1] * 70, [100 + 3 * i for i in range(70)]),
+}
+
+
+@gpu
+@pytest.mark.parametrize("device_table", [False, True])
+@pytest.mark.parametrize("kind", sorted(EVERY))
+def test_every_token_counts(rx, kind, device_table):  # noqa: F811
+    """For every token of every sequence and KV head a query that gives it all the weight, in the context's length and cut of the call: the answer is its value, at the first token and the last one and on
+    either side of every border of steps, wavefronts, parts and lookups.  A lost token is an answer from another."""
+    shape, q_lens, kv_lens = EVERY[kind]
+    rng = np.random.default_rng(seed_of(kind))
+    slots = [int(x) for x in rng.permutation(len(q_lens))]
+    b = Bench(rx, rng, *shape, 64, q_lens, kv_lens, slots, device_table=device_table)
+    exact_scores(b, rng, lambda s_: np.full(s_, 2.0 ** -11))
+    h, g, d = shape
+    rep = h // g
+    seqs, (ws, ws_bytes) = b.seqs(), b.workspace()
+    kv = [[held(b, name, slot, L) for name in "kv"] for slot, L in zip(slots, kv_lens)]
+    starts = np.concatenate([[0], np.cumsum(q_lens)])
+    calls = max(-(-L // (ql * rep)) for ql, L in zip(q_lens, kv_lens)) + 1
+    chosen = []                                                # [calls, rows, rep]: the token of a row and head of the group, at most the row's own
+    for ql, L in zip(q_lens, kv_lens):
+        at = torch.arange(calls * ql * rep, device="cuda").view(calls, ql, rep)
+        chosen.append(torch.minimum(at, torch.arange(L - ql, L, device="cuda")[None, :, None]))
+        assert len(torch.unique(chosen[-1])) == L
+    mass = 0.0                                                 # of all other tokens, at most: a score is 64 |k|^2 / sqrt d and theirs are 64 k . k' / sqrt d, exact in fp32
+    for (k, _), _ in kv:
+        for j in range(g):
+            for first in range(0, k.shape[1], 8192):
+                s = k[j, first:first + 8192] @ k[j].t().contiguous() * (64 / d ** 0.5)
+                mine = s[torch.arange(s.shape[0]), first + torch.arange(s.shape[0])].clone()
+                s[torch.arange(s.shape[0]), first + torch.arange(s.shape[0])] = -float("inf")
+                mass = max(mass, float((s - mine[:, None]).exp_().sum(dim=1).max()))
+    assert mass < 2.0 ** -12, mass
+    step, wrong = max(1, (1 << 28) // (b.n * h * d)), 0
+    for lo in range(0, calls, step):
+        hi = min(calls, lo + step)
+        q = torch.empty((hi - lo, b.n, g, rep, d), dtype=torch.float16, device="cuda")
+        for i, ((k, _), _) in enumerate(kv):
+            q[:, starts[i]:starts[i + 1]] = (64 * k[:, chosen[i][lo:hi]]).permute(1, 2, 0, 3, 4).half()
+        out = torch.full_like(q, float("nan"))
+        for c in range(hi - lo):
+            rx.check(rx.relax_paged4_attention(q[c], b.cache, seqs, b.dims, out[c], b.n, ws, ws_bytes))
+        for i, (_, (v, s)) in enumerate(kv):
+            want = v[:, chosen[i][lo:hi]].permute(1, 2, 0, 3, 4)
+            wrong += int(misses(out[:, starts[i]:starts[i + 1]].float(), want, s, mass).any(dim=4).sum()) + int(out[:, starts[i]:starts[i + 1]].isnan().sum())
+        del q, out
+    assert wrong == 0 and b.error() == 0
+
+
+ONCE = {
+    "few": ((64, 8, 128), [1], [3001]), "few_4": ((8, 2, 64), [2], [2500]), "drafts": ((64, 8, 128), [3], [30011]), "tiles": ((16, 2, 64), [7, 1], [9000, 700]),
+    "ungrouped": ((40, 40, 128), [1], [3001]), "ragged": ((16, 2, 64), [1] * 7, [40, 3000, 1, 700, 16, 2900, 129]), "chunk": ((8, 1, 128), [40, 3], [5000, 1030]),
+    "rows": ((200, 200, 64), [256], [8200]), "short": ((32, 32, 64), [1] * 70, [100 + 3 * i for i in range(70)]),
+}
+
+
+@gpu
+@pytest.mark.parametrize("device_table", [False, True])
+@pytest.mark.parametrize("kind", sorted(ONCE))
+def test_every_token_counts_once(rx, kind, device_table):  # noqa: F811
+    """Equal scores, and of each element of a head one token alone whose value is not zero: its part of the sum.  A token that two wavefronts or parts count is twice that.
+    The product of weight and scale, the weight in the denominator and the output are rounded, 3 times 2^-11; sums in fp32 as in narrow()."""
+    shape, q_lens, kv_lens = ONCE[kind]
+    rng = np.random.default_rng(seed_of(kind))
+    slots = [int(x) for x in rng.permutation(len(q_lens))]
+    b = Bench(rx, rng, *shape, 64, q_lens, kv_lens, slots, device_table=device_table)
+    exact_scores(b, rng, lambda s_: np.full(s_, 512.0))
+    b.pool["vs"] = np.abs(b.pool["vs"])
+    b.dev["vs"].copy_(torch.from_numpy(b.pool["vs"]))
+    h, g, d = shape
+    rep = h // g
+    seqs, (ws, ws_bytes) = b.seqs(), b.workspace()
+    byte, shift = (torch.from_numpy(x).cuda() for x in po.code_place("v", d))
+    q, wrong = torch.zeros((b.n, h, d), dtype=torch.float16, device="cuda"), 0
+    starts = np.concatenate([[0], np.cumsum(q_lens)])
+    for call in range(-(-max(kv_lens) // (g * d))):
+        b.dev["v"].fill_(0x88)
+        token = ((call * g + torch.arange(g, device="cuda"))[:, None] * d + torch.arange(d, device="cuda")).expand(g, d)
+        for slot, L in zip(slots, kv_lens):
+            j, e = torch.nonzero(token < L, as_tuple=True)
+            t = token[j, e]
+            page, at, sh = torch.from_numpy(b.pages[slot]).cuda().long()[t // 64], byte[t % 16, e], shift[t % 16, e]
+            b.dev["v"][page, j, t % 64 // 16, at] = torch.where(sh == 0, 0x8F, 0xF8).to(torch.uint8)
+        out = torch.full_like(q, float("nan"))
+        rx.check(rx.relax_paged4_attention(q, b.cache, seqs, b.dims, out, b.n, ws, ws_bytes))
+        for i, (ql, L) in enumerate(zip(q_lens, kv_lens)):
+            vis = torch.arange(L - ql, L, device="cuda")[:, None, None] + 1
+            want = torch.where(token < vis, 7 * 512.0 / vis, 0.0)[:, :, None]              # [rows, g, 1, d]
+            got = out[starts[i]:starts[i + 1]].view(ql, g, rep, d).float()
+            few = 1 <= ql * rep % 32 <= 8                      # a tile of codes 0..15 against -8 sum p s: sums of 512 scales, whose terms cancel but for one
+            tol = 3 * 2.0 ** -11 * want + (L / 32 + 8) * 4 * 2.0 ** -24 * (23 * 512.0 if few else want)
+            assert bool((tol[want > 0] < want[want > 0] / 2).all())
+            wrong += int((~((got - want).abs() <= tol)).sum())
+    assert wrong == 0 and b.error() == 0
+
+
+def test_a_lost_token_is_a_miss():
+    """The check above on an oracle that leaves a token out: its answer is another token's value, which differs by codes, many tolerances."""
+    torch.manual_seed(3)
+    u, s = torch.randint(0, 16, (500, 64)), torch.full((500, 64), 2.0 ** -11)
+    v = (u - 8) * s
+    assert not misses(v.half().float(), v, s, 2.0 ** -12).any()
+    assert misses(v.roll(1, 0).half().float(), v, s, 2.0 ** -12).any(dim=1).all() and misses(torch.zeros_like(v), v, s, 2.0 ** -12).any(dim=1).all()
