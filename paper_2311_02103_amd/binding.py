@@ -251,7 +251,7 @@ def _ref(obj):
     return None if obj is None else C.byref(obj)
 
 
-# Arguments of the calls that _call makes, a letter each: p device memory, i integer, r struct, s stream (csrc/marshal.c)
+# Arguments of the calls that _bind makes, a letter each: p device memory, i integer, r struct, s stream (csrc/marshal.c)
 _KINDS = {
     "relax_rope_table_scaled": "rips",
     "relax_head_norm_rope": "pipipipirrripis",
@@ -263,17 +263,24 @@ _bound = {}
 
 
 def _bind(name: str):
-    """The function of the library as one that takes tensors, objects of this module and streams; made at its first call."""
+    """The function of the library as one that takes tensors, objects of this module and streams; made at its first call.  A struct is None or of its own type: the
+    library reads whatever it is given as that."""
     fn, kinds = getattr(lib(), name), _KINDS[name]
+    wanted = [_STRUCTS[cls] for cls in _TAKES[name]]
     if _marshal is not None:
         _marshal.slow_stream(_stream)
-        call = _marshal.Call(C.cast(fn, C.c_void_p).value, kinds)
+        call = _marshal.Call(C.cast(fn, C.c_void_p).value, kinds, tuple(wanted))
     else:
         convert = {"p": _ptr, "i": lambda i: i, "r": lambda o: _ref(o.c() if hasattr(o, "c") else o), "s": _stream}
+        types = iter(wanted)
+        checks = [next(types) if kind == "r" else None for kind in kinds]
 
         def call(*args):
             if len(args) != len(kinds):
                 raise TypeError("%d positional arguments" % len(kinds))
+            for check, arg in zip(checks, args):
+                if check is not None and arg is not None and not isinstance(arg, check):
+                    raise TypeError("%s, not %s" % (type(arg).__name__, check[0].__name__))
             return fn(*[convert[kind](arg) for kind, arg in zip(kinds, args)])
     _bound[name] = call
     return call
@@ -386,6 +393,18 @@ class Seqs(_PySeqs if _marshal is None else _marshal.Seqs):
             struct_ = SeqsC.from_address(self._at)
             struct_._seqs = self               # its memory
             return struct_
+
+
+# What a struct argument may be: this module's object or the C struct itself
+_STRUCTS = {Seqs: (_PySeqs if _marshal is None else _marshal.Seqs, SeqsC), LayerDims: (LayerDims,), Paged4Cache: (Paged4Cache, Paged4CacheC), HeadPrep: (HeadPrep, HeadPrepC),
+            RopeScaling: (RopeScaling,)}
+_TAKES = {
+    "relax_rope_table_scaled": (RopeScaling,),
+    "relax_head_norm_rope": (HeadPrep, Seqs, LayerDims),
+    "relax_paged4_append": (HeadPrep, Paged4Cache, Seqs, LayerDims),
+    "relax_paged4_attention": (Paged4Cache, Seqs, LayerDims),
+    "relax_paged4_read": (Paged4Cache, Seqs, LayerDims),
+}
 
 
 def make_dims(hidden, n_heads, n_kv_heads, head_dim, ffn, kv_capacity, kv_slots=1, rms_eps=1e-5, rope_base=10000.0,

@@ -1,10 +1,10 @@
 /* Argument marshalling of binding.py's calls, as a CPython extension: what ctypes does with a call of fifteen arguments, and building a descriptor, took longer than the library's own
  * part of the call and the launch together.
  *
- *   Call(address, kinds)(*args) -> int      calls the C function at `address`, which takes integers and pointers alone and returns an int32; `kinds` has a letter per argument
+ *   Call(address, kinds, types)(*args) -> int      calls the C function at `address`, which takes integers and pointers alone and returns an int32; `kinds` has a letter per argument
  *     p  a pointer to device memory: None, an address, or a tensor (contiguous: its data_ptr())
  *     i  an integer
- *     r  a pointer to a struct: None, a Seqs, a ctypes structure, or an object whose _at is an address
+ *     r  a pointer to a struct: None, a Seqs, a ctypes structure, or an object whose _at is an address; of `types`, if given, which has a type, or a tuple of types, per r
  *     s  a stream: None (the current one), an address, or an object whose cuda_stream is one
  *   Seqs(q_lens, kv_lens, slots, device_table)      relax_seqs with arrays of its own
  */
@@ -156,14 +156,25 @@ typedef struct {
     void *fn;
     int count;
     char kinds[MAX_ARGS + 1];
+    PyObject *types;                            /* a tuple of tuples of types, or NULL */
 } Call;
 
-static int struct_of(PyObject *o, void **out)
+/* The library reads what it is given as the struct of that argument: nothing else may get there. */
+static int type_fits(PyObject *o, PyObject *types)
+{
+    for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(types); ++i)
+        if (PyObject_TypeCheck(o, (PyTypeObject *)PyTuple_GET_ITEM(types, i))) return 1;
+    PyErr_Format(PyExc_TypeError, "%.100s, not %.100s", Py_TYPE(o)->tp_name, ((PyTypeObject *)PyTuple_GET_ITEM(types, 0))->tp_name);
+    return 0;
+}
+
+static int struct_of(PyObject *o, PyObject *types, void **out)
 {
     if (o == Py_None) {
         *out = NULL;
         return 0;
     }
+    if (types && !type_fits(o, types)) return -1;
     if (PyObject_TypeCheck(o, &SeqsType)) {
         *out = &((Seqs *)o)->c;
         return 0;
@@ -205,11 +216,11 @@ static PyObject *call_run(Call *self, PyObject *const *args, size_t flags, PyObj
         return NULL;
     }
     void *a[MAX_ARGS] = {0};
-    for (int i = 0; i < self->count; ++i) {
+    for (int i = 0, structs = 0; i < self->count; ++i) {
         int bad = 0;
         switch (self->kinds[i]) {
         case 'p': bad = pointer_of(args[i], &a[i]); break;
-        case 'r': bad = struct_of(args[i], &a[i]); break;
+        case 'r': bad = struct_of(args[i], self->types ? PyTuple_GET_ITEM(self->types, structs++) : NULL, &a[i]); break;
         case 's': bad = stream_of(args[i], &a[i]); break;
         default: {
             const long long v = PyLong_AsLongLong(args[i]);
@@ -228,11 +239,34 @@ static PyObject *call_run(Call *self, PyObject *const *args, size_t flags, PyObj
     return PyLong_FromLong(rc);
 }
 
+/* tuples of types for `count` structs, from a tuple of types and of tuples of types */
+static PyObject *types_of(PyObject *given, Py_ssize_t count)
+{
+    if (!PyTuple_Check(given) || PyTuple_GET_SIZE(given) != count) {
+        PyErr_SetString(PyExc_ValueError, "a tuple with the type of each struct");
+        return NULL;
+    }
+    PyObject *all = PyTuple_New(count);
+    for (Py_ssize_t i = 0; all && i < count; ++i) {
+        PyObject *one = PyTuple_GET_ITEM(given, i);
+        one = PyTuple_Check(one) ? Py_NewRef(one) : PyTuple_Pack(1, one);
+        int ok = one && PyTuple_GET_SIZE(one) > 0;
+        for (Py_ssize_t j = 0; ok && j < PyTuple_GET_SIZE(one); ++j) ok = PyType_Check(PyTuple_GET_ITEM(one, j));
+        if (ok) PyTuple_SET_ITEM(all, i, one);
+        else {
+            if (one) PyErr_SetString(PyExc_TypeError, "types, or tuples of types");
+            Py_XDECREF(one);
+            Py_CLEAR(all);
+        }
+    }
+    return all;
+}
+
 static PyObject *call_new(PyTypeObject *type, PyObject *args, PyObject *kw)
 {
-    PyObject *address;
+    PyObject *address, *given = Py_None, *types = NULL;
     const char *kinds;
-    if (!PyArg_ParseTuple(args, "Os", &address, &kinds)) return NULL;
+    if (!PyArg_ParseTuple(args, "Os|O", &address, &kinds, &given)) return NULL;
     const size_t count = strlen(kinds);
     void *fn = PyLong_AsVoidPtr(address);
     if (PyErr_Occurred()) return NULL;
@@ -240,13 +274,29 @@ static PyObject *call_new(PyTypeObject *type, PyObject *args, PyObject *kw)
         PyErr_SetString(PyExc_ValueError, "an address and at most 16 of the letters p, i, r, s");
         return NULL;
     }
+    if (given != Py_None) {
+        Py_ssize_t structs = 0;
+        for (size_t i = 0; i < count; ++i) structs += kinds[i] == 'r';
+        types = types_of(given, structs);
+        if (!types) return NULL;
+    }
     Call *self = (Call *)type->tp_alloc(type, 0);
-    if (!self) return NULL;
+    if (!self) {
+        Py_XDECREF(types);
+        return NULL;
+    }
     self->vectorcall = (vectorcallfunc)call_run;
     self->fn = fn;
     self->count = (int)count;
+    self->types = types;
     memcpy(self->kinds, kinds, count + 1);
     return (PyObject *)self;
+}
+
+static void call_dealloc(Call *self)
+{
+    Py_XDECREF(self->types);
+    Py_TYPE(self)->tp_free((PyObject *)self);
 }
 
 static PyTypeObject CallType = {
@@ -254,6 +304,7 @@ static PyTypeObject CallType = {
     .tp_basicsize = sizeof(Call),
     .tp_flags = Py_TPFLAGS_DEFAULT | Py_TPFLAGS_HAVE_VECTORCALL,
     .tp_new = call_new,
+    .tp_dealloc = (destructor)call_dealloc,
     .tp_call = PyVectorcall_Call,
     .tp_vectorcall_offset = offsetof(Call, vectorcall),
 };

@@ -140,3 +140,52 @@ def test_the_python_form_says_the_same(monkeypatch):
     assert codes() == fast and len(set(fast)) >= 4
     with pytest.raises(TypeError):
         rx._bound["relax_paged4_read"](1, 2)
+
+
+def struct_calls():
+    """(name, its arguments, {place of a struct among them: what belongs there}) of each call with structs."""
+    P, s, d, cache, prep, scaling = 0x10000, rx.Seqs([2], [5]), rx.make_dims(256, 4, 4, 64, 688, 64, 2), rx.Paged4Cache(*[0x10000] * 5, 10, 16, 4), rx.HeadPrep(), rx.RopeScaling(7, 64)
+    return [("relax_rope_table_scaled", [scaling, 4, P, 0], {0: scaling}), ("relax_head_norm_rope", [P, 256, None, 0, P, 256, None, 0, prep, s, d, 2, P, 8, 0], {8: prep, 9: s, 10: d}),
+            ("relax_paged4_append", [P, 256, P, P, 256, P, prep, cache, s, d, 2, P, 8, 0], {6: prep, 7: cache, 8: s, 9: d}),
+            ("relax_paged4_attention", [P, cache, s, d, P, 2, P, 8, 0], {1: cache, 2: s, 3: d}), ("relax_paged4_read", [cache, s, d, P, None, 2, P, 8, 0], {0: cache, 1: s, 2: d})]
+
+
+@pytest.mark.parametrize("in_c", [True, False])
+@pytest.mark.parametrize("name,args,places", struct_calls(), ids=lambda x: x if isinstance(x, str) else "")
+def test_structs_of_another_type_are_refused(monkeypatch, name, args, places, in_c):
+    """Anything but None and the struct that an argument is for: the library would read it as that struct.  (Those here have 4 KB of zeros behind their addresses.)"""
+    monkeypatch.setattr(rx, "_bound", {})
+    if not in_c:
+        monkeypatch.setattr(rx, "_marshal", None)
+    room = (C.c_char * 4096)()
+    wrong = [bytearray(4096), np.zeros(1024, np.int32), torch.zeros(1024, dtype=torch.int32), [2], "x", 0x10000, At(C.addressof(room)), room, object(), rx.KVCache(1, 2, 3)]
+    wrong += list({id(x): x for _, _, p in struct_calls() for x in p.values()}.values())
+    call = getattr(rx, name)
+    right = call(*args)
+    for at, mine in places.items():
+        for other in wrong:
+            if type(other) is type(mine):
+                continue
+            with pytest.raises(TypeError):
+                call(*args[:at], other, *args[at + 1:])
+        assert call(*args[:at], None, *args[at + 1:]) == (right if name == "relax_paged4_append" and at == 6 else rx.ERR_NULL)      # (no preparation)
+        raw = mine.c() if hasattr(mine, "c") else mine             # the C struct itself, and a subclass
+        assert call(*args[:at], raw, *args[at + 1:]) == right
+    assert call(*args) == right
+
+
+def test_types_of_a_call():
+    rec = Recorder(3)
+    call = marshal.Call(rec.address, "rir", (At, (rx.LayerDims, rx.Seqs)))
+    dims, seqs = rx.make_dims(64, 1, 1, 64, 64, 8), rx.Seqs([1], [2])
+
+    class Other(At):
+        pass
+    assert call(Other(5), 1, dims) == 0 and call(None, 2, seqs) == 0 and call(At(7), 3, None) == 0
+    assert [a[:2] for a in rec.got] == [(5, 1), (0, 2), (7, 3)]
+    for args in ((dims, 1, dims), (At(1), 1, At(1)), (At(1), 1, bytearray(64))):
+        with pytest.raises(TypeError):
+            call(*args)
+    for types in ((At,), (At, At, At), (At, 5), [At, At], (At, (At, 5))):
+        with pytest.raises((TypeError, ValueError)):
+            marshal.Call(rec.address, "rir", types)
