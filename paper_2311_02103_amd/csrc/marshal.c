@@ -130,6 +130,47 @@ done:
     return ok ? 0 : -1;
 }
 
+/* Twins by copy and deepcopy: what the constructor takes, and the attributes that Python code has added */
+static PyObject *list_of(const int32_t *at, Py_ssize_t n)
+{
+    PyObject *list = PyList_New(n);
+    for (Py_ssize_t i = 0; list && i < n; ++i) {
+        PyObject *item = PyLong_FromLong(at[i]);
+        if (!item) Py_CLEAR(list);
+        else PyList_SET_ITEM(list, i, item);
+    }
+    return list;
+}
+
+static PyObject *seqs_getstate(Seqs *s, PyObject *unused)
+{
+    PyObject *more = PyObject_GetAttrString((PyObject *)s, "__dict__"), *q, *kv, *slots;
+    if (!more) {
+        if (!PyErr_ExceptionMatches(PyExc_AttributeError)) return NULL;
+        PyErr_Clear();
+        more = Py_NewRef(Py_None);
+    }
+    q = list_of(s->c.q_lens, s->c.B), kv = list_of(s->c.kv_lens, s->c.B), slots = s->c.slots ? list_of(s->c.slots, s->c.B) : Py_NewRef(Py_None);
+    PyObject *state = q && kv && slots ? Py_BuildValue("((OOOO)O)", q, kv, slots, s->table ? s->table : Py_None, more) : NULL;
+    Py_XDECREF(q), Py_XDECREF(kv), Py_XDECREF(slots);
+    Py_DECREF(more);
+    return state;
+}
+
+static PyObject *seqs_setstate(Seqs *s, PyObject *state)
+{
+    PyObject *args, *more;
+    if (!PyArg_ParseTuple(state, "O!O", &PyTuple_Type, &args, &more) || seqs_init(s, args, NULL) < 0) return NULL;
+    if (more != Py_None) {
+        PyObject *dict = PyObject_GetAttrString((PyObject *)s, "__dict__");
+        const int bad = dict ? PyDict_Update(dict, more) : -1;
+        Py_XDECREF(dict);
+        if (bad < 0) return NULL;
+    }
+    Py_RETURN_NONE;
+}
+static PyMethodDef seqs_methods[] = {{"__getstate__", (PyCFunction)seqs_getstate, METH_NOARGS, NULL}, {"__setstate__", (PyCFunction)seqs_setstate, METH_O, NULL}, {0}};
+
 static void seqs_dealloc(Seqs *s)
 {
     seqs_clear(s);
@@ -147,6 +188,7 @@ static PyTypeObject SeqsType = {
     .tp_init = (initproc)seqs_init,
     .tp_dealloc = (destructor)seqs_dealloc,
     .tp_getset = seqs_get,
+    .tp_methods = seqs_methods,
 };
 
 /* ---- calls ------------------------------------------------------------------------------------------------------- */

@@ -189,3 +189,26 @@ def test_types_of_a_call():
     for types in ((At,), (At, At, At), (At, 5), [At, At], (At, (At, 5))):
         with pytest.raises((TypeError, ValueError)):
             marshal.Call(rec.address, "rir", types)
+
+
+@pytest.mark.parametrize("kind", [rx._PySeqs, rx.Seqs])
+def test_descriptors_are_copied(kind):
+    """Equal lengths, in memory that lives as long as the twin; the table is shared by a copy, copied by a deepcopy."""
+    import copy
+
+    class Mine(kind):
+        pass
+    table = torch.arange(8, dtype=torch.int32)
+    for cls in (kind, Mine):
+        seqs = cls([3, 1], [3, 900], [7, 2], table)
+        if cls is Mine:
+            seqs.note = "kept"
+        for twin, shared in ((copy.copy(seqs), True), (copy.deepcopy(seqs), False)):
+            assert type(twin) is cls and getattr(twin, "note", None) == getattr(seqs, "note", None)
+            a, b = descriptor(seqs), descriptor(twin)
+            assert a[:4] == b[:4] == (2, [3, 1], [3, 900], [7, 2])
+            assert (a[4] == b[4]) == shared and b[4]
+        alone = copy.deepcopy(cls(list(range(1, 50)), list(range(100, 149))))
+        gc.collect()
+        assert descriptor(alone) == (49, list(range(1, 50)), list(range(100, 149)), None, None)
+    assert descriptor(copy.copy(kind([], []))) == (0, [], [], None, None)
