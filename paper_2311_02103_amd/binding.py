@@ -9,6 +9,7 @@ There is no fallback: if the HIP library is missing, loading raises.
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 import struct
 import sys
@@ -374,10 +375,21 @@ class _PySeqs:
     def __init__(self, q_lens, kv_lens, slots=None, device_table=None):
         if len(kv_lens) < len(q_lens) or (slots is not None and len(slots) < len(q_lens)):
             raise ValueError("a length and a slot for each sequence")
-        self.B = len(q_lens)
         self._q, self._kv = _int32s(q_lens), _int32s(kv_lens)
         self._sl = None if slots is None else _int32s(slots)
         self._table = device_table
+        self.B = len(q_lens)
+
+    @property
+    def B(self) -> int:
+        return self._B
+
+    @B.setter
+    def B(self, B):
+        B = operator.index(B)
+        if not -1 << 31 <= B <= len(self._q):
+            raise ValueError("a length and a slot for each sequence")
+        self._B = B
 
     def c(self) -> SeqsC:
         return SeqsC(self.B, self._q, self._kv, self._sl, _ptr(self._table))       # arrays convert to pointers, and are kept alive by the struct

@@ -26,6 +26,7 @@ static PyObject *slow_stream;                   /* binding._stream */
 typedef struct {
     PyObject_HEAD
     relax_seqs c;
+    int32_t count;                              /* sequences that there are lengths for: c.B is at most that */
     int32_t *lens;
     PyObject *table;
 } Seqs;
@@ -74,6 +75,7 @@ static void seqs_clear(Seqs *s)
     s->lens = NULL;
     Py_CLEAR(s->table);
     s->c = (relax_seqs){0};
+    s->count = 0;
 }
 
 static int seqs_init(Seqs *s, PyObject *args, PyObject *kw)
@@ -123,6 +125,7 @@ static int seqs_init(Seqs *s, PyObject *args, PyObject *kw)
     seqs_clear(s);
     s->lens = lens;
     s->table = Py_NewRef(table);
+    s->count = (int32_t)n[0];
     s->c = (relax_seqs){(int32_t)n[0], start[0], start[1], start[2], device};
     ok = 1;
 done:
@@ -150,8 +153,8 @@ static PyObject *seqs_getstate(Seqs *s, PyObject *unused)
         PyErr_Clear();
         more = Py_NewRef(Py_None);
     }
-    q = list_of(s->c.q_lens, s->c.B), kv = list_of(s->c.kv_lens, s->c.B), slots = s->c.slots ? list_of(s->c.slots, s->c.B) : Py_NewRef(Py_None);
-    PyObject *state = q && kv && slots ? Py_BuildValue("((OOOO)O)", q, kv, slots, s->table ? s->table : Py_None, more) : NULL;
+    q = list_of(s->c.q_lens, s->count), kv = list_of(s->c.kv_lens, s->count), slots = s->c.slots ? list_of(s->c.slots, s->count) : Py_NewRef(Py_None);
+    PyObject *state = q && kv && slots ? Py_BuildValue("((OOOO)iO)", q, kv, slots, s->table ? s->table : Py_None, (int)s->c.B, more) : NULL;
     Py_XDECREF(q), Py_XDECREF(kv), Py_XDECREF(slots);
     Py_DECREF(more);
     return state;
@@ -160,7 +163,9 @@ static PyObject *seqs_getstate(Seqs *s, PyObject *unused)
 static PyObject *seqs_setstate(Seqs *s, PyObject *state)
 {
     PyObject *args, *more;
-    if (!PyArg_ParseTuple(state, "O!O", &PyTuple_Type, &args, &more) || seqs_init(s, args, NULL) < 0) return NULL;
+    int B;
+    if (!PyArg_ParseTuple(state, "O!iO", &PyTuple_Type, &args, &B, &more) || seqs_init(s, args, NULL) < 0) return NULL;
+    s->c.B = B < s->count ? B : s->count;
     if (more != Py_None) {
         PyObject *dict = PyObject_GetAttrString((PyObject *)s, "__dict__");
         const int bad = dict ? PyDict_Update(dict, more) : -1;
@@ -179,7 +184,22 @@ static void seqs_dealloc(Seqs *s)
 
 static PyObject *seqs_at(Seqs *s, void *unused) { return PyLong_FromVoidPtr(&s->c); }
 static PyObject *seqs_B(Seqs *s, void *unused) { return PyLong_FromLong(s->c.B); }
-static PyGetSetDef seqs_get[] = {{"_at", (getter)seqs_at, NULL, "address of the struct", NULL}, {"B", (getter)seqs_B, NULL, "number of sequences", NULL}, {0}};
+static int seqs_set_B(Seqs *s, PyObject *value, void *unused)
+{
+    if (!value || !PyIndex_Check(value)) {
+        PyErr_SetString(PyExc_TypeError, "the number of sequences is an integer");
+        return -1;
+    }
+    const Py_ssize_t B = PyNumber_AsSsize_t(value, PyExc_OverflowError);
+    if (B == -1 && PyErr_Occurred()) return -1;
+    if (B > s->count || B < INT32_MIN) {
+        PyErr_SetString(PyExc_ValueError, "a length and a slot for each sequence");
+        return -1;
+    }
+    s->c.B = (int32_t)B;
+    return 0;
+}
+static PyGetSetDef seqs_get[] = {{"_at", (getter)seqs_at, NULL, "address of the struct", NULL}, {"B", (getter)seqs_B, (setter)seqs_set_B, "number of sequences", NULL}, {0}};
 static PyTypeObject SeqsType = {
     PyVarObject_HEAD_INIT(NULL, 0).tp_name = "_marshal.Seqs",
     .tp_basicsize = sizeof(Seqs),

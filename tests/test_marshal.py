@@ -212,3 +212,36 @@ def test_descriptors_are_copied(kind):
         gc.collect()
         assert descriptor(alone) == (49, list(range(1, 50)), list(range(100, 149)), None, None)
     assert descriptor(copy.copy(kind([], []))) == (0, [], [], None, None)
+
+
+@pytest.mark.parametrize("kind", [rx._PySeqs, rx.Seqs])
+def test_the_number_of_sequences_can_be_set(kind):
+    """The first B of those that there are lengths for; more would be read behind the arrays."""
+    import copy
+    seqs = kind([3, 1, 2], [3, 900, 4, 5], [7, 2, 0])
+    for B in (2, 3, 1, 0, -1, 3):
+        seqs.B = B
+        assert seqs.B == seqs.c().B == copy.copy(seqs).B == copy.deepcopy(seqs).c().B == B
+        if B > 0:
+            assert descriptor(copy.copy(seqs)) == descriptor(seqs) == (B, [3, 1, 2][:B], [3, 900, 4][:B], [7, 2, 0][:B], None)
+    for bad in (4, 1 << 31, -(1 << 31) - 1, 1 << 70):
+        with pytest.raises((ValueError, OverflowError)):
+            seqs.B = bad
+    for bad in ("2", None, 1.5):
+        with pytest.raises(TypeError):
+            seqs.B = bad
+    with pytest.raises((TypeError, AttributeError)):
+        del seqs.B
+    twin = copy.deepcopy(seqs)
+    seqs.B, twin.B = 1, 2
+    assert descriptor(seqs)[0] == 1 and descriptor(twin)[:2] == (2, [3, 1])
+    twin.B = 3
+    assert descriptor(twin)[1] == [3, 1, 2]
+    rec = Recorder(1)
+    if kind is rx.Seqs:
+        got = []
+        fn = C.CFUNCTYPE(C.c_int32, C.POINTER(rx.SeqsC))(lambda p: got.append((p[0].B, [p[0].q_lens[i] for i in range(p[0].B)])) or 0)
+        call = marshal.Call(C.cast(fn, C.c_void_p).value, "r")
+        seqs.B = 2
+        assert call(seqs) == 0 and call(twin) == 0 and got == [(2, [3, 1]), (3, [3, 1, 2])]
+    del rec
