@@ -402,8 +402,9 @@ class Seqs(_PySeqs if _marshal is None else _marshal.Seqs):
 
     if _marshal is not None:
         def c(self) -> SeqsC:
-            struct_ = SeqsC.from_address(self._at)
-            struct_._seqs = self               # its memory
+            at, memory = self._pin
+            struct_ = SeqsC.from_address(at)
+            struct_._seqs = memory, self       # the arrays, and the table
             return struct_
 
 

@@ -6,7 +6,7 @@
  *     i  an integer
  *     r  a pointer to a struct: None, a Seqs, a ctypes structure, or an object whose _at is an address; of `types`, if given, which has a type, or a tuple of types, per r
  *     s  a stream: None (the current one), an address, or an object whose cuda_stream is one
- *   Seqs(q_lens, kv_lens, slots, device_table)      relax_seqs with arrays of its own
+ *   Seqs(q_lens, kv_lens, slots, device_table)      relax_seqs with arrays of its own; the address of a table is asked for at each call
  */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -23,13 +23,19 @@ static PyObject *get_device, *get_stream;       /* torch's, once it has initiali
 static PyObject *slow_stream;                   /* binding._stream */
 
 /* ---- descriptor -------------------------------------------------------------------------------------------------- */
+/* A struct and its arrays are one bytes object that does not change: what changes a descriptor gives it another one, and a call holds the one that it was made with. */
 typedef struct {
     PyObject_HEAD
-    relax_seqs c;
-    int32_t count;                              /* sequences that there are lengths for: c.B is at most that */
-    int32_t *lens;
+    PyObject *block;                            /* relax_seqs, q_lens, kv_lens, slots; NULL: no sequence yet */
+    int32_t count;                              /* sequences that there are lengths for: B is at most that */
     PyObject *table;
 } Seqs;
+
+static relax_seqs *struct_in(PyObject *block)
+{
+    static relax_seqs none;
+    return block ? (relax_seqs *)PyBytes_AS_STRING(block) : &none;
+}
 
 static int pointer_of(PyObject *o, void **out)
 {
@@ -69,13 +75,34 @@ static int int32_of(PyObject *o, int32_t *out)
     return 0;
 }
 
-static void seqs_clear(Seqs *s)
+/* a block for `all` numbers */
+static PyObject *block_of(Py_ssize_t all) { return PyBytes_FromStringAndSize(NULL, (Py_ssize_t)sizeof(relax_seqs) + all * (Py_ssize_t)sizeof(int32_t)); }
+
+/* the same lengths and slots with another number of sequences or address of a table */
+static int seqs_change(Seqs *s, int32_t B, const int32_t *device)
 {
-    PyMem_Free(s->lens);
-    s->lens = NULL;
-    Py_CLEAR(s->table);
-    s->c = (relax_seqs){0};
-    s->count = 0;
+    const relax_seqs *old = struct_in(s->block);
+    if (!s->block || (old->B == B && old->device_table == device)) return 0;
+    const Py_ssize_t size = PyBytes_GET_SIZE(s->block);
+    PyObject *block = PyBytes_FromStringAndSize(PyBytes_AS_STRING(s->block), size);
+    if (!block) return -1;
+    relax_seqs *c = struct_in(block);
+    const ptrdiff_t by = (char *)c - (const char *)old;
+    c->B = B, c->device_table = device;
+    c->q_lens = (const int32_t *)((const char *)c->q_lens + by), c->kv_lens = (const int32_t *)((const char *)c->kv_lens + by);
+    if (c->slots) c->slots = (const int32_t *)((const char *)c->slots + by);
+    Py_SETREF(s->block, block);
+    return 0;
+}
+
+static int seqs_refresh(Seqs *s)
+{
+    void *device = NULL;
+    PyObject *table = s->table;                 /* (asking it runs code that may give the descriptor another one) */
+    Py_XINCREF(table);
+    const int bad = table ? pointer_of(table, &device) : 0;
+    Py_XDECREF(table);
+    return bad < 0 ? -1 : seqs_change(s, struct_in(s->block)->B, device);
 }
 
 static int seqs_init(Seqs *s, PyObject *args, PyObject *kw)
@@ -96,11 +123,9 @@ static int seqs_init(Seqs *s, PyObject *args, PyObject *kw)
             goto done;
         }
     }
-    int32_t *lens = PyMem_Malloc((size_t)(all + 1) * sizeof(int32_t)), *at = lens;
-    if (!lens) {
-        PyErr_NoMemory();
-        goto done;
-    }
+    PyObject *block = block_of(all);
+    if (!block) goto done;
+    int32_t *at = (int32_t *)(struct_in(block) + 1);
     const int32_t *start[3] = {NULL, NULL, NULL};
     for (int k = 0; k < 3; ++k) {
         if (!list[k]) continue;
@@ -112,21 +137,20 @@ static int seqs_init(Seqs *s, PyObject *args, PyObject *kw)
             Py_XDECREF(item);
             if (bad) {
                 if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, "the sequence changed");
-                PyMem_Free(lens);
+                Py_DECREF(block);
                 goto done;
             }
         }
     }
     void *device = NULL;
     if (pointer_of(table, &device) < 0) {
-        PyMem_Free(lens);
+        Py_DECREF(block);
         goto done;
     }
-    seqs_clear(s);
-    s->lens = lens;
-    s->table = Py_NewRef(table);
+    *struct_in(block) = (relax_seqs){(int32_t)n[0], start[0], start[1], start[2], device};
     s->count = (int32_t)n[0];
-    s->c = (relax_seqs){(int32_t)n[0], start[0], start[1], start[2], device};
+    Py_XSETREF(s->block, block);
+    Py_XSETREF(s->table, Py_NewRef(table));
     ok = 1;
 done:
     for (int k = 0; k < 3; ++k) Py_XDECREF(list[k]);
@@ -153,8 +177,9 @@ static PyObject *seqs_getstate(Seqs *s, PyObject *unused)
         PyErr_Clear();
         more = Py_NewRef(Py_None);
     }
-    q = list_of(s->c.q_lens, s->count), kv = list_of(s->c.kv_lens, s->count), slots = s->c.slots ? list_of(s->c.slots, s->count) : Py_NewRef(Py_None);
-    PyObject *state = q && kv && slots ? Py_BuildValue("((OOOO)iO)", q, kv, slots, s->table ? s->table : Py_None, (int)s->c.B, more) : NULL;
+    const relax_seqs *c = struct_in(s->block);
+    q = list_of(c->q_lens, s->count), kv = list_of(c->kv_lens, s->count), slots = c->slots ? list_of(c->slots, s->count) : Py_NewRef(Py_None);
+    PyObject *state = q && kv && slots ? Py_BuildValue("((OOOO)iO)", q, kv, slots, s->table ? s->table : Py_None, (int)c->B, more) : NULL;
     Py_XDECREF(q), Py_XDECREF(kv), Py_XDECREF(slots);
     Py_DECREF(more);
     return state;
@@ -164,8 +189,9 @@ static PyObject *seqs_setstate(Seqs *s, PyObject *state)
 {
     PyObject *args, *more;
     int B;
-    if (!PyArg_ParseTuple(state, "O!iO", &PyTuple_Type, &args, &B, &more) || seqs_init(s, args, NULL) < 0) return NULL;
-    s->c.B = B < s->count ? B : s->count;
+    if (!PyArg_ParseTuple(state, "O!iO", &PyTuple_Type, &args, &B, &more) || seqs_init(s, args, NULL) < 0 ||
+        seqs_change(s, B < s->count ? B : s->count, struct_in(s->block)->device_table) < 0)
+        return NULL;
     if (more != Py_None) {
         PyObject *dict = PyObject_GetAttrString((PyObject *)s, "__dict__");
         const int bad = dict ? PyDict_Update(dict, more) : -1;
@@ -178,12 +204,17 @@ static PyMethodDef seqs_methods[] = {{"__getstate__", (PyCFunction)seqs_getstate
 
 static void seqs_dealloc(Seqs *s)
 {
-    seqs_clear(s);
+    Py_CLEAR(s->block);
+    Py_CLEAR(s->table);
     Py_TYPE(s)->tp_free((PyObject *)s);
 }
 
-static PyObject *seqs_at(Seqs *s, void *unused) { return PyLong_FromVoidPtr(&s->c); }
-static PyObject *seqs_B(Seqs *s, void *unused) { return PyLong_FromLong(s->c.B); }
+static PyObject *seqs_at(Seqs *s, void *unused) { return seqs_refresh(s) < 0 ? NULL : PyLong_FromVoidPtr(struct_in(s->block)); }
+static PyObject *seqs_pin(Seqs *s, void *unused)
+{
+    return seqs_refresh(s) < 0 ? NULL : Py_BuildValue("NO", PyLong_FromVoidPtr(struct_in(s->block)), s->block ? s->block : Py_None);
+}
+static PyObject *seqs_B(Seqs *s, void *unused) { return PyLong_FromLong(struct_in(s->block)->B); }
 static int seqs_set_B(Seqs *s, PyObject *value, void *unused)
 {
     if (!value || !PyIndex_Check(value)) {
@@ -196,10 +227,9 @@ static int seqs_set_B(Seqs *s, PyObject *value, void *unused)
         PyErr_SetString(PyExc_ValueError, "a length and a slot for each sequence");
         return -1;
     }
-    s->c.B = (int32_t)B;
-    return 0;
+    return seqs_change(s, (int32_t)B, struct_in(s->block)->device_table);
 }
-static PyGetSetDef seqs_get[] = {{"_at", (getter)seqs_at, NULL, "address of the struct", NULL}, {"B", (getter)seqs_B, (setter)seqs_set_B, "number of sequences", NULL}, {0}};
+static PyGetSetDef seqs_get[] = {{"_at", (getter)seqs_at, NULL, "address of the struct", NULL}, {"_pin", (getter)seqs_pin, NULL, "(address of the struct, its memory)", NULL}, {"B", (getter)seqs_B, (setter)seqs_set_B, "number of sequences", NULL}, {0}};
 static PyTypeObject SeqsType = {
     PyVarObject_HEAD_INIT(NULL, 0).tp_name = "_marshal.Seqs",
     .tp_basicsize = sizeof(Seqs),
@@ -230,7 +260,8 @@ static int type_fits(PyObject *o, PyObject *types)
     return 0;
 }
 
-static int struct_of(PyObject *o, PyObject *types, void **out)
+/* hold: what has to live as long as *out, or NULL */
+static int struct_of(PyObject *o, PyObject *types, PyObject **hold, void **out)
 {
     if (o == Py_None) {
         *out = NULL;
@@ -238,7 +269,10 @@ static int struct_of(PyObject *o, PyObject *types, void **out)
     }
     if (types && !type_fits(o, types)) return -1;
     if (PyObject_TypeCheck(o, &SeqsType)) {
-        *out = &((Seqs *)o)->c;
+        if (seqs_refresh((Seqs *)o) < 0) return -1;
+        *hold = ((Seqs *)o)->block;
+        Py_XINCREF(*hold);
+        *out = struct_in(*hold);
         return 0;
     }
     if (PyObject_CheckBuffer(o)) {              /* (its owner holds it for the length of the call) */
@@ -278,11 +312,17 @@ static PyObject *call_run(Call *self, PyObject *const *args, size_t flags, PyObj
         return NULL;
     }
     void *a[MAX_ARGS] = {0};
-    for (int i = 0, structs = 0; i < self->count; ++i) {
+    PyObject *held[MAX_ARGS];
+    int structs = 0;
+    for (int i = 0; i < self->count; ++i) {
         int bad = 0;
         switch (self->kinds[i]) {
         case 'p': bad = pointer_of(args[i], &a[i]); break;
-        case 'r': bad = struct_of(args[i], self->types ? PyTuple_GET_ITEM(self->types, structs++) : NULL, &a[i]); break;
+        case 'r':
+            held[structs] = NULL;
+            bad = struct_of(args[i], self->types ? PyTuple_GET_ITEM(self->types, structs) : NULL, &held[structs], &a[i]);
+            ++structs;
+            break;
         case 's': bad = stream_of(args[i], &a[i]); break;
         default: {
             const long long v = PyLong_AsLongLong(args[i]);
@@ -290,7 +330,10 @@ static PyObject *call_run(Call *self, PyObject *const *args, size_t flags, PyObj
             a[i] = (void *)(intptr_t)v;
         }
         }
-        if (bad < 0) return NULL;
+        if (bad < 0) {
+            while (structs > 0) Py_XDECREF(held[--structs]);
+            return NULL;
+        }
     }
     int32_t rc;
     /* arguments of this class are passed alike whatever their width, and a function does not look at those behind its last */
@@ -298,6 +341,7 @@ static PyObject *call_run(Call *self, PyObject *const *args, size_t flags, PyObj
     Py_BEGIN_ALLOW_THREADS
     rc = ((fn_t)self->fn)(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[11], a[12], a[13], a[14], a[15]);
     Py_END_ALLOW_THREADS
+    while (structs > 0) Py_XDECREF(held[--structs]);
     return PyLong_FromLong(rc);
 }
 

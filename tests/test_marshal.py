@@ -245,3 +245,44 @@ def test_the_number_of_sequences_can_be_set(kind):
         seqs.B = 2
         assert call(seqs) == 0 and call(twin) == 0 and got == [(2, [3, 1]), (3, [3, 1, 2])]
     del rec
+
+
+@pytest.mark.parametrize("kind", [rx._PySeqs, rx.Seqs])
+def test_the_tables_address_is_that_of_the_call(kind):
+    """A tensor whose storage is exchanged, the old one freed: each call takes the address that it has then, and refuses one that is not contiguous."""
+    table = torch.zeros(8, dtype=torch.int32)
+    seqs = kind([3, 1], [3, 900], device_table=table)
+    first = table.data_ptr()
+    assert seqs.c().device_table == first
+    other = torch.ones(64, dtype=torch.int32)
+    for change in (lambda: setattr(table, "data", other), lambda: table.set_(other, 8, (8,), (1,))):
+        change()
+        assert table.data_ptr() != first and seqs.c().device_table == table.data_ptr()
+        if kind is rx.Seqs:
+            got = []
+            fn = C.CFUNCTYPE(C.c_int32, C.POINTER(rx.SeqsC))(lambda p: got.append(p[0].device_table) or 0)
+            assert marshal.Call(C.cast(fn, C.c_void_p).value, "r")(seqs) == 0 and got == [table.data_ptr()]
+            assert rx.SeqsC.from_address(seqs._at).device_table == table.data_ptr()
+    table.set_(other, 0, (4, 2), (1, 4))
+    with pytest.raises(ValueError):
+        seqs.c()
+    if kind is rx.Seqs:
+        with pytest.raises(ValueError):
+            marshal.Call(Recorder(1).address, "r")(seqs)
+
+
+def test_a_call_keeps_the_descriptor_it_was_made_with():
+    """Lengths that are given anew while the call runs, as by another thread, do not reach it, and its arrays stay."""
+    seqs, got = rx.Seqs(list(range(1, 50)), list(range(100, 149))), []
+
+    def during(p):
+        rx.Seqs.__init__(seqs, [7], [8])
+        seqs.B = 0
+        gc.collect()
+        junk = [rx.Seqs([9] * 49, [9] * 49) for _ in range(100)]
+        got.append((p[0].B, [p[0].q_lens[i] for i in range(49)], [p[0].kv_lens[i] for i in range(49)], len(junk)))
+        return 0
+    fn = C.CFUNCTYPE(C.c_int32, C.POINTER(rx.SeqsC))(during)
+    assert marshal.Call(C.cast(fn, C.c_void_p).value, "r")(seqs) == 0
+    assert got == [(49, list(range(1, 50)), list(range(100, 149)), 100)]
+    assert descriptor(seqs) == (0, [], [], None, None)
