@@ -9,13 +9,14 @@ import sys
 import sysconfig
 import tempfile
 from concurrent.futures import ThreadPoolExecutor
+from typing import Optional
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "librelax_mi355.so")
-MARSHAL = os.path.join(HERE, "_marshal.so")
+MARSHAL = os.path.join(HERE, "_marshal" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))      # another interpreter does not take it for its own
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
@@ -180,11 +181,19 @@ def _compile(src: str) -> str:
     return obj
 
 
-def build_marshal() -> str:
-    """The Python extension of csrc/marshal.c (host code alone)."""
+def build_marshal() -> Optional[str]:
+    """The Python extension of csrc/marshal.c (host code alone).  None where it cannot be built, for want of a C compiler or Python's headers: binding.py then does the same in Python, and
+    an extension of an earlier build, which may be of other sources, does not stay."""
+    for name in os.listdir(HERE):
+        if name.startswith("_marshal.") and name.endswith(".so"):
+            os.remove(os.path.join(HERE, name))
     cmd = [os.environ.get("CC", "gcc"), "-O2", "-Wall", "-shared", "-fPIC", "-I" + sysconfig.get_paths()["include"], "-I" + os.path.join(ROOT, "include"),
            "-o", MARSHAL, os.path.join(CSRC, "marshal.c")]
-    subprocess.run(cmd, check=True)
+    try:
+        subprocess.run(cmd, check=True)
+    except (OSError, subprocess.CalledProcessError) as e:
+        sys.stderr.write("csrc/marshal.c is not built, its calls are marshalled in Python: %s\n" % e)
+        return None
     return MARSHAL
 
 
