@@ -277,7 +277,8 @@ class DevicePaged4Cache:
             self._check_shared(share_from, rope, where)
             self.rotary, self.rope, self.pages, self.ws, self.ws_bytes = share_from.rotary, share_from.rope, share_from.pages, share_from.ws, share_from.ws_bytes
         else:
-            self.rotary = rope if rope is not _NOT_GIVEN else rx.RopeScaling(rx.ROPE_PLAIN, head_dim, 10000.0, 1.0)
+            # (a copy: the table's sizes are its, whatever the program writes into its own afterwards)
+            self.rotary = rx.RopeScaling(rx.ROPE_PLAIN, head_dim, 10000.0, 1.0) if rope is _NOT_GIVEN else None if rope is None else rx.RopeScaling.from_buffer_copy(rope)
             self.pages = torch.full((kv_slots, -(-kv_capacity // page_size)), -1, dtype=torch.int32, device=device)
             self.rope = None if self.rotary is None else rope_table(self.rotary, kv_capacity, device)
             self.ws_bytes = rx.relax_paged4_workspace_bytes(self.dims, n_max, kv_capacity, self.B_max)

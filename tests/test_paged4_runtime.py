@@ -119,3 +119,16 @@ def test_tensors_that_do_not_fit(calls):
     assert not calls
     layer.append(new(3, 520)[:, :512], seqs, new(3, 256)), layer.attention(new(3, 256), seqs, new(3, 4, 64))
     assert [name for name, _ in calls] == ["relax_paged4_append", "relax_paged4_attention"]
+
+
+def test_a_scaling_that_changes_does_not_change_a_layer(calls):
+    """The program fills the struct anew for its next model: layers that share a table still turn what that table is for, and read no row past its end."""
+    mine = rx.RopeScaling(rx.ROPE_LINEAR, 32, 10000.0, 4.0)
+    first = cache(rope=mine)
+    mine.rotary_dim, mine.factor = 64, 2.0
+    assert first.rope.shape == (100, 16, 2) and first.rotary.rotary_dim == 32 and first.prep.c().rotary_dim == 32
+    second = cache(share_from=first)
+    assert second.prep.c().rotary_dim == 32 and second.rotary.rotary_dim == 32
+    with pytest.raises(ValueError):
+        cache(share_from=first, rope=mine)
+    assert cache(share_from=first, rope=rx.RopeScaling(rx.ROPE_LINEAR, 32, 10000.0, 4.0)).prep.c().rotary_dim == 32
