@@ -488,7 +488,8 @@ relax_status relax_head_norm_rope(const uint16_t *q, int64_t q_stride, const uin
 /* ---- Paged KV cache in 4 bits ------------------------------------------------------------------------------------------------
  * relax_paged_cache in little more than half its bytes: pages, blocks of RELAX_PAGED_BLOCK tokens, page table and descriptor are the same.  Every RELAX_PAGED4_GROUP elements of a token and
  * KV head have a scale of their own and codes u in 0..15 that stand for (u - 8) * scale:
- *   scale = round8(x* / -8), x* the element of the largest magnitude (the positive one of two), round8 to eight significant bits, at most 8160 in size
+ *   scale = round8(x* / -8), x* the element of the largest magnitude (the positive one of two), round8 to eight significant bits and to fp16, at most 8160 in size
+ *           (fp16's step is 2^-24: a scale below 2^-17 has fewer bits)
  *   u     = 8 + round(x / scale), kept in 0..15 (8 where the scale is 0)
  * Eight bits times a code is exact in fp16, so no call rounds what the cache holds, and tokens share nothing, so an append touches no other token.
  * 32 bits, four bytes b, of a block of one KV head hold
@@ -497,7 +498,7 @@ relax_status relax_head_norm_rope(const uint16_t *q, int64_t q_stride, const uin
  *   scales at  [page][head][block][t / 4][e / 32][t % 4], fp16
  * (fragments of the matrix products that read them).  Codes and scales behind a sequence's last token, blocks without a page and lengths beyond the capacity: as relax_paged_cache.
  * An element that is infinite counts as +-65504 and a NaN as 0, in front of norm and rotation; values beyond 65280 are held as 65280 or, where the scale's sign
- * gives them code 15, as 57120; a group whose largest magnitude is below 2^-22 is held as zeros.                                  */
+ * gives them code 15, as 57120; a group whose scale in eight bits is 2^-25 or less in size (of a largest magnitude of 2^-22 or less, in prepared keys 2^-22 (1 + 2^-8)) is held as zeros. */
 #define RELAX_PAGED4_GROUP 32
 typedef struct {
     uint8_t *k, *v;                   /* codes, [n_pages][g][page_size / 16][8 * d] bytes each, 16-byte aligned                    */

@@ -1040,3 +1040,17 @@ def test_a_model_of_one_layer_with_normalised_heads(rx):
                     c, s_ = po.values(pool, name, pages, page, slot, np.arange(L - ql, L), d)
                     assert np.array_equal(got[row:row + ql].cpu().numpy().astype(np.float64), c * s_)
     assert rx.relax_workspace_error(first.dims, first.ws) == 0
+
+
+def test_the_smallest_groups_that_are_held(rx):
+    """A largest magnitude of 2^-22 is held as zeros, the next fp16 number above it as itself; 8 to 20 times 2^-24 by scales of one and two steps."""
+    b = Bench(rx, np.random.default_rng(93), 4, 4, 64, 16, [9], [9])
+    qkv = np.zeros((9, 12 * 64), np.float16)
+    tops = [1, 3, 4, 5, 8, 11, 12, 20, -5]
+    for row, top in enumerate(tops):
+        qkv[row, 256:].reshape(-1, 32)[:, row] = np.float16(top * 2.0 ** -24)
+    check_append(b, qkv, b.append(qkv))
+    for got in b.read():
+        for row, want in enumerate((0, 0, 0, 5, 8, 8, 12, 16, -5)):
+            x = got[row].reshape(-1, 32).astype(np.float64)
+            assert (x[:, row] == want * 2.0 ** -24).all() and (np.delete(x, row, axis=1) == 0).all(), tops[row]

@@ -163,3 +163,13 @@ def test_plain_frequencies():
     f = po.frequencies(64, 10000.0, "index", 4.0, 2048.0, 1.0, 32.0)
     first, last = math.floor(64 * math.log(2048 / (64 * math.pi)) / (2 * math.log(1e4))), math.ceil(64 * math.log(2048 / (2 * math.pi)) / (2 * math.log(1e4)))
     assert np.allclose(f[:first + 1], plain[:first + 1]) and np.allclose(f[last:], plain[last:] / 4) and first + 1 < last < 32
+
+
+def test_plain_quantisation_of_the_smallest_groups():
+    """What the header says of them: those of 2^-22 and less are zeros, 2^-25 being a tie between 0 and the smallest scale, and what eight bits round to that; beyond, the scale is a multiple of 2^-24."""
+    tiny = 2.0 ** -24
+    for largest, scale, held in ((1, 0, 0), (3, 0, 0), (4, 0, 0), (4 * (1 + 2.0 ** -8), 0, 0), (4 * (1 + 2.0 ** -7), -1, 4), (5, -1, 5), (8, -1, 8), (11, -1, 8), (12, -2, 12), (20, -2, 16), (-4, 0, 0), (-5, 1, -5), (-8, 1, -8)):
+        x = np.zeros((1, 32), np.float32)
+        x[0, 7] = largest * tiny
+        u, s = po.quantise(x)
+        assert float(s[0, 0]) == scale * tiny and (float(u[0, 7]) - 8) * float(s[0, 0]) == held * tiny, largest
