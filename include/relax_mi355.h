@@ -522,7 +522,7 @@ relax_status relax_paged4_append(const uint16_t *q, int64_t q_stride, const uint
 /* relax_paged_attention over the 4-bit cache.  Scores, softmax and sums are fp32; the one rounding between what the cache holds and the result is that of the
  * probabilities, or in rows of few (row, head) pairs of the probabilities times their values' scale, to fp16: 2^-11 of each, and below fp16's normal range
  * 2^-36 of the row's largest probability, or 2^-35 of the largest one times the largest scale (2^-14 at least) of its four tokens (times the code, at most 8).
- * Scores are told apart up to 2^25 in size; beyond, results are unspecified.  A row that no token is left for is zeros.  out may be q. */
+ * Scores are told apart up to 2^23 in size; beyond, results are unspecified.  A row that no token is left for is zeros.  out may be q. */
 relax_status relax_paged4_attention(const uint16_t *q, const relax_paged4_cache *cache, const relax_seqs *seqs, const relax_layer_dims *dims,
                                     uint16_t *out, int32_t n, void *ws, size_t ws_bytes, relax_stream stream);
 

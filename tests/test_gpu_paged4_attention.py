@@ -18,8 +18,8 @@ def exact_scores(b, rng, v_scale):
         b.dev[key].copy_(torch.from_numpy(b.pool[key]))
 
 
-def narrow(q, b):
-    """(out, tolerance), float64 [n, h, d].  What is rounded, each to nearest:
+def narrow(q, b, rows=None, heads=None):
+    """(out, tolerance), float64 [n, h, d], of the given rows of a sequence and heads (None: all; of others the tolerance is infinite).  What is rounded, each to nearest:
       the output to fp16                             2^-11 |o|, 2^-25 below fp16's normal range
       weights, or weights times scales, to fp16      2^-11 sum p |v|; with a sum of the rounded ones 2^-11 |o| more
       ... below fp16's normal range                  a step is 2^-24; the largest weight times the root of the sum of squares of a lane's scales, sixteen, is 2^12 at least, so times the largest of
@@ -28,13 +28,13 @@ def narrow(q, b):
       exponents                                      scores are exact; times c and minus the reference they are below 2^6 in size: c is off by 4 2^-24 of itself, the multiply-add by 2^-24, the
                                                      exponential by 2^-22 of itself: below 2^-15 of a weight, in numerator and denominator
       sums in fp32                                   a product of 32 tokens is off by 4 2^-24 of its terms, at most 23 |s| p each (codes 0..15 against -8 sum p s): T / 32 + 8 of them in a row"""
-    out, tol = np.zeros(q.shape), np.zeros(q.shape)
+    out, tol = np.zeros(q.shape), np.full(q.shape, np.inf)
     rep = b.h // b.g
     for row, ql, L, slot in po.sequences(b.q_lens, b.kv_lens, b.slots):
         (kc, ks), (vc, vs) = (po.values(b.pool, name, b.pages, b.page_size, slot, np.arange(L), b.d) for name in "kv")
-        for i in range(ql):
+        for i in range(ql) if rows is None else rows:
             seen = L - ql + i + 1
-            for head in range(b.h):
+            for head in range(b.h) if heads is None else heads:
                 j = head // rep
                 s = (kc * ks)[:seen, j] @ q[row + i, head] / np.sqrt(b.d)
                 p = np.exp(s - s.max())
@@ -93,7 +93,7 @@ def test_a_tail_of_small_weights(rx, shape, rows, L, exponent, at):  # noqa: F81
 @gpu
 @pytest.mark.parametrize("shape,rows", [((8, 1, 128), 1), ((4, 4, 64), 3), ((8, 2, 64), 5)], ids=str)
 def test_scores_far_from_zero(rx, shape, rows):  # noqa: F811
-    """Every score of a row is far below or above zero, up to 2^25: whatever the weights are held against stays a number.  (Beyond that fp32 tells scores apart by four and more.)"""
+    """Every score of a row is far below or above zero, up to 2.8e7, where fp32 tells scores apart by two: whatever the weights are held against stays a number."""
     h, g, d = shape
     for sign, size in ((-1, 100.0), (-1, 30000.0), (1, 30000.0)):
         for key_scale in (0.125, 8.0) + ((4096.0,) if size == 100.0 else ()):
@@ -237,3 +237,30 @@ def test_a_lost_token_is_a_miss():
     v = (u - 8) * s
     assert not misses(v.half().float(), v, s, 2.0 ** -12).any()
     assert misses(v.roll(1, 0).half().float(), v, s, 2.0 ** -12).any(dim=1).all() and misses(torch.zeros_like(v), v, s, 2.0 ** -12).any(dim=1).all()
+
+
+@gpu
+@pytest.mark.parametrize("size,rising", [(96.0, False), (30000.0, False), (96.0, True), (30000.0, True)])
+@pytest.mark.parametrize("shape,rows,L", [((8, 1, 128), 1, 9000), ((8, 1, 128), 3, 9000), ((4, 4, 64), 9, 2000), ((2, 1, 128), 30, 2000), ((100, 100, 128), 257, 1000)], ids=str)
+def test_large_scores_that_differ_little(rx, shape, rows, L, size, rising):  # noqa: F811
+    """Scores of 600 to 250000 that differ by some units from token to token, exact in fp32: wavefronts and parts, whose references differ, agree on the weights, and so does a row whose reference moves."""
+    h, g, d = shape
+    rng = np.random.default_rng(seed_of(shape, rows, L))
+    b = Bench(rx, rng, *shape, 64, [rows], [L])
+    exact_scores(b, rng, lambda s: np.full(s, 0.25))
+    b.pool["k"][:] = 0xEE                                      # codes of 14: 6 / 8
+    codes = 16 * np.arange(L) // L if rising else rng.integers(0, 16, L)      # of element 5, which makes the difference
+    byte, shift = po.code_place("k", d)
+    for pos in range(L):
+        at = b.pool["k"][b.pages[0, pos // 64], :, pos % 64 // 16]
+        t = pos % 16
+        at[:, byte[t, 5]] = (at[:, byte[t, 5]] & (0xF0 if shift[t, 5] == 0 else 0x0F)) | codes[pos] << shift[t, 5]
+    b.pool["ks"] = np.abs(b.pool["ks"])
+    for key in ("k", "ks"):
+        b.dev[key].copy_(torch.from_numpy(b.pool[key]))
+    q = np.full((rows, h, d), size, np.float16)
+    q[:, :, 5] = 64
+    got = b.attention(q).astype(np.float64)
+    want, tol = narrow(q.astype(np.float64), b, sorted({0, rows // 2, rows - 1}), sorted({0, h - 1}))
+    over = np.abs(got - want) / tol
+    assert (over <= 1).all(), float(over.max())
