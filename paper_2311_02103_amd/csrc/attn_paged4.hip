@@ -16,8 +16,8 @@
 // exact (eight and four bits).  The products need no factor; the weight is rounded to fp16 and its sum is that of the rounded ones, from a product with ones.
 // (300 rows of 32 / 8 heads on 1201 tokens beside eight sequences of five: 30.7 us; with codes and scales of columns as above 36.7.)
 //
-// Few pairs are bound by bytes, with what a workgroup's beginning and end and the merge take on top (about 3.8 and 3.9 us): heads of 128, 64 / 8 heads, one sequence of 120001 tokens 28.7 us, 4.8 TB/s
-// (23.0 at a long stream's rate), 16 of 100 to 8000 tokens 21.3 (12.5).  17 to 32 pairs are bound by the vector unit beside the matrix pipe: some 270 instructions per 32 tokens and 34 products.
+// Few pairs are bound by bytes, with what a workgroup's beginning and end and the merge take on top (about 3.8 and 3.9 us): heads of 128, 64 / 8 heads, one sequence of 120001 tokens 29.3 us, 4.7 TB/s
+// (23.0 at a long stream's rate), 16 of 100 to 8000 tokens 21.7 (12.5).  17 to 32 pairs are bound by the vector unit beside the matrix pipe: some 270 instructions per 32 tokens and 34 products.
 // (Tiles of 48 pairs, queries in LDS: 29.2 us for 30.6 in the call above, but 38.2 for 34.9 with 1200 rows on nothing.)
 #include <algorithm>
 #include <type_traits>
@@ -393,7 +393,7 @@ __device__ __forceinline__ void attend(Lds &lds, const Task &k, const uint16_t *
 }
 
 // grid: item * g + KV head, an item being a part of a tile (the tiles of a part side by side: they read the same tokens).  per_seq: as tile_of takes it.  part: [row][head][splits][D + 2], of
-// rows that have more than one part.  FEW: no sequence has more than eight pairs; three wavefronts per SIMD (64 sequences of 100 to 730 tokens, 32 / 32 heads: 28.2 us for 31.2 with two; the fewest
+// rows that have more than one part.  FEW: no sequence has more than eight pairs; three wavefronts per SIMD (64 sequences of 100 to 730 tokens, 32 / 32 heads: 28.0 us for 31.2 with two; the fewest
 // sequences as before).
 struct Grid {
     int h, g, rep, per_seq, chunk, splits, least;
@@ -432,7 +432,7 @@ __global__ __launch_bounds__(64 * W, FEW ? 3 : 2) void attn_paged4_kernel(PagedS
 // one, four and eight wavefronts (kWideGroupUs: with four and eight, where a sequence has more than 16 pairs); kStepUs: a step of 32 tokens with up to three wavefronts on a SIMD (kWideStepUs: up to
 // two); heads of 64: times kHalfHead.  kTail: the share of the longest workgroup that comes on top when there are more of them than at a time.  A merge, and each of its partial results; the
 // cache's bytes.
-// One wavefront alone has no states to merge and the shortest end, which counts when there are several rounds of workgroups: 128 sequences of 20 to 530 tokens, 32 / 32 heads, 33.0 us for 39.5 with four;
+// One wavefront alone has no states to merge and the shortest end, which counts when there are several rounds of workgroups: 128 sequences of 20 to 530 tokens, 32 / 32 heads, 32.9 us for 40.8 with four;
 // two are between them (never more than 12 % better than the best of the others) and are not built.
 constexpr int kWaves[3] = {1, 4, 8};
 constexpr float kGroupUs[3] = {3.0f, 3.5f, 5.4f}, kWideGroupUs[3] = {0.0f, 3.2f, 7.1f}, kStepUs[3] = {0.96f, 1.14f, 1.19f}, kWideStepUs[2] = {1.1f, 1.11f}, kHalfHead = 0.89f, kTail = 0.15f, kMergeUs = 3.45f,
@@ -506,6 +506,8 @@ Cut cut(const PagedPlan &pl, const relax_layer_dims &dm, const PagedSeqs &st, co
         }
     };
     consider(chunk);
+    // From 2048 workgroups on no cut has been estimated to be faster (us, with the search / without: 64 sequences of 800 tokens, 32 / 32 heads, 41.9 / 42.2; 128 of 300 to 935 71.5 / 71.7), and the
+    // search is host time
     if (tiles * g < 2048) {
         const int64_t most_parts = std::max<int64_t>(1, kPagedPartials / ((int64_t)st.n * dm.n_heads)), least = (std::max<int64_t>(kLeast, L_max / most_parts + 1) + 31) & ~31;
         for (int parts = 2; parts <= (sq.B <= 4 ? 64 : sq.B <= 24 ? 16 : 4); parts += parts < 4 ? 1 : parts / 2) {
@@ -638,6 +640,8 @@ hipError_t launch_d(const uint16_t *q, const Paged4Args &pa, const relax_layer_d
         constexpr int P = 256 / (D / 4 * G);
         hipLaunchKernelGGL((attn_paged4_merge_kernel<D, G>), dim3((count + P - 1) / P), dim3(256), 0, stream, rows, partials, out, gr, divisor(dm.n_heads), count, pa.cap, all);
     };
+    // threads that share a row's parts, four times as many or fewer (us of the call: one row of 64 / 8 heads with 28 parts 30.6 / 32.1, with nine 7.7 / 8.1; 16 rows of them with up to six parts
+    // 24.1 / 23.3, 25 rows of 32 / 8 heads with two 32.0 / 31.1: many parts are few rows)
     if (c.splits > 16) merge(std::integral_constant<int, 1024 / D>{});
     else merge(std::integral_constant<int, 256 / D>{});
     return hipGetLastError();

@@ -2,8 +2,8 @@
 // (heads.hip) and the one that quantises them (paged4_append.hip).
 //
 // A lane holds a unit of eight consecutive elements, a head is d / 8 neighbouring lanes, so every access is 16 bytes per lane and d * 2 consecutive bytes per head.
-// The sum of squares goes through DPP moves in fp64 (the squares of fp16 numbers are exact in fp32, their sum is not; with an fp64 sum
-// the fp32 factor is the correctly rounded one whatever the order, so that a quantised key does not depend on the order either); the
+// The sum of squares goes through DPP moves in fp64: the squares of fp16 numbers are exact in fp32, and their sum in fp64 is exact where a head's elements but zeros lie within 2^12 of each
+// other, else off by 2^-49 of itself at most, so that the fp32 factor, and a quantised key, depends on the order of the sum for less than one in 2^24 of those.  The
 // pair of an element of the halves layout lies rotary_dim / 16 lanes away.
 #pragma once
 
@@ -72,7 +72,7 @@ __device__ __forceinline__ double lane_xor(double v)
     return __builtin_bit_cast(double, (uint64_t)__builtin_bit_cast(uint32_t, hi) << 32 | __builtin_bit_cast(uint32_t, lo));
 }
 
-// 1 / sqrt(ms) rounded once to fp32: the hardware's estimate in fp64 (2^-24; the one in fp32 has no estimate of a subnormal number, which eps may be) and two steps of Newton's method (2^-46,
+// 1 / sqrt(ms) in fp32, the correctly rounded one but for one value in about 2^26: the hardware's estimate in fp64 (2^-24; the one in fp32 has no estimate of a subnormal number, which eps may be) and two steps of Newton's method (2^-46,
 // then fp64's own 2^-52), a sixth of the instructions of a square root and a division.  0 for infinity and for 0
 __device__ __forceinline__ float rsqrt_once(double ms)
 {
