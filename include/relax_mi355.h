@@ -463,7 +463,7 @@ typedef struct {
  *                                  i(b) = rotary_dim * ln(trained / (2 pi b)) / (2 ln base) is the index whose pair makes b turns within `trained` positions
  *                                  (the two meet: a ramp of 0.001)
  *     RELAX_ROPE_WAVELENGTH_RAMP   w = (turns_t - slow) / (fast - slow), kept in 0..1, turns_t = trained * f_t / (2 pi)
- * amplitude is 1 unless the model scales its angles' entries (0 reads as 1).  base > 1, factor > 0, for ramps trained >= 1 and 0 < slow < fast, all finite:
+ * amplitude is 1 unless the model scales its angles' entries (0 reads as 1).  base > 1, factor > 0, for ramps trained >= 1 and 0 < slow < fast, all and 1 / factor finite:
  * else RELAX_ERR_SHAPE.  rotary_dim even, 2 .. 256, positions 1 .. 2^30: else RELAX_ERR_UNSUPPORTED (RELAX_ERR_SHAPE below 1).                        */
 enum { RELAX_ROPE_PLAIN = 0, RELAX_ROPE_LINEAR = 1, RELAX_ROPE_INDEX_RAMP = 2, RELAX_ROPE_WAVELENGTH_RAMP = 3 };
 typedef struct {

@@ -1501,7 +1501,7 @@ relax_status check_scaling(const relax_rope_scaling *sc, int32_t positions)
     if (sc->scaling < RELAX_ROPE_PLAIN || sc->scaling > RELAX_ROPE_WAVELENGTH_RAMP || positions > kMaxPagedCapacity || sc->rotary_dim > 256 || sc->rotary_dim % 2 != 0)
         return RELAX_ERR_UNSUPPORTED;
     if (!std::isfinite(sc->base) || !(sc->base > 1.0) || !std::isfinite(sc->amplitude)) return RELAX_ERR_SHAPE;
-    if (sc->scaling != RELAX_ROPE_PLAIN && (!std::isfinite(sc->factor) || !(sc->factor > 0.0))) return RELAX_ERR_SHAPE;
+    if (sc->scaling != RELAX_ROPE_PLAIN && (!std::isfinite(sc->factor) || !(sc->factor > 0.0) || !std::isfinite(1.0 / sc->factor))) return RELAX_ERR_SHAPE;
     if (sc->scaling >= RELAX_ROPE_INDEX_RAMP &&
         (!std::isfinite(sc->trained) || !std::isfinite(sc->fast) || !(sc->trained >= 1.0) || !(sc->slow > 0.0) || !(sc->fast > sc->slow)))
         return RELAX_ERR_SHAPE;

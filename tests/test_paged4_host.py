@@ -173,3 +173,13 @@ def test_plain_quantisation_of_the_smallest_groups():
         x[0, 7] = largest * tiny
         u, s = po.quantise(x)
         assert float(s[0, 0]) == scale * tiny and (float(u[0, 7]) - 8) * float(s[0, 0]) == held * tiny, largest
+
+
+def test_a_factor_whose_inverse_is_no_number_is_refused():
+    """The smallest numbers of fp64: pairs that a ramp leaves as they are would be 0 * infinity."""
+    for scaling in (rx.ROPE_LINEAR, rx.ROPE_INDEX_RAMP, rx.ROPE_WAVELENGTH_RAMP):
+        make = lambda factor: rx.RopeScaling(scaling, 64, 10000.0, factor, 2048.0, 1.0, 4.0, 1.0)
+        for factor in (5e-324, 1e-310, 5.5e-309):
+            assert rx.relax_rope_table_scaled(make(factor), 10, P) == rx.ERR_SHAPE and rx.relax_rope_scaled_bytes(make(factor), 10) == 0
+        assert rx.relax_rope_scaled_bytes(make(6e-309), 10) == rx.relax_rope_scaled_bytes(make(1e308), 10) == 10 * 64 * 4
+    assert rx.relax_rope_scaled_bytes(rx.RopeScaling(rx.ROPE_PLAIN, 64, 10000.0, 1e-310), 10) == 10 * 64 * 4       # (not used there)
