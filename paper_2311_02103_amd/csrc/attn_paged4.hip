@@ -12,12 +12,13 @@
 // largest score + log2 s of a lane's four tokens, s the root of the sum of squares of their scales, and moves when w s is about to leave fp16's range: the largest of these products is
 // 2^12 .. 65000 whatever the size of the values, and an operand below fp16's normal range is off by 2^-37 of it.  (A reference that follows the score alone has to leave room for the
 // largest scale, 8160, and rounds the tails of ordinary values away.)
-// More pairs: the vector unit bounds it, and a column costs more than a token, so operands are the numbers that the cache stands for, (u - 8) s = u s + (-8 s), one multiply-add per two and
+// More pairs: a column costs more vector instructions than a token, so operands are the numbers that the cache stands for, (u - 8) s = u s + (-8 s), one multiply-add per two and
 // exact (eight and four bits).  The products need no factor; the weight is rounded to fp16 and its sum is that of the rounded ones, from a product with ones.
 // (300 rows of 32 / 8 heads on 1201 tokens beside eight sequences of five: 30.7 us; with codes and scales of columns as above 36.7.)
 //
 // Few pairs are bound by bytes, with what a workgroup's beginning and end and the merge take on top (about 3.8 and 3.9 us): heads of 128, 64 / 8 heads, one sequence of 120001 tokens 29.3 us, 4.7 TB/s
-// (23.0 at a long stream's rate), 16 of 100 to 8000 tokens 21.7 (12.5).  17 to 32 pairs are bound by the vector unit beside the matrix pipe: some 270 instructions per 32 tokens and 34 products.
+// (23.0 at a long stream's rate), 16 of 100 to 8000 tokens 21.7 (12.5).  17 to 32 pairs are bound by a wavefront's chain of decoding, products and exponentials, some 270
+// instructions and 34 products per 32 tokens, with one to two wavefronts per SIMD: in the call above the vector unit is busy for 46 %, the matrix pipe for 15 %.
 // (Tiles of 48 pairs, queries in LDS: 29.2 us for 30.6 in the call above, but 38.2 for 34.9 with 1200 rows on nothing.)
 #include <algorithm>
 #include <type_traits>
